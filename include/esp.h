@@ -73,7 +73,11 @@ enum {
   ESP_DEV_LEN_OVER_BOUND = 1,  /* kv.len[b] + n_rows[b] exceeds kv.len_bound or seq capacity */
   ESP_DEV_BAD_TREE = 2,        /* parent not before child, n_nodes/n_rows out of range, list */
                                /* entries above 1 that keep a node without its parent        */
-  ESP_DEV_BAD_TOKEN = 4        /* token id outside the vocabulary                            */
+  ESP_DEV_BAD_TOKEN = 4,       /* token id outside the vocabulary                            */
+  ESP_DEV_BAD_ROWS = 8,        /* esp_chunk.row0 descends, or a sequence has more rows than   */
+                               /* max_rows or rows past total_rows                            */
+  ESP_DEV_BAD_PAGE = 16,       /* a page that is needed lies outside the pool                 */
+  ESP_DEV_BAD_PATH = 32        /* an accepted path that is none (esp_paged_commit)            */
 };
 
 typedef struct {
@@ -359,6 +363,115 @@ esp_status esp_softmax_topk(void *stream, const float *logits, int32_t rows, int
  * Errors: EINVAL as esp_softmax_topk, ECAPACITY, EDEVICE (symbol lookup or launch failed). */
 esp_status esp_softmax_topk_static(void *stream, const float *logits, int32_t rows, int32_t vocab,
                                    int32_t Kp, int32_t *ids, float *probs);
+
+/* ---- paged KV cache ------------------------------------------------------------------------
+ * A cache whose sequences own pages anywhere in a pool, the rotation and the norms that come before it, and the
+ * attention that reads it.  The calls take a stream and no context; the device that is current at the call must
+ * be the stream's.  They allocate nothing, synchronise nothing and can be captured into a graph. */
+
+/* Rotary positions of a head: the first rot_dim features turn in pairs, (i, i + rot_dim/2) or, interleaved,
+ * (2i, 2i+1); the others pass.  Pair i turns by position * turns[i] revolutions, and the turned features are
+ * multiplied by `amplitude`.  Filled by esp_rope_make (host only); `turns` may hold any other finite speeds. */
+typedef struct {
+  int32_t head_dim;     /* 64 or 128                                     */
+  int32_t rot_dim;      /* multiple of 16, 16 .. head_dim                */
+  int32_t interleaved;
+  float amplitude;
+  double turns[64];     /* [rot_dim/2] revolutions per position          */
+} esp_rope;
+
+/* f_i = theta^(-2i/rot_dim) radians a position.  factor > 1 stretches the positions for contexts longer than the
+ * model was trained on: n_i = orig_len f_i / 2 pi is how often pair i turns in the trained context, keep_i =
+ * clamp((n_i - low_turns) / (high_turns - low_turns), 0, 1), and the pair's speed is f_i (keep_i + (1 - keep_i) /
+ * factor): what turns often keeps its speed, what turns seldom is slowed down.  orig_len 0: all are slowed down
+ * (positions divided by factor).
+ * Errors: EINVAL (out null, theta or factor not positive and finite, orig_len < 0, low_turns >= high_turns with orig_len > 0,
+ * amplitude not finite), ESHAPE (head_dim, rot_dim). */
+esp_status esp_rope_make(int32_t head_dim, int32_t rot_dim, int32_t interleaved, double theta, double factor,
+                         int32_t orig_len, double low_turns, double high_turns, double amplitude, esp_rope *out);
+
+/* Rotary positions on rows of queries and keys, with the RMS norm of every head (over head_dim, gain [head_dim] in
+ * `dtype`) before it where a gain is given.  q [rows][n_q_heads][head_dim], k [rows][n_kv_heads][head_dim]: heads lie
+ * side by side, rows *_stride elements apart (parts of one projection's rows are taken as they are).  The outputs
+ * have strides of their own; an output may be its input with the same stride, and otherwise must not overlap any input.
+ * positions device [rows].  Either of q and k may be NULL with its output (its head count is then not looked at).  The
+ * arithmetic is fp32 (the angle fp64), rounded once.
+ * Errors: EINVAL (null pointers, rows < 0, n_* < 1, eps negative or not finite), ESHAPE (strides below heads * head_dim), EDTYPE,
+ * ECAPACITY (more than 2^31 - 1 rows x heads). */
+esp_status esp_rope_qk(void *stream, int32_t dtype, const esp_rope *rope, int32_t rows, int32_t n_q_heads, int32_t n_kv_heads,
+                       const void *q, int64_t q_stride, const void *k, int64_t k_stride, const int32_t *positions,
+                       const void *q_gain, const void *k_gain, float eps, void *q_out, int64_t q_out_stride, void *k_out,
+                       int64_t k_out_stride);
+
+/* The pool.  k and v each hold [n_layers][n_pages][n_kv_heads] planes of page_size * head_dim elements in the block order
+ * of esp_kv (blocks of 32 slots); 16-byte aligned.  Slot s of sequence b lies in page page_table[b][s / page_size], at slot
+ * s % page_size; entries of pages that hold no token of the sequence are never used.  Two sequences may share pages that
+ * nobody writes.  Slots [0, len[b]) hold committed tokens. */
+typedef struct {
+  void *k, *v;                /* device                                                                          */
+  const int32_t *page_table;  /* device [batch][table_stride]                                                    */
+  const int32_t *len;         /* device [batch]                                                                  */
+  int32_t *status;            /* device, one word that collects ESP_DEV_ bits (the caller clears it), or NULL    */
+  int32_t dtype, n_layers, n_kv_heads;
+  int32_t head_dim;           /* 64 or 128                                                                       */
+  int32_t page_size;          /* slots of a page, multiple of 32                                                 */
+  int32_t n_pages;            /* of the pool                                                                     */
+  int32_t batch;
+  int32_t table_stride;       /* entries of the page table per sequence: it holds table_stride * page_size slots */
+  int32_t len_bound;          /* host: upper bound of len[b] for this call                                       */
+} esp_paged_kv;
+
+/* New rows of the sequences, packed: sequence b has rows row0[b] .. row0[b+1] - 1 (none, one or many), in the order of
+ * its slots: row r of it belongs into slot len[b] + r.  Rows from row0[batch] on are not touched. */
+typedef struct {
+  const int32_t *row0;        /* device [batch + 1], ascending                                                   */
+  int32_t total_rows;         /* host: rows that the buffers hold, at least row0[batch]                          */
+  int32_t max_rows;           /* host: upper bound of a sequence's rows                                          */
+} esp_chunk;
+
+/* What only the device can see -- len[b] negative, above len_bound or with its rows past the table, row0 or pages out of
+ * range -- sets bits in *status.  Of a sequence with bad lengths or rows nothing is read or written; a slot in
+ * a page outside the pool is not written (append, commit), and not seen (attention). */
+
+/* Writes K and V of the chunk's rows into their slots of `layer`, K normed and rotated on the way, and the rows' queries,
+ * normed and rotated, to q_out [total_rows][n_q_heads][head_dim] (rows q_out_stride elements apart).  rope NULL: no rotation.
+ * positions device [total_rows], or NULL: a row's position is its slot (a tree's rows have len + depth).  q and q_out may
+ * both be NULL, and q_out may be q with the same stride.  len is not advanced.
+ * Errors: as esp_rope_qk; EINVAL also for a malformed esp_paged_kv or esp_chunk or a layer outside it; ESHAPE for head_dim other than the
+ * rope's. */
+esp_status esp_paged_append(void *stream, const esp_paged_kv *kv, int32_t layer, const esp_chunk *rows, const esp_rope *rope,
+                            const int32_t *positions, int32_t n_q_heads, const void *q, int64_t q_stride, const void *k,
+                            int64_t k_stride, const void *v, int64_t v_stride, const void *q_gain, const void *k_gain, float eps,
+                            void *q_out, int64_t q_out_stride);
+
+/* Grouped-query attention of the chunk's rows, whose K and V are in their slots already: row r of sequence b sees slots
+ * [0, len[b]) and, of the chunk, rows 0..r (anc NULL) or the rows c whose bit is set in its ancestor bitset anc
+ * [total_rows][anc_words] (as esp_block).  out = softmax(scale q k) v; a row that sees nothing gets zeros.  What a row does
+ * not see does not reach it, whatever it holds.  q as in esp_paged_append; out device [total_rows][n_q_heads][head_dim],
+ * contiguous, no overlap with q.  A value that is not finite makes the output of the rows that see it not finite.
+ * scratch: device, 16-byte aligned, esp_paged_attn_scratch_bytes() bytes (0: it may be NULL), which depend on the host's values
+ * alone, len_bound among them; calls that overlap in time need one each.  Results do not depend on what it held.
+ * Errors: EINVAL (null pointers, scale below 1e-20 or not finite, ...), ESHAPE (n_q_heads not a multiple of n_kv_heads, anc_words * 64
+ * < max_rows, q_stride), EDTYPE, ECAPACITY (scratch). */
+size_t esp_paged_attn_scratch_bytes(const esp_paged_kv *kv, const esp_chunk *rows, int32_t n_q_heads);
+esp_status esp_paged_attn(void *stream, const esp_paged_kv *kv, int32_t layer, const esp_chunk *rows, int32_t n_q_heads,
+                          const void *q, int64_t q_stride, float scale, const uint64_t *anc, int32_t anc_words, void *out,
+                          void *scratch, size_t scratch_bytes);
+
+/* After a verified block whose rows were appended: moves K and V of the accepted rows, in every layer, from slots len[b] +
+ * accepted_row[b][i] to len[b] + i, i = 1 .. n_emit[b] - 1 (accepted_row[b][0], the root, sits at len[b] already), and writes
+ * len_out[b] = len[b] + n_emit[b]; len_out may be kv->len.  accepted_row [batch][ESP_MAX_MASKS + 1] and n_emit [batch] are
+ * what esp_verify_accept hands out.  A path is ascending rows from 1 on, n_emit[b] 0 .. ESP_MAX_MASKS + 1; of a sequence with another
+ * one nothing moves, len_out[b] = len[b], and ESP_DEV_BAD_PATH is set.
+ * Errors: EINVAL. */
+esp_status esp_paged_commit(void *stream, const esp_paged_kv *kv, const int32_t *n_emit, const int32_t *accepted_row,
+                            int32_t *len_out);
+
+/* Copies slots first_slot .. of sequence seq, one layer, out of the pool to plain rows [n_slots][n_kv_heads][head_dim].
+ * Slots of a page outside the pool come back as zeros.
+ * Errors: EINVAL, ECAPACITY (slots past the table). */
+esp_status esp_paged_load(void *stream, const esp_paged_kv *kv, int32_t layer, int32_t seq, int32_t first_slot, int32_t n_slots,
+                          void *k_rows, void *v_rows);
 
 /* Optional timing of launch sites with HIP events recorded on the ctx stream (benchmarks).
  * esp_profile_enable: bit s of site_mask turns site s on (0 = off, the default; events are host

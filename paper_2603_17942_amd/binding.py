@@ -20,7 +20,7 @@ ESP_OK = 0
 ESP_F32, ESP_BF16 = 0, 1
 LAYOUT_PER_NODE, LAYOUT_ROOT_CHAIN = 0, 1
 MAX_MASKS, MAX_ROWS_PER_SEQ, MAX_TOPK, MAX_TREE_NODES = 8, 1024, 32, 256
-DEV_LEN_OVER_BOUND, DEV_BAD_TREE, DEV_BAD_TOKEN = 1, 2, 4
+DEV_LEN_OVER_BOUND, DEV_BAD_TREE, DEV_BAD_TOKEN, DEV_BAD_ROWS, DEV_BAD_PAGE, DEV_BAD_PATH = 1, 2, 4, 8, 16, 32
 STATUS_NAMES = {0: "ESP_OK", 1: "ESP_EINVAL", 2: "ESP_ESHAPE", 3: "ESP_ECAPACITY", 4: "ESP_EDTYPE",
                 5: "ESP_EDEVICE", 6: "ESP_ESTATE"}
 
@@ -56,11 +56,27 @@ class TreeParams(C.Structure):
                 ("prune_last", _i32), ("layout", _i32), ("static_widths", _i32 * MAX_MASKS)]
 
 
+class Rope(C.Structure):
+    _fields_ = [("head_dim", _i32), ("rot_dim", _i32), ("interleaved", _i32), ("amplitude", _f32), ("turns", C.c_double * 64)]
+
+
+class PagedKvStruct(C.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("page_table", _vp), ("len", _vp), ("status", _vp), ("dtype", _i32), ("n_layers", _i32),
+                ("n_kv_heads", _i32), ("head_dim", _i32), ("page_size", _i32), ("n_pages", _i32), ("batch", _i32),
+                ("table_stride", _i32), ("len_bound", _i32)]
+
+
+class ChunkStruct(C.Structure):
+    _fields_ = [("row0", _vp), ("total_rows", _i32), ("max_rows", _i32)]
+
+
 EXPORTS = ["esp_status_str", "esp_workspace_bytes", "esp_create", "esp_destroy", "esp_last_device_status",
            "esp_tree_forward", "esp_verify_accept", "esp_mask_topk", "esp_build_prune_tree",
            "esp_block_from_tree", "esp_mask_mean", "esp_mask_ema", "esp_set_mask_batch", "esp_mask_ema_batch", "esp_mask_last_k", "esp_mask_gaussian", "esp_kv_store", "esp_kv_load",
            "esp_gemm_scratch_bytes", "esp_gemm", "esp_gemm_argmax_scratch_bytes", "esp_gemm_argmax", "esp_attn_tree", "esp_softmax_topk_scratch_bytes",
-           "esp_softmax_topk", "esp_softmax_topk_static", "esp_profile_enable", "esp_profile_read", "esp_pack_weight", "esp_set_sampling"]
+           "esp_softmax_topk", "esp_softmax_topk_static", "esp_profile_enable", "esp_profile_read", "esp_pack_weight", "esp_set_sampling",
+           "esp_rope_make", "esp_rope_qk", "esp_paged_append", "esp_paged_attn_scratch_bytes", "esp_paged_attn", "esp_paged_commit",
+           "esp_paged_load"]
 SITES = {"gemm_layer": 0, "attn": 1, "attn_merge": 2, "lm_head": 3, "topk": 4, "tree": 5, "glue": 6}
 
 _lib = None
@@ -117,6 +133,16 @@ def load_library() -> C.CDLL:
     lib.esp_profile_enable.argtypes = [_vp, C.c_uint32]
     lib.esp_set_sampling.argtypes = [_vp, C.c_int32, C.c_uint32]
     lib.esp_profile_read.argtypes = [_vp, _i32, P(_i64), P(C.c_double)]
+    _f64 = C.c_double
+    lib.esp_rope_make.argtypes = [_i32, _i32, _i32, _f64, _f64, _i32, _f64, _f64, _f64, P(Rope)]
+    lib.esp_rope_qk.argtypes = [_vp, _i32, P(Rope), _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _f32, _vp, _i64, _vp, _i64]
+    lib.esp_paged_append.argtypes = [_vp, P(PagedKvStruct), _i32, P(ChunkStruct), P(Rope), _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64,
+                                     _vp, _vp, _f32, _vp, _i64]
+    lib.esp_paged_attn_scratch_bytes.restype = C.c_size_t
+    lib.esp_paged_attn_scratch_bytes.argtypes = [P(PagedKvStruct), P(ChunkStruct), _i32]
+    lib.esp_paged_attn.argtypes = [_vp, P(PagedKvStruct), _i32, P(ChunkStruct), _i32, _vp, _i64, _f32, _vp, _i32, _vp, _vp, C.c_size_t]
+    lib.esp_paged_commit.argtypes = [_vp, P(PagedKvStruct), _vp, _vp, _vp]
+    lib.esp_paged_load.argtypes = [_vp, P(PagedKvStruct), _i32, _i32, _i32, _i32, _vp, _vp]
     for name in EXPORTS:
         getattr(lib, name)          # AttributeError here = a declared entry point is not exported
     _lib = lib
@@ -494,3 +520,229 @@ def softmax_topk_static(logits: torch.Tensor, kp: int, ids: torch.Tensor, ps: to
     _check(lib.esp_softmax_topk_static(_stream_ptr(), _ptr(logits), rows, vocab, kp, _ptr(ids), _ptr(ps)),
            "esp_softmax_topk_static")
     return ids, ps
+
+
+# ---- paged KV cache -------------------------------------------------------------------------------------
+# Functions on tensors, on the current stream of the tensors' device (which need not be the current one).
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dtype_of(t: torch.Tensor) -> int:
+    _need(t.dtype in (torch.bfloat16, torch.float32), f"bfloat16 or float32 wanted, got {t.dtype}")
+    return ESP_BF16 if t.dtype == torch.bfloat16 else ESP_F32
+
+
+def _on_device(dev: torch.device, fn, where: str, *args):
+    _need(dev.type == "cuda", f"{where}: the tensors are on {dev}; there is no CPU fallback")
+    if dev.index == torch.cuda.current_device():
+        code = fn(_stream_ptr(), *args)
+    else:
+        with torch.cuda.device(dev):
+            code = fn(_stream_ptr(), *args)
+    if code != ESP_OK:
+        raise EspError(code, where)
+
+
+def _heads(t: torch.Tensor, name: str, dev, dtype, rows: int, hd: int):
+    """(pointer, row stride, heads) of [rows, heads, hd] whose heads lie side by side; rows may lie further apart."""
+    _need(t.dim() == 3 and t.shape[0] == rows and t.shape[2] == hd and t.dtype == dtype and t.device == dev,
+          f"{name}: [{rows}, heads, {hd}] of {dtype} on {dev} wanted, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    n = t.shape[1]
+    s0, s1, s2 = t.stride()
+    _need((s2 == 1 or hd == 1) and (s1 == hd or n == 1), f"{name}: the features of a head and the heads of a row have to lie side by side")
+    return t.data_ptr(), (s0 if rows > 1 else n * hd), n
+
+
+def _ints(t: Optional[torch.Tensor], name: str, dev, shape) -> Optional[int]:
+    if t is None:
+        return None
+    _need(t.dtype == torch.int32 and t.device == dev and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+          f"{name}: contiguous int32 {tuple(shape)} on {dev} wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _gain(t: Optional[torch.Tensor], name: str, dev, dtype, hd: int) -> Optional[int]:
+    if t is None:
+        return None
+    _need(t.dtype == dtype and t.device == dev and tuple(t.shape) == (hd,) and t.is_contiguous(), f"{name}: contiguous [{hd}] of {dtype} on {dev} wanted")
+    return t.data_ptr()
+
+
+def rope_spec(head_dim: int, rot_dim: Optional[int] = None, theta: float = 1.0e4, interleaved: bool = False, factor: float = 1.0,
+              orig_len: int = 0, low_turns: float = 1.0, high_turns: float = 32.0, amplitude: float = 1.0) -> Rope:
+    """Rotary positions (esp_rope_make): of the first rot_dim features (all by default), pairs (i, i + rot_dim/2) or interleaved
+    (2i, 2i+1), pair i at theta^(-2i/rot_dim) radians a position.  factor > 1 stretches positions: by all of it where orig_len is 0,
+    otherwise pairs keep their speed that turn high_turns times or more within orig_len positions, and those below low_turns get
+    all of it."""
+    r = Rope()
+    _check(load_library().esp_rope_make(head_dim, head_dim if rot_dim is None else rot_dim, int(interleaved), theta, factor, orig_len,
+                                        low_turns, high_turns, amplitude, C.byref(r)), "esp_rope_make")
+    return r
+
+
+def rope_qk(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor, rope: Rope, q_gain=None, k_gain=None,
+            eps: float = 1.0e-6, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """(q_out, k_out): q [rows, n_q, head_dim] and k [rows, n_kv, head_dim] (rows may lie further apart: parts of one projection)
+    turned to their positions [rows], after the RMS norm of every head where a gain [head_dim] is given.  Outputs may be the inputs."""
+    lib = load_library()
+    x = q if q is not None else k
+    _need(x is not None and x.dim() == 3, "q or k wanted")
+    dev, dt, rows, hd = x.device, x.dtype, x.shape[0], rope.head_dim
+    code = _dtype_of(x)
+    qp = qs = qo = qos = nq = kp = ks = ko = kos = nk = 0
+    if q is not None:
+        qp, qs, nq = _heads(q, "q", dev, dt, rows, hd)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        qo, qos, n = _heads(q_out, "q_out", dev, dt, rows, hd)
+        _need(n == nq, "q_out: as many heads as q wanted")
+    if k is not None:
+        kp, ks, nk = _heads(k, "k", dev, dt, rows, hd)
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=dt, device=dev)
+        ko, kos, n = _heads(k_out, "k_out", dev, dt, rows, hd)
+        _need(n == nk, "k_out: as many heads as k wanted")
+    if rows:
+        _on_device(dev, lib.esp_rope_qk, "esp_rope_qk", code, C.byref(rope), rows, nq, nk, qp, qs, kp, ks, _ints(positions, "positions", dev, (rows,)),
+                   _gain(q_gain, "q_gain", dev, dt, hd), _gain(k_gain, "k_gain", dev, dt, hd), eps, qo, qos, ko, kos)
+    return q_out, k_out
+
+
+class PagedKv:
+    """A paged KV cache over the caller's tensors: k and v [n_layers, n_pages, n_kv_heads, page_size, head_dim] (contiguous; the
+    slots of a page in the library's block order, so only paged_append writes and paged_load reads them), page_table
+    [batch, pages of a sequence] and lens [batch] int32.  len_bound: upper bound of lens, which the caller advances.  status: one
+    int32 that collects DEV_ bits."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, len_bound: int,
+                 status: Optional[torch.Tensor] = None):
+        dev = k.device
+        _need(k.dim() == 5 and k.shape == v.shape and k.dtype == v.dtype and v.device == dev and k.is_contiguous() and v.is_contiguous(),
+              "k and v: contiguous [layers, pages, kv heads, page size, head dim] alike wanted")
+        _need(page_table.dim() == 2, "page_table: [batch, pages of a sequence] wanted")
+        self.k, self.v, self.page_table, self.lens, self.device = k, v, page_table, lens, dev
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
+        batch = page_table.shape[0]
+        s = PagedKvStruct(k.data_ptr(), v.data_ptr(), _ints(page_table, "page_table", dev, page_table.shape), _ints(lens, "lens", dev, (batch,)),
+                          _ints(self.status, "status", dev, (1,)), _dtype_of(k), k.shape[0], k.shape[2], k.shape[4], k.shape[3], k.shape[1], batch,
+                          page_table.shape[1], len_bound)
+        self.struct, self._ref = s, C.byref(s)
+        self.dtype, self.head_dim, self.n_kv_heads, self.batch = k.dtype, k.shape[4], k.shape[2], batch
+
+    @classmethod
+    def zeros(cls, n_layers: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, batch: int, pages_per_seq: int,
+              dtype=torch.bfloat16, device="cuda") -> "PagedKv":
+        shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+        return cls(torch.zeros(shape, dtype=dtype, device=device), torch.zeros(shape, dtype=dtype, device=device),
+                   torch.zeros((batch, pages_per_seq), dtype=torch.int32, device=device), torch.zeros(batch, dtype=torch.int32, device=device), 0)
+
+    @property
+    def len_bound(self) -> int:
+        return self.struct.len_bound
+
+    @len_bound.setter
+    def len_bound(self, n: int):
+        self.struct.len_bound = int(n)
+
+    def device_status(self) -> int:
+        """The DEV_ bits so far, cleared (synchronises)."""
+        v = int(self.status.item())
+        if v:
+            self.status.zero_()
+        return v
+
+
+class ChunkRows:
+    """New rows of a batch, packed: sequence b has rows row0[b] .. row0[b + 1] - 1.  row0 [batch + 1] int32 on the device; total_rows:
+    rows of the buffers, max_rows: upper bound of one sequence's."""
+
+    def __init__(self, row0: torch.Tensor, total_rows: int, max_rows: int):
+        self.row0, self.total_rows, self.max_rows = row0, int(total_rows), int(max_rows)
+        self.struct = ChunkStruct(_ints(row0, "row0", row0.device, (row0.numel(),)), self.total_rows, self.max_rows)
+        self._ref = C.byref(self.struct)
+
+
+def _same_batch(kv: PagedKv, rows: ChunkRows):
+    _need(rows.row0.device == kv.device and rows.row0.numel() == kv.batch + 1, "row0: [batch + 1] on the cache's device wanted")
+
+
+def paged_append(kv: PagedKv, layer: int, rows: ChunkRows, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                 rope: Optional[Rope] = None, positions: Optional[torch.Tensor] = None, q_gain=None, k_gain=None, eps: float = 1.0e-6,
+                 q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """K and V rows of the chunk into the pages of their slots, K normed (k_gain) and rotated (rope) on the way; returns q treated the same
+    (q None: nothing).  Positions are the slots' unless given."""
+    lib = load_library()
+    _same_batch(kv, rows)
+    dev, dt, hd, n = kv.device, kv.dtype, kv.head_dim, rows.total_rows
+    kp, ks, nk = _heads(k, "k", dev, dt, n, hd)
+    vp, vs, nv = _heads(v, "v", dev, dt, n, hd)
+    _need(nk == kv.n_kv_heads and nv == nk, f"k and v: {kv.n_kv_heads} heads wanted")
+    qp = qs = qo = qos = nq = 0
+    if q is not None:
+        qp, qs, nq = _heads(q, "q", dev, dt, n, hd)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        qo, qos, m = _heads(q_out, "q_out", dev, dt, n, hd)
+        _need(m == nq, "q_out: as many heads as q wanted")
+    if n == 0:
+        return q_out
+    _on_device(dev, lib.esp_paged_append, "esp_paged_append", kv._ref, layer, rows._ref, None if rope is None else C.byref(rope),
+               _ints(positions, "positions", dev, (n,)), nq, qp, qs, kp, ks, vp, vs, _gain(q_gain, "q_gain", dev, dt, hd),
+               _gain(k_gain, "k_gain", dev, dt, hd), eps, qo, qos)
+    return q_out
+
+
+def paged_attn_scratch_bytes(kv: PagedKv, rows: ChunkRows, n_q_heads: int) -> int:
+    return load_library().esp_paged_attn_scratch_bytes(kv._ref, rows._ref, n_q_heads)
+
+
+def paged_attn(kv: PagedKv, layer: int, rows: ChunkRows, q: torch.Tensor, scale: Optional[float] = None, anc: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the chunk's rows over the cache (their K and V appended before): causal, or the chunk's rows that the bits of anc
+    [total_rows, words] int64 name.  scale: 1 / sqrt(head_dim) unless given.  out [total_rows, n_q, head_dim] and scratch (uint8,
+    paged_attn_scratch_bytes) may be passed in to keep allocation out of a loop."""
+    lib = load_library()
+    _same_batch(kv, rows)
+    dev, dt, hd, n = kv.device, kv.dtype, kv.head_dim, rows.total_rows
+    qp, qs, nq = _heads(q, "q", dev, dt, n, hd)
+    if out is None:
+        out = torch.empty((n, nq, hd), dtype=dt, device=dev)
+    _need(out.dtype == dt and out.device == dev and tuple(out.shape) == (n, nq, hd) and out.is_contiguous(), f"out: contiguous [{n}, {nq}, {hd}] wanted")
+    words = 0
+    if anc is not None:
+        _need(anc.dtype == torch.int64 and anc.device == dev and anc.dim() == 2 and anc.shape[0] == n and anc.is_contiguous(),
+              f"anc: contiguous int64 [{n}, words] wanted")
+        words = anc.shape[1]
+    if scratch is None:
+        nb = paged_attn_scratch_bytes(kv, rows, nq)
+        scratch = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
+    _need(scratch is None or (scratch.dtype == torch.uint8 and scratch.device == dev and scratch.is_contiguous()), "scratch: contiguous uint8 wanted")
+    if n == 0:
+        return out
+    _on_device(dev, lib.esp_paged_attn, "esp_paged_attn", kv._ref, layer, rows._ref, nq, qp, qs, hd ** -0.5 if scale is None else scale,
+               None if anc is None else anc.data_ptr(), words, out.data_ptr(), None if scratch is None else scratch.data_ptr(),
+               0 if scratch is None else scratch.numel())
+    return out
+
+
+def paged_commit(kv: PagedKv, n_emit: torch.Tensor, accepted_row: torch.Tensor, len_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Moves the accepted rows of a verified block behind the committed tokens, in all layers, and writes the new lengths to len_out
+    (kv.lens itself by default)."""
+    lib = load_library()
+    out = kv.lens if len_out is None else len_out
+    _on_device(kv.device, lib.esp_paged_commit, "esp_paged_commit", kv._ref, _ints(n_emit, "n_emit", kv.device, (kv.batch,)),
+               _ints(accepted_row, "accepted_row", kv.device, (kv.batch, MAX_MASKS + 1)), _ints(out, "len_out", kv.device, (kv.batch,)))
+    return out
+
+
+def paged_load(kv: PagedKv, layer: int, seq: int, first_slot: int, n_slots: int):
+    """Plain K and V rows [n_slots, n_kv_heads, head_dim] of a sequence's slots."""
+    lib = load_library()
+    k = torch.empty((n_slots, kv.n_kv_heads, kv.head_dim), dtype=kv.dtype, device=kv.device)
+    v = torch.empty_like(k)
+    if n_slots:
+        _on_device(kv.device, lib.esp_paged_load, "esp_paged_load", kv._ref, layer, seq, first_slot, n_slots, k.data_ptr(), v.data_ptr())
+    return k, v

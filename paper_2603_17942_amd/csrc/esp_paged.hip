@@ -1,0 +1,362 @@
+// Rotary positions with head norms, the append into a paged KV cache, the move of accepted rows, and the way back to
+// plain rows.  The attention over the pages is in esp_paged_attn.hip.
+#include "esp_paged.h"
+
+namespace {
+
+// sine and cosine of t revolutions: whole and quarter turns come off in fp64, so a far position costs nothing (position 2^20 at one
+// radian a position is 1.7e5 turns, known to 2^-36), and what is left, an eighth of a turn at most, is exact to half a step of fp32
+__device__ __forceinline__ void turn_sincos(double t, float& s, float& c) {
+  t -= rint(t);
+  const double q = rint(4.0 * t);
+  float s0, c0;
+  sincospif((float)(2.0 * (t - 0.25 * q)), &s0, &c0);
+  const int quarter = (int)q & 3;
+  const float a = quarter & 1 ? c0 : s0, b = quarter & 1 ? s0 : c0;
+  s = quarter & 2 ? -a : a;
+  c = (quarter == 1 || quarter == 2) ? -b : b;
+}
+
+// eight consecutive elements; VEC: 16-byte aligned
+template <bool VEC, typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+  if constexpr (VEC && sizeof(T) == 4) {
+    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(p), b = *reinterpret_cast<const f32x4_t*>(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+  } else if constexpr (VEC) {
+    const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)a[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = to_f32(p[e]);
+  }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+  if constexpr (VEC && sizeof(T) == 4) {
+    *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+  } else if constexpr (VEC) {
+    bf16x8_t a;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = (bf16_t)v[e];
+    *reinterpret_cast<bf16x8_t*>(p) = a;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = from_f32<T>(v[e]);
+  }
+}
+
+// the sequence that row m belongs to, by the whole wave: the last that begins at or before it; -1 if none holds it
+__device__ __forceinline__ int find_seq(const ChunkDev& ch, int batch, int m, int lane) {
+  int n = 0;
+  for (int b = 0; b < batch; b += 64) {
+    const bool before = b + lane < batch && ch.row0[b + lane] <= m;
+    n += __popcll(__builtin_amdgcn_ballot_w64(before));
+  }
+  return n - 1;
+}
+
+// Sixteen features of a head in two pieces of eight, one thread: of a part that turns the pieces hold its pairs, so a thread
+// needs nothing of its neighbours.  HD / 16 threads of a head lie side by side in a wave and add up the squares for the norm.
+template <typename T, int HD>
+__device__ __forceinline__ void norm_rotate(const RopeRows& a, const T* gain, int j, int u0, int u1, const float2* cs, float (&x0)[8],
+                                            float (&x1)[8]) {
+  if (gain) {
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss += x0[e] * x0[e] + x1[e] * x1[e];
+#pragma unroll
+    for (int o = HD / 32; o > 0; o >>= 1) ss += __shfl_xor(ss, o, 64);
+    const float inv = 1.0f / sqrtf(ss / (float)HD + a.eps);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x0[e] *= inv * to_f32(gain[8 * u0 + e]);
+      x1[e] *= inv * to_f32(gain[8 * u1 + e]);
+    }
+  }
+  if (16 * j < a.rot) {
+    if (a.interleaved) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float2 t0 = cs[4 * u0 + e / 2], t1 = cs[4 * u1 + e / 2];
+        const float p0 = x0[e], p1 = x1[e];
+        x0[e] = p0 * t0.x - x0[e + 1] * t0.y;
+        x0[e + 1] = x0[e + 1] * t0.x + p0 * t0.y;
+        x1[e] = p1 * t1.x - x1[e + 1] * t1.y;
+        x1[e + 1] = x1[e + 1] * t1.x + p1 * t1.y;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float2 t = cs[8 * j + e];
+        const float p = x0[e];
+        x0[e] = p * t.x - x1[e] * t.y;
+        x1[e] = x1[e] * t.x + p * t.y;
+      }
+    }
+  }
+}
+// the two pieces of thread j of a head: pairs (j, j + rot/16) where the head turns, neighbours behind that
+__device__ __forceinline__ void pieces_of(int j, int rot, int& u0, int& u1) {
+  const bool turns = 16 * j < rot;
+  u0 = turns ? j : 2 * j;
+  u1 = turns ? j + rot / 16 : 2 * j + 1;
+}
+
+// R rows a workgroup, a wave finds a row's place and fills its table of cosines and sines, then all threads take the heads.
+template <typename T, int HD, bool PAGED, bool VEC, int R>
+__global__ __launch_bounds__(256) void k_rope_rows(RopeRows a, PagedDev kv, ChunkDev ch) {
+  constexpr int LPH = HD / 16;
+  __shared__ float2 cs[R][HD / 2];
+  __shared__ int page_of[R], slot_of[R];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int m0 = blockIdx.x * R;
+  for (int i = wave; i < R; i += 4) {
+    const int m = m0 + i;
+    int page = -1, slot = 0, pos = 0;
+    if (m < a.rows) {
+      if (PAGED) {
+        const int seq = find_seq(ch, kv.batch, m, lane);
+        if (seq >= 0) {
+          const ChunkSeq s = chunk_seq(kv, ch, seq);
+          if (s.ok && m - s.row0 < s.rows) {
+            slot = s.len + (m - s.row0);
+            pos = slot;
+            page = kv.table[(size_t)seq * kv.stride + slot / kv.page_size];
+            slot %= kv.page_size;
+            if ((unsigned)page >= (unsigned)kv.n_pages) {
+              if (lane == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+              page = -2;                                  // the query is there, the slot is not
+            }
+          }
+        }
+      } else {
+        page = 0;
+      }
+      if (a.positions) pos = a.positions[m];
+    }
+    if (lane == 0) { page_of[i] = page; slot_of[i] = slot; }
+    if (page != -1 && lane < a.rot / 2) {
+      float s, c;
+      turn_sincos((double)pos * a.turns[lane], s, c);
+      cs[i][lane] = float2{c * a.amplitude, s * a.amplitude};
+    }
+  }
+  if (PAGED && blockIdx.x == 0)
+    for (int b = tid; b < kv.batch; b += 256)
+      if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(kv, ch, b));
+  __syncthreads();
+  const int heads = a.hq + (PAGED ? 2 : 1) * a.hkv, per_row = heads * LPH;
+  for (int t = tid; t < R * per_row; t += 256) {
+    const int i = t / per_row, head = (t - i * per_row) / LPH, j = t % LPH, m = m0 + i;
+    const int page = page_of[i];
+    if (page == -1) continue;
+    float x0[8], x1[8];
+    if (head >= a.hq + a.hkv) {
+      if (page < 0) continue;
+      const int kvh = head - a.hq - a.hkv;
+      const T* src = (const T*)a.v + (int64_t)m * a.v_stride + kvh * HD;
+      load8<VEC>(src + 8 * j, x0);
+      load8<VEC>(src + 8 * (j + LPH), x1);
+      T* dst = (T*)kv.v + page_plane(page, kvh, kv.hkv, kv.page_size, HD);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dst[v_off(slot_of[i], 8 * j + e, HD)] = from_f32<T>(x0[e]);
+        dst[v_off(slot_of[i], 8 * (j + LPH) + e, HD)] = from_f32<T>(x1[e]);
+      }
+      continue;
+    }
+    int u0, u1;
+    pieces_of(j, a.rot, u0, u1);
+    const bool is_q = head < a.hq;
+    const T* src = is_q ? (const T*)a.q + (int64_t)m * a.q_stride + head * HD : (const T*)a.k + (int64_t)m * a.k_stride + (head - a.hq) * HD;
+    load8<VEC>(src + 8 * u0, x0);
+    load8<VEC>(src + 8 * u1, x1);
+    norm_rotate<T, HD>(a, (const T*)(is_q ? a.q_gain : a.k_gain), j, u0, u1, cs[i], x0, x1);
+    if (is_q) {
+      T* dst = (T*)a.q_out + (int64_t)m * a.q_out_stride + head * HD;
+      store8<VEC>(dst + 8 * u0, x0);
+      store8<VEC>(dst + 8 * u1, x1);
+    } else if (PAGED) {
+      if (page < 0) continue;
+      T* dst = (T*)kv.k + page_plane(page, head - a.hq, kv.hkv, kv.page_size, HD);
+      store8<true>(dst + k_off(slot_of[i], 8 * u0, HD), x0);
+      store8<true>(dst + k_off(slot_of[i], 8 * u1, HD), x1);
+    } else {
+      T* dst = (T*)a.k_out + (int64_t)m * a.k_out_stride + (head - a.hq) * HD;
+      store8<VEC>(dst + 8 * u0, x0);
+      store8<VEC>(dst + 8 * u1, x1);
+    }
+  }
+}
+
+// What is wrong with a sequence's path (0: nothing): its rows ascend from 1 on, and rows and places lie in the table.
+__device__ __forceinline__ int path_fault(const PagedDev& kv, int L, int n, const int32_t* path) {
+  const int64_t cap = (int64_t)kv.stride * kv.page_size;
+  if (n < 0 || n > ESP_MAX_MASKS + 1) return ESP_DEV_BAD_PATH;
+  if (L < 0 || L > kv.len_bound || (int64_t)L + n > cap) return ESP_DEV_LEN_OVER_BOUND;
+  bool ok = true;
+#pragma unroll
+  for (int i = 1; i <= ESP_MAX_MASKS; ++i) {
+    const int r = path[i], before = i > 1 ? path[i - 1] : 0;
+    ok &= i >= n || ((r > before) & ((int64_t)L + r < cap));
+  }
+  return ok ? 0 : ESP_DEV_BAD_PATH;
+}
+
+// A workgroup moves one (layer, kv head) of a sequence's path: everything is read before anything is written, since a row's
+// place may be another's source.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_paged_commit(PagedDev kv, const int32_t* __restrict__ n_emit, const int32_t* __restrict__ accepted,
+                                                      int32_t* len_out) {
+  constexpr int MOST = ESP_MAX_MASKS;                  // rows that can move
+  typedef T piece_t __attribute__((ext_vector_type(8)));
+  const int seq = blockIdx.y, layer = blockIdx.x / kv.hkv, kvh = blockIdx.x % kv.hkv, tid = threadIdx.x;
+  const int L = kv.len[seq], n = n_emit[seq];
+  const int32_t* path = accepted + (size_t)seq * (ESP_MAX_MASKS + 1);
+  const int fault = path_fault(kv, L, n, path);
+  if (blockIdx.x == 0 && tid == 0) {
+    if (fault) set_status(kv.status, fault);
+    if (len_out) len_out[seq] = fault ? L : L + n;
+  }
+  if (fault) return;
+  const size_t layer0 = (size_t)layer * kv.n_pages * kv.hkv * kv.page_size * HD;
+  T* kp = (T*)kv.k + layer0;
+  T* vp = (T*)kv.v + layer0;
+  const int32_t* table = kv.table + (size_t)seq * kv.stride;
+  auto place = [&](int s, size_t& plane, int& inside) {
+    const int page = table[s / kv.page_size];
+    inside = s % kv.page_size;
+    const bool there = (unsigned)page < (unsigned)kv.n_pages;
+    if (!there && tid == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+    plane = page_plane(there ? page : 0, kvh, kv.hkv, kv.page_size, HD);
+    return there;
+  };
+  constexpr int VROWS = MOST * HD / 256, KROWS = (MOST * HD / 8 + 255) / 256;
+  T v[VROWS];
+  piece_t k[KROWS];
+  bool v_there[VROWS], k_there[KROWS];
+  size_t plane;
+  int inside;
+#pragma unroll
+  for (int x = 0; x < VROWS; ++x) {
+    const int i = 1 + (tid + 256 * x) / HD, d = tid % HD;
+    v_there[x] = i < n && place(L + path[i], plane, inside);
+    if (v_there[x]) v[x] = vp[plane + v_off(inside, d, HD)];
+  }
+#pragma unroll
+  for (int x = 0; x < KROWS; ++x) {
+    const int i = 1 + (tid + 256 * x) / (HD / 8), u = tid % (HD / 8);
+    k_there[x] = i < n && place(L + path[i], plane, inside);
+    if (k_there[x]) k[x] = *reinterpret_cast<const piece_t*>(kp + plane + k_off(inside, 8 * u, HD));
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < VROWS; ++x) {
+    const int i = 1 + (tid + 256 * x) / HD, d = tid % HD;
+    if (v_there[x] && place(L + i, plane, inside)) vp[plane + v_off(inside, d, HD)] = v[x];
+  }
+#pragma unroll
+  for (int x = 0; x < KROWS; ++x) {
+    const int i = 1 + (tid + 256 * x) / (HD / 8), u = tid % (HD / 8);
+    if (k_there[x] && place(L + i, plane, inside)) *reinterpret_cast<piece_t*>(kp + plane + k_off(inside, 8 * u, HD)) = k[x];
+  }
+}
+
+// the lengths, where they are advanced in place: the workgroups that move rows read them
+__global__ void k_paged_advance(PagedDev kv, const int32_t* __restrict__ n_emit, const int32_t* __restrict__ accepted, int32_t* len) {
+  const int seq = blockIdx.x * blockDim.x + threadIdx.x;
+  if (seq >= kv.batch) return;
+  const int L = len[seq], n = n_emit[seq];
+  if (path_fault(kv, L, n, accepted + (size_t)seq * (ESP_MAX_MASKS + 1)) == 0) len[seq] = L + n;
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_paged_load(PagedDev kv, int seq, int first_slot, size_t n, T* __restrict__ k_rows,
+                                                    T* __restrict__ v_rows) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int d = (int)(i % HD), kvh = (int)(i / HD % kv.hkv), s = first_slot + (int)(i / ((size_t)HD * kv.hkv));
+  const int page = kv.table[(size_t)seq * kv.stride + s / kv.page_size], inside = s % kv.page_size;
+  T k = from_f32<T>(0.f), v = k;
+  if ((unsigned)page < (unsigned)kv.n_pages) {
+    const size_t plane = page_plane(page, kvh, kv.hkv, kv.page_size, HD);
+    k = ((const T*)kv.k)[plane + k_off(inside, d, HD)];
+    v = ((const T*)kv.v)[plane + v_off(inside, d, HD)];
+  } else {
+    set_status(kv.status, ESP_DEV_BAD_PAGE);
+  }
+  k_rows[i] = k;
+  v_rows[i] = v;
+}
+
+template <typename T>
+bool rows_aligned(const RopeRows& a, bool paged) {
+  auto fits = [](const void* p, int64_t stride) { return (uintptr_t)p % 16 == 0 && stride * (int64_t)sizeof(T) % 16 == 0; };
+  bool ok = true;
+  if (a.hq) ok = ok && fits(a.q, a.q_stride) && fits(a.q_out, a.q_out_stride);
+  if (a.hkv) ok = ok && fits(a.k, a.k_stride) && (paged ? fits(a.v, a.v_stride) : fits(a.k_out, a.k_out_stride));
+  return ok;
+}
+
+template <typename T, int HD, bool PAGED>
+hipError_t launch_rows(hipStream_t st, const RopeRows& a, const PagedDev& kv, const ChunkDev& ch) {
+  const bool vec = rows_aligned<T>(a, PAGED);
+  const int r = a.rows >= 1024 ? 4 : 1;
+  const dim3 grid((unsigned)((a.rows + r - 1) / r));
+#define ESP_ROPE_ROWS(V_, R_) hipLaunchKernelGGL((k_rope_rows<T, HD, PAGED, V_, R_>), grid, dim3(256), 0, st, a, kv, ch)
+  if (r == 4) { if (vec) ESP_ROPE_ROWS(true, 4); else ESP_ROPE_ROWS(false, 4); }
+  else { if (vec) ESP_ROPE_ROWS(true, 1); else ESP_ROPE_ROWS(false, 1); }
+#undef ESP_ROPE_ROWS
+  return hipGetLastError();
+}
+
+template <typename T, int HD>
+hipError_t launch_commit(hipStream_t st, const PagedDev& kv, int layers, const int32_t* n_emit, const int32_t* accepted, int32_t* len_out) {
+  const bool in_place = len_out == kv.len;
+  hipLaunchKernelGGL((k_paged_commit<T, HD>), dim3(layers * kv.hkv, kv.batch), dim3(256), 0, st, kv, n_emit, accepted, in_place ? nullptr : len_out);
+  if (in_place) hipLaunchKernelGGL(k_paged_advance, dim3((kv.batch + 255) / 256), dim3(256), 0, st, kv, n_emit, accepted, len_out);
+  return hipGetLastError();
+}
+template <typename T, int HD>
+hipError_t launch_load(hipStream_t st, const PagedDev& kv, int seq, int first_slot, size_t n, void* k_rows, void* v_rows) {
+  hipLaunchKernelGGL((k_paged_load<T, HD>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, kv, seq, first_slot, n, (T*)k_rows, (T*)v_rows);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+#define ESP_BY_TYPE(CALL)                                                        \
+  (dtype == ESP_F32 ? (hd == 64 ? CALL(float, 64) : CALL(float, 128)) : (hd == 64 ? CALL(bf16_t, 64) : CALL(bf16_t, 128)))
+
+hipError_t launch_rope_rows(hipStream_t st, int dtype, int hd, const RopeRows& a) {
+#define ESP_CALL(T_, HD_) (launch_rows<T_, HD_, false>(st, a, PagedDev{}, ChunkDev{}))
+  return ESP_BY_TYPE(ESP_CALL);
+#undef ESP_CALL
+}
+
+hipError_t launch_paged_append(hipStream_t st, int dtype, int hd, const PagedDev& kv, const ChunkDev& ch, const RopeRows& a) {
+#define ESP_CALL(T_, HD_) (launch_rows<T_, HD_, true>(st, a, kv, ch))
+  return ESP_BY_TYPE(ESP_CALL);
+#undef ESP_CALL
+}
+
+hipError_t launch_paged_commit(hipStream_t st, int dtype, int hd, const PagedDev& kv, int layers, const int32_t* n_emit,
+                               const int32_t* accepted, int32_t* len_out) {
+#define ESP_CALL(T_, HD_) (launch_commit<T_, HD_>(st, kv, layers, n_emit, accepted, len_out))
+  return ESP_BY_TYPE(ESP_CALL);
+#undef ESP_CALL
+}
+
+hipError_t launch_paged_load(hipStream_t st, int dtype, int hd, const PagedDev& kv, int seq, int first_slot, int n_slots, void* k_rows,
+                             void* v_rows) {
+  const size_t n = (size_t)n_slots * kv.hkv * hd;
+  if (n == 0) return hipSuccess;
+#define ESP_CALL(T_, HD_) (launch_load<T_, HD_>(st, kv, seq, first_slot, n, k_rows, v_rows))
+  return ESP_BY_TYPE(ESP_CALL);
+#undef ESP_CALL
+}

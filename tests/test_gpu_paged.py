@@ -1,0 +1,713 @@
+"""The paged KV cache on the GPU against plain forms in 64 bits: rotation and head norms, the append, attention over pages, the move of
+accepted rows, and a run of all of them.
+
+Tolerances.  A result stored in a type is off by half a step of it, H = finfo.eps / 2 (bf16 2^-8, fp32 2^-24), of its value.
+Rotation: y = A (x c - w s) after x = x0 inv gain, in fp32.  Cosine and sine: 1 step for the function, half for the rounded angle, half for
+the amplitude, so 2 steps = 4 halves; inv: (hd / 16 + 6) additions in a row, halved by the root, and 3 more; products and the sum: 4.
+All below 32 halves of a step of A (|x| + |w|) with hd up to 128.
+Attention: o = sum p v / sum p.  Scores are sums of hd products, off by hd 2^-24 sum |q k| at most; scale, reference and exponent add
+4 roundings of the largest score; a probability is off by that, by 2^-22 of the exponential instruction and by H where it is rounded for the
+product; the sums of n keys in fp32 by (n + 64) 2^-24 of sum p |v|.  Numerator and denominator: twice what the probabilities are off by."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from util import ROOT  # noqa: F401
+
+from paper_2603_17942_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+U = 2.0 ** -24
+
+
+def half(dt):
+    return torch.finfo(dt).eps / 2
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+# ---- the cache's layout, from its description ----------------------------------------------------------------
+
+def k_place(s, d, hd):
+    return s // 32 * hd * 32 + ((d // 16) * 64 + ((d // 8) % 2) * 32 + s % 32) * 8 + d % 8
+
+
+def v_place(s, d, hd):
+    key = s % 32
+    return s // 32 * hd * 32 + (((d // 32) * 2 + key // 16) * 64 + ((key // 4) % 2) * 32 + d % 32) * 8 + 4 * ((key // 8) % 2) + key % 4
+
+
+class Cache:
+    """A paged cache whose contents the test knows: K and V of every sequence as plain rows, everything else NaN."""
+
+    def __init__(self, dt, hkv, hd, page, lens, rows, seed, layers=1, layer=0, spare=3, rows_too=True, pages_per_seq=None, std=1.0):
+        g = gen(seed)
+        self.dt, self.hd, self.page, self.lens, self.rows, self.layer = dt, hd, page, lens, rows, layer
+        need = [(l + r + page - 1) // page for l, r in zip(lens, rows)]
+        n = sum(need) + spare
+        order = torch.randperm(n, generator=g).tolist()
+        stride = pages_per_seq or max(max(need), 1)
+        table = torch.full((len(lens), stride), 2 ** 31 - 1, dtype=torch.int32)     # entries nobody needs are no pages at all
+        at = 0
+        for b, k in enumerate(need):
+            table[b, :k] = torch.tensor(order[at:at + k], dtype=torch.int32)
+            at += k
+        self.table = table
+        kp = np.full((layers, n, hkv, page * hd), np.nan, dtype=np.float32)
+        vp = kp.copy()
+        self.k, self.v = [], []
+        d = np.arange(hd)
+        for b, (l, r) in enumerate(zip(lens, rows)):
+            k = torch.randn((l + r, hkv, hd), generator=g).mul_(std).to(dt)
+            v = torch.randn((l + r, hkv, hd), generator=g).to(dt)
+            self.k.append(k)
+            self.v.append(v)
+            for s in range(l + r if rows_too else l):
+                pg, inside = int(table[b, s // page]), s % page
+                kp[layer, pg][:, k_place(inside, d, hd)] = k[s].float().numpy()
+                vp[layer, pg][:, v_place(inside, d, hd)] = v[s].float().numpy()
+        shape = (layers, n, hkv, page, hd)
+        self.kv = B.PagedKv(torch.from_numpy(kp).to(dt).reshape(shape).cuda(), torch.from_numpy(vp).to(dt).reshape(shape).cuda(), table.cuda(),
+                            i32(lens), max(lens))
+        starts = np.concatenate([[0], np.cumsum(rows)]).tolist()
+        self.starts = starts
+        self.chunk = B.ChunkRows(i32(starts), starts[-1], max(max(rows), 1))
+
+    def plain(self, pool_k, pool_v, b, s):
+        """K and V of a slot, read back by the layout's description."""
+        d = np.arange(self.hd)
+        pg, inside = int(self.table[b, s // self.page]), s % self.page
+        k = pool_k[self.layer, pg].reshape(pool_k.shape[2], -1)[:, k_place(inside, d, self.hd)]
+        v = pool_v[self.layer, pg].reshape(pool_v.shape[2], -1)[:, v_place(inside, d, self.hd)]
+        return k, v
+
+
+def visible(l, r, anc=None):
+    """[rows, l + rows]: what the rows of a chunk see."""
+    m = torch.ones((r, l + r), dtype=torch.bool)
+    m[:, l:] = torch.tril(torch.ones((r, r), dtype=torch.bool)) if anc is None else anc
+    return m
+
+
+def attention(q, k, v, seen, scale):
+    """(out, tolerance) of one sequence in 64 bits: q [r, hq, hd], k, v [t, hkv, hd], seen [r, t]."""
+    G, dt, hd = q.shape[1] // k.shape[1], q.dtype, q.shape[2]
+    q, kd, vd = q.double(), k.double().repeat_interleave(G, 1), v.double().repeat_interleave(G, 1)
+    hidden = ~seen[:, None, :]
+    # what nobody sees may hold anything
+    kd = torch.where(seen.any(0)[:, None, None], kd, 0.0)
+    x = torch.einsum("rhd,thd->rht", q, kd)
+    size = torch.einsum("rhd,thd->rht", q.abs(), kd.abs()).masked_fill(hidden, 0.0) * scale
+    x = x.masked_fill(hidden, -math.inf) * scale
+    top = x.amax(-1, keepdim=True)
+    p = torch.where(hidden, 0.0, (x - top.clamp_min(-1e300)).exp())
+    total = p.sum(-1, keepdim=True)
+    p = p / total.clamp_min(1e-300)
+    out, weight = torch.zeros_like(q), torch.zeros_like(q)
+    for r in range(q.shape[0]):
+        s = seen[r]
+        out[r] = torch.einsum("ht,thd->hd", p[r][:, s], vd[s])
+        weight[r] = torch.einsum("ht,thd->hd", p[r][:, s], vd[s].abs())
+    off = U * (hd * size.amax(-1) + 4 * torch.where(hidden, 0.0, x.abs()).amax(-1)) + 2.0 ** -22 + (half(dt) if dt == torch.bfloat16 else 0.0)
+    n = seen.sum(-1).double()[:, None, None]
+    return out, half(dt) * out.abs() + (2 * off[..., None] + (n + 64) * U) * weight
+
+
+def check_attention(c, q, out, ancs=None, scale=None):
+    scale = c.hd ** -0.5 if scale is None else scale
+    for b, (l, r) in enumerate(zip(c.lens, c.rows)):
+        if r == 0:
+            continue
+        a, e = c.starts[b], c.starts[b + 1]
+        want, tol = attention(q[a:e].cpu(), c.k[b], c.v[b], visible(l, r, None if ancs is None else ancs[b]), scale)
+        got = out[a:e].cpu().double()
+        assert torch.isfinite(got).all(), b
+        worst = ((got - want).abs() - tol).max()
+        assert worst <= 0, (b, float(worst), float((got - want).abs().max()))
+
+
+def pack_anc(ancs, rows, words):
+    t = torch.zeros((sum(rows), words), dtype=torch.int64)
+    at = 0
+    for m in ancs:
+        for r in range(m.shape[0]):
+            for c in torch.nonzero(m[r]).flatten().tolist():
+                bit = 1 << (c % 64)
+                t[at + r, c // 64] |= bit - (1 << 64) if c % 64 == 63 else bit
+        at += m.shape[0]
+    return t.cuda()
+
+
+def queries(n, hq, hd, dt, seed, std=1.5):
+    return (torch.randn((n, hq, hd), generator=gen(seed)) * std).to(dt).cuda()
+
+
+ATTN = [  # dtype, hd, hq, hkv, page, lens, rows
+    ("bf16", 128, 32, 8, 64, [0], [1]),
+    ("bf16", 128, 32, 8, 64, [2047], [1]),
+    ("bf16", 128, 8, 2, 32, [31, 32, 33, 0, 127, 128, 129], [1] * 7),
+    ("bf16", 128, 32, 8, 64, [0, 1, 63, 64, 500], [1, 7, 8, 9, 0]),
+    ("bf16", 128, 4, 4, 96, [95, 96, 97, 191, 300], [33, 1, 2, 65, 31]),
+    ("bf16", 128, 28, 4, 128, [130, 700], [5, 40]),
+    ("bf16", 128, 8, 1, 32, [64, 5], [3, 300]),
+    ("bf16", 128, 16, 2, 64, [0, 1000], [257, 129]),
+    ("bf16", 128, 6, 2, 64, [4000, 3], [1, 1]),
+    ("bf16", 128, 5, 5, 32, [0, 0, 0], [1, 2, 3]),
+    ("bf16", 64, 8, 2, 64, [0, 33, 1000], [1, 31, 100]),
+    ("bf16", 64, 3, 1, 32, [77, 640], [1, 1]),
+    ("bf16", 64, 12, 12, 256, [300], [70]),
+    ("bf16", 128, 64, 1, 64, [200, 70], [1, 6]),
+    ("f32", 64, 4, 4, 32, [128], [60]),
+    ("f32", 64, 8, 2, 64, [0, 1, 31, 500], [1, 1, 1, 1]),
+    ("f32", 128, 8, 2, 64, [0, 65, 700], [40, 3, 130]),
+    ("f32", 128, 4, 1, 32, [1500], [1]),
+    ("f32", 128, 7, 7, 96, [95, 10], [33, 9]),
+]
+
+
+@pytest.mark.parametrize("dtype,hd,hq,hkv,page,lens,rows", ATTN)
+def test_attention_causal(dtype, hd, hq, hkv, page, lens, rows):
+    dt = DT[dtype]
+    c = Cache(dt, hkv, hd, page, lens, rows, 11, layers=2, layer=1)
+    q = queries(c.starts[-1], hq, hd, dt, 12)
+    out = torch.full_like(q, 7.0)
+    got = B.paged_attn(c.kv, 1, c.chunk, q, out=out)
+    assert got is out
+    check_attention(c, q, out)
+    assert c.kv.device_status() == 0
+    again = B.paged_attn(c.kv, 1, c.chunk, q)
+    assert torch.equal(out, again)                     # the same bits every time
+
+
+def random_tree(n, seed):
+    """Ancestor bits of a random tree's rows."""
+    g = np.random.default_rng(seed)
+    m = torch.zeros((n, n), dtype=torch.bool)
+    for r in range(n):
+        if r:
+            m[r] = m[int(g.integers(0, r))]
+        m[r, r] = True
+    return m
+
+
+@pytest.mark.parametrize("dtype,hd,hq,hkv,page,lens,rows", ATTN)
+def test_attention_tree(dtype, hd, hq, hkv, page, lens, rows):
+    dt = DT[dtype]
+    c = Cache(dt, hkv, hd, page, lens, rows, 21)
+    q = queries(c.starts[-1], hq, hd, dt, 22)
+    ancs = [random_tree(r, 100 + b) for b, r in enumerate(rows)]
+    words = (max(rows) + 63) // 64 + 1                 # a word more than is needed
+    out = B.paged_attn(c.kv, 0, c.chunk, q, anc=pack_anc(ancs, rows, words))
+    check_attention(c, q, out, ancs)
+    assert c.kv.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("n", [1, 5, 70])
+def test_rows_that_see_nothing_are_zero(dtype, hd, n):
+    dt = DT[dtype]
+    c = Cache(dt, 2, hd, 32, [0, 40], [n, n], 31)
+    q = queries(2 * n, 8, hd, dt, 32)
+    ancs = [random_tree(n, 5), random_tree(n, 6)]
+    ancs[0][::2] = False                               # no cache before them, no bit
+    ancs[1][::3] = False                               # these still see the cache
+    out = B.paged_attn(c.kv, 0, c.chunk, q, anc=pack_anc(ancs, [n, n], (n + 63) // 64))
+    assert (out[:n:2] == 0).all()
+    check_attention(c, q, out, ancs)
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("n,l", [(6, 50), (100, 20), (100, 0)])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_hidden_rows_that_are_not_finite_stay_hidden(dtype, hd, n, l, what):
+    """K and V of some of the chunk's rows are no numbers; rows that do not see them are as without them, others are not finite."""
+    dt = DT[dtype]
+    c = Cache(dt, 2, hd, 64, [l], [n], 41, rows_too=True)
+    bad = [n - 1, n // 2]
+    d = np.arange(hd)
+    for r in bad:
+        pg, inside = int(c.table[0, (l + r) // 64]), (l + r) % 64
+        c.kv.k[0, pg].view(2, -1)[:, torch.from_numpy(k_place(inside, d, hd)).cuda()] = what
+        c.kv.v[0, pg].view(2, -1)[:, torch.from_numpy(v_place(inside, d, hd)).cuda()] = what
+    q = queries(n, 8, hd, dt, 42)
+    for anc in (None, random_tree(n, 43)):
+        out = B.paged_attn(c.kv, 0, c.chunk, q, anc=None if anc is None else pack_anc([anc], [n], (n + 63) // 64)).cpu().double()
+        seen = visible(l, n, anc)
+        hit = seen[:, [l + r for r in bad]].any(1)
+        assert not torch.isfinite(out[hit]).all(-1).any() or not hit.any()
+        want, tol = attention(q.cpu()[~hit], c.k[0], c.v[0], seen[~hit], hd ** -0.5)
+        assert ((out[~hit] - want).abs() <= tol).all(), anc is None
+
+
+def test_value_not_finite_with_finite_key():
+    """Only V is no number: the rows behind it have an infinite or undefined output there, the rows before it their own."""
+    c = Cache(torch.bfloat16, 2, 128, 64, [10], [40], 44)
+    pg, inside = int(c.table[0, 0]), 10 + 20
+    c.kv.v[0, pg, 1].view(-1)[v_place(inside, 5, 128)] = math.nan
+    q = queries(40, 4, 128, torch.bfloat16, 45)
+    out = B.paged_attn(c.kv, 0, c.chunk, q).cpu().double()
+    want, tol = attention(q.cpu(), c.k[0], c.v[0], visible(10, 40), 128 ** -0.5)
+    assert not torch.isfinite(out[20:, 2:, 5]).any()
+    out[20:, 2:, 5] = want[20:, 2:, 5]
+    assert ((out - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype,hd,hq,hkv,len_,rows,bound", [
+    ("bf16", 128, 8, 2, 20011, 1, 20011), ("bf16", 128, 4, 1, 9000, 3, 33000), ("bf16", 128, 32, 8, 100, 1, 130000), ("bf16", 64, 2, 2, 12345, 40, 12345),
+    ("f32", 64, 2, 1, 9001, 2, 9001), ("f32", 128, 2, 1, 5001, 20, 70000)])
+def test_long_caches_and_loose_bounds(dtype, hd, hq, hkv, len_, rows, bound):
+    dt = DT[dtype]
+    c = Cache(dt, hkv, hd, 64, [len_], [rows], 51, pages_per_seq=(bound + rows + 63) // 64, std=2.0)
+    c.kv.len_bound = bound
+    q = queries(rows, hq, hd, dt, 52, 2.0)
+    out = B.paged_attn(c.kv, 0, c.chunk, q)
+    check_attention(c, q, out)
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 64)])
+def test_large_scores_and_other_scales(dtype, hd):
+    dt = DT[dtype]
+    c = Cache(dt, 2, hd, 32, [300, 0], [40, 12], 61, std=6.0)
+    q = queries(52, 6, hd, dt, 62, 6.0)
+    for scale in (1.0, 0.01, 1e-6):
+        check_attention(c, q, B.paged_attn(c.kv, 0, c.chunk, q, scale=scale), scale=scale)
+
+
+@pytest.mark.parametrize("shift", [0, 1, 3])
+def test_queries_at_any_stride_and_alignment(shift):
+    for dt in (torch.bfloat16, torch.float32):
+        c = Cache(dt, 2, 128, 32, [50, 9], [20, 3], 71)
+        buf = (torch.randn((23, 14 * 128 + shift), generator=gen(72))).to(dt).cuda()
+        q = buf[:, shift:shift + 8 * 128].unflatten(1, (8, 128))
+        out = B.paged_attn(c.kv, 0, c.chunk, q)
+        assert torch.equal(out, B.paged_attn(c.kv, 0, c.chunk, q.contiguous()))
+        check_attention(c, q, out)
+        raw = torch.zeros(23 * 8 * 128 + 1, dtype=dt, device="cuda")                     # an output that is not 16-byte aligned
+        odd = raw[1:].view(23, 8, 128)
+        B.paged_attn(c.kv, 0, c.chunk, q, out=odd)
+        assert torch.equal(odd, out)
+
+
+def test_rows_behind_the_last_sequence_and_scratch_do_not_matter():
+    c = Cache(torch.bfloat16, 8, 128, 64, [1500, 70], [2, 3], 81)
+    q = queries(9, 32, 128, torch.bfloat16, 82)
+    q[5:] = math.nan
+    rows = B.ChunkRows(i32(c.starts), 9, 5)
+    out = torch.full_like(q, 3.0)
+    n = B.paged_attn_scratch_bytes(c.kv, rows, 32)
+    assert n > 0
+    scratch = torch.full((n + 64,), 0xff, dtype=torch.uint8, device="cuda")
+    B.paged_attn(c.kv, 0, rows, q, out=out, scratch=scratch[:n])
+    assert (out[5:] == 3.0).all() and (scratch[n:] == 0xff).all()
+    check_attention(c, q, out)
+
+
+def test_sequences_may_share_pages():
+    c = Cache(torch.bfloat16, 2, 128, 32, [96, 96], [4, 4], 91)
+    c.kv.page_table[1, :3] = c.kv.page_table[0, :3]
+    c.k[1][:96], c.v[1][:96] = c.k[0][:96], c.v[0][:96]
+    q = queries(8, 8, 128, torch.bfloat16, 92)
+    check_attention(c, q, B.paged_attn(c.kv, 0, c.chunk, q))
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_malformed_sequences_are_left_alone(rows):
+    """Bad lengths and rows: the sequence's output is not touched, the others' is right, the status says what it was."""
+    for what, bit in (("len_over_bound", 1), ("len_negative", 1), ("len_past_table", 1), ("rows_over_max", 8), ("rows_descend", 8), ("rows_past_end", 8)):
+        c = Cache(torch.bfloat16, 2, 128, 32, [40, 50, 60], [rows] * 3, 101)
+        q = queries(3 * rows, 4, 128, torch.bfloat16, 102)
+        table = c.kv.page_table.shape[1] * 32
+        max_rows, starts = rows, list(c.starts)
+        if what == "len_over_bound":
+            c.kv.lens[2] = 61
+        elif what == "len_negative":
+            c.kv.lens[2] = -1
+        elif what == "len_past_table":
+            c.kv.lens[2], c.kv.len_bound = table - rows + 1, table
+        elif what == "rows_over_max":
+            max_rows = rows - 1 or 1
+            starts = [0, 0, 0, 3 * rows] if rows == 1 else [0, 0, 0, rows]
+        elif what == "rows_descend":
+            starts = [0, rows, 2 * rows, rows]
+        else:
+            starts = [0, rows, 2 * rows, 3 * rows + 1]
+            max_rows = rows + 1
+        ch = B.ChunkRows(i32(starts), 3 * rows, max_rows)
+        out = torch.full_like(q, 5.0)
+        B.paged_attn(c.kv, 0, ch, q, out=out)
+        assert c.kv.device_status() == bit, what
+        keep = 0 if what == "rows_over_max" else 2 * rows
+        assert (out[keep:] == 5.0).all(), what
+        for b in range(2 if keep else 0):
+            want, tol = attention(q[c.starts[b]:c.starts[b + 1]].cpu(), c.k[b], c.v[b], visible(c.lens[b], rows), 128 ** -0.5)
+            assert ((out[c.starts[b]:c.starts[b + 1]].cpu().double() - want).abs() <= tol).all(), what
+
+
+@pytest.mark.parametrize("hd,rows", [(128, 1), (128, 70), (64, 3)])
+@pytest.mark.parametrize("bad", [-1, 10 ** 6])
+def test_keys_in_pages_outside_the_pool_are_not_seen(hd, rows, bad):
+    c = Cache(torch.bfloat16, 2, hd, 32, [200], [rows], 111)
+    c.kv.page_table[0, 2] = bad
+    q = queries(rows, 4, hd, torch.bfloat16, 112)
+    out = B.paged_attn(c.kv, 0, c.chunk, q)
+    seen = visible(200, rows)
+    seen[:, 64:96] = False
+    want, tol = attention(q.cpu(), c.k[0], c.v[0], seen, hd ** -0.5)
+    assert ((out.cpu().double() - want).abs() <= tol).all()
+    assert c.kv.device_status() == 16 and c.kv.device_status() == 0
+
+
+def test_attention_in_a_graph_follows_lengths_rows_and_pages():
+    """A captured call replays with what the device holds by then."""
+    c = Cache(torch.bfloat16, 2, 128, 32, [900, 64], [3, 2], 121)
+    c.kv.len_bound = 1000
+    q = queries(5, 8, 128, torch.bfloat16, 122)
+    lens, table = c.kv.lens.clone(), c.kv.page_table.clone()
+    scratch = torch.empty(B.paged_attn_scratch_bytes(c.kv, c.chunk, 8), dtype=torch.uint8, device="cuda")
+    out = torch.zeros_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        B.paged_attn(c.kv, 0, c.chunk, q, out=out, scratch=scratch)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            B.paged_attn(c.kv, 0, c.chunk, q, out=out, scratch=scratch)
+    torch.cuda.synchronize()
+    for step, (a, b, swap) in enumerate([(900, 64, False), (333, 61, False), (0, 0, True), (900, 64, False)]):
+        c.kv.lens.copy_(i32([a, b]))
+        c.kv.page_table.copy_(table if not swap else table.flip(1).clamp(0, c.kv.k.shape[1] - 1))
+        want = B.paged_attn(c.kv, 0, c.chunk, q)
+        out.fill_(-1.0)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        if not swap:
+            assert torch.equal(out, want), step
+    c.kv.lens.copy_(lens)
+    check_attention(c, q, out)
+
+
+def test_two_streams_with_a_scratch_each():
+    c = Cache(torch.bfloat16, 8, 128, 64, [3000, 100], [2, 1], 131)
+    qs = [queries(3, 32, 128, torch.bfloat16, 132 + i) for i in range(2)]
+    want = [B.paged_attn(c.kv, 0, c.chunk, q) for q in qs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        for s, q in zip(streams, qs):
+            with torch.cuda.stream(s):
+                got.append(B.paged_attn(c.kv, 0, c.chunk, q))
+    torch.cuda.synchronize()
+    for i, o in enumerate(got):
+        assert torch.equal(o, want[i % 2])
+
+
+# ---- rotation, norms, append ------------------------------------------------------------------------------------
+
+def rotated(x, gain, pos, rot, theta, interleaved, factor, orig, low, high, amp, eps=1e-6):
+    """(y, tolerance) in 64 bits: [rows, heads, hd]."""
+    dt, hd = x.dtype, x.shape[-1]
+    x = x.double()
+    if gain is not None:
+        x = x / (x.square().mean(-1, keepdim=True) + eps).sqrt() * gain.double()
+    y, size = x.clone(), x.abs().clone()
+    for i in range(rot // 2):
+        f = theta ** (-2.0 * i / rot)
+        keep = min(1.0, max(0.0, (orig * f / (2 * math.pi) - low) / (high - low))) if orig else 0.0
+        a = pos.double() * (f * (keep + (1 - keep) / factor))
+        c, s = amp * a.cos()[:, None], amp * a.sin()[:, None]
+        j, k = (2 * i, 2 * i + 1) if interleaved else (i, i + rot // 2)
+        y[..., j] = x[..., j] * c - x[..., k] * s
+        y[..., k] = x[..., k] * c + x[..., j] * s
+        size[..., j] = size[..., k] = max(amp, 1.0) * (x[..., j].abs() + x[..., k].abs())
+    exact = (gain is None) & (torch.arange(hd) >= rot)          # passed on as it is
+    return y, torch.where(exact, 0.0, half(dt) * y.abs() + 32 * U * size)
+
+
+ROPE = [  # hd, rot, interleaved, factor, orig, amplitude, norm
+    (128, 128, False, 1.0, 0, 1.0, False), (128, 128, False, 8.0, 8192, 1.2, True), (128, 64, True, 1.0, 0, 1.0, False), (128, 32, False, 4.0, 0, 1.0, True),
+    (128, 96, True, 2.0, 4096, 1.1, True), (64, 64, False, 1.0, 0, 1.0, True), (64, 16, True, 1.0, 0, 1.0, False), (64, 48, False, 32.0, 1024, 0.9, False),
+    (128, 16, False, 1.0, 0, 1.0, True),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd,rot,interleaved,factor,orig,amp,norm", ROPE)
+@pytest.mark.parametrize("rows,hq,hkv", [(1, 32, 8), (7, 5, 1), (33, 28, 4)])
+def test_rope_qk(dtype, hd, rot, interleaved, factor, orig, amp, norm, rows, hq, hkv):
+    dt, g = DT[dtype], gen(hd + rot + rows)
+    x = torch.randn((rows, hq + 2 * hkv, hd), generator=g).to(dt)
+    qg, kg = ((1 + 0.2 * torch.randn(hd, generator=g)).to(dt) for _ in range(2))
+    pos = torch.randint(0, 1 << 20, (rows,), generator=g, dtype=torch.int32)
+    pos[0] = (1 << 20) - 1 if rows > 1 else 0
+    xc = x.cuda()
+    q, k = xc[:, :hq], xc[:, hq:hq + hkv]
+    spec = B.rope_spec(hd, rot, 5e5, interleaved, factor, orig, 1.0, 4.0, amp)
+    args = dict(q_gain=qg.cuda(), k_gain=kg.cuda()) if norm else {}
+    qo, ko = B.rope_qk(q, k, pos.cuda(), spec, **args)
+    for got, t, gain in ((qo, x[:, :hq], qg), (ko, x[:, hq:hq + hkv], kg)):
+        want, tol = rotated(t, gain if norm else None, pos, rot, 5e5, interleaved, factor, orig, 1.0, 4.0, float(np.float32(amp)))
+        assert ((got.cpu().double() - want).abs() <= tol).all()
+    # one of the two, and in place: the same values, the rest of the rows as it was
+    only, none = B.rope_qk(None, k, pos.cuda(), spec, **args)[::-1]
+    assert none is None and torch.equal(only, ko)
+    B.rope_qk(q, k, pos.cuda(), spec, q_out=q, k_out=k, **args)
+    assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(xc[:, hq + hkv:].cpu(), x[:, hq + hkv:])
+
+
+@pytest.mark.parametrize("rows", [1023, 1025, 2050])
+def test_rope_many_rows(rows):
+    for dt in (torch.bfloat16, torch.float32):
+        x = torch.randn((rows, 6, 128), generator=gen(rows)).to(dt)
+        pos = torch.arange(rows, dtype=torch.int32) * 7
+        q, k = B.rope_qk(x.cuda()[:, :4], x.cuda()[:, 4:], pos.cuda(), B.rope_spec(128, 128, 1e4))
+        want, tol = rotated(x, None, pos, 128, 1e4, False, 1.0, 0, 1.0, 4.0, 1.0)
+        assert ((torch.cat([q, k], 1).cpu().double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rope_at_any_alignment(dtype):
+    dt = DT[dtype]
+    buf = torch.randn((5, 6 * 64 + 3), generator=gen(3)).to(dt).cuda()
+    x = buf[:, 3:].unflatten(1, (6, 64))
+    pos = i32([0, 1, 5, 100, 7])
+    spec = B.rope_spec(64, 32, interleaved=True)
+    want = B.rope_qk(x.contiguous(), None, pos, spec)[0]
+    out = torch.zeros((5, 6 * 64 + 1), dtype=dt, device="cuda")
+    B.rope_qk(x, None, pos, spec, q_out=out[:, 1:].unflatten(1, (6, 64)))
+    assert torch.equal(out[:, 1:].unflatten(1, (6, 64)), want) and (out[:, 0] == 0).all()
+
+
+APPEND = [  # dtype, hd, hq, hkv, page, lens, rows
+    ("bf16", 128, 32, 8, 64, [0], [1]), ("bf16", 128, 32, 8, 64, [63, 64, 100, 0], [1, 1, 1, 1]), ("bf16", 128, 4, 2, 32, [31, 5, 0], [2, 0, 70]),
+    ("bf16", 128, 7, 1, 96, [95, 0], [200, 33]), ("bf16", 64, 8, 4, 32, [17, 3], [5, 40]), ("f32", 128, 4, 2, 64, [30, 62], [3, 66]),
+    ("f32", 64, 4, 4, 32, [1, 0, 0], [1, 31, 32]), ("bf16", 128, 8, 2, 128, [129, 7], [130, 1100]), ("f32", 64, 2, 1, 64, [3], [1200]),
+    ("bf16", 64, 3, 3, 32, [0, 1, 2, 3, 4, 5, 6, 7] * 9, [1, 2, 0, 3] * 18),
+]
+
+
+@pytest.mark.parametrize("dtype,hd,hq,hkv,page,lens,rows", APPEND)
+@pytest.mark.parametrize("how", ["plain", "rope", "norm_given"])
+def test_append(dtype, hd, hq, hkv, page, lens, rows, how):
+    dt, g = DT[dtype], gen(7 * hd + len(lens))
+    c = Cache(dt, hkv, hd, page, lens, rows, 201, layers=2, layer=1, rows_too=False)
+    n = c.starts[-1]
+    x = torch.randn((n + 2, hq + 2 * hkv, hd), generator=g).to(dt)
+    xc = x.cuda()
+    ch = B.ChunkRows(c.chunk.row0, n + 2, c.chunk.max_rows)              # two rows behind the last sequence
+    q, k, v = xc[:, :hq], xc[:, hq:hq + hkv], xc[:, hq + hkv:]
+    slot = torch.tensor([l + i for l, r in zip(lens, rows) for i in range(r)] + [0, 0], dtype=torch.int32)
+    pos = torch.randint(0, 5000, (n + 2,), generator=g, dtype=torch.int32) if how == "norm_given" else slot
+    qg, kg = ((1 + 0.2 * torch.randn(hd, generator=g)).to(dt) for _ in range(2))
+    spec = None if how == "plain" else B.rope_spec(hd, hd if how == "rope" else hd // 2, 1e4, how != "rope", 2.0, 64, 1.0, 4.0, 1.0)
+    more = dict(positions=pos.cuda(), q_gain=qg.cuda(), k_gain=kg.cuda()) if how == "norm_given" else {}
+    before = [t.cpu().float().numpy() for t in (c.kv.k, c.kv.v)]
+    q_out = torch.full((n + 2, hq, hd), 9.0, dtype=dt, device="cuda")
+    B.paged_append(c.kv, 1, ch, q, k, v, rope=spec, q_out=q_out, **more)
+    after = [t.cpu().float().numpy() for t in (c.kv.k, c.kv.v)]
+    args = (0, 1e4, False, 1.0, 0, 1.0, 4.0, 1.0) if spec is None else (spec.rot_dim, 1e4, how != "rope", 2.0, 64, 1.0, 4.0, 1.0)
+    norm = how == "norm_given"
+    want_q, tol_q = rotated(x[:, :hq], qg if norm else None, pos, *args)
+    want_k, tol_k = rotated(x[:, hq:hq + hkv], kg if norm else None, pos, *args)
+    assert ((q_out[:n].cpu().double() - want_q[:n]).abs() <= tol_q[:n]).all() and (q_out[n:] == 9.0).all()
+    at = 0
+    touched = [np.zeros(t.shape, dtype=bool) for t in before]
+    d = np.arange(hd)
+    for b, (l, r) in enumerate(zip(lens, rows)):
+        for i in range(r):
+            gk, gv = c.plain(after[0], after[1], b, l + i)
+            assert (np.abs(gk - want_k[at].numpy()) <= tol_k[at].numpy()).all(), (b, i)
+            assert (gv == x[at, hq + hkv:].float().numpy()).all(), (b, i)
+            pg, inside = int(c.table[b, (l + i) // page]), (l + i) % page
+            touched[0][1, pg].reshape(hkv, -1)[:, k_place(inside, d, hd)] = True
+            touched[1][1, pg].reshape(hkv, -1)[:, v_place(inside, d, hd)] = True
+            at += 1
+    for t, a, m in zip(before, after, touched):          # all other slots, pages and layers hold what they held
+        assert ((t == a) | (np.isnan(t) & np.isnan(a)) | m).all()
+    assert c.kv.device_status() == 0
+    pool = c.kv.k.clone()                                 # without queries, at other strides: the same cache
+    B.paged_append(c.kv, 1, ch, None, k.contiguous(), v.contiguous(), rope=spec, **more)
+    assert torch.equal(pool.view(torch.int16 if dt == torch.bfloat16 else torch.int32), c.kv.k.view(torch.int16 if dt == torch.bfloat16 else torch.int32))
+
+
+@pytest.mark.parametrize("rows", [2, 40])
+def test_append_skips_what_is_malformed(rows):
+    for what, bit in (("len", 1), ("rows", 8), ("page", 16)):
+        c = Cache(torch.bfloat16, 2, 128, 32, [10, 20], [rows, rows], 211, rows_too=False)
+        x = torch.randn((2 * rows, 4, 128), generator=gen(5)).to(torch.bfloat16).cuda()
+        starts = list(c.starts)
+        if what == "len":
+            c.kv.lens[1] = 21
+        elif what == "rows":
+            starts[2] = 2 * rows + 1
+        else:
+            c.kv.page_table[1, 0] = c.kv.k.shape[1]
+        before = c.kv.k.clone()
+        q_out = torch.full((2 * rows, 4, 128), 9.0, dtype=torch.bfloat16, device="cuda")
+        B.paged_append(c.kv, 0, B.ChunkRows(i32(starts), 2 * rows, rows), x, x[:, :2], x[:, 2:], q_out=q_out)
+        assert c.kv.device_status() == bit
+        assert torch.equal(q_out[:rows], x[:rows])
+        k, v = B.paged_load(c.kv, 0, 0, 10, rows)
+        assert torch.equal(k, x[:rows, :2]) and torch.equal(v, x[:rows, 2:])
+        if what == "page":                               # the queries are there, the slots of that page are not
+            assert torch.equal(q_out, x)
+            k, _ = B.paged_load(c.kv, 0, 1, 20, rows)
+            assert (k[:min(rows, 12)] == 0).all() and torch.equal(k[12:], x[rows + 12:, :2])
+            assert c.kv.device_status() == 16
+        else:
+            assert (q_out[rows:] == 9.0).all()
+            pages = [int(p) for p in c.table[1] if p < before.shape[1]]
+            assert torch.equal(before[:, pages].view(torch.int16), c.kv.k[:, pages].view(torch.int16))
+
+
+def test_load_gives_back_what_is_in_the_slots():
+    for dt in (torch.bfloat16, torch.float32):
+        c = Cache(dt, 3, 64, 96, [200, 50], [0, 0], 221, layers=3, layer=2)
+        for b, (first, n) in enumerate([(90, 110), (0, 50)]):
+            k, v = B.paged_load(c.kv, 2, b, first, n)
+            assert torch.equal(k.cpu(), c.k[b][first:first + n]) and torch.equal(v.cpu(), c.v[b][first:first + n])
+
+
+# ---- commit --------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,hd,page", [("bf16", 128, 64), ("bf16", 64, 32), ("f32", 128, 32), ("f32", 64, 96)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_commit(dtype, hd, page, in_place):
+    """Paths of one to nine rows, among them rows whose place is another's source, over page borders."""
+    dt = DT[dtype]
+    paths = [[0], [0, 1], [0, 2], [0, 1, 2, 3], [0, 2, 4, 6, 8], [0, 3, 4, 5, 20, 21, 22, 23, 24], [], [0, 24], [0, 1, 3, 4]]
+    lens = [0, 31, 30, 63, 60, 90, 17, 95, 28]
+    c = Cache(dt, 2, hd, page, lens, [25] * 9, 231)
+    layers = 3
+    ks = torch.cat([c.kv.k + i for i in range(layers)])
+    vs = torch.cat([c.kv.v - i for i in range(layers)])
+    kv = B.PagedKv(ks, vs, c.kv.page_table, i32(lens), max(lens))
+    plain = [[[t.clone() for t in B.paged_load(kv, layer, b, 0, lens[b] + 25)] for b in range(9)] for layer in range(layers)]
+    assert kv.device_status() == 0
+    acc = i32([p + [-7] * (9 - len(p)) for p in paths])
+    before = kv.lens.clone()
+    out = None if in_place else torch.full((9,), -1, dtype=torch.int32, device="cuda")
+    got = B.paged_commit(kv, i32([len(p) for p in paths]), acc, out)
+    assert got.tolist() == [l + len(p) for l, p in zip(lens, paths)]
+    assert (got is kv.lens) == in_place and (in_place or torch.equal(kv.lens, before))
+    for layer in range(layers):
+        for b, p in enumerate(paths):
+            for now, was in zip(B.paged_load(kv, layer, b, 0, lens[b] + 25), plain[layer][b]):
+                want = was.clone()
+                for i, r in enumerate(p):
+                    want[lens[b] + i] = was[lens[b] + r]
+                assert torch.equal(now, want), (layer, b)
+    assert kv.device_status() == 0
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_commit_refuses_paths_that_are_none(in_place):
+    c = Cache(torch.bfloat16, 2, 128, 32, [10, 10], [20, 20], 241)
+    for n, path, bit in ((10, [0] * 9, 32), (-1, [0] * 9, 32), (3, [0, 2, 2], 32), (3, [0, 3, 1], 32), (2, [0, 0], 32), (2, [0, 2 ** 31 - 5], 32), (2, [0, 200], 32)):
+        kv = B.PagedKv(c.kv.k.clone(), c.kv.v.clone(), c.kv.page_table, i32([10, 10]), 10)
+        k0 = kv.k.clone()
+        acc = i32([path + [0] * (9 - len(path)), [0, 5] + [0] * 7])
+        out = B.paged_commit(kv, i32([n, 2]), acc, None if in_place else torch.zeros(2, dtype=torch.int32, device="cuda"))
+        assert out.tolist() == [10, 12] and kv.device_status() == bit, (n, path)
+        pages = [int(p) for p in c.table[0]]
+        assert torch.equal(kv.k[:, pages].view(torch.int16), k0[:, pages].view(torch.int16))
+        k, _ = B.paged_load(kv, 0, 1, 11, 1)
+        assert torch.equal(k.cpu()[0], c.k[1][15])
+    kv = B.PagedKv(c.kv.k.clone(), c.kv.v.clone(), c.kv.page_table, i32([10, 11]), 10)          # a length above its bound
+    out = B.paged_commit(kv, i32([1, 2]), i32([[0] * 9, [0, 5] + [0] * 7]), None if in_place else torch.zeros(2, dtype=torch.int32, device="cuda"))
+    assert out.tolist() == [11, 11] and kv.device_status() == 1
+
+
+# ---- together --------------------------------------------------------------------------------------------------------
+
+def test_verified_steps_over_a_paged_cache():
+    """A prompt by chunks, then three steps of tree block, attention, commit: outputs of every step against attention over the plain rows
+    that the sequences have by then."""
+    dt, hq, hkv, hd, page = torch.bfloat16, 8, 2, 128, 32
+    g = gen(301)
+    batch, prompts = 3, [70, 5, 33]
+    kv = B.PagedKv.zeros(1, 40, hkv, page, hd, batch, 8, dt)
+    kv.k.fill_(math.nan)
+    kv.v.fill_(math.nan)
+    kv.page_table.copy_(torch.randperm(40, generator=g)[:24].view(3, 8).to(torch.int32))
+    spec = B.rope_spec(hd, hd, 1e4)
+    plain_k, plain_v = [torch.zeros((0, hkv, hd), dtype=dt) for _ in prompts], [torch.zeros((0, hkv, hd), dtype=dt) for _ in prompts]
+    lens = [0] * batch
+
+    def run(rows, trees):
+        starts = np.concatenate([[0], np.cumsum(rows)]).tolist()
+        ch = B.ChunkRows(i32(starts), starts[-1], max(rows))
+        x = torch.randn((starts[-1], hq + 2 * hkv, hd), generator=g).to(dt).cuda()
+        pos = None
+        if trees is not None:
+            pos = i32([lens[b] + int(t.sum(1)[r]) - 1 for b, t in enumerate(trees) for r in range(rows[b])])
+        q = B.paged_append(kv, 0, ch, x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], rope=spec, positions=pos)
+        out = B.paged_attn(kv, 0, ch, q, anc=None if trees is None else pack_anc(trees, rows, 1))
+        new = []
+        for b in range(batch):
+            k, v = (t.cpu() for t in B.paged_load(kv, 0, b, lens[b], rows[b]))
+            assert torch.equal(v, x[starts[b]:starts[b + 1], hq + hkv:].cpu())
+            new.append((k, v))
+            want, tol = attention(q[starts[b]:starts[b + 1]].cpu(), torch.cat([plain_k[b], k]), torch.cat([plain_v[b], v]),
+                                  visible(lens[b], rows[b], None if trees is None else trees[b]), hd ** -0.5)
+            assert ((out[starts[b]:starts[b + 1]].cpu().double() - want).abs() <= tol).all(), b
+        return new
+
+    left = list(prompts)
+    while any(left):
+        rows = [min(40, n) for n in left]
+        new = run(rows, None)
+        for b in range(batch):
+            plain_k[b], plain_v[b] = torch.cat([plain_k[b], new[b][0]]), torch.cat([plain_v[b], new[b][1]])
+            lens[b] += rows[b]
+            left[b] -= rows[b]
+        kv.lens.copy_(i32(lens))
+        kv.len_bound = max(lens)
+    for step in range(3):
+        rows = [12, 7, 20]
+        trees = [random_tree(n, 310 + step + b) for b, n in enumerate(rows)]
+        new = run(rows, trees)
+        paths = []
+        for b, t in enumerate(trees):                     # down to a leaf, four rows at most
+            paths.append(torch.nonzero(t[rows[b] - 1 - step]).flatten().tolist()[:4])
+        B.paged_commit(kv, i32([len(p) for p in paths]), i32([p + [0] * (9 - len(p)) for p in paths]))
+        for b, p in enumerate(paths):
+            plain_k[b], plain_v[b] = torch.cat([plain_k[b], new[b][0][p]]), torch.cat([plain_v[b], new[b][1][p]])
+            lens[b] += len(p)
+            k, v = B.paged_load(kv, 0, b, 0, lens[b])
+            assert torch.equal(k.cpu(), plain_k[b]) and torch.equal(v.cpu(), plain_v[b])
+        assert kv.lens.tolist() == lens
+        kv.len_bound = max(lens)
+    assert kv.device_status() == 0
+
+
+def test_paged_attention_agrees_with_the_contiguous_cache():
+    """The same rows in the framework's contiguous cache and in pages: the two attentions agree to their types."""
+    from paper_2603_17942_amd import synth
+    shape = synth.SHAPES["llama3_8b"].replace(n_layers=1, vocab=64, d_ff=64, d_model=64)
+    eng = B.Engine(shape, synth.make_weights(shape, device="cuda"), 1, 64, 1024)
+    L, n = 300, 40
+    c = Cache(torch.bfloat16, 8, 128, 64, [L], [n], 321)
+    kvc = B.KvCache(shape, [512])
+    eng.kv_store(kvc, 0, 0, 0, c.k[0].cuda().contiguous(), c.v[0].cuda().contiguous())
+    kvc.set_len([L])
+    blk = B.BlockBuffers(1, n, 0, B.LAYOUT_PER_NODE)
+    blk.upload_trees([[1] * n], [[-1] + list(range(n - 1))])
+    eng.block_from_tree(blk)
+    q = queries(n, 32, 128, torch.bfloat16, 322)
+    want = torch.zeros_like(q)
+    eng.attn_tree(blk, kvc, 0, q, want)
+    check_attention(c, q, want)
+    check_attention(c, q, B.paged_attn(c.kv, 0, c.chunk, q))
+    assert torch.equal(blk.anc.view(n, -1), pack_anc([torch.tril(torch.ones((n, n), dtype=torch.bool))], [n], 1))
