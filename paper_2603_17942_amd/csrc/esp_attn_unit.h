@@ -108,22 +108,7 @@ __device__ __forceinline__ unsigned attn_window(const uint64_t* anc, int anc_wor
   return (unsigned)w & (left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u);
 }
 
-// is there an infinity or NaN (all bits of an exponent set) among a fragment's values
-__device__ __forceinline__ bool attn_not_finite(bf16x8_t f) {
-  const u32x4_t w = __builtin_bit_cast(u32x4_t, f);
-  unsigned any = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) any |= (w[i] & 0x7f807f80u) + 0x00800080u;
-  return (any & 0x80008000u) != 0;
-}
-__device__ __forceinline__ bool attn_not_finite(f32x8_t f) {
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) any |= (__float_as_uint(f[i]) & 0x7f800000u) == 0x7f800000u;
-  return any;
-}
-
-// takes infinities and NaN out of a fragment, and ones in their places
+// takes infinities and NaN (all bits of the exponent set) out of a fragment; ones in their places, zeros elsewhere
 __device__ __forceinline__ bf16x8_t attn_take_odd(bf16x8_t& f) {
   u32x4_t w = __builtin_bit_cast(u32x4_t, f), ones;
 #pragma unroll
@@ -145,26 +130,16 @@ __device__ __forceinline__ f32x8_t attn_take_odd(f32x8_t& f) {
   }
   return ones;
 }
-// A unit some of whose keys not every column sees, with infinities or NaN among its values: in the product with P they would reach
-// the columns that do not see them, as 0 times them.  They are taken out, and a column that does see one gets an infinity there.
-// v: fragment (db, u) at 2 db + u; seen: bits of this lane's keys.
-template <typename T, int DB>
-__device__ __forceinline__ void attn_keep_hidden(typename AttnFrag<T>::type (&v)[2 * DB], unsigned seen, f32x16_t (&o)[DB]) {
-  typename AttnFrag<T>::type s[2];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) s[i >> 3][i & 7] = from_f32<T>((seen >> (8 * (i >> 2) + (i & 3))) & 1u ? 1.f : 0.f);
-#pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    f32x16_t n;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) n[i] = 0.f;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) n = attn_mma(attn_take_odd(v[2 * db + u]), s[u], n);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[db][i] += n[i] > 0.f ? __builtin_inff() : 0.f;
-  }
+__device__ __forceinline__ bool attn_any(bf16x8_t f) {
+  const u32x4_t w = __builtin_bit_cast(u32x4_t, f);
+  return (w[0] | w[1] | w[2] | w[3]) != 0;
 }
-
+__device__ __forceinline__ bool attn_any(f32x8_t f) {
+  float any = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) any += f[i];
+  return any > 0.f;
+}
 // V of keys past the sequence's end (left keys of the unit are there) as zeros: memory there may hold anything, and 0 times NaN is NaN
 __device__ __forceinline__ f32x8_t attn_zero_tail(f32x8_t f, int u, int lane, int left) {
 #pragma unroll
@@ -180,4 +155,80 @@ __device__ __forceinline__ bf16x8_t attn_zero_tail(bf16x8_t f, int u, int lane, 
     w[i] &= k + 1 < left ? 0xffffffffu : k < left ? 0x0000ffffu : 0u;
   }
   return __builtin_bit_cast(bf16x8_t, w);
+}
+
+// In a unit some of whose keys not every column sees, infinities and NaN among the values would reach the columns that do not see them, as 0
+// times them.  So they are taken out there, and where that took any out (odd) the columns that do see them get theirs when all else is
+// done: this adds an infinity for each to the outputs.  v: the unit's fragments in memory; seen: bits of this lane's keys.
+template <typename T, int HD>
+__device__ __forceinline__ void attn_add_odd(const T* v, unsigned seen, int left, int lane, f32x16_t (&o)[HD / 32]) {
+  typedef typename AttnFrag<T>::type frag_t;
+  frag_t s[2];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i >> 3][i & 7] = from_f32<T>((seen >> (8 * (i >> 2) + (i & 3))) & 1u ? 1.f : 0.f);
+#pragma unroll
+  for (int db = 0; db < HD / 32; ++db) {
+    f32x16_t n;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) n[i] = 0.f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      frag_t f = attn_zero_tail(*reinterpret_cast<const frag_t*>(v + (2 * db + u) * 512 + lane * 8), u, lane, left);
+      n = attn_mma(attn_take_odd(f), s[u], n);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] += n[i] > 0.f ? __builtin_inff() : 0.f;
+  }
+}
+
+// One unit out of LDS.  k, v: this lane's share of the unit's first K and first V fragment, fragments FRAG bytes apart, of V (db, u) at
+// 2 db + u.  window: bits of the column's keys, looked at where `masked`; left: keys of the sequence in the unit.
+// Fragments are read PF matrix steps ahead and held there (left to itself the compiler reads them all and runs out of registers); the matrix
+// phases run at raised wave priority, so that of the waves of a SIMD one has matrix work and the others fill in with their softmax.
+template <typename T, int HD>
+__device__ __forceinline__ void attn_unit(const unsigned char* k, const unsigned char* v, bool masked, unsigned window, int left, int lane, float scale,
+                                          const typename AttnFrag<T>::type (&q)[HD / 16], f32x16_t (&o)[HD / 32], float& m, float& l, bool& odd) {
+  typedef typename AttnFrag<T>::type frag_t;
+  constexpr int NS = HD / 16, DB = HD / 32, FRAG = 512 * sizeof(T), PF = sizeof(T) == 2 ? 3 : 1, NF = PF + 1;
+  frag_t fr[NF];
+  // fragment j: K steps 0 .. NS - 1, then V in the order (u, db)
+  auto frag_at = [&](int j) {
+    const int i = j - NS;
+    return j < NS ? *reinterpret_cast<const frag_t*>(k + j * FRAG) : *reinterpret_cast<const frag_t*>(v + (i % DB * 2 + i / DB) * FRAG);
+  };
+  f32x16_t sc;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+  for (int j = 0; j < PF; ++j) fr[j] = frag_at(j);
+  __builtin_amdgcn_s_setprio(2);
+#pragma unroll
+  for (int j = 0; j < NS; ++j) {
+    fr[(j + PF) % NF] = frag_at(j + PF);
+    __builtin_amdgcn_sched_barrier(0);
+    sc = attn_mma(fr[j % NF], q[j], sc);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __builtin_amdgcn_s_setprio(0);
+  frag_t p[2];
+  attn_softmax<T, DB>(sc, masked, window >> (4 * (lane >> 5)), scale, o, m, l, p);
+  if (masked) {
+#pragma unroll
+    for (int i = 0; i < 2 * DB; ++i) {
+      frag_t f = *reinterpret_cast<const frag_t*>(v + (i % DB * 2 + i / DB) * FRAG);
+      if (left < 32) f = attn_zero_tail(f, i / DB, lane, left);
+      odd |= attn_any(attn_take_odd(f));
+      o[i % DB] = attn_mma(f, p[i / DB], o[i % DB]);
+    }
+    return;
+  }
+  __builtin_amdgcn_s_setprio(2);
+#pragma unroll
+  for (int i = 0; i < 2 * DB; ++i) {              // i = u DB + db
+    if (i + PF < 2 * DB) fr[(NS + i + PF) % NF] = frag_at(NS + i + PF);
+    __builtin_amdgcn_sched_barrier(0);
+    o[i % DB] = attn_mma(fr[(NS + i) % NF], p[i / DB], o[i % DB]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __builtin_amdgcn_s_setprio(0);
 }

@@ -142,14 +142,20 @@ def test_rope_make_frequencies(rot, factor, orig):
         assert abs(r.turns[0] * 2 * math.pi - 1) < 1e-15
 
 
-def test_scratch_covers_the_splits(lib):
-    """Partials of a split are (head_dim + 2) floats a row and head; a call without splits wants nothing."""
-    for batch, rows, bound, nq, nkv, hd in ((1, 1, 2000, 32, 8, 128), (1, 1, 10 ** 6, 8, 1, 64), (64, 64, 200, 32, 8, 128), (1, 8192, 0, 32, 8, 128),
-                                            (3, 9, 0, 6, 2, 64)):
-        kv, ch = paged(batch=batch, table_stride=20000, len_bound=bound, n_kv_heads=nkv, head_dim=hd), chunk(total_rows=rows, max_rows=max(1, rows // batch))
-        n = lib.esp_paged_attn_scratch_bytes(C.byref(kv), C.byref(ch), nq)
-        one = rows * nq * (hd + 2) * 4
-        assert n % one == 0 and (n == 0 or n // one >= 2), (batch, rows, bound, n, one)
+def test_scratch_is_for_work_that_is_cut(lib):
+    """Where every workgroup has whole items nothing is wanted; where work is cut, what it wants does not grow with the batch's rows
+    beyond what all workgroups' pieces take, and a refused call wants nothing."""
+    def need(batch, rows, max_rows, bound, nq=32, nkv=8, hd=128, dtype=B.ESP_BF16):
+        kv, ch = paged(batch=batch, table_stride=30000, len_bound=bound, n_kv_heads=nkv, head_dim=hd, dtype=dtype), chunk(total_rows=rows, max_rows=max_rows)
+        return lib.esp_paged_attn_scratch_bytes(C.byref(kv), C.byref(ch), nq)
+    assert need(1, 1, 1, 40) == 0 and need(3, 9, 3, 0) == 0                   # a few keys
+    assert need(1, 8192, 8192, 0) == 0                                          # enough items
+    assert need(1, 1, 1, 2000) > 0 and need(1, 1, 1, 10 ** 6, 8, 1, 64) > 0
+    assert need(1, 300, 300, 2000) > 0 and need(1, 300, 300, 2000, dtype=B.ESP_F32) > 0
+    for hd in (64, 128):
+        for rows in (1, 8, 33, 500):
+            for bound in (0, 100, 5000, 10 ** 6):
+                assert need(4, 4 * rows, rows, bound, hd=hd) <= 2 * 512 * (32 * (hd + 2) * 4 + 16) * (1 if rows <= 8 else 4) + 4096
     assert lib.esp_paged_attn_scratch_bytes(C.byref(paged()), C.byref(chunk()), 12) == 0
 
 
