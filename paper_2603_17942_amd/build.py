@@ -20,8 +20,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + os.path.j
 
 # per-source additions: the attention kernels never produce or test NaN / infinity (masked scores are a
 # large finite negative), and telling the compiler so drops the canonicalising copy in front of
-# every maximum of the online softmax
-EXTRA_FLAGS = {"esp_attn.hip": ["-fno-honor-nans"]}
+# every maximum of the online softmax; the paged attention's scores are wanted in VGPRs, where its softmax reads
+# them, also in kernels with more than 256 registers
+EXTRA_FLAGS = {"esp_attn.hip": ["-fno-honor-nans"], "esp_paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def _compile(src: str) -> str:

@@ -90,22 +90,23 @@ __device__ __forceinline__ float attn_weight(float m, float top, float scale) {
 
 // Bits of 32 keys of a unit that begins c_lo places behind the first row of the chunk (negative: before it), of nr rows: committed keys, and
 // of the chunk the rows up to r (anc null) or those in the row's ancestor bitset.
-__device__ __forceinline__ unsigned attn_window(const uint64_t* anc, int anc_words, int r, int c_lo, int nr) {
+__device__ __forceinline__ unsigned attn_low_bits(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+template <typename WORD>                          // word(i): of the row's ancestor bitset, 0 from its end on
+__device__ __forceinline__ unsigned attn_tree_window(WORD word, int c_lo, int nr) {
   if (c_lo <= -32) return ~0u;
-  if (!anc) {
-    const int n = min(r, nr - 1) + 1 - c_lo;
-    return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
-  }
   uint64_t w;
   if (c_lo < 0) {
-    w = (anc[0] << -c_lo) | ((1ull << -c_lo) - 1ull);
+    w = (word(0) << -c_lo) | ((1ull << -c_lo) - 1ull);
   } else {
     const int i = c_lo >> 6, sh = c_lo & 63;
-    const uint64_t a = i < anc_words ? anc[i] : 0ull, b = i + 1 < anc_words ? anc[i + 1] : 0ull;
+    const uint64_t a = word(i), b = word(i + 1);
     w = sh ? (a >> sh) | (b << (64 - sh)) : a;
   }
-  const int left = nr - c_lo;                     // keys of the sequence in the unit
-  return (unsigned)w & (left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1u);
+  return (unsigned)w & attn_low_bits(nr - c_lo);  // (keys of the sequence in the unit)
+}
+__device__ __forceinline__ unsigned attn_window(const uint64_t* anc, int anc_words, int r, int c_lo, int nr) {
+  if (!anc) return c_lo <= -32 ? ~0u : attn_low_bits(min(r, nr - 1) + 1 - c_lo);
+  return attn_tree_window([&](int i) { return i < anc_words ? anc[i] : 0ull; }, c_lo, nr);
 }
 
 // takes infinities and NaN (all bits of the exponent set) out of a fragment; ones in their places, zeros elsewhere
@@ -140,6 +141,7 @@ __device__ __forceinline__ bool attn_any(f32x8_t f) {
   for (int i = 0; i < 8; ++i) any += f[i];
   return any > 0.f;
 }
+
 // V of keys past the sequence's end (left keys of the unit are there) as zeros: memory there may hold anything, and 0 times NaN is NaN
 __device__ __forceinline__ f32x8_t attn_zero_tail(f32x8_t f, int u, int lane, int left) {
 #pragma unroll
@@ -182,12 +184,12 @@ __device__ __forceinline__ void attn_add_odd(const T* v, unsigned seen, int left
 }
 
 // One unit out of LDS.  k, v: this lane's share of the unit's first K and first V fragment, fragments FRAG bytes apart, of V (db, u) at
-// 2 db + u.  window: bits of the column's keys, looked at where `masked`; left: keys of the sequence in the unit.
+// 2 db + u.  seen: bits of this lane's keys, looked at where `masked`.
 // Fragments are read PF matrix steps ahead and held there (left to itself the compiler reads them all and runs out of registers); the matrix
 // phases run at raised wave priority, so that of the waves of a SIMD one has matrix work and the others fill in with their softmax.
 template <typename T, int HD>
-__device__ __forceinline__ void attn_unit(const unsigned char* k, const unsigned char* v, bool masked, unsigned window, int left, int lane, float scale,
-                                          const typename AttnFrag<T>::type (&q)[HD / 16], f32x16_t (&o)[HD / 32], float& m, float& l, bool& odd) {
+__device__ __forceinline__ void attn_unit(const unsigned char* k, const unsigned char* v, bool masked, unsigned seen, float scale,
+                                          const typename AttnFrag<T>::type (&q)[HD / 16], f32x16_t (&o)[HD / 32], float& m, float& l) {
   typedef typename AttnFrag<T>::type frag_t;
   constexpr int NS = HD / 16, DB = HD / 32, FRAG = 512 * sizeof(T), PF = sizeof(T) == 2 ? 3 : 1, NF = PF + 1;
   frag_t fr[NF];
@@ -211,17 +213,7 @@ __device__ __forceinline__ void attn_unit(const unsigned char* k, const unsigned
   }
   __builtin_amdgcn_s_setprio(0);
   frag_t p[2];
-  attn_softmax<T, DB>(sc, masked, window >> (4 * (lane >> 5)), scale, o, m, l, p);
-  if (masked) {
-#pragma unroll
-    for (int i = 0; i < 2 * DB; ++i) {
-      frag_t f = *reinterpret_cast<const frag_t*>(v + (i % DB * 2 + i / DB) * FRAG);
-      if (left < 32) f = attn_zero_tail(f, i / DB, lane, left);
-      odd |= attn_any(attn_take_odd(f));
-      o[i % DB] = attn_mma(f, p[i / DB], o[i % DB]);
-    }
-    return;
-  }
+  attn_softmax<T, DB>(sc, masked, seen, scale, o, m, l, p);
   __builtin_amdgcn_s_setprio(2);
 #pragma unroll
   for (int i = 0; i < 2 * DB; ++i) {              // i = u DB + db

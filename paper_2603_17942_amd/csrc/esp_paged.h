@@ -62,7 +62,7 @@ struct PagedAttnPlan {
   int least = 1;              // key tiles of a share at least
 };
 PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int len_bound);
-size_t paged_attn_partial_floats(const PagedAttnPlan& p, int hd);
+size_t paged_attn_partial_floats(const PagedAttnPlan& p, int dtype, int hd);
 struct PagedAttnArgs {
   const void* q;
   int64_t q_stride;

@@ -6,8 +6,8 @@
 // shares, one a workgroup: the pieces of an item that a cut went through leave (m, l, O) in memory, and k_paged_merge adds them up in the
 // line's order, so results do not depend on scheduling.  Only the device knows lengths and rows; every workgroup looks its share up.
 //
-// k_paged_stream (up to 32 columns an item, four waves that share them, TK 128) is for decoding, bound by the memory that K and V come
-// from; k_paged_tile (up to 256 columns, eight waves around a ring of key tiles in LDS, TK 64) for chunks and trees, bound by the matrix cores.
+// k_paged_stream (up to 32 columns an item, four waves that share them) is for decoding, bound by the memory that K and V come from;
+// k_paged_tile (up to 256 columns in bf16, 128 in fp32) for chunks and trees, bound by the matrix cores: it walks a ring of key tiles in LDS.
 #include <algorithm>
 #include <atomic>
 
@@ -17,156 +17,140 @@
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int MOST_SHARES = 512;
 constexpr int STREAM_WAVES = 4, STREAM_TK = 32 * STREAM_WAVES;
-constexpr int TILE_WAVES = 8, TILE_TK = 64, TILE_CAP = 8;
+constexpr int TILE_WAVES = 4, TILE_TK = 64;
+template <typename T> constexpr int TILE_NT = sizeof(T) == 2 ? 2 : 1;              // column tiles of a wave
+template <typename T> constexpr int TILE_CAP = TILE_WAVES * TILE_NT<T>;            // and of an item
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// a value that the compiler does not see through: what is computed from it stays where it is used.  (Addresses that it takes out of a loop
+// cost registers over all of it, and a register that it saves to memory it has restored in front of the end of a branch, with the
+// branch's lanes only.  The kernels here are to have none that are saved.)
+__device__ __forceinline__ int opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
 // ---- the line of work --------------------------------------------------------------------------------------------
 struct Item { int seq, kvh, qt; };
 struct Cut { Item item; int tile; };            // before key tile `tile` of the item
 
-// what a sequence's items are: n of them for each kv head, of `per` column tiles (the last may have fewer)
+// what a sequence's items are: n of them for each kv head, of `per` column tiles, the last one of what is left
 struct Items { int n, per; };
 __host__ __device__ __forceinline__ Items items_of(int rows, int G, int cap) {
-  const int ct = (int)(((int64_t)rows * G + 31) / 32), n = (ct + cap - 1) / cap;
-  return {n, n ? (ct + n - 1) / n : 0};
+  const int ct = (rows * G + 31) / 32, n = (ct + cap - 1) / cap;      // (the host has checked rows * G)
+  return {n, min(ct, cap)};
 }
 // keys that item qt sees
 __device__ __forceinline__ int keys_of(const ChunkSeq& s, int G, int per, int qt, bool causal) {
-  const int rows = causal ? min(s.rows, (int)((((int64_t)qt + 1) * per * 32 + G - 1) / G)) : s.rows;
+  const int rows = causal ? min(s.rows, ((qt + 1) * per * 32 + G - 1) / G) : s.rows;
   return s.len + rows;
 }
-// Weights along the line, in keys x G x time of a key tile: an item counts START keys for its beginning and end and the keys that it
-// sees.  Cuts need not be exact, only the same for everybody.
+// Weights along the line, in keys x time of a key tile: an item counts `start` for its beginning and end and its keys.  Cuts need not be
+// exact, only the same for everybody; doubles hold them.
 struct Weights {
-  int64_t first, slope;                         // item k weighs first + slope (k + 1)
-  int64_t tile, start;
-  __device__ __forceinline__ int64_t upto(int64_t k) const { return first * k + slope * (k * (k + 1) / 2); }
+  double first, slope;                            // item k weighs first + slope (k + 1)
+  __device__ __forceinline__ double upto(int k) const { return first * k + slope * (0.5 * k * (k + 1)); }
 };
+// time of a key tile of an item with that many column tiles, and of its start and end, in units of a key's time
+__host__ __device__ constexpr int tile_time(int cap, int per) { return cap == 1 ? 1 : cap == 4 || per > 4 ? 10 : 7; }
+constexpr int start_time(int cap) { return cap == 1 ? 64 : cap == 4 ? 400 : 1600; }
 template <int CAP>
 __device__ __forceinline__ Weights weights_of(const ChunkSeq& s, int G, int per, bool causal) {
-  // time of a key tile with that many column tiles (k_paged_tile): 0.7 us with one to 1.5 us with eight; START is 4 us of the latter
-  constexpr int TK = CAP == 1 ? STREAM_TK : TILE_TK, START = CAP == 1 ? 64 : 160;
-  const int64_t t = CAP == 1 ? 1 : 5 + per;
-  return {t * G * ((int64_t)START * (CAP == 1 ? 1 : 13) / t + s.len + (causal ? 0 : s.rows)), causal ? t * per * 32 : 0, t * G * TK,
-          (int64_t)G * START * (CAP == 1 ? 1 : 13)};
-}
-
-// exclusive sum over the workgroup's threads; total: of all.  sums: LDS, NT / 64 of them
-template <int NT>
-__device__ __forceinline__ int64_t sum_before(int64_t x, int64_t* sums, int64_t& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t upto = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(upto, o, 64);
-    if (lane >= o) upto += y;
-  }
-  if (lane == 63) sums[wave] = upto;
-  __syncthreads();
-  int64_t before = upto - x;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < NT / 64; ++w) {
-    if (w < wave) before += sums[w];
-    total += sums[w];
-  }
-  __syncthreads();
-  return before;
+  const int t = tile_time(CAP, per);
+  return {(double)start_time(CAP) + (double)t * (s.len + (causal ? 0 : s.rows)), causal ? (double)(t * per * 32) / G : 0.0};
 }
 
 // Where share w of `shares` begins and ends.  Order of the line: kv heads, sequences, column groups from the last.  The device may use fewer
-// shares than were launched: none with less than `least` of weight in key tiles.  False: no such share.
-template <int NT, int CAP>
-__device__ bool share_of(const PagedDev& kv, const ChunkDev& ch, int hq, bool causal, int w, int shares, int least, Cut& lo, Cut& hi) {
-  __shared__ int64_t sums[NT / 64];
-  __shared__ Cut cuts[2];
-  const int tid = threadIdx.x, G = hq / kv.hkv;
+// shares than were launched: none with less than `least` key tiles.  False: no such share.  Every wave finds out for itself: a lane a
+// sequence, 64 at a time, then even lanes for the beginning and odd ones for the end.
+template <int CAP>
+__device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch, int G, bool causal, int w, int shares, int least, Cut& lo, Cut& hi) {
   constexpr int TK = CAP == 1 ? STREAM_TK : TILE_TK;
-  auto weight = [&](int b, ChunkSeq& s, Items& it, Weights& wt) -> int64_t {
-    if (b >= kv.batch) return 0;
-    s = chunk_seq(kv, ch, b);
-    if (!s.ok) return 0;
-    it = items_of(s.rows, G, CAP);
-    wt = weights_of<CAP>(s, G, it.per, causal);
-    return wt.upto(it.n);
-  };
+  const int lane = threadIdx.x & 63;
+  const bool one = kv.batch == 1;
   ChunkSeq s;
   Items it;
   Weights wt;
-  int64_t per_head = 0, mine = 0, before = 0;
-  for (int b0 = 0; b0 < kv.batch; b0 += NT) {
-    int64_t total;
-    mine = weight(b0 + tid, s, it, wt);
-    before = sum_before<NT>(mine, sums, total);
-    per_head += total;
-  }
-  const int64_t all = per_head * kv.hkv;
-  const int64_t tile_weight = (int64_t)(CAP == 1 ? 1 : 13) * G * TK;
-  const int n = (int)max((int64_t)1, min((int64_t)shares, all / (tile_weight * least)));
-  if (w >= n || all == 0) return false;
-  // position x * all / n on the line, without overflow
-  auto at = [&](int x) { return all / n * x + all % n * x / n; };
-  const int64_t want[2] = {at(w), at(w + 1)};
-  if (tid < 2) cuts[tid] = Cut{{kv.batch, kv.hkv, 0}, 0};           // the line's end
-  __syncthreads();
-  int64_t base = 0;
-  for (int b0 = 0; b0 < kv.batch; b0 += NT) {
-    if (kv.batch > NT) {
-      int64_t total;
-      mine = weight(b0 + tid, s, it, wt);
-      before = base + sum_before<NT>(mine, sums, total);
-      base += total;
-    }
+  double mine, upto;
+  auto weigh = [&](int b) {
+    s = chunk_seq(kv, ch, min(b, kv.batch - 1));
+    it = items_of(s.rows, G, CAP);
+    wt = weights_of<CAP>(s, G, it.per, causal);
+    mine = upto = s.ok && b < kv.batch ? wt.upto(it.n) : 0.0;
+    if (one) return;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int64_t head = want[e] / per_head, off = want[e] - head * per_head - before;
-      if (head >= kv.hkv || off < 0 || off >= mine) continue;
-      // item j of the line is column group n - 1 - j, so what is in front is all behind group k: weight of groups 0 .. k is more than rest
-      const int64_t rest = mine - off;                              // weight from here to the sequence's end, > 0
-      int64_t k;                                                    // the group with upto(k) < rest <= upto(k + 1)
-      if (wt.slope > 0) {
-        const double a = 0.5 * (double)wt.slope, c = (double)wt.first + a;
-        k = (int64_t)((sqrt(c * c + 4.0 * a * (double)rest) - c) / (2.0 * a));
-      } else {
-        k = rest / wt.first;
-      }
-      k = max((int64_t)0, min(k, (int64_t)it.n - 1));
-      while (k > 0 && wt.upto(k) >= rest) --k;
-      while (k + 1 < it.n && wt.upto(k + 1) < rest) ++k;
-      const int64_t into = wt.upto(k + 1) - rest - wt.start;        // weight of this item in front of the cut, but for its start
-      const int tiles = (keys_of(s, G, it.per, (int)k, causal) + TK - 1) / TK;
-      const int tile = into <= 0 ? 0 : (int)min((into + wt.tile - 1) / wt.tile, (int64_t)tiles);
-      cuts[e] = Cut{{b0 + tid, (int)head, (int)k}, tile};
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
     }
+  };
+  double per_head = 0.0;
+  for (int b0 = 0; b0 < kv.batch; b0 += 64) {
+    weigh(b0 + lane);
+    per_head += __shfl(upto, one ? 0 : 63, 64);
   }
-  __syncthreads();
-  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-  auto take = [&](const Cut& c) { return Cut{{uniform(c.item.seq), uniform(c.item.kvh), uniform(c.item.qt)}, uniform(c.tile)}; };
-  lo = take(cuts[0]);
-  hi = take(cuts[1]);
+  const double all = per_head * kv.hkv;
+  if (uniform(all > 0.0) == 0) return false;
+  const int n = uniform(max(1, (int)min((double)shares, all / ((double)tile_time(CAP, CAP) * TK * least))));
+  if (w >= n) return false;
+  const double at = all / n * (w + (lane & 1));
+  const int head = min((int)(at / per_head), kv.hkv - 1);
+  const double off = max(at - head * per_head, 0.0);
+  // the last sequence with work that begins at or before this place
+  double begin = 0.0, size = 0.0, first = 1.0, slope = 0.0, base = 0.0;
+  int seq = 0, rows = 0, len = 0, items = 1, per = 1;
+  for (int b0 = 0; b0 < kv.batch; b0 += 64) {
+    if (kv.batch > 64) weigh(b0 + lane);
+    const double before = base + (upto - mine);
+    const bool work = mine > 0.0;
+    const double off0 = __shfl(off, 0, 64), off1 = __shfl(off, 1, 64);
+    const uint64_t in0 = __builtin_amdgcn_ballot_w64(work && before <= off0), in1 = __builtin_amdgcn_ballot_w64(work && before <= off1);
+    const uint64_t in = lane & 1 ? in1 : in0;
+    const int l = in ? 63 - __clzll((long long)in) : 0;
+    const double b_ = __shfl(before, l, 64), m_ = __shfl(mine, l, 64), f_ = __shfl(wt.first, l, 64), s_ = __shfl(wt.slope, l, 64);
+    const int r_ = __shfl(s.rows, l, 64), n_ = __shfl(s.len, l, 64), i_ = __shfl(it.n, l, 64), p_ = __shfl(it.per, l, 64);
+    if (in) { begin = b_; size = m_; first = f_; slope = s_; rows = r_; len = n_; items = i_; per = p_; seq = b0 + l; }
+    base += __shfl(upto, one ? 0 : 63, 64);
+  }
+  // item j of the sequence is column group items - 1 - j, so what lies behind is the groups below: k with upto(k) < rest <= upto(k + 1)
+  const Weights q{first, slope};
+  const double rest = max(size - (off - begin), 0.5);
+  const float c = (float)(first + 0.5 * slope);
+  int k = min((int)(2.f * (float)rest / (c + sqrtf(c * c + 2.f * (float)slope * (float)rest))), items - 1);
+  while (k > 0 && q.upto(k) >= rest) --k;
+  while (k + 1 < items && q.upto(k + 1) < rest) ++k;
+  const double into = q.upto(k + 1) - rest - start_time(CAP);     // weight of this item in front of the cut, but for its start
+  const ChunkSeq found{0, rows, len, true};
+  const int tiles = (keys_of(found, G, per, k, causal) + TK - 1) / TK;
+  const double tile_weight = (double)tile_time(CAP, per) * TK;
+  int tile = into > 0.0 ? (int)min(ceil(into / tile_weight), (double)tiles) : 0;
+  auto take = [&](int x, int e) { return uniform(__shfl(x, e, 64)); };
+  lo = Cut{{take(seq, 0), take(head, 0), take(k, 0)}, take(tile, 0)};
+  hi = w + 1 == n ? Cut{{kv.batch, kv.hkv, 0}, 0} : Cut{{take(seq, 1), take(head, 1), take(k, 1)}, take(tile, 1)};
   return true;
 }
 // a sequence's scalars, the same for the whole wave
 __device__ __forceinline__ ChunkSeq uniform_seq(const PagedDev& kv, const ChunkDev& ch, int seq) {
   const ChunkSeq s = chunk_seq(kv, ch, seq);
-  return {__builtin_amdgcn_readfirstlane(s.row0), __builtin_amdgcn_readfirstlane(s.rows), __builtin_amdgcn_readfirstlane(s.len),
-          (bool)__builtin_amdgcn_readfirstlane((int)s.ok)};
+  return {uniform(s.row0), uniform(s.rows), uniform(s.len), uniform((int)s.ok) != 0};
 }
 __device__ __forceinline__ bool same(const Item& a, const Item& b) { return a.seq == b.seq && a.kvh == b.kvh && a.qt == b.qt; }
 
 // Partials: slots of CAP x 32 columns, [slot][column][HD] then (m in powers of two, l) [slot][column][2].  Share w has slots 2 w, for the piece
 // that it begins with if that is not an item's first, and 2 w + 1, for the piece that it ends with if that is an item's first and not its last.
-// What a share leaves for the merge: the item that begins in slot 2 w + 1 (seq -1: none), and of slot 2 w whether there is anything in it
-// (HAS) and whether the item ends in this share, or there is none (ENDS).
-struct ShareNote { Item begun; int first; };
+// What a share leaves for the merge: the item that begins in slot 2 w + 1 (columns 0: none), and of slot 2 w whether there is anything in
+// it (HAS) and whether the item ends in this share, or there is none (ENDS).
+struct alignas(16) ShareNote { int columns, col0, row0, kvh, first, pad[3]; };
 enum { HAS = 1, ENDS = 2 };
 struct Partials {
   ShareNote* notes;
   float *o, *ml;
 };
-__host__ __device__ inline size_t notes_floats(int shares) { return ((size_t)shares * sizeof(ShareNote) / 4 + 3) / 4 * 4; }
+inline size_t notes_floats(int shares) { return (size_t)shares * sizeof(ShareNote) / 4; }
 __device__ __forceinline__ Partials partials_of(float* base, int shares, int cols, int hd) {
-  float* o = base + notes_floats(shares);
+  float* o = base + (size_t)shares * sizeof(ShareNote) / 4;
   return {(ShareNote*)base, o, o + (size_t)2 * shares * cols * hd};
 }
 
@@ -196,9 +180,9 @@ __device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, con
     const int per_xcd = (shares + 7) >> 3;
     w = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if (w >= shares) return;
-    if (!share_of<NT, CAP>(kv, ch, a.hq, causal, w, shares, least, lo, hi)) lo = Cut{{0, kv.hkv, 0}, 0};
+    if (!share_of<CAP>(kv, ch, G, causal, w, shares, least, lo, hi)) lo = Cut{{0, kv.hkv, 0}, 0};
   }
-  ShareNote note{{-1, 0, 0}, ENDS};
+  ShareNote note{0, 0, 0, 0, ENDS, {0, 0, 0}};
   Item item = lo.item;
   int t0 = lo.tile;
   while (item.kvh < kv.hkv) {
@@ -210,8 +194,12 @@ __device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, con
       const int tiles = (keys_of(s, G, it.per, item.qt, causal) + TK - 1) / TK, t1 = last ? min(hi.tile, tiles) : tiles;
       const bool ends = t1 >= tiles;
       if (t0 > 0) note.first = (t1 > t0 ? HAS : 0) | (ends ? ENDS : 0);
-      else if (!ends && t1 > 0) note.begun = item;
-      if (t1 > t0) run(item, s, it, t0, t1, t0 > 0 ? 2 * w : ends ? -1 : 2 * w + 1);
+      else if (!ends && t1 > 0) {
+        const int col0 = item.qt * it.per * 32;
+        note.columns = min(it.per * 32, s.rows * G - col0); note.col0 = col0; note.row0 = s.row0; note.kvh = item.kvh;
+      }
+      if (t1 > t0)
+        run(Item{uniform(item.seq), uniform(item.kvh), uniform(item.qt)}, s, it, uniform(t0), uniform(t1), t0 > 0 ? 2 * w : ends ? -1 : 2 * w + 1);
     }
     if (last) break;
     t0 = 0;
@@ -275,7 +263,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) v
   __shared__ __align__(16) float xo[W][32 * HD];
   __shared__ float xm[W][32], xl[W][32];
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, lg = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = uniform(tid >> 6);
   const int G = a.hq / kv.hkv, blocks = kv.page_size >> 5;
 
   walk<64 * W, 1>(kv, ch, a, shares, least, q_tiles, [&](const Item& item, const ChunkSeq& s, const Items&, int t0, int t1, int slot) {
@@ -381,9 +369,10 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) v
       }
     l += __shfl_xor(l, 32, 64);
     // the waves' parts meet in LDS
+    const int tid = opaque(threadIdx.x), lane = tid & 63;
     if (live) {
       put_columns<HD>(xo[wave], o, lane);
-      if (lg == 0) { xm[wave][lr] = m; xl[wave][lr] = l; }
+      if (lane < 32) { xm[wave][lane] = m; xl[wave][lane] = l; }
     }
     __syncthreads();
     const int n_live = min(32, ncols - col0);
@@ -415,20 +404,6 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) v
   });
 }
 
-// --------------------------------------------------------------------------------------------------
-// k_paged_tile: key tiles of 64 go from memory straight into a ring of LDS stages (a linear copy, the cache's blocks being in
-// operand order), each brought by all eight waves and read by all of them.  A wave has a column tile, or, of the first or second half
-// of each key tile's keys, shares one with its neighbour: waves go to SIMDs round-robin, and eight waves over 1 to 8 column tiles
-// come out with the SIMDs' loads as even as they can be (5 tiles: 3, 3, 2, 2 half tiles of keys instead of 4, 2, 2, 2).
-template <typename T, int HD> struct TileRing {
-  static constexpr int BLOCK = 32 * HD * sizeof(T);               // 32 keys of K, or of V
-  static constexpr int STAGE = 4 * BLOCK;                         // K and V of a tile
-  static constexpr int STAGES = STAGE > 32768 ? 2 : 4;
-  static constexpr int LPW = STAGE / TILE_WAVES / 1024;           // 1 KB loads of a wave for a tile
-  static constexpr int BYTES = STAGE * STAGES;
-  static_assert(BYTES >= TILE_WAVES * 32 * HD * 4, "the columns of all waves go there at the end");
-};
-
 template <int LPW>
 __device__ __forceinline__ void load_run(const unsigned char* src, uint32_t lane_off, uint32_t dst) {
   load_to_lds16_sbase<0>(src, lane_off, dst);
@@ -447,42 +422,136 @@ __device__ __forceinline__ void wait_tiles_but(int n) {
 
 typedef const int __attribute__((address_space(4))) scalar_int;     // memory that no kernel writes meanwhile, read through the scalar cache
 
+// --------------------------------------------------------------------------------------------------
+// k_paged_tile: key tiles of 64 go from memory straight into a ring of LDS stages (a linear copy, the cache's blocks being in operand order),
+// a block by each of four waves, and are read by all of them.  A fragment that feeds one 32 x 32 x 16 instruction is read from LDS at the full rate of LDS (1 KB in the 32 clocks
+// that the instruction takes on each of four SIMDs), so eight waves with 32 columns each waited for LDS (2.4 us a key tile and 256
+// columns).  In bf16 a wave has 64 columns, two tiles that share every fragment, and 512 registers: one wave a SIMD, which has to overlap its
+// own matrix work and softmax.  Its two column tiles run half a unit apart: while one's scores or outputs are on the matrix
+// cores, the other's exponentials are computed between the instructions, in four groups a unit of 32 keys:
+//   scores of tile 0, next unit  | exponentials of tile 1        outputs of tile 0            | exponentials of tile 1; maximum of tile 0, next unit
+//   scores of tile 1, next unit  | exponentials of tile 0, next  outputs of tile 1            | exponentials of tile 0, next; maximum of tile 1, next
+// Outputs and queries sit in AGPRs (the instructions that touch the outputs are text, so that the compiler moves neither).  In fp32 a wave has
+// one tile: its matrix instructions take 16 times as long, and softmax beside them is an eighth.
+template <typename T, int HD> struct TileRing {
+  static constexpr int BLOCK = 32 * HD * sizeof(T), STAGE = 4 * BLOCK, STAGES = STAGE > 32768 ? 2 : 4, LPW = BLOCK / 1024;
+  // Tiles that are asked for ahead.  With two column tiles a wave is half a tile into the next scores when it stops at the barrier, so
+  // the stage it came from is not free yet.
+  static constexpr int AHEAD = STAGES - (TILE_NT<T> - 1);
+  static constexpr int BYTES = STAGE * STAGES;
+  static_assert(BYTES >= TILE_CAP<T> * 32 * HD * 4, "the columns of all waves go there at the end");
+};
+constexpr int TILE_ANC = 2560;                    // 64-bit words of ancestor bitsets that are kept in LDS
+
+__device__ __forceinline__ void tile_out(f32x16_t& o, bf16x8_t v, bf16x8_t p) {
+  asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(o) : "v"(v), "v"(p));
+}
+// The text's matrix instructions, of which the compiler knows nothing, have their results before it reads these registers ...
+template <int DB>
+__device__ __forceinline__ void tile_settle(f32x16_t (&o)[DB]) {
+  asm volatile("s_nop 15\n\ts_nop 15" : "+a"(o[0]));
+#pragma unroll
+  for (int i = 1; i < DB; ++i) asm volatile("" : "+a"(o[i]));
+}
+// ... and begin two instructions or more behind the last that wrote one of their operands
+__device__ __forceinline__ void tile_begin() { asm volatile("s_nop 1"); }
+__device__ __forceinline__ void tile_zero(f32x16_t& x) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = 0.f;
+}
+
+// A column tile of a wave
+template <typename T, int HD> struct ColumnTile {
+  f32x16_t sc;                                    // scores of a unit
+  float m, mb, l, limit;                          // reference of the exponents, the same scaled, sum, and the score from which the reference moves
+  typename AttnFrag<T>::type p[2];                // probabilities: rounded to bf16 for the product, their sum is of the unrounded ones
+  __device__ __forceinline__ void start() {
+    m = ATTN_UNSEEN; mb = 0.f; l = 0.f; limit = ATTN_UNSEEN;
+  }
+  // (the empty statement keeps the exponential at its place beside the matrix instructions: its results are used blocks of code later, and
+  // the compiler would compute them there)
+  __device__ __forceinline__ void exp_of(int e, float scale) {
+    float x = __builtin_amdgcn_exp2f(fmaf(sc[e], scale, -mb));
+    l += x;
+    asm volatile("" : "+v"(x), "+v"(l));
+    p[e >> 3][e & 7] = from_f32<T>(x);
+  }
+  __device__ __forceinline__ void hide(unsigned seen) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sc[v] = ((seen >> (8 * (v >> 2) + (v & 3))) & 1u) ? sc[v] : ATTN_UNSEEN;
+  }
+  __device__ __forceinline__ void top_of(float& top, int i) { top = attn_max3(top, sc[2 * i], sc[2 * i + 1]); }
+  // Moves the reference where a score is above its limit; o: the outputs so far, all of whose sums are of units before this one.
+  __device__ __forceinline__ void follow(float top, float scale, float slack, f32x16_t (&o)[HD / 32]) {
+    if (__builtin_amdgcn_ballot_w64(top > limit) == 0ull) return;
+    top = attn_max_of_halves(top);
+    const float was = mb;
+    const bool moves = top > limit, had = m > 0.5f * ATTN_UNSEEN;
+    if (moves) { m = top; mb = top * scale; limit = top + slack; }
+    if (__builtin_amdgcn_ballot_w64(moves && had) == 0ull) return;
+    const float f = moves && had ? __builtin_amdgcn_exp2f(was - mb) : 1.f;
+    l *= f;
+    tile_settle(o);
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[i][v] *= f;
+  }
+};
+
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * TILE_WAVES) void k_paged_tile(PagedDev kv, ChunkDev ch, PagedAttnArgs a, int shares, int least, int q_tiles,
-                                                               bool vec_q, bool vec_out) {
+__global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, ChunkDev ch, PagedAttnArgs a, int shares, int least, int q_tiles,
+                                                                  bool vec_q, bool vec_out) {
   typedef TileRing<T, HD> R;
   typedef typename AttnFrag<T>::type frag_t;
-  constexpr int NS = HD / 16, DB = HD / 32, PIECES = HD / 4;
+  constexpr int NT = TILE_NT<T>, NS = HD / 16, DB = HD / 32, PIECES = HD / 4, EPI = 8 / NS;   // EPI: exponentials beside a matrix instruction
   extern __shared__ __align__(16) unsigned char lds[];
+  uint64_t* anc_lds = reinterpret_cast<uint64_t*>(lds + R::BYTES);
   __shared__ float xm[TILE_WAVES][32], xl[TILE_WAVES][32];
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, lg = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = uniform(tid >> 6);
   const int G = a.hq / kv.hkv, blocks = kv.page_size >> 5;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-  // what this wave brings of a tile: a run of one block of K (waves 0-3) or V
-  const int my_block = (wave >> 1) & 1;
-  const size_t my_off = (size_t)(wave & 1) * (R::BLOCK / 2);
-  const unsigned char* my_pool = (const unsigned char*)(wave < 4 ? kv.k : kv.v) + my_off;
-  const uint32_t my_lds = lds0 + (uint32_t)((wave < 4 ? 0 : 2 * R::BLOCK) + my_block * R::BLOCK + my_off);
+  const bool causal = a.anc == nullptr;
+  const float slack = ATTN_SLACK / a.scale;
+  // what this wave brings of a tile: a block of K (waves 0 and 1) or V
+  const unsigned char* my_pool = (const unsigned char*)(wave < 2 ? kv.k : kv.v);
+  const uint32_t my_lds = lds0 + (uint32_t)wave * R::BLOCK;
 
-  walk<64 * TILE_WAVES, TILE_CAP>(kv, ch, a, shares, least, q_tiles, [&](const Item& item, const ChunkSeq& s, const Items& it, int t0, int t1, int slot) {
-    const int seq = __builtin_amdgcn_readfirstlane(item.seq), kvh = __builtin_amdgcn_readfirstlane(item.kvh);
-    const int qt = __builtin_amdgcn_readfirstlane(item.qt);
-    const bool causal = a.anc == nullptr;
+  walk<64 * TILE_WAVES, TILE_CAP<T>>(kv, ch, a, shares, least, q_tiles, [&](const Item& item, const ChunkSeq& s, const Items& it, int t0, int t1, int slot) {
+    const int seq = item.seq, kvh = item.kvh, qt = item.qt;
     const int ncols = s.rows * G, total = s.len + s.rows, keys = keys_of(s, G, it.per, qt, causal);
-    const int nt = t1 - t0;
-    const int ct = min(it.per, (ncols + 31) / 32 - qt * it.per);              // column tiles of this item
-    const int pairs = min(ct, TILE_WAVES - ct), full = ct - pairs;             // tiles shared by two waves, and those that have one
-    const bool paired = wave >= full;
-    const int ctl = paired ? full + ((wave - full) >> 1) : wave;
-    const int kh0 = paired ? (wave - full) & 1 : 0, kh1 = paired ? kh0 : 1;    // halves of the key tiles
-    const bool works = ctl < ct;
-    const int col = (qt * it.per + ctl) * 32 + lr;
-    const bool live = works && col < ncols;
-    const int r = live ? col / G : 0, h = kvh * G + (live ? col % G : 0);
-    const int r_lo = works ? (qt * it.per + ctl) * 32 / G : 0, r_hi = min(s.rows - 1, ((qt * it.per + ctl) * 32 + 31) / G);
-    const int64_t row = s.row0 + r;
+    const int nt = t1 - t0, col0 = qt * it.per * 32;
+    const int ct = min(it.per, (ncols - col0 + 31) / 32);                     // column tiles of this item
+    // Wave w has tiles w and w + 4.  One or two tiles are shared by two waves each, which have the halves of every key tile.
+    const bool halves = ct <= 2;
+    const int kh0 = halves ? wave >> 1 : 0, kh1 = halves ? kh0 : 1, ct0 = halves ? wave & 1 : wave;
+    const int mine = ct0 >= ct ? 0 : NT == 2 && ct0 + 4 < ct ? 2 : 1;
     scalar_int* table = (scalar_int*)(uintptr_t)(kv.table + (size_t)seq * kv.stride);
+
+    int col[NT], r[NT], r_lo[NT];
+    bool live[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) {
+      const int first = col0 + (ct0 + 4 * c) * 32;
+      col[c] = first + lr;
+      live[c] = c < mine && col[c] < ncols;
+      r[c] = live[c] ? col[c] / G : 0;
+      r_lo[c] = first / G;
+    }
+    // ancestor bitsets of the item's rows in LDS, where they fit
+    const int row_lo = col0 / G, n_rows = (min(ncols, col0 + ct * 32) - 1) / G - row_lo + 1;
+    const bool anc_here = !causal && (int64_t)n_rows * a.anc_words <= TILE_ANC;
+    if (anc_here)
+      for (int i = tid; i < n_rows * a.anc_words; i += 64 * TILE_WAVES) anc_lds[i] = a.anc[(size_t)(s.row0 + row_lo) * a.anc_words + i];
+    auto window_of = [&](int c, int c_lo) {
+      if (causal) return attn_low_bits(min(r[c], s.rows - 1) + 1 - c_lo);
+      const int at = (r[c] - row_lo) * a.anc_words;
+      if (anc_here)
+        return attn_tree_window([&](int i) { return i < a.anc_words && live[c] ? anc_lds[at + i] : 0ull; }, c_lo, s.rows);
+      const uint64_t* w = a.anc + (size_t)(s.row0 + r[c]) * a.anc_words;
+      return attn_tree_window([&](int i) { return i < a.anc_words ? w[i] : 0ull; }, c_lo, s.rows);
+    };
 
     // are all pages there?  (Where one is not, its keys are looked at one block after the other.)
     bool bad = false;
@@ -491,132 +560,279 @@ __global__ __launch_bounds__(64 * TILE_WAVES) void k_paged_tile(PagedDev kv, Chu
       bad |= (unsigned)kv.table[(size_t)seq * kv.stride + p] >= (unsigned)kv.n_pages;
     if (bad) set_status(kv.status, ESP_DEV_BAD_PAGE);
     const bool any_bad = __syncthreads_or(bad);
+    const bool hides = (int64_t)t1 * TILE_TK > s.len && s.rows > 1;           // some key of the piece may be hidden from some column
 
-    // this wave's next block: page number in the table, place in it; a block behind the last that is needed is that one
-    int n = 2 * t0 + my_block, pg = min(n, last_block) / blocks, in = min(n, last_block) - pg * blocks;
-    int page = table[pg];
-    auto issue = [&](int i) {                     // tile t0 + i into stage i % STAGES; called for i = 0, 1, 2, ...
-      const int p = (unsigned)page < (unsigned)kv.n_pages ? page : 0;
-      const unsigned char* src = my_pool + ((size_t)(p * kv.hkv + kvh) * blocks + in) * R::BLOCK;
-      load_run<R::LPW>(src, (uint32_t)lane * 16, my_lds + (uint32_t)(i % R::STAGES) * R::STAGE);
-      n += 2;
-      if (n <= last_block) {
-        in += 2;
-        while (in >= blocks) { in -= blocks; ++pg; }
-        page = table[pg];
-      } else if (n - 1 == last_block) {
-        in += 1;
-        if (in >= blocks) { in -= blocks; ++pg; }
-        page = table[pg];
+    frag_t qf[NT][NS];
+    f32x16_t o[NT][DB];
+    ColumnTile<T, HD> tile[NT];
+    // Once; and where the outputs hold infinities or NaN that may come from values which some columns do not see (0 times them), again with
+    // these taken out of the tiles (safe), and infinities added where they are seen.
+    for (int safe = 0;; ++safe) {
+      int n = 2 * t0 + (wave & 1), pg = min(n, last_block) / blocks, in = min(n, last_block) - pg * blocks;
+      int page = table[pg];
+      auto issue = [&](int i) {                   // tile t0 + i into its stage; called for i = 0, 1, 2, ...
+        const int p = (unsigned)page < (unsigned)kv.n_pages ? page : 0;
+        const unsigned char* src = my_pool + ((size_t)(p * kv.hkv + kvh) * blocks + in) * R::BLOCK;
+        load_run<R::LPW>(src, (uint32_t)lane * 16, my_lds + (uint32_t)(i % R::STAGES) * R::STAGE);
+        n += 2;
+        const int on = n <= last_block ? 2 : n - 1 == last_block ? 1 : 0;     // (a block behind the last that is needed is that one)
+        if (on) {
+          in += on;
+          while (in >= blocks) { in -= blocks; ++pg; }
+          page = table[pg];
+        }
+      };
+      // The last tile of the sequence: V of keys past its end as zeros (memory there may hold anything).  Safe: infinities and NaN out.
+      auto clean = [&](int i) {
+        const int left = total - (t0 + i) * TILE_TK;
+        const bool tail = left < TILE_TK, odd = safe && left - TILE_TK < s.rows;
+        if (!tail && !odd) return;
+        unsigned char* v = lds + (i % R::STAGES) * R::STAGE + 2 * R::BLOCK;
+        constexpr int PIECE = 8 * sizeof(T), IN = R::BLOCK / PIECE;
+        for (int x = tid; x < 2 * IN; x += 64 * TILE_WAVES) {                  // piece x: block, fragment (db, u), lane
+          const int in_block = x % IN, u = (in_block >> 6) & 1;
+          frag_t f = *reinterpret_cast<const frag_t*>(v + x * PIECE);
+          if (tail) f = attn_zero_tail(f, u, in_block & 63, left - (x >= IN ? 32 : 0));
+          if (odd) attn_take_odd(f);
+          *reinterpret_cast<frag_t*>(v + x * PIECE) = f;
+        }
+        __syncthreads();
+      };
+      issue(0);
+      // The queries between the first tile's loads and the others': the compiler's wait for them, held here by the empty statement, covers
+      // the first tile too, and no load that the compiler knows of is in flight in the loop (its wait would drain the ring).
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        const T* qp = (const T*)a.q + (int64_t)(s.row0 + r[c]) * a.q_stride + (kvh * G + (live[c] ? col[c] % G : 0)) * HD + 8 * lg;
+#pragma unroll
+        for (int i = 0; i < NS; ++i) qf[c][i] = load_query(qp + 16 * i, vec_q);
       }
-    };
-    issue(0);
-    // The queries between the first tile's loads and the others': the compiler's wait for them, held here by the empty statement, covers
-    // the first tile too, and no load that the compiler knows of is in flight in the loop (its wait would drain the ring).
-    frag_t qf[NS];
-    {
-      const T* qp = (const T*)a.q + row * a.q_stride + h * HD + 8 * lg;
 #pragma unroll
-      for (int i = 0; i < NS; ++i) qf[i] = load_query(qp + 16 * i, vec_q);
+      for (int c = 0; c < NT; ++c) {
 #pragma unroll
-      for (int i = 0; i < NS; ++i) asm volatile("" : "+v"(qf[i])::"memory");
-    }
-    for (int i = 1; i < R::STAGES - 1; ++i)
-      if (i < nt) issue(i);
-    const uint64_t* anc = causal ? nullptr : a.anc + row * a.anc_words;
-    f32x16_t o[DB];
+        for (int i = 0; i < NS; ++i) asm volatile("" : "+a"(qf[c][i])::"memory");
 #pragma unroll
-    for (int i = 0; i < DB; ++i)
+        for (int i = 0; i < DB; ++i) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) o[i][v] = 0.f;
-    float m = ATTN_UNSEEN, l = 0.f;
-    bool odd = false;
-
-    const unsigned char* frag = lds + lane * 8 * sizeof(T);
-    for (int i = 0; i < nt; ++i) {
-      // tile i has landed (this wave's loads retire in order; the barrier covers the other waves'), and every wave is done with tile i - 1,
-      // whose stage takes tile i + STAGES - 1
-      wait_tiles_but<R::LPW>(min(R::STAGES - 2, nt - 1 - i));
+          for (int v = 0; v < 16; ++v) o[c][i][v] = 0.f;
+          asm volatile("" : "+a"(o[c][i]));
+        }
+        tile[c].start();
+      }
+      for (int i = 1; i < R::AHEAD; ++i)
+        if (i < nt) issue(i);
+      // tile 0 is here for everybody (this wave's loads retire in order, the barrier covers the others')
+      wait_tiles_but<R::LPW>(min(R::AHEAD - 1, nt - 1));
       __syncthreads();
-      if (i + R::STAGES - 1 < nt) issue(i + R::STAGES - 1);
-      if (!works) continue;
-      const unsigned char* st = frag + (i % R::STAGES) * R::STAGE;
-      for (int kh = kh0; kh <= kh1; ++kh) {
-        const int key0 = (t0 + i) * TILE_TK + 32 * kh, c_lo = key0 - s.len;
-        if (key0 >= total || (causal && c_lo > r_hi)) continue;                 // nobody here sees any of it
-        bool there = true;
-        if (any_bad) there = (unsigned)table[(key0 >> 5) / blocks] < (unsigned)kv.n_pages;
-        const bool masked = !there || c_lo + 32 > (causal ? r_lo + 1 : 0);
-        unsigned window = ~0u;
-        if (masked) window = there ? attn_window(anc, a.anc_words, r, c_lo, s.rows) : 0u;
-        attn_unit<T, HD>(st + kh * R::BLOCK, st + (2 + kh) * R::BLOCK, masked, window, total - key0, lane, a.scale, qf, o, m, l, odd);
-      }
-    }
-    if (__builtin_amdgcn_ballot_w64(odd) != 0ull)
-      for (int i = 0; i < 2 * nt; ++i) {
-        const int n = 2 * t0 + i, c_lo = 32 * n - s.len;
-        if ((i & 1) < kh0 || (i & 1) > kh1 || 32 * n >= keys || c_lo + 32 <= 0) continue;
-        const int p = table[n / blocks];
-        if ((unsigned)p >= (unsigned)kv.n_pages) continue;
-        attn_add_odd<T, HD>((const T*)kv.v + ((size_t)(p * kv.hkv + kvh) * blocks + n % blocks) * (32 * HD),
-                            attn_window(anc, a.anc_words, r, c_lo, s.rows) >> (4 * lg), total - 32 * n, lane, o);
-      }
-    l += __shfl_xor(l, 32, 64);
+      clean(0);
+      // Tile i + 1 is here, and all are done with tile i (with two column tiles: i - 1), whose stage takes the next that is asked for.
+      auto next_tile = [&](int i) {
+        if (i + 1 >= nt) return;
+        wait_tiles_but<R::LPW>(min(R::AHEAD - 2, nt - 2 - i));
+        __syncthreads();
+        if (i + R::AHEAD < nt) issue(i + R::AHEAD);
+        clean(i + 1);
+      };
+      const unsigned char* frag = lds + lane * 8 * sizeof(T);
+      // units from hide_at[c] on hold keys that some column of tile c does not see
+      int hide_at[NT];
+#pragma unroll
+      for (int c = 0; c < NT; ++c)
+        hide_at[c] = any_bad ? 0 : max(0, ((s.len - 32 - t0 * TILE_TK + (causal ? r_lo[c] + 1 : 0)) >> 5) + 1);
+      auto seen_of = [&](int c, int u) -> unsigned {                          // bits of this lane's keys of unit u
+        const int key0 = t0 * TILE_TK + 32 * u;
+        if (any_bad && (key0 >= keys || (unsigned)table[(key0 >> 5) / blocks] >= (unsigned)kv.n_pages)) return 0u;
+        return window_of(c, key0 - s.len) >> (4 * lg);
+      };
 
-    // the ring is done with: columns of wave w at its place in it
-    __syncthreads();
-    float* xo = reinterpret_cast<float*>(lds) + wave * (32 * HD);
-    if (works && kh0 == 1) {
-      put_columns<HD>(xo, o, lane);
-      if (lg == 0) { xm[wave][lr] = m; xl[wave][lr] = l; }
+      auto two_tiles = [&]() {
+        if constexpr (NT == 2) {
+        bf16x8_t kf[NS], vf[NS];                  // V: fragment (db, u) at 2 db + u
+        auto unit_at = [&](int u) { return frag + ((u >> 1) % R::STAGES) * R::STAGE + (u & 1) * R::BLOCK; };
+#pragma unroll
+        for (int j = 0; j < NS; ++j) kf[j] = *reinterpret_cast<const bf16x8_t*>(unit_at(0) + j * 1024);
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+          tile_zero(tile[c].sc);
+#pragma unroll
+          for (int j = 0; j < NS; ++j) tile[c].sc = attn_mma(kf[j], qf[c][j], tile[c].sc);
+          if (hide_at[c] <= 0) tile[c].hide(seen_of(c, 0));
+          float top = ATTN_UNSEEN;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) tile[c].top_of(top, e);
+          tile[c].follow(top, a.scale, slack, o[c]);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) tile[0].exp_of(e, a.scale);
+#pragma unroll
+        for (int j = 0; j < NS; ++j) kf[j] = *reinterpret_cast<const bf16x8_t*>(unit_at(1) + j * 1024);
+        float l0 = 0.f;
+        for (int u = 0; u < 2 * nt; ++u) {
+          // (behind the last unit the scores are of what lies in LDS, and for nothing)
+          const unsigned char* v = unit_at(u) + 2 * R::BLOCK;
+          const bool more = u + 1 < 2 * nt;
+          f32x16_t next;
+          float top;
+          tile_zero(next);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < NS; ++j) {
+            vf[j] = *reinterpret_cast<const bf16x8_t*>(v + j * 1024);
+            next = attn_mma(kf[j], qf[0][j], next);
+#pragma unroll
+            for (int e = 0; e < EPI; ++e) tile[1].exp_of(j * EPI + e, a.scale);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          tile[0].sc = next;
+          if (more && u + 1 >= hide_at[0]) tile[0].hide(seen_of(0, u + 1));
+          top = ATTN_UNSEEN;
+          tile_begin();
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < NS; ++j) {
+            tile_out(o[0][j % DB], vf[2 * (j % DB) + j / DB], tile[0].p[j / DB]);
+#pragma unroll
+            for (int e = 0; e < EPI; ++e) tile[1].exp_of(8 + j * EPI + e, a.scale);
+            if (j >= NS / 2) {                    // (the scores are there by now)
+#pragma unroll
+              for (int e = 0; e < 2 * EPI; ++e) tile[0].top_of(top, (j - NS / 2) * 2 * EPI + e);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          if (more) tile[0].follow(top, a.scale, slack, o[0]);
+          l0 = tile[0].l;
+          tile_zero(next);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < NS; ++j) {
+            next = attn_mma(kf[j], qf[1][j], next);
+#pragma unroll
+            for (int e = 0; e < EPI; ++e) tile[0].exp_of(j * EPI + e, a.scale);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          tile[1].sc = next;
+          if (more && u + 1 >= hide_at[1]) tile[1].hide(seen_of(1, u + 1));
+          if ((u & 1) == 0) next_tile(u >> 1);
+          const unsigned char* k = unit_at(u + 2);
+          top = ATTN_UNSEEN;
+          tile_begin();
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < NS; ++j) {
+            kf[j] = *reinterpret_cast<const bf16x8_t*>(k + j * 1024);
+            tile_out(o[1][j % DB], vf[2 * (j % DB) + j / DB], tile[1].p[j / DB]);
+#pragma unroll
+            for (int e = 0; e < EPI; ++e) tile[0].exp_of(8 + j * EPI + e, a.scale);
+            if (j >= NS / 2) {
+#pragma unroll
+              for (int e = 0; e < 2 * EPI; ++e) tile[1].top_of(top, (j - NS / 2) * 2 * EPI + e);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          if (more) tile[1].follow(top, a.scale, slack, o[1]);
+        }
+        tile[0].l = l0;                           // (without the exponentials behind the last unit)
+        }
+      };
+      if (mine == 2) {
+        two_tiles();
+      } else {
+        for (int i = 0; i < nt; ++i) {
+          if (mine == 1)
+            for (int kh = kh0; kh <= kh1; ++kh) {
+              const int u = 2 * i + kh;
+              const unsigned char* st = frag + (i % R::STAGES) * R::STAGE + kh * R::BLOCK;
+              const bool masked = u >= hide_at[0];
+              attn_unit<T, HD>(st, st + 2 * R::BLOCK, masked, masked ? seen_of(0, u) : ~0u, a.scale, qf[0], o[0], tile[0].m, tile[0].l);
+            }
+          next_tile(i);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < NT; ++c) tile_settle(o[c]);
+      if (safe) {
+        for (int u = 0; u < 2 * nt; ++u) {
+          const int n = 2 * t0 + u, key0 = 32 * n;
+          if ((key0 & ~(TILE_TK - 1)) + TILE_TK <= s.len || key0 >= keys || (halves && (u & 1) != kh0)) continue;
+          const int p = table[n / blocks];
+          if ((unsigned)p >= (unsigned)kv.n_pages) continue;
+          const T* v = (const T*)kv.v + ((size_t)(p * kv.hkv + kvh) * blocks + n % blocks) * (32 * HD);
+#pragma unroll
+          for (int c = 0; c < NT; ++c)
+            if (c < mine) attn_add_odd<T, HD>(v, window_of(c, key0 - s.len) >> (4 * lg), total - key0, lane, o[c]);
+        }
+        break;
+      }
+      if (!hides) break;
+      unsigned most = 0;
+#pragma unroll
+      for (int c = 0; c < NT; ++c)
+        if (c < mine) {
+#pragma unroll
+          for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) most = max(most, __float_as_uint(o[c][i][v]) & 0x7fffffffu);
+        }
+      if (!__syncthreads_or(most >= 0x7f800000u)) break;
     }
+
+    // the ring is done with: a wave's columns, [tile][32][HD], one wave's behind the other's
     __syncthreads();
-    if (works && kh0 == 0) {
-      float fa = 1.f, fb = 0.f, mo = ATTN_UNSEEN, lo = 0.f;
-      if (paired) {
-        mo = xm[wave + 1][lr];
-        lo = xl[wave + 1][lr];
-        const float top = fmaxf(m, mo);
-        fa = attn_weight(m, top, a.scale);
-        fb = attn_weight(mo, top, a.scale);
-        l = l * fa + lo * fb;
-        m = top;
+    const int lane = opaque(threadIdx.x) & 63, lr = lane & 31, lg = lane >> 5;
+    float* xo = reinterpret_cast<float*>(lds) + wave * (32 * NT * HD);
+#pragma unroll
+    for (int c = 0; c < NT; ++c) tile[c].l += __shfl_xor(tile[c].l, 32, 64);
+    if (halves) {                                 // the second half of the keys goes to the wave that has the first
+      if (mine == 1 && kh0 == 1) {
+        put_columns<HD>(xo, o[0], lane);
+        if (lg == 0) { xm[wave][lr] = tile[0].m; xl[wave][lr] = tile[0].l; }
+      }
+      __syncthreads();
+      if (mine == 1 && kh0 == 0) {
+        const float mo = xm[wave + 2][lr], lo = xl[wave + 2][lr], top = fmaxf(tile[0].m, mo);
+        const float fa = attn_weight(tile[0].m, top, a.scale), fb = attn_weight(mo, top, a.scale);
+        tile[0].l = tile[0].l * fa + lo * fb;
+        tile[0].m = top;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int v = 0; v < 16; v += 4) {
-            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(column_piece<HD>(xo + 32 * HD, lr, db * 8 + 2 * (v >> 2) + lg));
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(column_piece<HD>(xo + 2 * (32 * NT * HD), lr, db * 8 + 2 * (v >> 2) + lg));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[db][v + e] = o[db][v + e] * fa + x[e] * fb;
+            for (int e = 0; e < 4; ++e) o[0][db][v + e] = o[0][db][v + e] * fa + x[e] * fb;
           }
       }
-      const float inv = l > 0.f ? 1.f / l : 0.f;
-      if (slot < 0) {
+    }
+    const Partials part = partials_of(a.partials, shares, 32 * TILE_CAP<T>, HD);
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+    for (int c = 0; c < NT; ++c) {
+      if (c >= mine || kh0 != 0) continue;
+      const float inv = slot >= 0 ? 1.f : tile[c].l > 0.f ? 1.f / tile[c].l : 0.f;
 #pragma unroll
-          for (int v = 0; v < 16; ++v) o[db][v] *= inv;
-      }
-      put_columns<HD>(xo, o, lane);
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[c][db][v] *= inv;
+      put_columns<HD>(xo, o[c], lane);
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");       // (a wave's LDS accesses are done in order: for the compiler)
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      const int c0 = (qt * it.per + ctl) * 32, n_live = min(32, ncols - c0);
-      if (slot < 0) {
-        for (int t = lane; t < n_live * PIECES; t += 64) {
-          const int c = t / PIECES, piece = t % PIECES, cc = c0 + c;
-          const int64_t at = ((int64_t)s.row0 + cc / G) * a.hq + kvh * G + cc % G;
-          store4((T*)a.out + at * HD + 4 * piece, *reinterpret_cast<const f32x4_t*>(column_piece<HD>(xo, c, piece)), vec_out);
+      const int tc = ct0 + 4 * c, c0 = col0 + tc * 32, n_live = min(32, ncols - c0);
+      const int64_t at = (int64_t)max(slot, 0) * (32 * TILE_CAP<T>) + tc * 32;
+      for (int t = lane; t < n_live * PIECES; t += 64) {
+        const int i = t / PIECES, piece = t % PIECES;
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(column_piece<HD>(xo, i, piece));
+        if (slot < 0) {
+          const int64_t row = s.row0 + (c0 + i) / G;
+          store4((T*)a.out + (row * a.hq + kvh * G + (c0 + i) % G) * HD + 4 * piece, x, vec_out);
+        } else {
+          *reinterpret_cast<f32x4_t*>(part.o + (at + i) * HD + 4 * piece) = x;
         }
-      } else {
-        const Partials p = partials_of(a.partials, shares, 32 * TILE_CAP, HD);
-        const int64_t at = (int64_t)slot * (32 * TILE_CAP) + ctl * 32;
-        for (int t = lane; t < n_live * PIECES; t += 64) {
-          const int c = t / PIECES, piece = t % PIECES;
-          *reinterpret_cast<f32x4_t*>(p.o + (at + c) * HD + 4 * piece) = *reinterpret_cast<const f32x4_t*>(column_piece<HD>(xo, c, piece));
-        }
-        if (lg == 0 && lr < n_live) { p.ml[2 * (at + lr)] = m * a.scale; p.ml[2 * (at + lr) + 1] = l; }
       }
+      if (slot >= 0 && lg == 0 && lr < n_live) {
+        part.ml[2 * (at + lr)] = tile[c].m * a.scale;
+        part.ml[2 * (at + lr) + 1] = tile[c].l;
+      }
+      xo += 32 * HD;
     }
     // the stores do not count as loads of the next piece, whose ring goes where the columns are
     wait_loads_but<0>();
@@ -625,43 +841,57 @@ __global__ __launch_bounds__(64 * TILE_WAVES) void k_paged_tile(PagedDev kv, Chu
 }
 
 // --------------------------------------------------------------------------------------------------
-// The pieces of an item that begins in share w and does not end there: those of the shares behind it, up to the one that ends it.
-// A workgroup has 32 columns, HD / 4 threads and more a column.
+// The pieces of an item that begins in share w and does not end there: that one and those of the shares behind it, up to the one that ends
+// it.  A workgroup has 32 columns, HD / 4 threads a column, four features each.
 template <typename T, int HD, int CAP>
-__global__ __launch_bounds__(256) void k_paged_merge(PagedDev kv, ChunkDev ch, PagedAttnArgs a, int shares, bool vec_out) {
-  constexpr int PIECES = HD / 4, COLS = 32 * CAP;
-  const int w = blockIdx.x, ctl = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+__global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs a, int hkv, int shares, bool vec_out) {
+  constexpr int PIECES = HD / 4, COLS = 32 * CAP, U = 4;
+  __shared__ int slots[2 * MOST_SHARES];
+  const int w = blockIdx.x, c0 = blockIdx.y * 32, tid = threadIdx.x, lane = tid & 63;
   const Partials p = partials_of(a.partials, shares, COLS, HD);
-  const Item item = p.notes[w].begun;
-  if (item.seq < 0) return;
-  const ChunkSeq s = chunk_seq(kv, ch, item.seq);
-  const int G = a.hq / kv.hkv, ncols = s.rows * G;
-  const Items it = items_of(s.rows, G, CAP);
-  const int c0 = (item.qt * it.per + ctl) * 32, n_live = min(32, ncols - c0);
-  if (ctl >= it.per || n_live <= 0) return;
+  const ShareNote note = p.notes[w];
+  int first = w + 1 + lane < shares ? p.notes[w + 1 + lane].first : ENDS;
+  if (note.columns <= c0) return;
+  // the pieces' slots, in order, by every wave alike
+  int n = 1;
+  if (tid == 0) slots[0] = 2 * w + 1;
+  for (int x0 = w + 1;; x0 += 64) {
+    if (x0 > w + 1) first = x0 + lane < shares ? p.notes[x0 + lane].first : ENDS;
+    const uint64_t ends = __builtin_amdgcn_ballot_w64((first & ENDS) != 0);
+    const uint64_t upto = ends ? (2ull << __builtin_ctzll(ends)) - 1ull : ~0ull;
+    const uint64_t has = __builtin_amdgcn_ballot_w64((first & HAS) != 0) & upto;
+    if (has >> lane & 1) slots[n + __popcll(has & ((1ull << lane) - 1ull))] = 2 * (x0 + lane);
+    n += __popcll(has);
+    if (ends) break;
+  }
+  __syncthreads();
+  const int G = a.hq / hkv, n_live = min(32, note.columns - c0);
   for (int t = tid; t < n_live * PIECES; t += 256) {
-    const int c = t / PIECES, piece = t % PIECES, cc = c0 + c;
-    const int64_t col = ctl * 32 + c;
-    int64_t at = (int64_t)(2 * w + 1) * COLS + col;
-    float top = p.ml[2 * at], lt = p.ml[2 * at + 1];
-    f32x4_t acc = *reinterpret_cast<const f32x4_t*>(p.o + at * HD + 4 * piece);
-    if (!(lt > 0.f)) top = -INFINITY;
-    for (int x = w + 1; x < shares; ++x) {
-      const int first = p.notes[x].first;
-      if (first & HAS) {
-        at = (int64_t)(2 * x) * COLS + col;
-        const float m = p.ml[2 * at], l = p.ml[2 * at + 1];
-        const f32x4_t o = *reinterpret_cast<const f32x4_t*>(p.o + at * HD + 4 * piece);
-        const float now = l > 0.f ? fmaxf(top, m) : top;
-        const float fa = top > -INFINITY ? __builtin_amdgcn_exp2f(top - now) : 0.f, fb = l > 0.f ? __builtin_amdgcn_exp2f(m - now) : 0.f;
-        lt = lt * fa + l * fb;
-        acc = acc * fa + o * fb;
+    const int c = c0 + t / PIECES, piece = t % PIECES;
+    float top = -INFINITY, lt = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; i += U) {              // U pieces on their way at once
+      float m[U], l[U];
+      f32x4_t o[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const size_t at = (size_t)slots[min(i + u, n - 1)] * COLS + c;
+        m[u] = p.ml[2 * at];
+        l[u] = p.ml[2 * at + 1];
+        o[u] = *reinterpret_cast<const f32x4_t*>(p.o + at * HD + 4 * piece);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i + u >= n) break;
+        const float now = l[u] > 0.f ? fmaxf(top, m[u]) : top;
+        const float fa = top > -INFINITY ? __builtin_amdgcn_exp2f(top - now) : 0.f, fb = l[u] > 0.f ? __builtin_amdgcn_exp2f(m[u] - now) : 0.f;
+        lt = lt * fa + l[u] * fb;
+        acc = acc * fa + o[u] * fb;
         top = now;
       }
-      if (first & ENDS) break;
     }
-    (void)lane;
-    const int64_t out = ((int64_t)s.row0 + cc / G) * a.hq + item.kvh * G + cc % G;
+    const int cc = note.col0 + c;
+    const int64_t out = ((int64_t)note.row0 + cc / G) * a.hq + note.kvh * G + cc % G;
     store4((T*)a.out + out * HD + 4 * piece, acc * (lt > 0.f ? 1.f / lt : 0.f), vec_out);
   }
 }
@@ -691,18 +921,18 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
     grid = (p.q_tiles > 1 && groups >= 8 ? (groups + 7) & ~7ll : groups) * p.q_tiles;
   }
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-  if (p.tile) {
-    constexpr unsigned bytes = TileRing<T, HD>::BYTES;
-    const hipError_t e = allow_lds<T, HD>(bytes);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_paged_tile<T, HD>), dim3((unsigned)grid), dim3(64 * TILE_WAVES), bytes, st, kv, ch, a, p.shares, p.least, p.q_tiles,
-                       vec_q, vec_out);
-    if (p.shares) hipLaunchKernelGGL((k_paged_merge<T, HD, TILE_CAP>), dim3(p.shares, TILE_CAP), dim3(256), 0, st, kv, ch, a, p.shares, vec_out);
-  } else {
-    hipLaunchKernelGGL((k_paged_stream<T, HD>), dim3((unsigned)grid), dim3(64 * STREAM_WAVES), 0, st, kv, ch, a, p.shares, p.least, p.q_tiles, vec_q,
-                       vec_out);
-    if (p.shares) hipLaunchKernelGGL((k_paged_merge<T, HD, 1>), dim3(p.shares, 1), dim3(256), 0, st, kv, ch, a, p.shares, vec_out);
+  const dim3 g((unsigned)grid);
+  if (!p.tile) {
+    hipLaunchKernelGGL((k_paged_stream<T, HD>), g, dim3(64 * STREAM_WAVES), 0, st, kv, ch, a, p.shares, p.least, p.q_tiles, vec_q, vec_out);
+    if (p.shares) hipLaunchKernelGGL((k_paged_merge<T, HD, 1>), dim3(p.shares, 1), dim3(256), 0, st, a, kv.hkv, p.shares, vec_out);
+    return hipGetLastError();
   }
+  constexpr unsigned bytes = TileRing<T, HD>::BYTES + TILE_ANC * 8;
+  constexpr int CAP = TILE_CAP<T>;
+  const hipError_t e = allow_lds<T, HD>(bytes);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_paged_tile<T, HD>), g, dim3(64 * TILE_WAVES), bytes, st, kv, ch, a, p.shares, p.least, p.q_tiles, vec_q, vec_out);
+  if (p.shares) hipLaunchKernelGGL((k_paged_merge<T, HD, CAP>), dim3(p.shares, CAP), dim3(256), 0, st, a, kv.hkv, p.shares, vec_out);
   return hipGetLastError();
 }
 
@@ -713,20 +943,19 @@ PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int
   const int G = hq / hkv;
   const int64_t cols = (int64_t)max_rows * G, keys = (int64_t)len_bound + max_rows;
   p.tile = cols > 32;
-  const int cap = p.tile ? TILE_CAP : 1, tk = p.tile ? TILE_TK : STREAM_TK;
+  const int tile_cap = dtype == ESP_F32 ? TILE_CAP<float> : TILE_CAP<bf16_t>, cap = p.tile ? tile_cap : 1, tk = p.tile ? TILE_TK : STREAM_TK;
   p.q_tiles = (int)std::max<int64_t>(1, ceil_div(ceil_div(cols, 32), cap));
   // items that there can be, and workgroups that have a place at once
   const int64_t items = (int64_t)hkv * std::min<int64_t>((int64_t)batch * p.q_tiles, ceil_div((int64_t)total_rows * G, 32 * cap) + batch);
-  const bool big = dtype == ESP_F32 || hd == 128;
   const int64_t places = 256 * (p.tile ? 1 : dtype == ESP_F32 && hd == 128 ? 1 : 2);
-  (void)big;
   p.least = p.tile ? 4 : 2;
   const int64_t tiles = ceil_div(keys, tk);
   if (tiles > p.least && items < 4 * places) p.shares = (int)std::min(places, ceil_div(items * tiles, p.least));
   return p;
 }
-size_t paged_attn_partial_floats(const PagedAttnPlan& p, int hd) {
-  return p.shares ? notes_floats(p.shares) + (size_t)2 * p.shares * 32 * (p.tile ? TILE_CAP : 1) * (hd + 2) : 0;
+size_t paged_attn_partial_floats(const PagedAttnPlan& p, int dtype, int hd) {
+  const int cap = !p.tile ? 1 : dtype == ESP_F32 ? TILE_CAP<float> : TILE_CAP<bf16_t>;
+  return p.shares ? notes_floats(p.shares) + (size_t)2 * p.shares * 32 * cap * (hd + 2) : 0;
 }
 
 hipError_t launch_paged_attn(hipStream_t st, int dtype, int hd, const PagedDev& kv, const ChunkDev& ch, const PagedAttnArgs& a,
