@@ -10,6 +10,7 @@
 // k_paged_tile (up to 256 columns in bf16, 128 in fp32) for chunks and trees, bound by the matrix cores: it walks a ring of key tiles in LDS.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "esp_attn_unit.h"
 #include "esp_paged.h"
@@ -404,13 +405,19 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) v
   });
 }
 
-template <int LPW>
-__device__ __forceinline__ void load_run(const unsigned char* src, uint32_t lane_off, uint32_t dst) {
-  load_to_lds16_sbase<0>(src, lane_off, dst);
-  if constexpr (LPW > 1) load_to_lds16_sbase<1024>(src, lane_off, dst);
-  if constexpr (LPW > 2) load_to_lds16_sbase<2048>(src, lane_off, dst);
-  if constexpr (LPW > 3) load_to_lds16_sbase<3072>(src, lane_off, dst);
-  if constexpr (LPW > 4) load_run<LPW - 4>(src + 4096, lane_off, dst + 4096);
+// piece J of a run of 1 KB pieces: a wave-uniform address and 16 bytes a lane, to dst + 16 x lane.  As text: the waits are counted by hand.
+template <int J>
+__device__ __forceinline__ void load_piece(const unsigned char* src, uint32_t lane_off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" ::"s"(dst + (J >> 2) * 4096), "v"(lane_off),
+               "s"(src + (J >> 2) * 4096), "n"((J & 3) * 1024)
+               : "memory", "m0");
+}
+template <int FROM, int TO>
+__device__ __forceinline__ void load_pieces(const unsigned char* src, uint32_t lane_off, uint32_t dst) {
+  if constexpr (FROM < TO) {
+    load_piece<FROM>(src, lane_off, dst);
+    load_pieces<FROM + 1, TO>(src, lane_off, dst);
+  }
 }
 // all but the youngest n tiles' loads of this wave have landed
 template <int LPW>
@@ -468,13 +475,25 @@ template <typename T, int HD> struct ColumnTile {
   __device__ __forceinline__ void start() {
     m = ATTN_UNSEEN; mb = 0.f; l = 0.f; limit = ATTN_UNSEEN;
   }
-  // (the empty statement keeps the exponential at its place beside the matrix instructions: its results are used blocks of code later, and
-  // the compiler would compute them there)
-  __device__ __forceinline__ void exp_of(int e, float scale) {
-    float x = __builtin_amdgcn_exp2f(fmaf(sc[e], scale, -mb));
-    l += x;
-    asm volatile("" : "+v"(x), "+v"(l));
-    p[e >> 3][e & 7] = from_f32<T>(x);
+  // Step s of a unit's exponentials, -2 .. 15: element s + 2 gets its exponent, s + 1 is raised, s goes to the sum and the operand.  A wave has
+  // its SIMD to itself, so what depends on each other is a step apart.  (The empty statements keep it beside the matrix instructions: the
+  // results are used blocks of code later, and the compiler would compute them there.)
+  __device__ __forceinline__ void exp_step(int s, float scale) {
+    if (s + 2 < 16) {
+      float x = fmaf(sc[s + 2], scale, -mb);
+      asm volatile("" : "+v"(x));
+      sc[s + 2] = x;
+    }
+    if (s + 1 >= 0 && s + 1 < 16) {
+      float x = __builtin_amdgcn_exp2f(sc[s + 1]);
+      asm volatile("" : "+v"(x));
+      sc[s + 1] = x;
+    }
+    if (s >= 0) {
+      l += sc[s];
+      asm volatile("" : "+v"(l));
+      p[s >> 3][s & 7] = from_f32<T>(sc[s]);
+    }
   }
   __device__ __forceinline__ void hide(unsigned seen) {
 #pragma unroll
@@ -570,10 +589,10 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
     for (int safe = 0;; ++safe) {
       int n = 2 * t0 + (wave & 1), pg = min(n, last_block) / blocks, in = min(n, last_block) - pg * blocks;
       int page = table[pg];
-      auto issue = [&](int i) {                   // tile t0 + i into its stage; called for i = 0, 1, 2, ...
+      // where this wave's part of the tile after the last that was asked for lies
+      auto next_source = [&]() {
         const int p = (unsigned)page < (unsigned)kv.n_pages ? page : 0;
         const unsigned char* src = my_pool + ((size_t)(p * kv.hkv + kvh) * blocks + in) * R::BLOCK;
-        load_run<R::LPW>(src, (uint32_t)lane * 16, my_lds + (uint32_t)(i % R::STAGES) * R::STAGE);
         n += 2;
         const int on = n <= last_block ? 2 : n - 1 == last_block ? 1 : 0;     // (a block behind the last that is needed is that one)
         if (on) {
@@ -581,7 +600,10 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
           while (in >= blocks) { in -= blocks; ++pg; }
           page = table[pg];
         }
+        return src;
       };
+      auto stage_of = [&](int i) { return my_lds + (uint32_t)(i % R::STAGES) * R::STAGE; };
+      auto issue = [&](int i) { load_pieces<0, R::LPW>(next_source(), (uint32_t)lane * 16, stage_of(i)); };   // tile t0 + i; for i = 0, 1, 2, ...
       // The last tile of the sequence: V of keys past its end as zeros (memory there may hold anything).  Safe: infinities and NaN out.
       auto clean = [&](int i) {
         const int left = total - (t0 + i) * TILE_TK;
@@ -630,7 +652,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
         if (i + 1 >= nt) return;
         wait_tiles_but<R::LPW>(min(R::AHEAD - 2, nt - 2 - i));
         __syncthreads();
-        if (i + R::AHEAD < nt) issue(i + R::AHEAD);
+        if (NT == 1 && i + R::AHEAD < nt) issue(i + R::AHEAD);
         clean(i + 1);
       };
       const unsigned char* frag = lds + lane * 8 * sizeof(T);
@@ -663,11 +685,21 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
           tile[c].follow(top, a.scale, slack, o[c]);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) tile[0].exp_of(e, a.scale);
+        for (int e = -2; e < 16; ++e) tile[0].exp_step(e, a.scale);
+        tile[1].exp_step(-2, a.scale);
+        tile[1].exp_step(-1, a.scale);
 #pragma unroll
         for (int j = 0; j < NS; ++j) kf[j] = *reinterpret_cast<const bf16x8_t*>(unit_at(1) + j * 1024);
+        auto load_pair = [&](int j, const unsigned char* src, uint32_t dst) {  // quarter j of a part; j a constant
+          constexpr int Q = R::LPW / (NS / 2);
+          if (j == 0) load_pieces<0, Q>(src, (uint32_t)lane * 16, dst);
+          else if (j == 1) load_pieces<Q, 2 * Q>(src, (uint32_t)lane * 16, dst);
+          else if (j == 2) load_pieces<2 * Q, 3 * Q>(src, (uint32_t)lane * 16, dst);
+          else load_pieces<3 * Q, 4 * Q>(src, (uint32_t)lane * 16, dst);
+        };
         float l0 = 0.f;
-        for (int u = 0; u < 2 * nt; ++u) {
+        auto unit = [&](auto odd_unit, int u) {
+          constexpr bool ODD = decltype(odd_unit)::value;
           // (behind the last unit the scores are of what lies in LDS, and for nothing)
           const unsigned char* v = unit_at(u) + 2 * R::BLOCK;
           const bool more = u + 1 < 2 * nt;
@@ -677,10 +709,13 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < NS; ++j) {
-            vf[j] = *reinterpret_cast<const bf16x8_t*>(v + j * 1024);
+            if (j < NS / 2) {                     // (half a group ahead of their use)
+              vf[2 * j] = *reinterpret_cast<const bf16x8_t*>(v + 2 * j * 1024);
+              vf[2 * j + 1] = *reinterpret_cast<const bf16x8_t*>(v + (2 * j + 1) * 1024);
+            }
             next = attn_mma(kf[j], qf[0][j], next);
 #pragma unroll
-            for (int e = 0; e < EPI; ++e) tile[1].exp_of(j * EPI + e, a.scale);
+            for (int e = 0; e < EPI; ++e) tile[1].exp_step(j * EPI + e, a.scale);
             __builtin_amdgcn_sched_barrier(0);
           }
           tile[0].sc = next;
@@ -692,7 +727,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
           for (int j = 0; j < NS; ++j) {
             tile_out(o[0][j % DB], vf[2 * (j % DB) + j / DB], tile[0].p[j / DB]);
 #pragma unroll
-            for (int e = 0; e < EPI; ++e) tile[1].exp_of(8 + j * EPI + e, a.scale);
+            for (int e = 0; e < EPI; ++e) tile[1].exp_step(8 + j * EPI + e, a.scale);
             if (j >= NS / 2) {                    // (the scores are there by now)
 #pragma unroll
               for (int e = 0; e < 2 * EPI; ++e) tile[0].top_of(top, (j - NS / 2) * 2 * EPI + e);
@@ -701,28 +736,42 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
           }
           if (more) tile[0].follow(top, a.scale, slack, o[0]);
           l0 = tile[0].l;
+          tile[0].exp_step(-2, a.scale);
+          tile[0].exp_step(-1, a.scale);
           tile_zero(next);
+          // in the second unit of a tile the loads of the tile after next, a few beside each matrix instruction: a wave that
+          // asks for them all at once has nothing else to do meanwhile
+          const bool ask = ODD && (u >> 1) + R::AHEAD < nt;
+          const unsigned char* src = nullptr;
+          if (ask) src = next_source();
+          const uint32_t dst = stage_of((u >> 1) + R::AHEAD);
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < NS; ++j) {
+            if (ODD && j % 2 == 0) {
+              if (ask) load_pair(j / 2, src, dst);
+            }
             next = attn_mma(kf[j], qf[1][j], next);
 #pragma unroll
-            for (int e = 0; e < EPI; ++e) tile[0].exp_of(j * EPI + e, a.scale);
+            for (int e = 0; e < EPI; ++e) tile[0].exp_step(j * EPI + e, a.scale);
             __builtin_amdgcn_sched_barrier(0);
           }
           tile[1].sc = next;
           if (more && u + 1 >= hide_at[1]) tile[1].hide(seen_of(1, u + 1));
-          if ((u & 1) == 0) next_tile(u >> 1);
+          if constexpr (!ODD) next_tile(u >> 1);
           const unsigned char* k = unit_at(u + 2);
           top = ATTN_UNSEEN;
           tile_begin();
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < NS; ++j) {
-            kf[j] = *reinterpret_cast<const bf16x8_t*>(k + j * 1024);
+            if (j < NS / 2) {
+              kf[2 * j] = *reinterpret_cast<const bf16x8_t*>(k + 2 * j * 1024);
+              kf[2 * j + 1] = *reinterpret_cast<const bf16x8_t*>(k + (2 * j + 1) * 1024);
+            }
             tile_out(o[1][j % DB], vf[2 * (j % DB) + j / DB], tile[1].p[j / DB]);
 #pragma unroll
-            for (int e = 0; e < EPI; ++e) tile[0].exp_of(8 + j * EPI + e, a.scale);
+            for (int e = 0; e < EPI; ++e) tile[0].exp_step(8 + j * EPI + e, a.scale);
             if (j >= NS / 2) {
 #pragma unroll
               for (int e = 0; e < 2 * EPI; ++e) tile[1].top_of(top, (j - NS / 2) * 2 * EPI + e);
@@ -730,6 +779,12 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
             __builtin_amdgcn_sched_barrier(0);
           }
           if (more) tile[1].follow(top, a.scale, slack, o[1]);
+          tile[1].exp_step(-2, a.scale);
+          tile[1].exp_step(-1, a.scale);
+        };
+        for (int i = 0; i < nt; ++i) {
+          unit(std::false_type{}, 2 * i);
+          unit(std::true_type{}, 2 * i + 1);
         }
         tile[0].l = l0;                           // (without the exponentials behind the last unit)
         }
@@ -746,6 +801,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
               attn_unit<T, HD>(st, st + 2 * R::BLOCK, masked, masked ? seen_of(0, u) : ~0u, a.scale, qf[0], o[0], tile[0].m, tile[0].l);
             }
           next_tile(i);
+          if (NT == 2 && i + R::AHEAD < nt) issue(i + R::AHEAD);
         }
       }
 #pragma unroll
