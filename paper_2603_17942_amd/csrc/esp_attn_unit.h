@@ -22,6 +22,12 @@ __device__ __forceinline__ f32x16_t attn_mma(f32x8_t a, f32x8_t b, f32x16_t c) {
   return c;
 }
 
+__device__ __forceinline__ float attn_sum_of_halves(float v) {
+  const unsigned u = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 constexpr float ATTN_UNSEEN = -1.0e30f;      // score of a hidden key, and start of a column's running maximum
 constexpr float ATTN_SLACK = 24.0f;          // powers of two by which a score may exceed the exponents' reference before that moves
 

@@ -33,6 +33,18 @@ __device__ __forceinline__ int opaque(int x) {
   return x;
 }
 
+// does a thread of the workgroup say so; said: LDS, a word a wave
+template <int WAVES>
+__device__ __forceinline__ bool any_thread(bool here, int* said) {
+  const bool mine = __builtin_amdgcn_ballot_w64(here) != 0ull;
+  said[threadIdx.x >> 6] = mine;                  // (all lanes the same)
+  __syncthreads();
+  int any = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) any |= said[w];
+  return uniform(any) != 0;
+}
+
 // ---- the line of work --------------------------------------------------------------------------------------------
 struct Item { int seq, kvh, qt; };
 struct Cut { Item item; int tile; };            // before key tile `tile` of the item
@@ -368,7 +380,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) v
         const int n = (key_lo >> 5) + wave + W * i, c_lo = 32 * n - s.len;
         if (c_lo + 32 > 0) add_odd(n, c_lo, total - 32 * n);
       }
-    l += __shfl_xor(l, 32, 64);
+    l = attn_sum_of_halves(l);
     // the waves' parts meet in LDS
     const int tid = opaque(threadIdx.x), lane = tid & 63;
     if (live) {
@@ -446,6 +458,7 @@ template <typename T, int HD> struct TileRing {
   // the stage it came from is not free yet.
   static constexpr int AHEAD = STAGES - (TILE_NT<T> - 1);
   static constexpr int BYTES = STAGE * STAGES;
+  static_assert((BYTES & (BYTES - 1)) == 0);
   static_assert(BYTES >= TILE_CAP<T> * 32 * HD * 4, "the columns of all waves go there at the end");
 };
 constexpr int TILE_ANC = 2560;                    // 64-bit words of ancestor bitsets that are kept in LDS
@@ -512,9 +525,11 @@ template <typename T, int HD> struct ColumnTile {
     l *= f;
     tile_settle(o);
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i)
+    for (int i = 0; i < HD / 32; ++i) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) o[i][v] *= f;
+      asm volatile("" : "+a"(o[i]));              // (back where it was, one after the other)
+    }
   }
 };
 
@@ -527,6 +542,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
   extern __shared__ __align__(16) unsigned char lds[];
   uint64_t* anc_lds = reinterpret_cast<uint64_t*>(lds + R::BYTES);
   __shared__ float xm[TILE_WAVES][32], xl[TILE_WAVES][32];
+  __shared__ int said[2][TILE_WAVES];
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, lg = lane >> 5;
   const int wave = uniform(tid >> 6);
   const int G = a.hq / kv.hkv, blocks = kv.page_size >> 5;
@@ -562,23 +578,25 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
     const int row_lo = col0 / G, n_rows = (min(ncols, col0 + ct * 32) - 1) / G - row_lo + 1;
     const bool anc_here = !causal && (int64_t)n_rows * a.anc_words <= TILE_ANC;
     if (anc_here)
-      for (int i = tid; i < n_rows * a.anc_words; i += 64 * TILE_WAVES) anc_lds[i] = a.anc[(size_t)(s.row0 + row_lo) * a.anc_words + i];
+      for (int i = opaque(tid); i < n_rows * a.anc_words; i += 64 * TILE_WAVES) anc_lds[i] = a.anc[(size_t)(s.row0 + row_lo) * a.anc_words + i];
     auto window_of = [&](int c, int c_lo) {
-      if (causal) return attn_low_bits(min(r[c], s.rows - 1) + 1 - c_lo);
-      const int at = (r[c] - row_lo) * a.anc_words;
-      if (anc_here)
-        return attn_tree_window([&](int i) { return i < a.anc_words && live[c] ? anc_lds[at + i] : 0ull; }, c_lo, s.rows);
-      const uint64_t* w = a.anc + (size_t)(s.row0 + r[c]) * a.anc_words;
+      const int row = opaque(r[c]);               // (of a dead column: the first)
+      if (causal) return attn_low_bits(row + 1 - c_lo);
+      if (anc_here) {
+        const uint64_t* w = anc_lds + max(row - row_lo, 0) * a.anc_words;
+        return attn_tree_window([&](int i) { return i < a.anc_words ? w[i] : 0ull; }, c_lo, s.rows);
+      }
+      const uint64_t* w = a.anc + (size_t)(s.row0 + row) * a.anc_words;
       return attn_tree_window([&](int i) { return i < a.anc_words ? w[i] : 0ull; }, c_lo, s.rows);
     };
 
     // are all pages there?  (Where one is not, its keys are looked at one block after the other.)
     bool bad = false;
     const int last_block = (min(keys, t1 * TILE_TK) - 1) >> 5;
-    for (int p = 2 * t0 / blocks + tid; p <= last_block / blocks; p += 64 * TILE_WAVES)
+    for (int p = 2 * t0 / blocks + opaque(tid); p <= last_block / blocks; p += 64 * TILE_WAVES)
       bad |= (unsigned)kv.table[(size_t)seq * kv.stride + p] >= (unsigned)kv.n_pages;
     if (bad) set_status(kv.status, ESP_DEV_BAD_PAGE);
-    const bool any_bad = __syncthreads_or(bad);
+    const bool any_bad = any_thread<TILE_WAVES>(bad, said[0]);
     const bool hides = (int64_t)t1 * TILE_TK > s.len && s.rows > 1;           // some key of the piece may be hidden from some column
 
     frag_t qf[NT][NS];
@@ -589,10 +607,12 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
     for (int safe = 0;; ++safe) {
       int n = 2 * t0 + (wave & 1), pg = min(n, last_block) / blocks, in = min(n, last_block) - pg * blocks;
       int page = table[pg];
-      // where this wave's part of the tile after the last that was asked for lies
-      auto next_source = [&]() {
+      // where this wave's part of the tile after the last that was asked for lies, and on to the next one
+      auto source = [&]() {
         const int p = (unsigned)page < (unsigned)kv.n_pages ? page : 0;
-        const unsigned char* src = my_pool + ((size_t)(p * kv.hkv + kvh) * blocks + in) * R::BLOCK;
+        return my_pool + ((size_t)(p * kv.hkv + kvh) * blocks + in) * R::BLOCK;
+      };
+      auto advance = [&]() {
         n += 2;
         const int on = n <= last_block ? 2 : n - 1 == last_block ? 1 : 0;     // (a block behind the last that is needed is that one)
         if (on) {
@@ -600,22 +620,25 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
           while (in >= blocks) { in -= blocks; ++pg; }
           page = table[pg];
         }
-        return src;
       };
       auto stage_of = [&](int i) { return my_lds + (uint32_t)(i % R::STAGES) * R::STAGE; };
-      auto issue = [&](int i) { load_pieces<0, R::LPW>(next_source(), (uint32_t)lane * 16, stage_of(i)); };   // tile t0 + i; for i = 0, 1, 2, ...
+      auto issue = [&](int i) {                   // tile t0 + i; called for i = 0, 1, 2, ...
+        load_pieces<0, R::LPW>(source(), (uint32_t)lane * 16, stage_of(i));
+        advance();
+      };
       // The last tile of the sequence: V of keys past its end as zeros (memory there may hold anything).  Safe: infinities and NaN out.
+      const int clean_from = (safe ? s.len : total) / TILE_TK - t0;
       auto clean = [&](int i) {
+        if (i < clean_from) return;
         const int left = total - (t0 + i) * TILE_TK;
-        const bool tail = left < TILE_TK, odd = safe && left - TILE_TK < s.rows;
-        if (!tail && !odd) return;
+        const bool tail = left < TILE_TK, odd = safe;
         unsigned char* v = lds + (i % R::STAGES) * R::STAGE + 2 * R::BLOCK;
         constexpr int PIECE = 8 * sizeof(T), IN = R::BLOCK / PIECE;
-        for (int x = tid; x < 2 * IN; x += 64 * TILE_WAVES) {                  // piece x: block, fragment (db, u), lane
+        for (int x = opaque(tid); x < 2 * IN; x += 64 * TILE_WAVES) {          // piece x: block, fragment (db, u), lane
           const int in_block = x % IN, u = (in_block >> 6) & 1;
           frag_t f = *reinterpret_cast<const frag_t*>(v + x * PIECE);
           if (tail) f = attn_zero_tail(f, u, in_block & 63, left - (x >= IN ? 32 : 0));
-          if (odd) attn_take_odd(f);
+          if (odd) attn_take_odd(f);              // (safe: of all tiles with rows of the chunk)
           *reinterpret_cast<frag_t*>(v + x * PIECE) = f;
         }
         __syncthreads();
@@ -664,129 +687,157 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
       auto seen_of = [&](int c, int u) -> unsigned {                          // bits of this lane's keys of unit u
         const int key0 = t0 * TILE_TK + 32 * u;
         if (any_bad && (key0 >= keys || (unsigned)table[(key0 >> 5) / blocks] >= (unsigned)kv.n_pages)) return 0u;
-        return window_of(c, key0 - s.len) >> (4 * lg);
+        return window_of(c, key0 - s.len) >> (opaque(lane) >> 5 << 2);
       };
 
       auto two_tiles = [&]() {
         if constexpr (NT == 2) {
-        bf16x8_t kf[NS], vf[NS];                  // V: fragment (db, u) at 2 db + u
-        auto unit_at = [&](int u) { return frag + ((u >> 1) % R::STAGES) * R::STAGE + (u & 1) * R::BLOCK; };
+          bf16x8_t kf[NS], vf[NS];                // V: fragment (db, u) at 2 db + u
+          auto read = [&](bf16x8_t (&f)[NS], const unsigned char* at, int j) { f[j] = *reinterpret_cast<const bf16x8_t*>(at + j * 1024); };
 #pragma unroll
-        for (int j = 0; j < NS; ++j) kf[j] = *reinterpret_cast<const bf16x8_t*>(unit_at(0) + j * 1024);
+          for (int j = 0; j < NS; ++j) read(kf, frag, j);
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-          tile_zero(tile[c].sc);
+          for (int c = 0; c < NT; ++c) {
+            tile_zero(tile[c].sc);
 #pragma unroll
-          for (int j = 0; j < NS; ++j) tile[c].sc = attn_mma(kf[j], qf[c][j], tile[c].sc);
-          if (hide_at[c] <= 0) tile[c].hide(seen_of(c, 0));
-          float top = ATTN_UNSEEN;
+            for (int j = 0; j < NS; ++j) tile[c].sc = attn_mma(kf[j], qf[c][j], tile[c].sc);
+            if (hide_at[c] <= 0) tile[c].hide(seen_of(c, 0));
+            float top = ATTN_UNSEEN;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) tile[c].top_of(top, e);
-          tile[c].follow(top, a.scale, slack, o[c]);
-        }
-#pragma unroll
-        for (int e = -2; e < 16; ++e) tile[0].exp_step(e, a.scale);
-        tile[1].exp_step(-2, a.scale);
-        tile[1].exp_step(-1, a.scale);
-#pragma unroll
-        for (int j = 0; j < NS; ++j) kf[j] = *reinterpret_cast<const bf16x8_t*>(unit_at(1) + j * 1024);
-        auto load_pair = [&](int j, const unsigned char* src, uint32_t dst) {  // quarter j of a part; j a constant
-          constexpr int Q = R::LPW / (NS / 2);
-          if (j == 0) load_pieces<0, Q>(src, (uint32_t)lane * 16, dst);
-          else if (j == 1) load_pieces<Q, 2 * Q>(src, (uint32_t)lane * 16, dst);
-          else if (j == 2) load_pieces<2 * Q, 3 * Q>(src, (uint32_t)lane * 16, dst);
-          else load_pieces<3 * Q, 4 * Q>(src, (uint32_t)lane * 16, dst);
-        };
-        float l0 = 0.f;
-        auto unit = [&](auto odd_unit, int u) {
-          constexpr bool ODD = decltype(odd_unit)::value;
-          // (behind the last unit the scores are of what lies in LDS, and for nothing)
-          const unsigned char* v = unit_at(u) + 2 * R::BLOCK;
-          const bool more = u + 1 < 2 * nt;
-          f32x16_t next;
-          float top;
-          tile_zero(next);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int j = 0; j < NS; ++j) {
-            if (j < NS / 2) {                     // (half a group ahead of their use)
-              vf[2 * j] = *reinterpret_cast<const bf16x8_t*>(v + 2 * j * 1024);
-              vf[2 * j + 1] = *reinterpret_cast<const bf16x8_t*>(v + (2 * j + 1) * 1024);
-            }
-            next = attn_mma(kf[j], qf[0][j], next);
-#pragma unroll
-            for (int e = 0; e < EPI; ++e) tile[1].exp_step(j * EPI + e, a.scale);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int e = 0; e < 8; ++e) tile[c].top_of(top, e);
+            tile[c].follow(top, a.scale, slack, o[c]);
           }
-          tile[0].sc = next;
-          if (more && u + 1 >= hide_at[0]) tile[0].hide(seen_of(0, u + 1));
-          top = ATTN_UNSEEN;
-          tile_begin();
-          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int j = 0; j < NS; ++j) {
-            tile_out(o[0][j % DB], vf[2 * (j % DB) + j / DB], tile[0].p[j / DB]);
-#pragma unroll
-            for (int e = 0; e < EPI; ++e) tile[1].exp_step(8 + j * EPI + e, a.scale);
-            if (j >= NS / 2) {                    // (the scores are there by now)
-#pragma unroll
-              for (int e = 0; e < 2 * EPI; ++e) tile[0].top_of(top, (j - NS / 2) * 2 * EPI + e);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          if (more) tile[0].follow(top, a.scale, slack, o[0]);
-          l0 = tile[0].l;
-          tile[0].exp_step(-2, a.scale);
-          tile[0].exp_step(-1, a.scale);
-          tile_zero(next);
-          // in the second unit of a tile the loads of the tile after next, a few beside each matrix instruction: a wave that
-          // asks for them all at once has nothing else to do meanwhile
-          const bool ask = ODD && (u >> 1) + R::AHEAD < nt;
-          const unsigned char* src = nullptr;
-          if (ask) src = next_source();
-          const uint32_t dst = stage_of((u >> 1) + R::AHEAD);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int j = 0; j < NS; ++j) {
-            if (ODD && j % 2 == 0) {
-              if (ask) load_pair(j / 2, src, dst);
-            }
-            next = attn_mma(kf[j], qf[1][j], next);
-#pragma unroll
-            for (int e = 0; e < EPI; ++e) tile[0].exp_step(j * EPI + e, a.scale);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          tile[1].sc = next;
-          if (more && u + 1 >= hide_at[1]) tile[1].hide(seen_of(1, u + 1));
-          if constexpr (!ODD) next_tile(u >> 1);
-          const unsigned char* k = unit_at(u + 2);
-          top = ATTN_UNSEEN;
-          tile_begin();
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int j = 0; j < NS; ++j) {
-            if (j < NS / 2) {
-              kf[2 * j] = *reinterpret_cast<const bf16x8_t*>(k + 2 * j * 1024);
-              kf[2 * j + 1] = *reinterpret_cast<const bf16x8_t*>(k + (2 * j + 1) * 1024);
-            }
-            tile_out(o[1][j % DB], vf[2 * (j % DB) + j / DB], tile[1].p[j / DB]);
-#pragma unroll
-            for (int e = 0; e < EPI; ++e) tile[0].exp_step(8 + j * EPI + e, a.scale);
-            if (j >= NS / 2) {
-#pragma unroll
-              for (int e = 0; e < 2 * EPI; ++e) tile[1].top_of(top, (j - NS / 2) * 2 * EPI + e);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          if (more) tile[1].follow(top, a.scale, slack, o[1]);
+          for (int e = -2; e < 16; ++e) tile[0].exp_step(e, a.scale);
           tile[1].exp_step(-2, a.scale);
           tile[1].exp_step(-1, a.scale);
-        };
-        for (int i = 0; i < nt; ++i) {
-          unit(std::false_type{}, 2 * i);
-          unit(std::true_type{}, 2 * i + 1);
+#pragma unroll
+          for (int j = 0; j < NS; ++j) read(kf, frag + R::BLOCK, j);
+          const int hide0 = hide_at[0] - 1, hide1 = hide_at[1] - 1;
+          uint32_t here = 0, then = R::STAGE;     // stages of this tile and the next
+          // One unit.  Everything scalar that can wait is put between matrix instructions too: a wave that does 30 scalar instructions in a
+          // row has let its matrix core run dry.  Behind the piece's last unit the scores are of what lies in LDS, and for nothing.
+          float l0 = 0.f;
+          auto unit = [&](auto odd_unit, int i) {
+            constexpr bool ODD = decltype(odd_unit)::value;
+            const int u = 2 * i + ODD;
+            const unsigned char* v = frag + here + (2 + ODD) * R::BLOCK;
+            f32x16_t next;
+            float top = ATTN_UNSEEN;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NS; ++j) {
+              if (j < NS / 2) { read(vf, v, 2 * j); read(vf, v, 2 * j + 1); }         // (half a group ahead of their use)
+              if (j == 0) tile_zero(next);
+              next = attn_mma(kf[j], qf[0][j], next);
+#pragma unroll
+              for (int e = 0; e < EPI; ++e) tile[1].exp_step(j * EPI + e, a.scale);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+            tile[0].sc = next;
+            if (u >= hide0) tile[0].hide(seen_of(0, u + 1));
+            // (in the second unit of a tile the tile after next is asked for)
+            const bool ask = ODD && i + R::AHEAD < nt;
+            const unsigned char* src = nullptr;
+            uint32_t dst = 0;
+            tile_begin();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NS; ++j) {
+              tile_out(o[0][j % DB], vf[2 * (j % DB) + j / DB], tile[0].p[j / DB]);
+#pragma unroll
+              for (int e = 0; e < EPI; ++e) tile[1].exp_step(8 + j * EPI + e, a.scale);
+              if (ODD && j == 1) {
+                src = source();
+                dst = stage_of(i + R::AHEAD);
+              }
+              if (j >= NS / 2) {         // (the scores are there by now)
+#pragma unroll
+                for (int e = 0; e < 2 * EPI; ++e) tile[0].top_of(top, (j - NS / 2) * 2 * EPI + e);
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+            tile[0].follow(top, a.scale, slack, o[0]);
+            l0 = tile[0].l;
+            tile[0].exp_step(-2, a.scale);
+            tile[0].exp_step(-1, a.scale);
+            tile_zero(next);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NS; ++j) {
+              next = attn_mma(kf[j], qf[1][j], next);
+              if (ODD && j % 2 == 0 && ask) {
+                constexpr int Q = R::LPW / (NS / 2);
+                if (j == 0) load_pieces<0, Q>(src, (uint32_t)lane * 16, dst);
+                if (j == 2) load_pieces<Q, 2 * Q>(src, (uint32_t)lane * 16, dst);
+                if (j == 4) load_pieces<2 * Q, 3 * Q>(src, (uint32_t)lane * 16, dst);
+                if (j == 6) load_pieces<3 * Q, 4 * Q>(src, (uint32_t)lane * 16, dst);
+              }
+#pragma unroll
+              for (int e = 0; e < EPI; ++e) tile[0].exp_step(j * EPI + e, a.scale);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+            tile[1].sc = next;
+            if (u >= hide1) tile[1].hide(seen_of(1, u + 1));
+            if constexpr (!ODD) next_tile(i);
+            const unsigned char* k = frag + then + ODD * R::BLOCK;
+            top = ATTN_UNSEEN;
+            tile_begin();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < NS; ++j) {
+              tile_out(o[1][j % DB], vf[2 * (j % DB) + j / DB], tile[1].p[j / DB]);
+              if (j < NS / 2) { read(kf, k, 2 * j); read(kf, k, 2 * j + 1); }
+#pragma unroll
+              for (int e = 0; e < EPI; ++e) tile[0].exp_step(8 + j * EPI + e, a.scale);
+              if (ODD && j == NS / 2 && ask) advance();
+              if (j >= NS / 2) {
+#pragma unroll
+                for (int e = 0; e < 2 * EPI; ++e) tile[1].top_of(top, (j - NS / 2) * 2 * EPI + e);
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+            tile[1].follow(top, a.scale, slack, o[1]);
+            tile[1].exp_step(-2, a.scale);
+            tile[1].exp_step(-1, a.scale);
+          };
+          for (int i = 0; i < nt; ++i) {
+            unit(std::false_type{}, i);
+            if (i + 1 == nt) tile[0].limit = tile[1].limit = INFINITY;        // (nothing moves the references any more)
+            unit(std::true_type{}, i);
+            here = then;
+            then = (then + R::STAGE) & (R::BYTES - 1);
+          }
+          tile[0].l = l0;
         }
-        tile[0].l = l0;                           // (without the exponentials behind the last unit)
+      };
+      // one column tile: a unit's steps one after the other
+      auto one_tile = [&](int u, const unsigned char* at) {
+        const bool masked = u >= hide_at[0];
+        if constexpr (NT == 1) {
+          attn_unit<T, HD>(at, at + 2 * R::BLOCK, masked, masked ? seen_of(0, u) : ~0u, a.scale, qf[0], o[0], tile[0].m, tile[0].l);
+        } else {
+          bf16x8_t f[NS];
+#pragma unroll
+          for (int j = 0; j < NS; ++j) f[j] = *reinterpret_cast<const bf16x8_t*>(at + j * 1024);
+          tile_zero(tile[0].sc);
+#pragma unroll
+          for (int j = 0; j < NS; ++j) tile[0].sc = attn_mma(f[j], qf[0][j], tile[0].sc);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < NS; ++j) f[j] = *reinterpret_cast<const bf16x8_t*>(at + 2 * R::BLOCK + j * 1024);
+          if (masked) tile[0].hide(seen_of(0, u));
+          float top = ATTN_UNSEEN;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) tile[0].top_of(top, e);
+          tile[0].follow(top, a.scale, slack, o[0]);
+#pragma unroll
+          for (int e = -2; e < 16; ++e) tile[0].exp_step(e, a.scale);
+          tile_begin();
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < NS; ++j) tile_out(o[0][j % DB], f[2 * (j % DB) + j / DB], tile[0].p[j / DB]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       };
       if (mine == 2) {
@@ -794,12 +845,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
       } else {
         for (int i = 0; i < nt; ++i) {
           if (mine == 1)
-            for (int kh = kh0; kh <= kh1; ++kh) {
-              const int u = 2 * i + kh;
-              const unsigned char* st = frag + (i % R::STAGES) * R::STAGE + kh * R::BLOCK;
-              const bool masked = u >= hide_at[0];
-              attn_unit<T, HD>(st, st + 2 * R::BLOCK, masked, masked ? seen_of(0, u) : ~0u, a.scale, qf[0], o[0], tile[0].m, tile[0].l);
-            }
+            for (int kh = kh0; kh <= kh1; ++kh) one_tile(2 * i + kh, frag + (i % R::STAGES) * R::STAGE + kh * R::BLOCK);
           next_tile(i);
           if (NT == 2 && i + R::AHEAD < nt) issue(i + R::AHEAD);
         }
@@ -815,7 +861,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
           const T* v = (const T*)kv.v + ((size_t)(p * kv.hkv + kvh) * blocks + n % blocks) * (32 * HD);
 #pragma unroll
           for (int c = 0; c < NT; ++c)
-            if (c < mine) attn_add_odd<T, HD>(v, window_of(c, key0 - s.len) >> (4 * lg), total - key0, lane, o[c]);
+            if (c < mine) attn_add_odd<T, HD>(v, window_of(c, key0 - s.len) >> (opaque(lane) >> 5 << 2), total - key0, opaque(lane), o[c]);
         }
         break;
       }
@@ -829,7 +875,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
 #pragma unroll
             for (int v = 0; v < 16; ++v) most = max(most, __float_as_uint(o[c][i][v]) & 0x7fffffffu);
         }
-      if (!__syncthreads_or(most >= 0x7f800000u)) break;
+      if (!any_thread<TILE_WAVES>(most >= 0x7f800000u, said[1])) break;
     }
 
     // the ring is done with: a wave's columns, [tile][32][HD], one wave's behind the other's
@@ -837,7 +883,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
     const int lane = opaque(threadIdx.x) & 63, lr = lane & 31, lg = lane >> 5;
     float* xo = reinterpret_cast<float*>(lds) + wave * (32 * NT * HD);
 #pragma unroll
-    for (int c = 0; c < NT; ++c) tile[c].l += __shfl_xor(tile[c].l, 32, 64);
+    for (int c = 0; c < NT; ++c) tile[c].l = attn_sum_of_halves(tile[c].l);
     if (halves) {                                 // the second half of the keys goes to the wave that has the first
       if (mine == 1 && kh0 == 1) {
         put_columns<HD>(xo, o[0], lane);
