@@ -56,13 +56,13 @@ hipError_t launch_paged_load(hipStream_t st, int dtype, int hd, const PagedDev& 
                              void* v_rows);
 
 struct PagedAttnPlan {
-  bool tile = false;          // k_paged_tile
+  int cap = 1;                // column tiles of an item at most; 1: k_paged_stream
   int q_tiles = 1;            // items of a sequence and kv head at most
   int shares = 0;             // 0: a workgroup an item
   int least = 1;              // key tiles of a share at least
 };
 PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int len_bound);
-size_t paged_attn_partial_floats(const PagedAttnPlan& p, int dtype, int hd);
+size_t paged_attn_partial_floats(const PagedAttnPlan& p, int hd);
 struct PagedAttnArgs {
   const void* q;
   int64_t q_stride;

@@ -131,7 +131,7 @@ size_t esp_paged_attn_scratch_bytes(const esp_paged_kv* kv, const esp_chunk* row
   if (check_paged(kv) != ESP_OK || check_chunk(kv, rows) != ESP_OK || n_q < 1 || n_q % kv->n_kv_heads) return 0;
   if (rows->total_rows == 0 || rows->max_rows == 0) return 0;
   const PagedAttnPlan p = paged_attn_plan(kv->dtype, kv->head_dim, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, kv->len_bound);
-  return paged_attn_partial_floats(p, kv->dtype, kv->head_dim) * 4;
+  return paged_attn_partial_floats(p, kv->head_dim) * 4;
 }
 
 esp_status esp_paged_attn(void* stream, const esp_paged_kv* kv, int32_t layer, const esp_chunk* rows, int32_t n_q, const void* q,
@@ -149,7 +149,7 @@ esp_status esp_paged_attn(void* stream, const esp_paged_kv* kv, int32_t layer, c
   if ((int64_t)rows->max_rows * (n_q / kv->n_kv_heads) > INT32_MAX / 2) return ESP_ECAPACITY;
   if (rows->total_rows == 0 || rows->max_rows == 0) return ESP_OK;
   const PagedAttnPlan p = paged_attn_plan(kv->dtype, kv->head_dim, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, kv->len_bound);
-  const size_t need = paged_attn_partial_floats(p, kv->dtype, kv->head_dim) * 4;
+  const size_t need = paged_attn_partial_floats(p, kv->head_dim) * 4;
   if (need && (!scratch || scratch_bytes < need)) return ESP_ECAPACITY;
   if (need && (uintptr_t)scratch % 16) return ESP_EINVAL;
   PagedAttnArgs a{q, q_stride, out, anc, anc_words, n_q, scale, (float*)scratch};

@@ -10,6 +10,7 @@
 // k_paged_tile (up to 256 columns in bf16, 128 in fp32) for chunks and trees, bound by the matrix cores: it walks a ring of key tiles in LDS.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <type_traits>
 
 #include "esp_attn_unit.h"
@@ -22,7 +23,7 @@ constexpr int MOST_SHARES = 512;
 constexpr int STREAM_WAVES = 4, STREAM_TK = 32 * STREAM_WAVES;
 constexpr int TILE_WAVES = 4, TILE_TK = 64;
 template <typename T> constexpr int TILE_NT = sizeof(T) == 2 ? 2 : 1;              // column tiles of a wave
-template <typename T> constexpr int TILE_CAP = TILE_WAVES * TILE_NT<T>;            // and of an item
+template <typename T> constexpr int TILE_CAP = TILE_WAVES * TILE_NT<T>;            // and of an item at most
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // a value that the compiler does not see through: what is computed from it stays where it is used.  (Addresses that it takes out of a loop
@@ -47,101 +48,119 @@ __device__ __forceinline__ bool any_thread(bool here, int* said) {
 
 // ---- the line of work --------------------------------------------------------------------------------------------
 struct Item { int seq, kvh, qt; };
-struct Cut { Item item; int tile; };            // before key tile `tile` of the item
+struct Place { int seq, kvh, at; };             // item `at` of a sequence and kv head in the line's order
+struct Cut { Place place; int tile; };          // before key tile `tile` of the item there
 
 // what a sequence's items are: n of them for each kv head, of `per` column tiles, the last one of what is left
 struct Items { int n, per; };
 __host__ __device__ __forceinline__ Items items_of(int rows, int G, int cap) {
   const int ct = (rows * G + 31) / 32, n = (ct + cap - 1) / cap;      // (the host has checked rows * G)
-  return {n, min(ct, cap)};
+  return {n, n ? (ct + n - 1) / n : 0};
 }
 // keys that item qt sees
 __device__ __forceinline__ int keys_of(const ChunkSeq& s, int G, int per, int qt, bool causal) {
   const int rows = causal ? min(s.rows, ((qt + 1) * per * 32 + G - 1) / G) : s.rows;
   return s.len + rows;
 }
+// The line's order of a sequence's items: the last (which sees the most keys), the first, the last but one, the second ..., so that two
+// neighbours weigh the same.
+__device__ __forceinline__ int item_at(int n, int at) { return at & 1 ? at >> 1 : n - 1 - (at >> 1); }
 // Weights along the line, in keys x time of a key tile: an item counts `start` for its beginning and end and its keys.  Cuts need not be
-// exact, only the same for everybody; doubles hold them.
+// exact, only the same for everybody, and never before the one in front.
 struct Weights {
-  double first, slope;                            // item k weighs first + slope (k + 1)
-  __device__ __forceinline__ double upto(int k) const { return first * k + slope * (0.5 * k * (k + 1)); }
+  float first, slope;                             // item k weighs first + slope (k + 1)
+  __device__ __forceinline__ float of(int k) const { return first + slope * (float)(k + 1); }
+  __device__ __forceinline__ float sum(int n) const { return first * (float)n + slope * (0.5f * (float)n * (float)(n + 1)); }
 };
+constexpr int SNAP = 4;                           // a cut this near to an item's beginning or end (key tiles, at most a quarter of a share) goes there
 // time of a key tile of an item with that many column tiles, and of its start and end, in units of a key's time
-__host__ __device__ constexpr int tile_time(int cap, int per) { return cap == 1 ? 1 : cap == 4 || per > 4 ? 10 : 7; }
-constexpr int start_time(int cap) { return cap == 1 ? 64 : cap == 4 ? 400 : 1600; }
-template <int CAP>
-__device__ __forceinline__ Weights weights_of(const ChunkSeq& s, int G, int per, bool causal) {
-  const int t = tile_time(CAP, per);
-  return {(double)start_time(CAP) + (double)t * (s.len + (causal ? 0 : s.rows)), causal ? (double)(t * per * 32) / G : 0.0};
+template <bool STREAM>
+__host__ __device__ constexpr int tile_time(int cap, int per) { return STREAM ? 1 : per > 4 ? 10 : per > 2 ? 7 : 5; }
+template <bool STREAM>
+constexpr int start_time() { return STREAM ? 64 : 4000; }
+template <bool STREAM>
+__device__ __forceinline__ Weights weights_of(const ChunkSeq& s, int G, int cap, int per, bool causal) {
+  const float t = (float)tile_time<STREAM>(cap, per);
+  return {(float)start_time<STREAM>() + t * (float)(s.len + (causal ? 0 : s.rows)), causal ? t * (float)(per * 32) / (float)G : 0.f};
 }
 
 // Where share w of `shares` begins and ends.  Order of the line: kv heads, sequences, column groups from the last.  The device may use fewer
 // shares than were launched: none with less than `least` key tiles.  False: no such share.  Every wave finds out for itself: a lane a
 // sequence, 64 at a time, then even lanes for the beginning and odd ones for the end.
-template <int CAP>
-__device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch, int G, bool causal, int w, int shares, int least, Cut& lo, Cut& hi) {
-  constexpr int TK = CAP == 1 ? STREAM_TK : TILE_TK;
+template <bool STREAM>
+__device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch, int G, int cap, bool causal, int w, int shares, int least, Cut& lo,
+                                         Cut& hi) {
+  constexpr int TK = STREAM ? STREAM_TK : TILE_TK;
   const int lane = threadIdx.x & 63;
-  const bool one = kv.batch == 1;
+  const bool one = kv.batch == 1;                 // (then every lane holds that sequence)
   ChunkSeq s;
   Items it;
   Weights wt;
-  double mine, upto;
+  float mine, upto;
   auto weigh = [&](int b) {
     s = chunk_seq(kv, ch, min(b, kv.batch - 1));
-    it = items_of(s.rows, G, CAP);
-    wt = weights_of<CAP>(s, G, it.per, causal);
-    mine = upto = s.ok && b < kv.batch ? wt.upto(it.n) : 0.0;
+    it = items_of(s.rows, G, cap);
+    wt = weights_of<STREAM>(s, G, cap, it.per, causal);
+    mine = upto = s.ok && (one || b < kv.batch) ? wt.sum(it.n) : 0.f;
     if (one) return;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(upto, o, 64);
+      const float y = __shfl_up(upto, o, 64);
       if (lane >= o) upto += y;
     }
   };
-  double per_head = 0.0;
+  float per_head = 0.f;
   for (int b0 = 0; b0 < kv.batch; b0 += 64) {
     weigh(b0 + lane);
-    per_head += __shfl(upto, one ? 0 : 63, 64);
+    per_head += one ? upto : __shfl(upto, 63, 64);
   }
-  const double all = per_head * kv.hkv;
-  if (uniform(all > 0.0) == 0) return false;
-  const int n = uniform(max(1, (int)min((double)shares, all / ((double)tile_time(CAP, CAP) * TK * least))));
+  const float all = per_head * (float)kv.hkv;
+  if (uniform(all > 0.f) == 0) return false;
+  const int n = uniform(max(1, (int)min((float)shares, all / (float)(tile_time<STREAM>(cap, cap) * TK * least))));
   if (w >= n) return false;
-  const double at = all / n * (w + (lane & 1));
+  const float at = all / (float)n * (float)(w + (lane & 1));
   const int head = min((int)(at / per_head), kv.hkv - 1);
-  const double off = max(at - head * per_head, 0.0);
+  const float off = max(at - (float)head * per_head, 0.f);
   // the last sequence with work that begins at or before this place
-  double begin = 0.0, size = 0.0, first = 1.0, slope = 0.0, base = 0.0;
-  int seq = 0, rows = 0, len = 0, items = 1, per = 1;
-  for (int b0 = 0; b0 < kv.batch; b0 += 64) {
-    if (kv.batch > 64) weigh(b0 + lane);
-    const double before = base + (upto - mine);
-    const bool work = mine > 0.0;
-    const double off0 = __shfl(off, 0, 64), off1 = __shfl(off, 1, 64);
-    const uint64_t in0 = __builtin_amdgcn_ballot_w64(work && before <= off0), in1 = __builtin_amdgcn_ballot_w64(work && before <= off1);
-    const uint64_t in = lane & 1 ? in1 : in0;
-    const int l = in ? 63 - __clzll((long long)in) : 0;
-    const double b_ = __shfl(before, l, 64), m_ = __shfl(mine, l, 64), f_ = __shfl(wt.first, l, 64), s_ = __shfl(wt.slope, l, 64);
-    const int r_ = __shfl(s.rows, l, 64), n_ = __shfl(s.len, l, 64), i_ = __shfl(it.n, l, 64), p_ = __shfl(it.per, l, 64);
-    if (in) { begin = b_; size = m_; first = f_; slope = s_; rows = r_; len = n_; items = i_; per = p_; seq = b0 + l; }
-    base += __shfl(upto, one ? 0 : 63, 64);
+  float begin = 0.f, size = mine, base = 0.f;
+  int seq = 0;
+  if (!one) {
+    Weights fw = wt;
+    ChunkSeq fs = s;
+    for (int b0 = 0; b0 < kv.batch; b0 += 64) {
+      if (kv.batch > 64) weigh(b0 + lane);
+      const float before = base + (upto - mine), off0 = __shfl(off, 0, 64), off1 = __shfl(off, 1, 64);
+      const uint64_t in0 = __builtin_amdgcn_ballot_w64(mine > 0.f && before <= off0), in1 = __builtin_amdgcn_ballot_w64(mine > 0.f && before <= off1);
+      const uint64_t in = lane & 1 ? in1 : in0;
+      const int l = in ? 63 - __clzll((long long)in) : 0;
+      const float b_ = __shfl(before, l, 64), m_ = __shfl(mine, l, 64);
+      const Weights w_{__shfl(wt.first, l, 64), __shfl(wt.slope, l, 64)};
+      const int r_ = __shfl(s.rows, l, 64), n_ = __shfl(s.len, l, 64);
+      if (in) { begin = b_; size = m_; fw = w_; fs.rows = r_; fs.len = n_; seq = b0 + l; }
+      base += __shfl(upto, 63, 64);
+    }
+    wt = fw;
+    s = fs;
+    it = items_of(s.rows, G, cap);
   }
-  // item j of the sequence is column group items - 1 - j, so what lies behind is the groups below: k with upto(k) < rest <= upto(k + 1)
-  const Weights q{first, slope};
-  const double rest = max(size - (off - begin), 0.5);
-  const float c = (float)(first + 0.5 * slope);
-  int k = min((int)(2.f * (float)rest / (c + sqrtf(c * c + 2.f * (float)slope * (float)rest))), items - 1);
-  while (k > 0 && q.upto(k) >= rest) --k;
-  while (k + 1 < items && q.upto(k + 1) < rest) ++k;
-  const double into = q.upto(k + 1) - rest - start_time(CAP);     // weight of this item in front of the cut, but for its start
-  const ChunkSeq found{0, rows, len, true};
-  const int tiles = (keys_of(found, G, per, k, causal) + TK - 1) / TK;
-  const double tile_weight = (double)tile_time(CAP, per) * TK;
-  int tile = into > 0.0 ? (int)min(ceil(into / tile_weight), (double)tiles) : 0;
+  const float into = max(off - begin, 0.f), pair = 2.f * wt.first + wt.slope * (float)(it.n + 1);
+  const int j = min((int)(into / pair), (it.n - 1) >> 1);
+  float in_item = max(into - (float)j * pair, 0.f);
+  const float heavy = wt.of(it.n - 1 - j);
+  int at_ = 2 * j;
+  if (in_item >= heavy && at_ + 1 < it.n) { in_item -= heavy; ++at_; }
+  in_item -= (float)start_time<STREAM>();
+  const float of_tile = (float)(tile_time<STREAM>(cap, it.per) * TK);
+  const int tiles = (keys_of(s, G, it.per, item_at(it.n, at_), causal) + TK - 1) / TK;
+  int tile = in_item > 0.f ? (int)min(ceilf(in_item / of_tile), (float)tiles) : 0;
+  // (an item that is cut costs a beginning, an end and two partials more than one that is not)
+  if (!STREAM) {
+    const int snap = min(SNAP, (int)(all / (float)n / (4.f * of_tile)));
+    tile = tile <= min(snap, tiles >> 1) ? 0 : tiles - tile <= snap ? tiles : tile;
+  }
   auto take = [&](int x, int e) { return uniform(__shfl(x, e, 64)); };
-  lo = Cut{{take(seq, 0), take(head, 0), take(k, 0)}, take(tile, 0)};
-  hi = w + 1 == n ? Cut{{kv.batch, kv.hkv, 0}, 0} : Cut{{take(seq, 1), take(head, 1), take(k, 1)}, take(tile, 1)};
+  lo = Cut{{take(seq, 0), take(head, 0), take(at_, 0)}, take(tile, 0)};
+  hi = w + 1 == n ? Cut{{kv.batch, kv.hkv, 0}, 0} : Cut{{take(seq, 1), take(head, 1), take(at_, 1)}, take(tile, 1)};
   return true;
 }
 // a sequence's scalars, the same for the whole wave
@@ -149,9 +168,9 @@ __device__ __forceinline__ ChunkSeq uniform_seq(const PagedDev& kv, const ChunkD
   const ChunkSeq s = chunk_seq(kv, ch, seq);
   return {uniform(s.row0), uniform(s.rows), uniform(s.len), uniform((int)s.ok) != 0};
 }
-__device__ __forceinline__ bool same(const Item& a, const Item& b) { return a.seq == b.seq && a.kvh == b.kvh && a.qt == b.qt; }
+__device__ __forceinline__ bool same(const Place& a, const Place& b) { return a.seq == b.seq && a.kvh == b.kvh && a.at == b.at; }
 
-// Partials: slots of CAP x 32 columns, [slot][column][HD] then (m in powers of two, l) [slot][column][2].  Share w has slots 2 w, for the piece
+// Partials: slots of 32 columns for each of an item's column tiles, [slot][column][HD] then (m in powers of two, l) [slot][column][2].  Share w has slots 2 w, for the piece
 // that it begins with if that is not an item's first, and 2 w + 1, for the piece that it ends with if that is an item's first and not its last.
 // What a share leaves for the merge: the item that begins in slot 2 w + 1 (columns 0: none), and of slot 2 w whether there is anything in
 // it (HAS) and whether the item ends in this share, or there is none (ENDS).
@@ -168,9 +187,10 @@ __device__ __forceinline__ Partials partials_of(float* base, int shares, int col
 }
 
 // Walks the pieces of a workgroup: run(item, sequence, its items, first and last key tile, slot of the partial or -1 for a whole item).
-template <int NT, int CAP, typename RUN>
-__device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, const PagedAttnArgs& a, int shares, int least, int q_tiles, RUN run) {
-  constexpr int TK = CAP == 1 ? STREAM_TK : TILE_TK;
+template <int NT, bool STREAM, typename RUN>
+__device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, const PagedAttnArgs& a, const PagedAttnPlan& plan, RUN run) {
+  constexpr int TK = STREAM ? STREAM_TK : TILE_TK;
+  const int shares = plan.shares, q_tiles = plan.q_tiles, CAP = STREAM ? 1 : plan.cap;
   const bool causal = a.anc == nullptr;
   const int G = a.hq / kv.hkv;
   int w = 0;
@@ -182,9 +202,9 @@ __device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, con
     const int g = blockIdx.x % step;
     if (g >= groups) return;
     lo = Cut{{g / kv.hkv, g % kv.hkv, q_tiles - 1 - (int)(blockIdx.x / step)}, 0};
-    hi = Cut{lo.item, INT32_MAX};
-    if (lo.item.kvh == 0 && lo.item.qt == 0 && threadIdx.x == 0 && !chunk_seq(kv, ch, lo.item.seq).ok)
-      set_status(kv.status, chunk_fault(kv, ch, lo.item.seq));
+    hi = Cut{lo.place, INT32_MAX};
+    if (lo.place.kvh == 0 && lo.place.at == 0 && threadIdx.x == 0 && !chunk_seq(kv, ch, lo.place.seq).ok)
+      set_status(kv.status, chunk_fault(kv, ch, lo.place.seq));
   } else {
     if (blockIdx.x == 0)
       for (int b = threadIdx.x; b < kv.batch; b += NT)
@@ -193,34 +213,34 @@ __device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, con
     const int per_xcd = (shares + 7) >> 3;
     w = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
     if (w >= shares) return;
-    if (!share_of<CAP>(kv, ch, G, causal, w, shares, least, lo, hi)) lo = Cut{{0, kv.hkv, 0}, 0};
+    if (!share_of<STREAM>(kv, ch, G, CAP, causal, w, shares, plan.least, lo, hi)) lo = Cut{{0, kv.hkv, 0}, 0};
   }
   ShareNote note{0, 0, 0, 0, ENDS, {0, 0, 0}};
-  Item item = lo.item;
+  Place pl = lo.place;
   int t0 = lo.tile;
-  while (item.kvh < kv.hkv) {
-    const ChunkSeq s = uniform_seq(kv, ch, item.seq);
+  while (pl.kvh < kv.hkv) {
+    const ChunkSeq s = uniform_seq(kv, ch, pl.seq);
     const Items it = items_of(s.rows, G, CAP);
-    if (s.ok && item.qt < 0) item.qt = it.n - 1;
-    const bool last = same(item, hi.item);
-    if (s.ok && item.qt >= 0 && item.qt < it.n) {
-      const int tiles = (keys_of(s, G, it.per, item.qt, causal) + TK - 1) / TK, t1 = last ? min(hi.tile, tiles) : tiles;
+    const bool last = same(pl, hi.place), there = s.ok && pl.at < it.n;
+    if (there) {
+      const int qt = shares == 0 ? pl.at : item_at(it.n, pl.at);
+      const int tiles = (keys_of(s, G, it.per, qt, causal) + TK - 1) / TK, t1 = last ? min(hi.tile, tiles) : tiles;
       const bool ends = t1 >= tiles;
       if (t0 > 0) note.first = (t1 > t0 ? HAS : 0) | (ends ? ENDS : 0);
       else if (!ends && t1 > 0) {
-        const int col0 = item.qt * it.per * 32;
-        note.columns = min(it.per * 32, s.rows * G - col0); note.col0 = col0; note.row0 = s.row0; note.kvh = item.kvh;
+        const int col0 = qt * it.per * 32;
+        note.columns = min(it.per * 32, s.rows * G - col0); note.col0 = col0; note.row0 = s.row0; note.kvh = pl.kvh;
       }
       if (t1 > t0)
-        run(Item{uniform(item.seq), uniform(item.kvh), uniform(item.qt)}, s, it, uniform(t0), uniform(t1), t0 > 0 ? 2 * w : ends ? -1 : 2 * w + 1);
+        run(Item{uniform(pl.seq), uniform(pl.kvh), uniform(qt)}, s, it, uniform(t0), uniform(t1), t0 > 0 ? 2 * w : ends ? -1 : 2 * w + 1);
     }
     if (last) break;
     t0 = 0;
-    if (s.ok && item.qt > 0) {
-      --item.qt;
-    } else {                                      // the next sequence's last group, or the next kv head's first sequence
-      item.qt = -1;
-      if (++item.seq == kv.batch) { item.seq = 0; ++item.kvh; }
+    if (there && pl.at + 1 < it.n) {
+      ++pl.at;
+    } else {                                      // the next sequence's, or the next kv head's first sequence's
+      pl.at = 0;
+      if (++pl.seq == kv.batch) { pl.seq = 0; ++pl.kvh; }
     }
   }
   if (shares != 0 && threadIdx.x == 0) ((ShareNote*)a.partials)[w] = note;
@@ -269,8 +289,7 @@ __device__ __forceinline__ void put_columns(float* xo, const f32x16_t (&o)[HD / 
 // for the next V behind the product with this one.
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) void k_paged_stream(PagedDev kv, ChunkDev ch, PagedAttnArgs a,
-                                                                                               int shares, int least, int q_tiles, bool vec_q,
-                                                                                               bool vec_out) {
+                                                                                               PagedAttnPlan plan, bool vec_q, bool vec_out) {
   constexpr int NS = HD / 16, DB = HD / 32, W = STREAM_WAVES, BLOCK = 32 * HD, PIECES = HD / 4;
   typedef typename AttnFrag<T>::type frag_t;
   __shared__ __align__(16) float xo[W][32 * HD];
@@ -279,7 +298,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) v
   const int wave = uniform(tid >> 6);
   const int G = a.hq / kv.hkv, blocks = kv.page_size >> 5;
 
-  walk<64 * W, 1>(kv, ch, a, shares, least, q_tiles, [&](const Item& item, const ChunkSeq& s, const Items&, int t0, int t1, int slot) {
+  walk<64 * W, true>(kv, ch, a, plan, [&](const Item& item, const ChunkSeq& s, const Items&, int t0, int t1, int slot) {
     const int ncols = s.rows * G, col0 = item.qt * 32, total = s.len + s.rows;
     const int key_end = keys_of(s, G, 1, item.qt, a.anc == nullptr), key_lo = t0 * STREAM_TK;
     const int key_hi = min(t1 * STREAM_TK, key_end);
@@ -359,6 +378,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) v
       frag_t pf[2];
       attn_softmax<T, DB>(sc, masked, window >> (4 * lg), a.scale, o, m, l, pf);
       if (masked) {
+        const int lane = opaque(threadIdx.x) & 63;
 #pragma unroll
         for (int j = 0; j < 2 * DB; ++j) {
           if (left < 32) vf[j] = attn_zero_tail(vf[j], j & 1, lane, left);
@@ -407,7 +427,7 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) v
         const int64_t at = ((int64_t)s.row0 + cc / G) * a.hq + item.kvh * G + cc % G;
         store4((T*)a.out + at * HD + 4 * piece, acc * (lt > 0.f ? 1.f / lt : 0.f), vec_out);
       } else {
-        const Partials p = partials_of(a.partials, shares, 32, HD);
+        const Partials p = partials_of(a.partials, plan.shares, 32, HD);
         const int64_t at = (int64_t)slot * 32 + c;
         *reinterpret_cast<f32x4_t*>(p.o + at * HD + 4 * piece) = acc;
         if (piece == 0) { p.ml[2 * at] = top * a.scale; p.ml[2 * at + 1] = lt; }
@@ -534,8 +554,8 @@ template <typename T, int HD> struct ColumnTile {
 };
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, ChunkDev ch, PagedAttnArgs a, int shares, int least, int q_tiles,
-                                                                  bool vec_q, bool vec_out) {
+__global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, ChunkDev ch, PagedAttnArgs a, PagedAttnPlan plan, bool vec_q,
+                                                                  bool vec_out) {
   typedef TileRing<T, HD> R;
   typedef typename AttnFrag<T>::type frag_t;
   constexpr int NT = TILE_NT<T>, NS = HD / 16, DB = HD / 32, PIECES = HD / 4, EPI = 8 / NS;   // EPI: exponentials beside a matrix instruction
@@ -553,7 +573,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
   const unsigned char* my_pool = (const unsigned char*)(wave < 2 ? kv.k : kv.v);
   const uint32_t my_lds = lds0 + (uint32_t)wave * R::BLOCK;
 
-  walk<64 * TILE_WAVES, TILE_CAP<T>>(kv, ch, a, shares, least, q_tiles, [&](const Item& item, const ChunkSeq& s, const Items& it, int t0, int t1, int slot) {
+  walk<64 * TILE_WAVES, false>(kv, ch, a, plan, [&](const Item& item, const ChunkSeq& s, const Items& it, int t0, int t1, int slot) {
     const int seq = item.seq, kvh = item.kvh, qt = item.qt;
     const int ncols = s.rows * G, total = s.len + s.rows, keys = keys_of(s, G, it.per, qt, causal);
     const int nt = t1 - t0, col0 = qt * it.per * 32;
@@ -590,13 +610,8 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
       return attn_tree_window([&](int i) { return i < a.anc_words ? w[i] : 0ull; }, c_lo, s.rows);
     };
 
-    // are all pages there?  (Where one is not, its keys are looked at one block after the other.)
-    bool bad = false;
     const int last_block = (min(keys, t1 * TILE_TK) - 1) >> 5;
-    for (int p = 2 * t0 / blocks + opaque(tid); p <= last_block / blocks; p += 64 * TILE_WAVES)
-      bad |= (unsigned)kv.table[(size_t)seq * kv.stride + p] >= (unsigned)kv.n_pages;
-    if (bad) set_status(kv.status, ESP_DEV_BAD_PAGE);
-    const bool any_bad = any_thread<TILE_WAVES>(bad, said[0]);
+    bool any_bad = false;
     const bool hides = (int64_t)t1 * TILE_TK > s.len && s.rows > 1;           // some key of the piece may be hidden from some column
 
     frag_t qf[NT][NS];
@@ -652,6 +667,10 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
 #pragma unroll
         for (int i = 0; i < NS; ++i) qf[c][i] = load_query(qp + 16 * i, vec_q);
       }
+      // are all pages there?  (Where one is not, its keys are looked at one block after the other.)
+      bool bad = false;
+      for (int p = 2 * t0 / blocks + opaque(tid); p <= last_block / blocks; p += 64 * TILE_WAVES)
+        bad |= (unsigned)kv.table[(size_t)seq * kv.stride + p] >= (unsigned)kv.n_pages;
 #pragma unroll
       for (int c = 0; c < NT; ++c) {
 #pragma unroll
@@ -668,7 +687,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
         if (i < nt) issue(i);
       // tile 0 is here for everybody (this wave's loads retire in order, the barrier covers the others')
       wait_tiles_but<R::LPW>(min(R::AHEAD - 1, nt - 1));
-      __syncthreads();
+      any_bad = any_thread<TILE_WAVES>(bad, said[0]);                          // (with its barrier)
       clean(0);
       // Tile i + 1 is here, and all are done with tile i (with two column tiles: i - 1), whose stage takes the next that is asked for.
       auto next_tile = [&](int i) {
@@ -840,6 +859,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
           __builtin_amdgcn_sched_barrier(0);
         }
       };
+      if (bad) set_status(kv.status, ESP_DEV_BAD_PAGE);
       if (mine == 2) {
         two_tiles();
       } else {
@@ -866,16 +886,16 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
         break;
       }
       if (!hides) break;
-      unsigned most = 0;
+      float zero[4] = {0.f, 0.f, 0.f, 0.f};       // (0 x infinity is NaN, and that stays)
 #pragma unroll
       for (int c = 0; c < NT; ++c)
         if (c < mine) {
 #pragma unroll
           for (int i = 0; i < DB; ++i)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) most = max(most, __float_as_uint(o[c][i][v]) & 0x7fffffffu);
+            for (int v = 0; v < 16; ++v) zero[v & 3] = fmaf(o[c][i][v], 0.f, zero[v & 3]);
         }
-      if (!any_thread<TILE_WAVES>(most >= 0x7f800000u, said[1])) break;
+      if (!any_thread<TILE_WAVES>(!((zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.f), said[1])) break;
     }
 
     // the ring is done with: a wave's columns, [tile][32][HD], one wave's behind the other's
@@ -905,11 +925,26 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
           }
       }
     }
-    const Partials part = partials_of(a.partials, shares, 32 * TILE_CAP<T>, HD);
+    const Partials part = partials_of(a.partials, plan.shares, 32 * plan.cap, HD);
 #pragma unroll
     for (int c = 0; c < NT; ++c) {
       if (c >= mine || kh0 != 0) continue;
-      const float inv = slot >= 0 ? 1.f : tile[c].l > 0.f ? 1.f / tile[c].l : 0.f;
+      const int tc = ct0 + 4 * c, c0 = col0 + tc * 32, n_live = min(32, ncols - c0);
+      if (slot >= 0) {                            // a partial as the registers hold it: [four features][column][4]
+        const int64_t at = (int64_t)slot * (32 * plan.cap) + tc * 32;
+        float* po = part.o + at * HD + (lg * 32 + lr) * 4;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; v += 4)
+            *reinterpret_cast<f32x4_t*>(po + (db * 8 + 2 * (v >> 2)) * 128) = f32x4_t{o[c][db][v], o[c][db][v + 1], o[c][db][v + 2], o[c][db][v + 3]};
+        if (lg == 0) {
+          part.ml[2 * (at + lr)] = tile[c].m * a.scale;
+          part.ml[2 * (at + lr) + 1] = tile[c].l;
+        }
+        continue;
+      }
+      const float inv = tile[c].l > 0.f ? 1.f / tile[c].l : 0.f;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -918,21 +953,11 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");       // (a wave's LDS accesses are done in order: for the compiler)
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      const int tc = ct0 + 4 * c, c0 = col0 + tc * 32, n_live = min(32, ncols - c0);
-      const int64_t at = (int64_t)max(slot, 0) * (32 * TILE_CAP<T>) + tc * 32;
-      for (int t = lane; t < n_live * PIECES; t += 64) {
-        const int i = t / PIECES, piece = t % PIECES;
+#pragma unroll 4
+      for (int t = lane; t < 32 * PIECES; t += 64) {
+        const int i = t / PIECES, piece = t % PIECES, row = (c0 + i) / G;
         const f32x4_t x = *reinterpret_cast<const f32x4_t*>(column_piece<HD>(xo, i, piece));
-        if (slot < 0) {
-          const int64_t row = s.row0 + (c0 + i) / G;
-          store4((T*)a.out + (row * a.hq + kvh * G + (c0 + i) % G) * HD + 4 * piece, x, vec_out);
-        } else {
-          *reinterpret_cast<f32x4_t*>(part.o + (at + i) * HD + 4 * piece) = x;
-        }
-      }
-      if (slot >= 0 && lg == 0 && lr < n_live) {
-        part.ml[2 * (at + lr)] = tile[c].m * a.scale;
-        part.ml[2 * (at + lr) + 1] = tile[c].l;
+        if (i < n_live) store4((T*)a.out + ((int64_t)(s.row0 + row) * a.hq + kvh * G + (c0 + i) - row * G) * HD + 4 * piece, x, vec_out);
       }
       xo += 32 * HD;
     }
@@ -944,13 +969,18 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
 
 // --------------------------------------------------------------------------------------------------
 // The pieces of an item that begins in share w and does not end there: that one and those of the shares behind it, up to the one that ends
-// it.  A workgroup has 32 columns, HD / 4 threads a column, four features each.
-template <typename T, int HD, int CAP>
-__global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs a, int hkv, int shares, bool vec_out) {
-  constexpr int PIECES = HD / 4, COLS = 32 * CAP, U = 4;
+// it.  A workgroup has 32 columns; four features of a column are a thread's, and where fewer than all threads have any, as many groups of them
+// as there is room for take the pieces in turn: nearly all of it is waiting for memory, so all loads are to be on their way at once.
+template <bool STREAM> constexpr int MERGE_THREADS = STREAM ? 1024 : 256;
+template <bool STREAM, int HD> constexpr int MERGE_COLUMNS = STREAM ? 32 : 4 * MERGE_THREADS<STREAM> / HD;
+template <typename T, int HD, bool STREAM>
+__global__ __launch_bounds__(MERGE_THREADS<STREAM>) void k_paged_merge(PagedAttnArgs a, int hkv, int shares, int cols, bool vec_out) {
+  constexpr int NT = MERGE_THREADS<STREAM>, NC = MERGE_COLUMNS<STREAM, HD>, PIECES = HD / 4, U = 8;
   __shared__ int slots[2 * MOST_SHARES];
-  const int w = blockIdx.x, c0 = blockIdx.y * 32, tid = threadIdx.x, lane = tid & 63;
-  const Partials p = partials_of(a.partials, shares, COLS, HD);
+  __shared__ __align__(16) f32x4_t part[NT];
+  __shared__ float part_m[NT], part_l[NT];
+  const int w = blockIdx.x, c0 = blockIdx.y * NC, tid = threadIdx.x, lane = tid & 63;
+  const Partials p = partials_of(a.partials, shares, cols, HD);
   const ShareNote note = p.notes[w];
   int first = w + 1 + lane < shares ? p.notes[w + 1 + lane].first : ENDS;
   if (note.columns <= c0) return;
@@ -967,35 +997,46 @@ __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs a, int hkv, i
     if (ends) break;
   }
   __syncthreads();
-  const int G = a.hq / hkv, n_live = min(32, note.columns - c0);
-  for (int t = tid; t < n_live * PIECES; t += 256) {
-    const int c = c0 + t / PIECES, piece = t % PIECES;
-    float top = -INFINITY, lt = 0.f;
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < n; i += U) {              // U pieces on their way at once
+  const int G = a.hq / hkv, live = min(NC, note.columns - c0), work = live * PIECES, groups = min(NT / work, n);
+  const int g = tid / work, t = tid - g * work, c = c0 + (STREAM ? t / PIECES : t % live), piece = STREAM ? t % PIECES : t / live;
+  // where these four features of a slot are: [column][HD], or of a tile of 32 columns [four features][column][4]
+  const size_t in_slot = STREAM ? (size_t)c * HD + 4 * piece : (size_t)(c & ~31) * HD + (piece * 32 + (c & 31)) * 4;
+  float top = -INFINITY, lt = 0.f;
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](float m, float l, f32x4_t o) {
+    const float now = l > 0.f ? fmaxf(top, m) : top;
+    const float fa = top > -INFINITY ? __builtin_amdgcn_exp2f(top - now) : 0.f, fb = l > 0.f ? __builtin_amdgcn_exp2f(m - now) : 0.f;
+    lt = lt * fa + l * fb;
+    acc = acc * fa + o * fb;
+    top = now;
+  };
+  if (g < groups)
+    for (int i = g; i < n; i += U * groups) {
       float m[U], l[U];
       f32x4_t o[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const size_t at = (size_t)slots[min(i + u, n - 1)] * COLS + c;
-        m[u] = p.ml[2 * at];
-        l[u] = p.ml[2 * at + 1];
-        o[u] = *reinterpret_cast<const f32x4_t*>(p.o + at * HD + 4 * piece);
+        const size_t slot = slots[min(i + u * groups, n - 1)];
+        m[u] = p.ml[2 * (slot * cols + c)];
+        l[u] = p.ml[2 * (slot * cols + c) + 1];
+        o[u] = *reinterpret_cast<const f32x4_t*>(p.o + slot * cols * HD + in_slot);
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (i + u >= n) break;
-        const float now = l[u] > 0.f ? fmaxf(top, m[u]) : top;
-        const float fa = top > -INFINITY ? __builtin_amdgcn_exp2f(top - now) : 0.f, fb = l[u] > 0.f ? __builtin_amdgcn_exp2f(m[u] - now) : 0.f;
-        lt = lt * fa + l[u] * fb;
-        acc = acc * fa + o[u] * fb;
-        top = now;
-      }
+      for (int u = 0; u < U; ++u)
+        if (i + u * groups < n) add(m[u], l[u], o[u]);
     }
-    const int cc = note.col0 + c;
-    const int64_t out = ((int64_t)note.row0 + cc / G) * a.hq + note.kvh * G + cc % G;
-    store4((T*)a.out + out * HD + 4 * piece, acc * (lt > 0.f ? 1.f / lt : 0.f), vec_out);
+  if (groups > 1) {
+    part[tid] = acc;
+    part_m[tid] = top;
+    part_l[tid] = lt;
+    __syncthreads();
+    if (g == 0)
+      for (int x = 1; x < groups; ++x) add(part_m[x * work + t], part_l[x * work + t], part[x * work + t]);
   }
+  if (g > 0) return;
+  const int cc = note.col0 + c;
+  const int64_t out = ((int64_t)note.row0 + cc / G) * a.hq + note.kvh * G + cc % G;
+  store4((T*)a.out + out * HD + 4 * piece, acc * (lt > 0.f ? 1.f / lt : 0.f), vec_out);
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -1024,17 +1065,19 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
   }
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   const dim3 g((unsigned)grid);
-  if (!p.tile) {
-    hipLaunchKernelGGL((k_paged_stream<T, HD>), g, dim3(64 * STREAM_WAVES), 0, st, kv, ch, a, p.shares, p.least, p.q_tiles, vec_q, vec_out);
-    if (p.shares) hipLaunchKernelGGL((k_paged_merge<T, HD, 1>), dim3(p.shares, 1), dim3(256), 0, st, a, kv.hkv, p.shares, vec_out);
-    return hipGetLastError();
+  if (p.cap == 1) {
+    hipLaunchKernelGGL((k_paged_stream<T, HD>), g, dim3(64 * STREAM_WAVES), 0, st, kv, ch, a, p, vec_q, vec_out);
+    if (p.shares)
+      hipLaunchKernelGGL((k_paged_merge<T, HD, true>), dim3(p.shares), dim3(MERGE_THREADS<true>), 0, st, a, kv.hkv, p.shares, 32, vec_out);
+  } else {
+    constexpr unsigned bytes = TileRing<T, HD>::BYTES + TILE_ANC * 8;
+    const hipError_t e = allow_lds<T, HD>(bytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_paged_tile<T, HD>), g, dim3(64 * TILE_WAVES), bytes, st, kv, ch, a, p, vec_q, vec_out);
+    if (p.shares)
+      hipLaunchKernelGGL((k_paged_merge<T, HD, false>), dim3(p.shares, 32 * p.cap / MERGE_COLUMNS<false, HD>), dim3(MERGE_THREADS<false>), 0, st, a,
+                         kv.hkv, p.shares, 32 * p.cap, vec_out);
   }
-  constexpr unsigned bytes = TileRing<T, HD>::BYTES + TILE_ANC * 8;
-  constexpr int CAP = TILE_CAP<T>;
-  const hipError_t e = allow_lds<T, HD>(bytes);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_paged_tile<T, HD>), g, dim3(64 * TILE_WAVES), bytes, st, kv, ch, a, p.shares, p.least, p.q_tiles, vec_q, vec_out);
-  if (p.shares) hipLaunchKernelGGL((k_paged_merge<T, HD, CAP>), dim3(p.shares, CAP), dim3(256), 0, st, a, kv.hkv, p.shares, vec_out);
   return hipGetLastError();
 }
 
@@ -1043,21 +1086,33 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
 PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int len_bound) {
   PagedAttnPlan p;
   const int G = hq / hkv;
-  const int64_t cols = (int64_t)max_rows * G, keys = (int64_t)len_bound + max_rows;
-  p.tile = cols > 32;
-  const int tile_cap = dtype == ESP_F32 ? TILE_CAP<float> : TILE_CAP<bf16_t>, cap = p.tile ? tile_cap : 1, tk = p.tile ? TILE_TK : STREAM_TK;
-  p.q_tiles = (int)std::max<int64_t>(1, ceil_div(ceil_div(cols, 32), cap));
-  // items that there can be, and workgroups that have a place at once
-  const int64_t items = (int64_t)hkv * std::min<int64_t>((int64_t)batch * p.q_tiles, ceil_div((int64_t)total_rows * G, 32 * cap) + batch);
-  const int64_t places = 256 * (p.tile ? 1 : dtype == ESP_F32 && hd == 128 ? 1 : 2);
-  p.least = p.tile ? 4 : 2;
-  const int64_t tiles = ceil_div(keys, tk);
-  if (tiles > p.least && items < 4 * places) p.shares = (int)std::min(places, ceil_div(items * tiles, p.least));
+  const int64_t cols = (int64_t)max_rows * G, keys = (int64_t)len_bound + max_rows, tiles = ceil_div(cols, 32);
+  const int most = dtype == ESP_F32 ? TILE_CAP<float> : TILE_CAP<bf16_t>;
+  // items that there can be with a cap
+  auto items = [&](int cap) {
+    return (int64_t)hkv * std::min<int64_t>((int64_t)batch * ceil_div(tiles, cap), ceil_div((int64_t)total_rows * G, 32 * cap) + batch);
+  };
+  p.cap = tiles == 1 ? 1 : most;
+  while (p.cap > 2 && items(p.cap) < 256 && p.cap / 2 >= tiles) p.cap /= 2;
+  const int tk = p.cap == 1 ? STREAM_TK : TILE_TK;
+  p.q_tiles = (int)std::max<int64_t>(1, ceil_div(tiles, p.cap));
+  const int64_t places = 256 * (p.cap > 1 || (dtype == ESP_F32 && hd == 128) ? 1 : 2);     // workgroups that have a place at once
+  p.least = p.cap == 1 ? 2 : 4;
+  const int64_t key_tiles = ceil_div(keys, tk), n = items(p.cap);
+  if (p.cap == 1) {
+    if (key_tiles > p.least && n < 4 * places) p.shares = (int)std::min(places, ceil_div(n * key_tiles, p.least));
+  } else if (n < (batch == 1 || key_tiles <= 20 ? places : 4 * places)) {
+    // us: 2 for a key tile, 13 for an item's beginning and end, 8 for the merge, 1/20 for a partial
+    const double alone = 2. * key_tiles + 13., parts = std::min(sqrt(40. * key_tiles / n), (double)places / n);
+    if (batch > 1 || 2. * key_tiles / parts + 0.05 * n * parts + 21. < alone) {
+      p.shares = (int)(batch > 1 ? std::min<double>(places, std::max(n * parts, (double)n)) : n * std::floor(parts));
+      if (batch == 1 && p.shares <= n) p.shares = 0;
+    }
+  }
   return p;
 }
-size_t paged_attn_partial_floats(const PagedAttnPlan& p, int dtype, int hd) {
-  const int cap = !p.tile ? 1 : dtype == ESP_F32 ? TILE_CAP<float> : TILE_CAP<bf16_t>;
-  return p.shares ? notes_floats(p.shares) + (size_t)2 * p.shares * 32 * cap * (hd + 2) : 0;
+size_t paged_attn_partial_floats(const PagedAttnPlan& p, int hd) {
+  return p.shares ? notes_floats(p.shares) + (size_t)2 * p.shares * 32 * p.cap * (hd + 2) : 0;
 }
 
 hipError_t launch_paged_attn(hipStream_t st, int dtype, int hd, const PagedDev& kv, const ChunkDev& ch, const PagedAttnArgs& a,
