@@ -170,21 +170,28 @@ __device__ __forceinline__ ChunkSeq uniform_seq(const PagedDev& kv, const ChunkD
 }
 __device__ __forceinline__ bool same(const Place& a, const Place& b) { return a.seq == b.seq && a.kvh == b.kvh && a.at == b.at; }
 
-// Partials: slots of 32 columns for each of an item's column tiles, [slot][column][HD] then (m in powers of two, l) [slot][column][2].  Share w has slots 2 w, for the piece
-// that it begins with if that is not an item's first, and 2 w + 1, for the piece that it ends with if that is an item's first and not its last.
+// Partials: a slot of 32 columns for each of an item's column tiles: their HD sums, then for every column m in powers of two and l.  Share w
+// has slots 2 w, for the piece that it begins with if that is not an item's first, and 2 w + 1, for the piece that it ends with if that is an
+// item's first and not its last.
 // What a share leaves for the merge: the item that begins in slot 2 w + 1 (columns 0: none), and of slot 2 w whether there is anything in
 // it (HAS) and whether the item ends in this share, or there is none (ENDS).
 struct alignas(16) ShareNote { int columns, col0, row0, kvh, first, pad[3]; };
 enum { HAS = 1, ENDS = 2 };
+inline size_t notes_floats(int shares) { return (size_t)shares * sizeof(ShareNote) / 4; }
+__host__ __device__ constexpr size_t slot_floats(int cols, int hd) { return (size_t)cols * (hd + 2); }
 struct Partials {
   ShareNote* notes;
-  float *o, *ml;
+  float* first;
+  int cols, hd;
+  __device__ __forceinline__ float* sums(int slot) const { return first + slot_floats(cols, hd) * slot; }
+  __device__ __forceinline__ float* stats(int slot) const { return sums(slot) + cols * hd; }
 };
-inline size_t notes_floats(int shares) { return (size_t)shares * sizeof(ShareNote) / 4; }
 __device__ __forceinline__ Partials partials_of(float* base, int shares, int cols, int hd) {
-  float* o = base + (size_t)shares * sizeof(ShareNote) / 4;
-  return {(ShareNote*)base, o, o + (size_t)2 * shares * cols * hd};
+  return {(ShareNote*)base, base + (size_t)shares * sizeof(ShareNote) / 4, cols, hd};
 }
+
+// share of a workgroup: the ones next to each other on the line, which read the same keys, on one XCD
+__device__ __forceinline__ int share_at(int block, int shares) { return (block & 7) * ((shares + 7) >> 3) + (block >> 3); }
 
 // Walks the pieces of a workgroup: run(item, sequence, its items, first and last key tile, slot of the partial or -1 for a whole item).
 template <int NT, bool STREAM, typename RUN>
@@ -209,9 +216,7 @@ __device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, con
     if (blockIdx.x == 0)
       for (int b = threadIdx.x; b < kv.batch; b += NT)
         if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(kv, ch, b));
-    // shares next to each other on the line, which read the same keys, on one XCD
-    const int per_xcd = (shares + 7) >> 3;
-    w = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    w = share_at(blockIdx.x, shares);
     if (w >= shares) return;
     if (!share_of<STREAM>(kv, ch, G, CAP, causal, w, shares, plan.least, lo, hi)) lo = Cut{{0, kv.hkv, 0}, 0};
   }
@@ -428,9 +433,8 @@ __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) v
         store4((T*)a.out + at * HD + 4 * piece, acc * (lt > 0.f ? 1.f / lt : 0.f), vec_out);
       } else {
         const Partials p = partials_of(a.partials, plan.shares, 32, HD);
-        const int64_t at = (int64_t)slot * 32 + c;
-        *reinterpret_cast<f32x4_t*>(p.o + at * HD + 4 * piece) = acc;
-        if (piece == 0) { p.ml[2 * at] = top * a.scale; p.ml[2 * at + 1] = lt; }
+        *reinterpret_cast<f32x4_t*>(p.sums(slot) + c * HD + 4 * piece) = acc;
+        if (piece == 0) { p.stats(slot)[2 * c] = top * a.scale; p.stats(slot)[2 * c + 1] = lt; }
       }
     }
     __syncthreads();                              // the next piece's parts go there
@@ -931,16 +935,16 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
       if (c >= mine || kh0 != 0) continue;
       const int tc = ct0 + 4 * c, c0 = col0 + tc * 32, n_live = min(32, ncols - c0);
       if (slot >= 0) {                            // a partial as the registers hold it: [four features][column][4]
-        const int64_t at = (int64_t)slot * (32 * plan.cap) + tc * 32;
-        float* po = part.o + at * HD + (lg * 32 + lr) * 4;
+        float* po = part.sums(slot) + tc * 32 * HD + (lg * 32 + lr) * 4;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int v = 0; v < 16; v += 4)
             *reinterpret_cast<f32x4_t*>(po + (db * 8 + 2 * (v >> 2)) * 128) = f32x4_t{o[c][db][v], o[c][db][v + 1], o[c][db][v + 2], o[c][db][v + 3]};
         if (lg == 0) {
-          part.ml[2 * (at + lr)] = tile[c].m * a.scale;
-          part.ml[2 * (at + lr) + 1] = tile[c].l;
+          float* ml = part.stats(slot) + 2 * (tc * 32 + lr);
+          ml[0] = tile[c].m * a.scale;
+          ml[1] = tile[c].l;
         }
         continue;
       }
@@ -979,7 +983,10 @@ __global__ __launch_bounds__(MERGE_THREADS<STREAM>) void k_paged_merge(PagedAttn
   __shared__ int slots[2 * MOST_SHARES];
   __shared__ __align__(16) f32x4_t part[NT];
   __shared__ float part_m[NT], part_l[NT];
-  const int w = blockIdx.x, c0 = blockIdx.y * NC, tid = threadIdx.x, lane = tid & 63;
+  // a share's workgroups where the share was, which spreads the items over the XCDs however many shares there are to one
+  const int of_share = cols / NC, w = share_at((blockIdx.x / (8 * of_share)) * 8 + (blockIdx.x & 7), shares);
+  const int c0 = (blockIdx.x >> 3) % of_share * NC, tid = threadIdx.x, lane = tid & 63;
+  if (w >= shares) return;
   const Partials p = partials_of(a.partials, shares, cols, HD);
   const ShareNote note = p.notes[w];
   int first = w + 1 + lane < shares ? p.notes[w + 1 + lane].first : ENDS;
@@ -1000,7 +1007,7 @@ __global__ __launch_bounds__(MERGE_THREADS<STREAM>) void k_paged_merge(PagedAttn
   const int G = a.hq / hkv, live = min(NC, note.columns - c0), work = live * PIECES, groups = min(NT / work, n);
   const int g = tid / work, t = tid - g * work, c = c0 + (STREAM ? t / PIECES : t % live), piece = STREAM ? t % PIECES : t / live;
   // where these four features of a slot are: [column][HD], or of a tile of 32 columns [four features][column][4]
-  const size_t in_slot = STREAM ? (size_t)c * HD + 4 * piece : (size_t)(c & ~31) * HD + (piece * 32 + (c & 31)) * 4;
+  const int in_slot = STREAM ? c * HD + 4 * piece : (c & ~31) * HD + (piece * 32 + (c & 31)) * 4;
   float top = -INFINITY, lt = 0.f;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
   auto add = [&](float m, float l, f32x4_t o) {
@@ -1016,10 +1023,10 @@ __global__ __launch_bounds__(MERGE_THREADS<STREAM>) void k_paged_merge(PagedAttn
       f32x4_t o[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const size_t slot = slots[min(i + u * groups, n - 1)];
-        m[u] = p.ml[2 * (slot * cols + c)];
-        l[u] = p.ml[2 * (slot * cols + c) + 1];
-        o[u] = *reinterpret_cast<const f32x4_t*>(p.o + slot * cols * HD + in_slot);
+        const int slot = slots[min(i + u * groups, n - 1)];
+        m[u] = p.stats(slot)[2 * c];
+        l[u] = p.stats(slot)[2 * c + 1];
+        o[u] = *reinterpret_cast<const f32x4_t*>(p.sums(slot) + in_slot);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -1068,14 +1075,14 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
   if (p.cap == 1) {
     hipLaunchKernelGGL((k_paged_stream<T, HD>), g, dim3(64 * STREAM_WAVES), 0, st, kv, ch, a, p, vec_q, vec_out);
     if (p.shares)
-      hipLaunchKernelGGL((k_paged_merge<T, HD, true>), dim3(p.shares), dim3(MERGE_THREADS<true>), 0, st, a, kv.hkv, p.shares, 32, vec_out);
+      hipLaunchKernelGGL((k_paged_merge<T, HD, true>), dim3((p.shares + 7) & ~7), dim3(MERGE_THREADS<true>), 0, st, a, kv.hkv, p.shares, 32, vec_out);
   } else {
     constexpr unsigned bytes = TileRing<T, HD>::BYTES + TILE_ANC * 8;
     const hipError_t e = allow_lds<T, HD>(bytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((k_paged_tile<T, HD>), g, dim3(64 * TILE_WAVES), bytes, st, kv, ch, a, p, vec_q, vec_out);
     if (p.shares)
-      hipLaunchKernelGGL((k_paged_merge<T, HD, false>), dim3(p.shares, 32 * p.cap / MERGE_COLUMNS<false, HD>), dim3(MERGE_THREADS<false>), 0, st, a,
+      hipLaunchKernelGGL((k_paged_merge<T, HD, false>), dim3(((p.shares + 7) & ~7) * (32 * p.cap / MERGE_COLUMNS<false, HD>)), dim3(MERGE_THREADS<false>), 0, st, a,
                          kv.hkv, p.shares, 32 * p.cap, vec_out);
   }
   return hipGetLastError();
@@ -1112,7 +1119,7 @@ PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int
   return p;
 }
 size_t paged_attn_partial_floats(const PagedAttnPlan& p, int hd) {
-  return p.shares ? notes_floats(p.shares) + (size_t)2 * p.shares * 32 * p.cap * (hd + 2) : 0;
+  return p.shares ? notes_floats(p.shares) + 2 * p.shares * slot_floats(32 * p.cap, hd) : 0;
 }
 
 hipError_t launch_paged_attn(hipStream_t st, int dtype, int hd, const PagedDev& kv, const ChunkDev& ch, const PagedAttnArgs& a,
