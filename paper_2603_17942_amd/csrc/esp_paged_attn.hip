@@ -1090,31 +1090,42 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
 
 }  // namespace
 
+// Which kernel, and how many shares.  The times are of bf16 with 32/8 heads of 128, in us, and fit what was measured from 1 to 32 sequences.
+// Stream or tile kernel: the stream kernel begins and ends sooner (7 against 13) and has the work in pieces of 32 columns for every place, but
+// reads every key again for each 32 columns, at best from its XCD's 4 MB of L2.  128 rows over 2048 / 8000 keys: 26 / 42 against 28 / 43;
+// 320 rows over 2048 / 8000: 38 / 78 against 39 / 70; 2048 rows from none: 64 against 72; 4 x 100 rows over 4000, whose keys are too much
+// for L2: 85 against 58.
+// Stream kernel, shares or an item a workgroup: an item alone takes 7 and 0.57 for 128 keys; shares with their merge 13.5 and what K and V take.
+// One row over 1000 / 4000 keys: 11.2 / 25.7 alone, 12.9 / 17.5 in shares; 32 sequences of 2000 / 4000: 45 / 97, 53 / 105 (but alone a batch
+// takes as long as its longest sequence, so a longer one is shared out).
+// Tile kernel: 2 for 64 keys, 13 for an item's beginning and end, 8 for the merge and 1/20 for a partial.  With as many items as places, one
+// sequence's go to the places by weight: 4096 rows from none 150 against 190 in shares.  So do a batch's if they are short; else they are
+// shared out, since nothing is known here of how their lengths differ (8 chunks of 189 to 512 rows over up to 8192 keys: 215 against 361;
+// 8 x 512 rows over 4096 each: 308 against 296).
 PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int len_bound) {
   PagedAttnPlan p;
   const int G = hq / hkv;
-  const int64_t cols = (int64_t)max_rows * G, keys = (int64_t)len_bound + max_rows, tiles = ceil_div(cols, 32);
-  const int most = dtype == ESP_F32 ? TILE_CAP<float> : TILE_CAP<bf16_t>;
+  const int64_t cols = (int64_t)max_rows * G, keys = (int64_t)len_bound + max_rows, tiles = std::max<int64_t>(1, ceil_div(cols, 32));
   // items that there can be with a cap
   auto items = [&](int cap) {
     return (int64_t)hkv * std::min<int64_t>((int64_t)batch * ceil_div(tiles, cap), ceil_div((int64_t)total_rows * G, 32 * cap) + batch);
   };
-  p.cap = tiles == 1 ? 1 : most;
-  while (p.cap > 2 && items(p.cap) < 256 && p.cap / 2 >= tiles) p.cap /= 2;
-  const int tk = p.cap == 1 ? STREAM_TK : TILE_TK;
-  p.q_tiles = (int)std::max<int64_t>(1, ceil_div(tiles, p.cap));
-  const int64_t places = 256 * (p.cap > 1 || (dtype == ESP_F32 && hd == 128) ? 1 : 2);     // workgroups that have a place at once
-  p.least = p.cap == 1 ? 2 : 4;
-  const int64_t key_tiles = ceil_div(keys, tk), n = items(p.cap);
+  const int64_t kv_bytes = ceil_div((int64_t)batch * hkv, 8) * keys * hd * (dtype == ESP_F32 ? 8 : 4);     // of an XCD's sequences and heads
+  const bool small = items(1) * keys * hd <= (int64_t)3 << 26 && (tiles <= 2 || kv_bytes <= 5 << 20);
+  p.cap = tiles == 1 || small ? 1 : dtype == ESP_F32 ? TILE_CAP<float> : TILE_CAP<bf16_t>;
+  while (p.cap > 2 && p.cap / 2 >= tiles && items(p.cap) < 256) p.cap /= 2;
+  const int64_t n = items(p.cap), key_tiles = ceil_div(keys, p.cap == 1 ? STREAM_TK : TILE_TK);
+  p.q_tiles = (int)ceil_div(tiles, p.cap);
   if (p.cap == 1) {
-    if (key_tiles > p.least && n < 4 * places) p.shares = (int)std::min(places, ceil_div(n * key_tiles, p.least));
-  } else if (n < (batch == 1 || key_tiles <= 20 ? places : 4 * places)) {
-    // us: 2 for a key tile, 13 for an item's beginning and end, 8 for the merge, 1/20 for a partial
-    const double alone = 2. * key_tiles + 13., parts = std::min(sqrt(40. * key_tiles / n), (double)places / n);
-    if (batch > 1 || 2. * key_tiles / parts + 0.05 * n * parts + 21. < alone) {
-      p.shares = (int)(batch > 1 ? std::min<double>(places, std::max(n * parts, (double)n)) : n * std::floor(parts));
-      if (batch == 1 && p.shares <= n) p.shares = 0;
-    }
+    const int64_t places = dtype == ESP_F32 && hd == 128 ? 256 : 512;        // workgroups that have a place at once
+    const double tile_us = dtype == ESP_F32 ? 3.5 * hd / 128 : 0.17 + 0.4 * hd / 128;
+    p.least = 2;
+    if (n < 4 * places && tile_us * key_tiles > 6.5 + 0.09 * std::min<int64_t>(n, 64)) p.shares = (int)std::min(places, ceil_div(n * key_tiles, p.least));
+  } else if (n < (batch == 1 || key_tiles <= 20 ? 256 : 4 * 256)) {
+    const double alone = 2. * key_tiles + 13., parts = std::min(sqrt(40. * key_tiles / n), 256. / n);
+    p.least = 4;
+    if (batch > 1 && key_tiles > 20) p.shares = (int)std::min(256., std::max(n * parts, (double)n));
+    else if (parts >= 2. && 2. * key_tiles / parts + 0.05 * n * parts + 21. < alone) p.shares = (int)(n * std::floor(parts));
   }
   return p;
 }

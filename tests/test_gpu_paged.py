@@ -50,13 +50,16 @@ def v_place(s, d, hd):
 class Cache:
     """A paged cache whose contents the test knows: K and V of every sequence as plain rows, everything else NaN."""
 
+    bound = 0                                          # the lengths' bound at least (a launch is planned for it)
+
     def __init__(self, dt, hkv, hd, page, lens, rows, seed, layers=1, layer=0, spare=3, rows_too=True, pages_per_seq=None, std=1.0):
         g = gen(seed)
         self.dt, self.hd, self.page, self.lens, self.rows, self.layer = dt, hd, page, lens, rows, layer
         need = [(l + r + page - 1) // page for l, r in zip(lens, rows)]
         n = sum(need) + spare
         order = torch.randperm(n, generator=g).tolist()
-        stride = pages_per_seq or max(max(need), 1)
+        bound = max(max(lens), self.bound)
+        stride = pages_per_seq or max(max(need), 1, (bound + max(rows) + page - 1) // page if self.bound else 0)
         table = torch.full((len(lens), stride), 2 ** 31 - 1, dtype=torch.int32)     # entries nobody needs are no pages at all
         at = 0
         for b, k in enumerate(need):
@@ -78,7 +81,7 @@ class Cache:
                 vp[layer, pg][:, v_place(inside, d, hd)] = v[s].float().numpy()
         shape = (layers, n, hkv, page, hd)
         self.kv = B.PagedKv(torch.from_numpy(kp).to(dt).reshape(shape).cuda(), torch.from_numpy(vp).to(dt).reshape(shape).cuda(), table.cuda(),
-                            i32(lens), max(lens))
+                            i32(lens), bound)
         starts = np.concatenate([[0], np.cumsum(rows)]).tolist()
         self.starts = starts
         self.chunk = B.ChunkRows(i32(starts), starts[-1], max(max(rows), 1))
@@ -90,6 +93,14 @@ class Cache:
         k = pool_k[self.layer, pg].reshape(pool_k.shape[2], -1)[:, k_place(inside, d, self.hd)]
         v = pool_v[self.layer, pg].reshape(pool_v.shape[2], -1)[:, v_place(inside, d, self.hd)]
         return k, v
+
+
+@pytest.fixture(params=["short", "far"])
+def planned(request):
+    """Attention over the same rows as planned for their lengths and as planned for a long cache: other kernels and shares."""
+    Cache.bound = 40000 if request.param == "far" else 0
+    yield request.param
+    Cache.bound = 0
 
 
 def visible(l, r, anc=None):
@@ -176,7 +187,7 @@ ATTN = [  # dtype, hd, hq, hkv, page, lens, rows
 
 
 @pytest.mark.parametrize("dtype,hd,hq,hkv,page,lens,rows", ATTN)
-def test_attention_causal(dtype, hd, hq, hkv, page, lens, rows):
+def test_attention_causal(dtype, hd, hq, hkv, page, lens, rows, planned):
     dt = DT[dtype]
     c = Cache(dt, hkv, hd, page, lens, rows, 11, layers=2, layer=1)
     q = queries(c.starts[-1], hq, hd, dt, 12)
@@ -201,7 +212,7 @@ def random_tree(n, seed):
 
 
 @pytest.mark.parametrize("dtype,hd,hq,hkv,page,lens,rows", ATTN)
-def test_attention_tree(dtype, hd, hq, hkv, page, lens, rows):
+def test_attention_tree(dtype, hd, hq, hkv, page, lens, rows, planned):
     dt = DT[dtype]
     c = Cache(dt, hkv, hd, page, lens, rows, 21)
     q = queries(c.starts[-1], hq, hd, dt, 22)
@@ -214,7 +225,7 @@ def test_attention_tree(dtype, hd, hq, hkv, page, lens, rows):
 
 @pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
 @pytest.mark.parametrize("n", [1, 5, 70])
-def test_rows_that_see_nothing_are_zero(dtype, hd, n):
+def test_rows_that_see_nothing_are_zero(dtype, hd, n, planned):
     dt = DT[dtype]
     c = Cache(dt, 2, hd, 32, [0, 40], [n, n], 31)
     q = queries(2 * n, 8, hd, dt, 32)
@@ -229,7 +240,7 @@ def test_rows_that_see_nothing_are_zero(dtype, hd, n):
 @pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
 @pytest.mark.parametrize("n,l", [(6, 50), (100, 20), (100, 0)])
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
-def test_hidden_rows_that_are_not_finite_stay_hidden(dtype, hd, n, l, what):
+def test_hidden_rows_that_are_not_finite_stay_hidden(dtype, hd, n, l, what, planned):
     """K and V of some of the chunk's rows are no numbers; rows that do not see them are as without them, others are not finite."""
     dt = DT[dtype]
     c = Cache(dt, 2, hd, 64, [l], [n], 41, rows_too=True)
@@ -249,7 +260,7 @@ def test_hidden_rows_that_are_not_finite_stay_hidden(dtype, hd, n, l, what):
         assert ((out[~hit] - want).abs() <= tol).all(), anc is None
 
 
-def test_value_not_finite_with_finite_key():
+def test_value_not_finite_with_finite_key(planned):
     """Only V is no number: the rows behind it have an infinite or undefined output there, the rows before it their own."""
     c = Cache(torch.bfloat16, 2, 128, 64, [10], [40], 44)
     pg, inside = int(c.table[0, 0]), 10 + 20
@@ -275,7 +286,7 @@ def test_long_caches_and_loose_bounds(dtype, hd, hq, hkv, len_, rows, bound):
 
 
 @pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 64)])
-def test_large_scores_and_other_scales(dtype, hd):
+def test_large_scores_and_other_scales(dtype, hd, planned):
     dt = DT[dtype]
     c = Cache(dt, 2, hd, 32, [300, 0], [40, 12], 61, std=6.0)
     q = queries(52, 6, hd, dt, 62, 6.0)
@@ -284,7 +295,7 @@ def test_large_scores_and_other_scales(dtype, hd):
 
 
 @pytest.mark.parametrize("shift", [0, 1, 3])
-def test_queries_at_any_stride_and_alignment(shift):
+def test_queries_at_any_stride_and_alignment(shift, planned):
     for dt in (torch.bfloat16, torch.float32):
         c = Cache(dt, 2, 128, 32, [50, 9], [20, 3], 71)
         buf = (torch.randn((23, 14 * 128 + shift), generator=gen(72))).to(dt).cuda()
@@ -298,21 +309,21 @@ def test_queries_at_any_stride_and_alignment(shift):
         assert torch.equal(odd, out)
 
 
-def test_rows_behind_the_last_sequence_and_scratch_do_not_matter():
+def test_rows_behind_the_last_sequence_and_scratch_do_not_matter(planned):
     c = Cache(torch.bfloat16, 8, 128, 64, [1500, 70], [2, 3], 81)
     q = queries(9, 32, 128, torch.bfloat16, 82)
     q[5:] = math.nan
     rows = B.ChunkRows(i32(c.starts), 9, 5)
     out = torch.full_like(q, 3.0)
     n = B.paged_attn_scratch_bytes(c.kv, rows, 32)
-    assert n > 0
+    assert n > 0 or planned == "short"
     scratch = torch.full((n + 64,), 0xff, dtype=torch.uint8, device="cuda")
     B.paged_attn(c.kv, 0, rows, q, out=out, scratch=scratch[:n])
     assert (out[5:] == 3.0).all() and (scratch[n:] == 0xff).all()
     check_attention(c, q, out)
 
 
-def test_sequences_may_share_pages():
+def test_sequences_may_share_pages(planned):
     c = Cache(torch.bfloat16, 2, 128, 32, [96, 96], [4, 4], 91)
     c.kv.page_table[1, :3] = c.kv.page_table[0, :3]
     c.k[1][:96], c.v[1][:96] = c.k[0][:96], c.v[0][:96]
@@ -321,7 +332,7 @@ def test_sequences_may_share_pages():
 
 
 @pytest.mark.parametrize("rows", [1, 40])
-def test_malformed_sequences_are_left_alone(rows):
+def test_malformed_sequences_are_left_alone(rows, planned):
     """Bad lengths and rows: the sequence's output is not touched, the others' is right, the status says what it was."""
     for what, bit in (("len_over_bound", 1), ("len_negative", 1), ("len_past_table", 1), ("rows_over_max", 8), ("rows_descend", 8), ("rows_past_end", 8)):
         c = Cache(torch.bfloat16, 2, 128, 32, [40, 50, 60], [rows] * 3, 101)
@@ -329,7 +340,7 @@ def test_malformed_sequences_are_left_alone(rows):
         table = c.kv.page_table.shape[1] * 32
         max_rows, starts = rows, list(c.starts)
         if what == "len_over_bound":
-            c.kv.lens[2] = 61
+            c.kv.lens[2] = c.kv.len_bound + 1
         elif what == "len_negative":
             c.kv.lens[2] = -1
         elif what == "len_past_table":
@@ -355,7 +366,7 @@ def test_malformed_sequences_are_left_alone(rows):
 
 @pytest.mark.parametrize("hd,rows", [(128, 1), (128, 70), (64, 3)])
 @pytest.mark.parametrize("bad", [-1, 10 ** 6])
-def test_keys_in_pages_outside_the_pool_are_not_seen(hd, rows, bad):
+def test_keys_in_pages_outside_the_pool_are_not_seen(hd, rows, bad, planned):
     c = Cache(torch.bfloat16, 2, hd, 32, [200], [rows], 111)
     c.kv.page_table[0, 2] = bad
     q = queries(rows, 4, hd, torch.bfloat16, 112)
