@@ -523,22 +523,22 @@ def softmax_topk_static(logits: torch.Tensor, kp: int, ids: torch.Tensor, ps: to
 
 
 # ---- paged KV cache -------------------------------------------------------------------------------------
-# Functions on tensors, on the current stream of the tensors' device (which need not be the current one).
-
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
-
+# Functions on tensors, on the current stream of the tensors' device (which need not be the current one).  Some of the kernels take less
+# time than formatting a message does, so that is done for the call that is refused only.
 
 def _dtype_of(t: torch.Tensor) -> int:
-    _need(t.dtype in (torch.bfloat16, torch.float32), f"bfloat16 or float32 wanted, got {t.dtype}")
-    return ESP_BF16 if t.dtype == torch.bfloat16 else ESP_F32
+    if t.dtype is torch.bfloat16:
+        return ESP_BF16
+    if t.dtype is not torch.float32:
+        raise ValueError(f"bfloat16 or float32 wanted, got {t.dtype}")
+    return ESP_F32
 
 
 def _on_device(dev: torch.device, fn, where: str, *args):
-    _need(dev.type == "cuda", f"{where}: the tensors are on {dev}; there is no CPU fallback")
+    if dev.type != "cuda":
+        raise ValueError(f"{where}: the tensors are on {dev}; there is no CPU fallback")
     if dev.index == torch.cuda.current_device():
-        code = fn(_stream_ptr(), *args)
+        code = fn(torch._C._cuda_getCurrentRawStream(dev.index), *args)       # (a Stream object, 2.7 us, only to be asked for this)
     else:
         with torch.cuda.device(dev):
             code = fn(_stream_ptr(), *args)
@@ -548,26 +548,29 @@ def _on_device(dev: torch.device, fn, where: str, *args):
 
 def _heads(t: torch.Tensor, name: str, dev, dtype, rows: int, hd: int):
     """(pointer, row stride, heads) of [rows, heads, hd] whose heads lie side by side; rows may lie further apart."""
-    _need(t.dim() == 3 and t.shape[0] == rows and t.shape[2] == hd and t.dtype == dtype and t.device == dev,
-          f"{name}: [{rows}, heads, {hd}] of {dtype} on {dev} wanted, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    n = t.shape[1]
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != rows or shape[2] != hd or t.dtype is not dtype or t.device != dev:
+        raise ValueError(f"{name}: [{rows}, heads, {hd}] of {dtype} on {dev} wanted, got {tuple(shape)} of {t.dtype} on {t.device}")
+    n = shape[1]
     s0, s1, s2 = t.stride()
-    _need((s2 == 1 or hd == 1) and (s1 == hd or n == 1), f"{name}: the features of a head and the heads of a row have to lie side by side")
+    if (s2 != 1 and hd != 1) or (s1 != hd and n != 1):
+        raise ValueError(f"{name}: the features of a head and the heads of a row have to lie side by side")
     return t.data_ptr(), (s0 if rows > 1 else n * hd), n
 
 
 def _ints(t: Optional[torch.Tensor], name: str, dev, shape) -> Optional[int]:
     if t is None:
         return None
-    _need(t.dtype == torch.int32 and t.device == dev and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
-          f"{name}: contiguous int32 {tuple(shape)} on {dev} wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not torch.int32 or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous int32 {tuple(shape)} on {dev} wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _gain(t: Optional[torch.Tensor], name: str, dev, dtype, hd: int) -> Optional[int]:
     if t is None:
         return None
-    _need(t.dtype == dtype and t.device == dev and tuple(t.shape) == (hd,) and t.is_contiguous(), f"{name}: contiguous [{hd}] of {dtype} on {dev} wanted")
+    if t.dtype is not dtype or t.shape != (hd,) or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous [{hd}] of {dtype} on {dev} wanted")
     return t.data_ptr()
 
 
@@ -589,7 +592,8 @@ def rope_qk(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: tor
     turned to their positions [rows], after the RMS norm of every head where a gain [head_dim] is given.  Outputs may be the inputs."""
     lib = load_library()
     x = q if q is not None else k
-    _need(x is not None and x.dim() == 3, "q or k wanted")
+    if x is None or x.dim() != 3:
+        raise ValueError("q or k wanted, [rows, heads, head_dim]")
     dev, dt, rows, hd = x.device, x.dtype, x.shape[0], rope.head_dim
     code = _dtype_of(x)
     qp = qs = qo = qos = nq = kp = ks = ko = kos = nk = 0
@@ -598,13 +602,15 @@ def rope_qk(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: tor
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=dt, device=dev)
         qo, qos, n = _heads(q_out, "q_out", dev, dt, rows, hd)
-        _need(n == nq, "q_out: as many heads as q wanted")
+        if n != nq:
+            raise ValueError("q_out: as many heads as q wanted")
     if k is not None:
         kp, ks, nk = _heads(k, "k", dev, dt, rows, hd)
         if k_out is None:
             k_out = torch.empty(k.shape, dtype=dt, device=dev)
         ko, kos, n = _heads(k_out, "k_out", dev, dt, rows, hd)
-        _need(n == nk, "k_out: as many heads as k wanted")
+        if n != nk:
+            raise ValueError("k_out: as many heads as k wanted")
     if rows:
         _on_device(dev, lib.esp_rope_qk, "esp_rope_qk", code, C.byref(rope), rows, nq, nk, qp, qs, kp, ks, _ints(positions, "positions", dev, (rows,)),
                    _gain(q_gain, "q_gain", dev, dt, hd), _gain(k_gain, "k_gain", dev, dt, hd), eps, qo, qos, ko, kos)
@@ -620,9 +626,10 @@ class PagedKv:
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, len_bound: int,
                  status: Optional[torch.Tensor] = None):
         dev = k.device
-        _need(k.dim() == 5 and k.shape == v.shape and k.dtype == v.dtype and v.device == dev and k.is_contiguous() and v.is_contiguous(),
-              "k and v: contiguous [layers, pages, kv heads, page size, head dim] alike wanted")
-        _need(page_table.dim() == 2, "page_table: [batch, pages of a sequence] wanted")
+        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or v.device != dev or not (k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("k and v: contiguous [layers, pages, kv heads, page size, head dim] alike wanted")
+        if page_table.dim() != 2:
+            raise ValueError("page_table: [batch, pages of a sequence] wanted")
         self.k, self.v, self.page_table, self.lens, self.device = k, v, page_table, lens, dev
         self.status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
         batch = page_table.shape[0]
@@ -666,7 +673,8 @@ class ChunkRows:
 
 
 def _same_batch(kv: PagedKv, rows: ChunkRows):
-    _need(rows.row0.device == kv.device and rows.row0.numel() == kv.batch + 1, "row0: [batch + 1] on the cache's device wanted")
+    if rows.row0.device != kv.device or rows.row0.numel() != kv.batch + 1:
+        raise ValueError("row0: [batch + 1] on the cache's device wanted")
 
 
 def paged_append(kv: PagedKv, layer: int, rows: ChunkRows, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
@@ -679,14 +687,16 @@ def paged_append(kv: PagedKv, layer: int, rows: ChunkRows, q: Optional[torch.Ten
     dev, dt, hd, n = kv.device, kv.dtype, kv.head_dim, rows.total_rows
     kp, ks, nk = _heads(k, "k", dev, dt, n, hd)
     vp, vs, nv = _heads(v, "v", dev, dt, n, hd)
-    _need(nk == kv.n_kv_heads and nv == nk, f"k and v: {kv.n_kv_heads} heads wanted")
+    if nk != kv.n_kv_heads or nv != nk:
+        raise ValueError(f"k and v: {kv.n_kv_heads} heads wanted")
     qp = qs = qo = qos = nq = 0
     if q is not None:
         qp, qs, nq = _heads(q, "q", dev, dt, n, hd)
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=dt, device=dev)
         qo, qos, m = _heads(q_out, "q_out", dev, dt, n, hd)
-        _need(m == nq, "q_out: as many heads as q wanted")
+        if m != nq:
+            raise ValueError("q_out: as many heads as q wanted")
     if n == 0:
         return q_out
     _on_device(dev, lib.esp_paged_append, "esp_paged_append", kv._ref, layer, rows._ref, None if rope is None else C.byref(rope),
@@ -710,16 +720,18 @@ def paged_attn(kv: PagedKv, layer: int, rows: ChunkRows, q: torch.Tensor, scale:
     qp, qs, nq = _heads(q, "q", dev, dt, n, hd)
     if out is None:
         out = torch.empty((n, nq, hd), dtype=dt, device=dev)
-    _need(out.dtype == dt and out.device == dev and tuple(out.shape) == (n, nq, hd) and out.is_contiguous(), f"out: contiguous [{n}, {nq}, {hd}] wanted")
+    if out.dtype is not dt or out.shape != (n, nq, hd) or out.device != dev or not out.is_contiguous():
+        raise ValueError(f"out: contiguous [{n}, {nq}, {hd}] wanted")
     words = 0
     if anc is not None:
-        _need(anc.dtype == torch.int64 and anc.device == dev and anc.dim() == 2 and anc.shape[0] == n and anc.is_contiguous(),
-              f"anc: contiguous int64 [{n}, words] wanted")
+        if anc.dtype is not torch.int64 or anc.device != dev or anc.dim() != 2 or anc.shape[0] != n or not anc.is_contiguous():
+            raise ValueError(f"anc: contiguous int64 [{n}, words] wanted")
         words = anc.shape[1]
     if scratch is None:
         nb = paged_attn_scratch_bytes(kv, rows, nq)
         scratch = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
-    _need(scratch is None or (scratch.dtype == torch.uint8 and scratch.device == dev and scratch.is_contiguous()), "scratch: contiguous uint8 wanted")
+    if scratch is not None and (scratch.dtype is not torch.uint8 or scratch.device != dev or not scratch.is_contiguous()):
+        raise ValueError("scratch: contiguous uint8 wanted")
     if n == 0:
         return out
     _on_device(dev, lib.esp_paged_attn, "esp_paged_attn", kv._ref, layer, rows._ref, nq, qp, qs, hd ** -0.5 if scale is None else scale,

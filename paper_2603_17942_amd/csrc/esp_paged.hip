@@ -108,12 +108,12 @@ __device__ __forceinline__ void pieces_of(int j, int rot, int& u0, int& u1) {
 
 // R rows a workgroup, a wave finds a row's place and fills its table of cosines and sines, then all threads take the heads.
 template <typename T, int HD, bool PAGED, bool VEC, int R>
-__global__ __launch_bounds__(256) void k_rope_rows(RopeRows a, PagedDev kv, ChunkDev ch) {
+__device__ __forceinline__ void rope_rows(const RopeRows& a, const PagedDev& kv, const ChunkDev& ch, int hkv, int block) {
   constexpr int LPH = HD / 16;
   __shared__ float2 cs[R][HD / 2];
   __shared__ int page_of[R], slot_of[R];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int m0 = blockIdx.x * R;
+  const int m0 = block * R;
   for (int i = wave; i < R; i += 4) {
     const int m = m0 + i;
     int page = -1, slot = 0, pos = 0;
@@ -145,19 +145,19 @@ __global__ __launch_bounds__(256) void k_rope_rows(RopeRows a, PagedDev kv, Chun
       cs[i][lane] = float2{c * a.amplitude, s * a.amplitude};
     }
   }
-  if (PAGED && blockIdx.x == 0)
+  if (PAGED && block == 0)
     for (int b = tid; b < kv.batch; b += 256)
       if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(kv, ch, b));
   __syncthreads();
-  const int heads = a.hq + (PAGED ? 2 : 1) * a.hkv, per_row = heads * LPH;
+  const int heads = a.hq + (PAGED ? 2 : 1) * hkv, per_row = heads * LPH;
   for (int t = tid; t < R * per_row; t += 256) {
     const int i = t / per_row, head = (t - i * per_row) / LPH, j = t % LPH, m = m0 + i;
     const int page = page_of[i];
     if (page == -1) continue;
     float x0[8], x1[8];
-    if (head >= a.hq + a.hkv) {
+    if (head >= a.hq + hkv) {
       if (page < 0) continue;
-      const int kvh = head - a.hq - a.hkv;
+      const int kvh = head - a.hq - hkv;
       const T* src = (const T*)a.v + (int64_t)m * a.v_stride + kvh * HD;
       load8<VEC>(src + 8 * j, x0);
       load8<VEC>(src + 8 * (j + LPH), x1);
@@ -193,6 +193,110 @@ __global__ __launch_bounds__(256) void k_rope_rows(RopeRows a, PagedDev kv, Chun
   }
 }
 
+template <typename T, int HD, bool PAGED, bool VEC, int R>
+__global__ __launch_bounds__(256) void k_rope_rows(RopeRows a, PagedDev kv, ChunkDev ch) {
+  rope_rows<T, HD, PAGED, VEC, R>(a, kv, ch, a.hkv, blockIdx.x);
+}
+
+// The same for chunks of many rows: K and V go by blocks of the cache, a workgroup takes 32 slots and HEADS kv heads and writes
+// whole 128-byte lines, V turned from rows to columns through LDS; the queries go by rows, in the workgroups behind these.  (By rows
+// a V row is HD stores of one element.)
+template <typename T, int HD> constexpr int BLOCK_HEADS = 128 / HD;
+template <typename T, int HD, bool VEC, int R>
+__global__ __launch_bounds__(256) void k_append_blocks(RopeRows a, PagedDev kv, ChunkDev ch, int block_groups, int head_groups) {
+  constexpr int LPH = HD / 16, HEADS = BLOCK_HEADS<T, HD>;
+  typedef T piece_t __attribute__((ext_vector_type(8)));
+  if ((int)blockIdx.x >= block_groups) {
+    rope_rows<T, HD, true, VEC, R>(a, kv, ch, 0, blockIdx.x - block_groups);
+    return;
+  }
+  __shared__ float2 cs[32][HD / 2];
+  __shared__ __align__(16) T vt[HEADS][32][HD + 8];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int kvh0 = blockIdx.x % head_groups * HEADS;
+  // the blocks of the sequences, one after the other: which one is this?
+  const int x = blockIdx.x / head_groups;
+  if (blockIdx.x == 0 && a.hq == 0)
+    for (int b = tid; b < kv.batch; b += 256)
+      if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(kv, ch, b));
+  int seq = -1, block = 0;
+  for (int b0 = 0, base = 0; b0 < kv.batch && seq < 0; b0 += 64) {
+    const ChunkSeq s = chunk_seq(kv, ch, min(b0 + lane, kv.batch - 1));
+    const int first = s.len >> 5, mine = s.ok && s.rows > 0 && b0 + lane < kv.batch ? ((s.len + s.rows - 1) >> 5) - first + 1 : 0;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
+    const uint64_t here = __builtin_amdgcn_ballot_w64(base + upto > x);
+    if (here) {
+      const int l = __builtin_ctzll(here);
+      seq = b0 + l;
+      block = __builtin_amdgcn_readlane(first, l) + x - base - __builtin_amdgcn_readlane(upto - mine, l);
+    }
+    base += __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (seq < 0) return;
+  const ChunkSeq s = chunk_seq(kv, ch, seq);
+  const int slot0 = 32 * block, page = kv.table[(size_t)seq * kv.stride + slot0 / kv.page_size], inside = slot0 % kv.page_size;
+  const int lo = max(s.len - slot0, 0), hi = min(s.len + s.rows - slot0, 32);       // of the block's slots
+  const int m0 = s.row0 + slot0 - s.len;                                            // row of its first slot
+  if ((unsigned)page >= (unsigned)kv.n_pages) {
+    if (tid == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+    return;
+  }
+  const int i = tid / LPH % 32, j = tid % LPH, h = tid / (LPH * 32), kvh = kvh0 + h, m = m0 + i;
+  const bool mine = i >= lo && i < hi && kvh < a.hkv;
+  int u0, u1;
+  pieces_of(j, a.rot, u0, u1);
+  float k0[8], k1[8], v0[8], v1[8];
+  if (mine) {
+    const T* ks = (const T*)a.k + (int64_t)m * a.k_stride + kvh * HD;
+    const T* vs = (const T*)a.v + (int64_t)m * a.v_stride + kvh * HD;
+    load8<VEC>(ks + 8 * u0, k0);
+    load8<VEC>(ks + 8 * u1, k1);
+    load8<VEC>(vs + 8 * j, v0);
+    load8<VEC>(vs + 8 * (j + LPH), v1);
+  }
+  for (int t = tid; t < 32 * (a.rot / 2); t += 256) {
+    const int r = t / (a.rot / 2), e = t - r * (a.rot / 2);
+    if (r < lo || r >= hi) continue;
+    float sn, c;
+    turn_sincos((double)(a.positions ? a.positions[m0 + r] : slot0 + r) * a.turns[e], sn, c);
+    cs[r][e] = float2{c * a.amplitude, sn * a.amplitude};
+  }
+  if (mine) {
+    store8<true>(&vt[h][i][8 * j], v0);
+    store8<true>(&vt[h][i][8 * (j + LPH)], v1);
+  }
+  __syncthreads();
+  if (mine) {
+    norm_rotate<T, HD>(a, (const T*)a.k_gain, j, u0, u1, cs[i], k0, k1);
+    T* dst = (T*)kv.k + page_plane(page, kvh, kv.hkv, kv.page_size, HD);
+    store8<true>(dst + k_off(inside + i, 8 * u0, HD), k0);
+    store8<true>(dst + k_off(inside + i, 8 * u1, HD), k1);
+  }
+#pragma unroll
+  for (int t = tid; t < HEADS * HD * 4; t += 256) {           // 16-byte pieces of V's block
+    const int hv = t / (HD * 4), at = t % (HD * 4), frag = at >> 6, l = at & 63, d = (frag >> 1) * 32 + (l & 31), key0 = (frag & 1) * 16 + 4 * (l >> 5);
+    if (kvh0 + hv >= a.hkv) continue;
+    T* dst = (T*)kv.v + page_plane(page, kvh0 + hv, kv.hkv, kv.page_size, HD) + (inside >> 5) * (32 * HD) + at * 8;
+    piece_t p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = vt[hv][key0 + (e & 3) + 8 * (e >> 2)][d];
+    if (key0 >= lo && key0 + 12 <= hi) {
+      *reinterpret_cast<piece_t*>(dst) = p;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int key = key0 + (e & 3) + 8 * (e >> 2);
+        if (key >= lo && key < hi) dst[e] = p[e];
+      }
+    }
+  }
+}
+
 // What is wrong with a sequence's path (0: nothing): its rows ascend from 1 on, and rows and places lie in the table.
 __device__ __forceinline__ int path_fault(const PagedDev& kv, int L, int n, const int32_t* path) {
   const int64_t cap = (int64_t)kv.stride * kv.page_size;
@@ -207,63 +311,61 @@ __device__ __forceinline__ int path_fault(const PagedDev& kv, int L, int n, cons
   return ok ? 0 : ESP_DEV_BAD_PATH;
 }
 
-// A workgroup moves one (layer, kv head) of a sequence's path: everything is read before anything is written, since a row's
-// place may be another's source.
+// A wave moves one (layer, kv head) of a sequence's path: everything is read before anything is written, since a row's place may be another's
+// source.
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_paged_commit(PagedDev kv, const int32_t* __restrict__ n_emit, const int32_t* __restrict__ accepted,
+__global__ __launch_bounds__(256) void k_paged_commit(PagedDev kv, int planes, const int32_t* __restrict__ n_emit, const int32_t* __restrict__ accepted,
                                                       int32_t* len_out) {
   constexpr int MOST = ESP_MAX_MASKS;                  // rows that can move
   typedef T piece_t __attribute__((ext_vector_type(8)));
-  const int seq = blockIdx.y, layer = blockIdx.x / kv.hkv, kvh = blockIdx.x % kv.hkv, tid = threadIdx.x;
+  const int seq = blockIdx.y, plane_of = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int layer = plane_of / kv.hkv, kvh = plane_of % kv.hkv;
   const int L = kv.len[seq], n = n_emit[seq];
   const int32_t* path = accepted + (size_t)seq * (ESP_MAX_MASKS + 1);
   const int fault = path_fault(kv, L, n, path);
-  if (blockIdx.x == 0 && tid == 0) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
     if (fault) set_status(kv.status, fault);
     if (len_out) len_out[seq] = fault ? L : L + n;
   }
-  if (fault) return;
+  if (fault || plane_of >= planes) return;
   const size_t layer0 = (size_t)layer * kv.n_pages * kv.hkv * kv.page_size * HD;
   T* kp = (T*)kv.k + layer0;
   T* vp = (T*)kv.v + layer0;
   const int32_t* table = kv.table + (size_t)seq * kv.stride;
+  // where rows lie and go: the same for the whole wave
+  size_t from[MOST], to[MOST];
+  int from_in[MOST], to_in[MOST];
+  bool moves[MOST], lands[MOST];
   auto place = [&](int s, size_t& plane, int& inside) {
     const int page = table[s / kv.page_size];
     inside = s % kv.page_size;
     const bool there = (unsigned)page < (unsigned)kv.n_pages;
-    if (!there && tid == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+    if (!there && lane == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
     plane = page_plane(there ? page : 0, kvh, kv.hkv, kv.page_size, HD);
     return there;
   };
-  constexpr int VROWS = MOST * HD / 256, KROWS = (MOST * HD / 8 + 255) / 256;
-  T v[VROWS];
-  piece_t k[KROWS];
-  bool v_there[VROWS], k_there[KROWS];
-  size_t plane;
-  int inside;
 #pragma unroll
-  for (int x = 0; x < VROWS; ++x) {
-    const int i = 1 + (tid + 256 * x) / HD, d = tid % HD;
-    v_there[x] = i < n && place(L + path[i], plane, inside);
-    if (v_there[x]) v[x] = vp[plane + v_off(inside, d, HD)];
+  for (int i = 0; i < MOST; ++i) {
+    moves[i] = i + 1 < n && path[i + 1] != i + 1 && place(L + path[i + 1], from[i], from_in[i]);
+    lands[i] = moves[i] && place(L + i + 1, to[i], to_in[i]);
   }
+  constexpr int VE = HD / 64, PIECES = HD / 8;
+  T v[MOST][VE];
+  piece_t k[MOST];
 #pragma unroll
-  for (int x = 0; x < KROWS; ++x) {
-    const int i = 1 + (tid + 256 * x) / (HD / 8), u = tid % (HD / 8);
-    k_there[x] = i < n && place(L + path[i], plane, inside);
-    if (k_there[x]) k[x] = *reinterpret_cast<const piece_t*>(kp + plane + k_off(inside, 8 * u, HD));
+  for (int i = 0; i < MOST; ++i) {
+    if (!moves[i]) continue;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) v[i][e] = vp[from[i] + v_off(from_in[i], lane + 64 * e, HD)];
+    if (lane < PIECES) k[i] = *reinterpret_cast<const piece_t*>(kp + from[i] + k_off(from_in[i], 8 * lane, HD));
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
 #pragma unroll
-  for (int x = 0; x < VROWS; ++x) {
-    const int i = 1 + (tid + 256 * x) / HD, d = tid % HD;
-    if (v_there[x] && place(L + i, plane, inside)) vp[plane + v_off(inside, d, HD)] = v[x];
-  }
+  for (int i = 0; i < MOST; ++i) {
+    if (!lands[i]) continue;
 #pragma unroll
-  for (int x = 0; x < KROWS; ++x) {
-    const int i = 1 + (tid + 256 * x) / (HD / 8), u = tid % (HD / 8);
-    if (k_there[x] && place(L + i, plane, inside)) *reinterpret_cast<piece_t*>(kp + plane + k_off(inside, 8 * u, HD)) = k[x];
+    for (int e = 0; e < VE; ++e) vp[to[i] + v_off(to_in[i], lane + 64 * e, HD)] = v[i][e];
+    if (lane < PIECES) *reinterpret_cast<piece_t*>(kp + to[i] + k_off(to_in[i], 8 * lane, HD)) = k[i];
   }
 }
 
@@ -316,9 +418,25 @@ hipError_t launch_rows(hipStream_t st, const RopeRows& a, const PagedDev& kv, co
 }
 
 template <typename T, int HD>
+hipError_t launch_append(hipStream_t st, const RopeRows& a, const PagedDev& kv, const ChunkDev& ch) {
+  // by rows / by blocks, 32/8 heads of 128 in bf16, us: 64 rows 5.3 / 7.0, 320 7.5 / 7.3, 32 x 8 7.0 / 7.6, 32 x 16 9.0 / 7.6, 8192 61 / 40
+  if (a.rows < 256 || a.rows < 16 * kv.batch) return launch_rows<T, HD, true>(st, a, kv, ch);
+  const bool vec = rows_aligned<T>(a, true);
+  const int r = a.rows >= 1024 ? 4 : 1, head_groups = (a.hkv + BLOCK_HEADS<T, HD> - 1) / BLOCK_HEADS<T, HD>;
+  const int64_t block_groups = ((int64_t)a.rows / 32 + 2 * kv.batch) * head_groups, grid = block_groups + (a.hq ? (a.rows + r - 1) / r : 0);
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+#define ESP_APPEND(V_, R_) \
+  hipLaunchKernelGGL((k_append_blocks<T, HD, V_, R_>), dim3((unsigned)grid), dim3(256), 0, st, a, kv, ch, (int)block_groups, head_groups)
+  if (r == 4) { if (vec) ESP_APPEND(true, 4); else ESP_APPEND(false, 4); }
+  else { if (vec) ESP_APPEND(true, 1); else ESP_APPEND(false, 1); }
+#undef ESP_APPEND
+  return hipGetLastError();
+}
+
+template <typename T, int HD>
 hipError_t launch_commit(hipStream_t st, const PagedDev& kv, int layers, const int32_t* n_emit, const int32_t* accepted, int32_t* len_out) {
   const bool in_place = len_out == kv.len;
-  hipLaunchKernelGGL((k_paged_commit<T, HD>), dim3(layers * kv.hkv, kv.batch), dim3(256), 0, st, kv, n_emit, accepted, in_place ? nullptr : len_out);
+  hipLaunchKernelGGL((k_paged_commit<T, HD>), dim3((layers * kv.hkv + 3) / 4, kv.batch), dim3(256), 0, st, kv, layers * kv.hkv, n_emit, accepted, in_place ? nullptr : len_out);
   if (in_place) hipLaunchKernelGGL(k_paged_advance, dim3((kv.batch + 255) / 256), dim3(256), 0, st, kv, n_emit, accepted, len_out);
   return hipGetLastError();
 }
@@ -340,7 +458,7 @@ hipError_t launch_rope_rows(hipStream_t st, int dtype, int hd, const RopeRows& a
 }
 
 hipError_t launch_paged_append(hipStream_t st, int dtype, int hd, const PagedDev& kv, const ChunkDev& ch, const RopeRows& a) {
-#define ESP_CALL(T_, HD_) (launch_rows<T_, HD_, true>(st, a, kv, ch))
+#define ESP_CALL(T_, HD_) (launch_append<T_, HD_>(st, a, kv, ch))
   return ESP_BY_TYPE(ESP_CALL);
 #undef ESP_CALL
 }

@@ -505,6 +505,7 @@ APPEND = [  # dtype, hd, hq, hkv, page, lens, rows
     ("bf16", 128, 7, 1, 96, [95, 0], [200, 33]), ("bf16", 64, 8, 4, 32, [17, 3], [5, 40]), ("f32", 128, 4, 2, 64, [30, 62], [3, 66]),
     ("f32", 64, 4, 4, 32, [1, 0, 0], [1, 31, 32]), ("bf16", 128, 8, 2, 128, [129, 7], [130, 1100]), ("f32", 64, 2, 1, 64, [3], [1200]),
     ("bf16", 64, 3, 3, 32, [0, 1, 2, 3, 4, 5, 6, 7] * 9, [1, 2, 0, 3] * 18),
+    ("bf16", 64, 3, 3, 32, [5, 0, 40], [300, 0, 7]), ("f32", 128, 4, 2, 64, [30, 62, 96], [3, 300, 32]), ("bf16", 128, 2, 1, 32, [9, 0, 31, 32, 70] * 14, [17, 33] * 35),
 ]
 
 
@@ -552,7 +553,7 @@ def test_append(dtype, hd, hq, hkv, page, lens, rows, how):
     assert torch.equal(pool.view(torch.int16 if dt == torch.bfloat16 else torch.int32), c.kv.k.view(torch.int16 if dt == torch.bfloat16 else torch.int32))
 
 
-@pytest.mark.parametrize("rows", [2, 40])
+@pytest.mark.parametrize("rows", [2, 40, 120])
 def test_append_skips_what_is_malformed(rows):
     for what, bit in (("len", 1), ("rows", 8), ("page", 16)):
         c = Cache(torch.bfloat16, 2, 128, 32, [10, 20], [rows, rows], 211, rows_too=False)
@@ -580,6 +581,20 @@ def test_append_skips_what_is_malformed(rows):
             assert (q_out[rows:] == 9.0).all()
             pages = [int(p) for p in c.table[1] if p < before.shape[1]]
             assert torch.equal(before[:, pages].view(torch.int16), c.kv.k[:, pages].view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [3, 300])
+def test_append_at_any_alignment(dtype, rows):
+    dt = DT[dtype]
+    x = torch.randn((rows, 6 * 128 + 1), generator=gen(221)).to(dt).cuda()
+    spec, got = B.rope_spec(128), []
+    for shift in (0, 1):
+        c = Cache(dt, 1, 128, 32, [11], [rows], 222, rows_too=False)
+        c.kv.k.zero_(), c.kv.v.zero_()
+        h = x[:, 1:].unflatten(1, (6, 128)) if shift else x[:, 1:].contiguous().unflatten(1, (6, 128))
+        got.append((B.paged_append(c.kv, 0, c.chunk, h[:, :4], h[:, 4:5], h[:, 5:], rope=spec), c.kv.k, c.kv.v))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
 def test_load_gives_back_what_is_in_the_slots():

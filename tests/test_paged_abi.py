@@ -71,9 +71,10 @@ def test_attention_refusals(lib):
     assert call(anc=P, words=0) == ESHAPE and call(ch=chunk(max_rows=65), anc=P, words=1) == ESHAPE
     assert call(kv=paged(len_bound=2 ** 31 - 10)) == ECAPACITY
     assert call(ch=chunk(total_rows=0)) == 0 and call(ch=chunk(max_rows=0)) == 0     # nothing to do
+    kv = paged(len_bound=3000)
     need = lib.esp_paged_attn_scratch_bytes(C.byref(kv), C.byref(chunk()), 32)
-    assert need > 0                                                                     # 8 rows on 1000 keys: splits
-    assert call(scratch=None) == ECAPACITY and call(n=need - 1) == ECAPACITY and call(scratch=P + 4) == EINVAL
+    assert need > 0                                                                     # 8 rows on 3000 keys: shares
+    assert call(kv, scratch=None) == ECAPACITY and call(kv, n=need - 1) == ECAPACITY and call(kv, scratch=P + 4) == EINVAL
 
 
 def test_append_and_rope_refusals(lib):
@@ -151,7 +152,7 @@ def test_scratch_is_for_work_that_is_cut(lib):
     assert need(1, 1, 1, 40) == 0 and need(3, 9, 3, 0) == 0                   # a few keys
     assert need(1, 8192, 8192, 0) == 0                                          # enough items
     assert need(1, 1, 1, 2000) > 0 and need(1, 1, 1, 10 ** 6, 8, 1, 64) > 0
-    assert need(1, 300, 300, 2000) > 0 and need(1, 300, 300, 2000, dtype=B.ESP_F32) > 0
+    assert need(1, 300, 300, 20000) > 0 and need(1, 300, 300, 20000, dtype=B.ESP_F32) > 0
     for hd in (64, 128):
         for rows in (1, 8, 33, 500):
             for bound in (0, 100, 5000, 10 ** 6):
