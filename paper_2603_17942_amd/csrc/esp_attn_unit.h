@@ -1,4 +1,4 @@
-// What the attention kernels on matrix cores share: one unit of 32 keys for a wave's 32 query columns, bf16 or fp32.
+// What the kernels of the paged attention share: one unit of 32 keys for a wave's 32 query columns, bf16 or fp32.
 //
 // S^T = K Q^T and O^T = V^T P^T on 32 x 32 matrix instructions (bf16: 16 features or keys at a time; fp32: two).  Computing the
 // transposed scores leaves a lane with one query column and 16 keys of the unit, register v <-> key 8 (v / 4) + 4 half + v % 4, which is

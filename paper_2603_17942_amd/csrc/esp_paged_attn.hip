@@ -73,14 +73,15 @@ struct Weights {
   __device__ __forceinline__ float sum(int n) const { return first * (float)n + slope * (0.5f * (float)n * (float)(n + 1)); }
 };
 constexpr int SNAP = 4;                           // a cut this near to an item's beginning or end (key tiles, at most a quarter of a share) goes there
-// time of a key tile of an item with that many column tiles, and of its start and end, in units of a key's time
+// time of a key tile of an item with that many column tiles, and of its start and end, in units of a key's time (tile kernel: 64 keys take
+// 1.95 us with more than four column tiles, 1.4 with three or four, 1 with less; a start and end 13)
 template <bool STREAM>
-__host__ __device__ constexpr int tile_time(int cap, int per) { return STREAM ? 1 : per > 4 ? 10 : per > 2 ? 7 : 5; }
+__host__ __device__ constexpr int tile_time(int per) { return STREAM ? 1 : per > 4 ? 10 : per > 2 ? 7 : 5; }
 template <bool STREAM>
 constexpr int start_time() { return STREAM ? 64 : 4000; }
 template <bool STREAM>
-__device__ __forceinline__ Weights weights_of(const ChunkSeq& s, int G, int cap, int per, bool causal) {
-  const float t = (float)tile_time<STREAM>(cap, per);
+__device__ __forceinline__ Weights weights_of(const ChunkSeq& s, int G, int per, bool causal) {
+  const float t = (float)tile_time<STREAM>(per);
   return {(float)start_time<STREAM>() + t * (float)(s.len + (causal ? 0 : s.rows)), causal ? t * (float)(per * 32) / (float)G : 0.f};
 }
 
@@ -100,7 +101,7 @@ __device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch,
   auto weigh = [&](int b) {
     s = chunk_seq(kv, ch, min(b, kv.batch - 1));
     it = items_of(s.rows, G, cap);
-    wt = weights_of<STREAM>(s, G, cap, it.per, causal);
+    wt = weights_of<STREAM>(s, G, it.per, causal);
     mine = upto = s.ok && (one || b < kv.batch) ? wt.sum(it.n) : 0.f;
     if (one) return;
 #pragma unroll
@@ -116,13 +117,13 @@ __device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch,
   }
   const float all = per_head * (float)kv.hkv;
   if (uniform(all > 0.f) == 0) return false;
-  const int n = uniform(max(1, (int)min((float)shares, all / (float)(tile_time<STREAM>(cap, cap) * TK * least))));
+  const int n = uniform(max(1, (int)min((float)shares, all / (float)(tile_time<STREAM>(cap) * TK * least))));
   if (w >= n) return false;
   const float at = all / (float)n * (float)(w + (lane & 1));
   const int head = min((int)(at / per_head), kv.hkv - 1);
   const float off = max(at - (float)head * per_head, 0.f);
   // the last sequence with work that begins at or before this place
-  float begin = 0.f, size = mine, base = 0.f;
+  float begin = 0.f, base = 0.f;
   int seq = 0;
   if (!one) {
     Weights fw = wt;
@@ -133,10 +134,10 @@ __device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch,
       const uint64_t in0 = __builtin_amdgcn_ballot_w64(mine > 0.f && before <= off0), in1 = __builtin_amdgcn_ballot_w64(mine > 0.f && before <= off1);
       const uint64_t in = lane & 1 ? in1 : in0;
       const int l = in ? 63 - __clzll((long long)in) : 0;
-      const float b_ = __shfl(before, l, 64), m_ = __shfl(mine, l, 64);
+      const float b_ = __shfl(before, l, 64);
       const Weights w_{__shfl(wt.first, l, 64), __shfl(wt.slope, l, 64)};
       const int r_ = __shfl(s.rows, l, 64), n_ = __shfl(s.len, l, 64);
-      if (in) { begin = b_; size = m_; fw = w_; fs.rows = r_; fs.len = n_; seq = b0 + l; }
+      if (in) { begin = b_; fw = w_; fs.rows = r_; fs.len = n_; seq = b0 + l; }
       base += __shfl(upto, 63, 64);
     }
     wt = fw;
@@ -150,7 +151,7 @@ __device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch,
   int at_ = 2 * j;
   if (in_item >= heavy && at_ + 1 < it.n) { in_item -= heavy; ++at_; }
   in_item -= (float)start_time<STREAM>();
-  const float of_tile = (float)(tile_time<STREAM>(cap, it.per) * TK);
+  const float of_tile = (float)(tile_time<STREAM>(it.per) * TK);
   const int tiles = (keys_of(s, G, it.per, item_at(it.n, at_), causal) + TK - 1) / TK;
   int tile = in_item > 0.f ? (int)min(ceilf(in_item / of_tile), (float)tiles) : 0;
   // (an item that is cut costs a beginning, an end and two partials more than one that is not)
@@ -1082,8 +1083,8 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((k_paged_tile<T, HD>), g, dim3(64 * TILE_WAVES), bytes, st, kv, ch, a, p, vec_q, vec_out);
     if (p.shares)
-      hipLaunchKernelGGL((k_paged_merge<T, HD, false>), dim3(((p.shares + 7) & ~7) * (32 * p.cap / MERGE_COLUMNS<false, HD>)), dim3(MERGE_THREADS<false>), 0, st, a,
-                         kv.hkv, p.shares, 32 * p.cap, vec_out);
+      hipLaunchKernelGGL((k_paged_merge<T, HD, false>), dim3(((p.shares + 7) & ~7) * (32 * p.cap / MERGE_COLUMNS<false, HD>)),
+                         dim3(MERGE_THREADS<false>), 0, st, a, kv.hkv, p.shares, 32 * p.cap, vec_out);
   }
   return hipGetLastError();
 }
@@ -1092,12 +1093,13 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
 
 // Which kernel, and how many shares.  The times are of bf16 with 32/8 heads of 128, in us, and fit what was measured from 1 to 32 sequences.
 // Stream or tile kernel: the stream kernel begins and ends sooner (7 against 13) and has the work in pieces of 32 columns for every place, but
-// reads every key again for each 32 columns, at best from its XCD's 4 MB of L2.  128 rows over 2048 / 8000 keys: 26 / 42 against 28 / 43;
-// 320 rows over 2048 / 8000: 38 / 78 against 39 / 70; 2048 rows from none: 64 against 72; 4 x 100 rows over 4000, whose keys are too much
-// for L2: 85 against 58.
-// Stream kernel, shares or an item a workgroup: an item alone takes 7 and 0.57 for 128 keys; shares with their merge 13.5 and what K and V take.
-// One row over 1000 / 4000 keys: 11.2 / 25.7 alone, 12.9 / 17.5 in shares; 32 sequences of 2000 / 4000: 45 / 97, 53 / 105 (but alone a batch
-// takes as long as its longest sequence, so a longer one is shared out).
+// reads every key again for each 32 columns, at best from its XCD's 4 MB of L2.  128 rows over 2048 / 8000 keys: 19 / 42 against 28 / 43;
+// 320 rows over 2048 / 8000: 31 / 78 against 39 / 70; 2048 rows from none: 64 against 72; 2000 in fp32: 332 against 299; 4 x 100 rows over
+// 4000, whose keys are too much for L2: 85 against 58; 32 x 40 over 1000: 115 against 48.
+// Stream kernel, shares or an item a workgroup: an item alone takes 7 and 0.57 for 128 keys (64 KB: a CU takes in 110 GB/s, and more waves on
+// an item do not change that); shares with their merge 13.5 and what K and V take.  One row over 1000 / 4000 keys: 11.2 / 25.7 alone,
+// 12.9 / 17.5 in shares; 32 sequences of 2000 / 4000: 45 / 97, 53 / 105 (but alone a batch takes as long as its longest sequence, so a longer
+// one is shared out).
 // Tile kernel: 2 for 64 keys, 13 for an item's beginning and end, 8 for the merge and 1/20 for a partial.  With as many items as places, one
 // sequence's go to the places by weight: 4096 rows from none 150 against 190 in shares.  So do a batch's if they are short; else they are
 // shared out, since nothing is known here of how their lengths differ (8 chunks of 189 to 512 rows over up to 8192 keys: 215 against 361;
@@ -1111,7 +1113,8 @@ PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int
     return (int64_t)hkv * std::min<int64_t>((int64_t)batch * ceil_div(tiles, cap), ceil_div((int64_t)total_rows * G, 32 * cap) + batch);
   };
   const int64_t kv_bytes = ceil_div((int64_t)batch * hkv, 8) * keys * hd * (dtype == ESP_F32 ? 8 : 4);     // of an XCD's sequences and heads
-  const bool small = items(1) * keys * hd <= (int64_t)3 << 26 && (tiles <= 2 || kv_bytes <= 5 << 20);
+  const int64_t work = items(1) * (len_bound + max_rows / 2) * hd * (dtype == ESP_F32 ? 4 : 2);
+  const bool small = work <= (int64_t)1 << 29 && (tiles <= 2 || kv_bytes <= 5 << 20);
   p.cap = tiles == 1 || small ? 1 : dtype == ESP_F32 ? TILE_CAP<float> : TILE_CAP<bf16_t>;
   while (p.cap > 2 && p.cap / 2 >= tiles && items(p.cap) < 256) p.cap /= 2;
   const int64_t n = items(p.cap), key_tiles = ceil_div(keys, p.cap == 1 ? STREAM_TK : TILE_TK);
@@ -1120,7 +1123,10 @@ PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int
     const int64_t places = dtype == ESP_F32 && hd == 128 ? 256 : 512;        // workgroups that have a place at once
     const double tile_us = dtype == ESP_F32 ? 3.5 * hd / 128 : 0.17 + 0.4 * hd / 128;
     p.least = 2;
-    if (n < 4 * places && tile_us * key_tiles > 6.5 + 0.09 * std::min<int64_t>(n, 64)) p.shares = (int)std::min(places, ceil_div(n * key_tiles, p.least));
+    if (n < 4 * places && tile_us * key_tiles > 6.5 + 0.09 * std::min<int64_t>(n, 64)) {
+      p.shares = (int)std::min(places, ceil_div(n * key_tiles, p.least));
+      if (batch == 1 && p.shares > n) p.shares = (int)(p.shares / n * n);    // (whole items come out: 17 us with two more shares, 14 without)
+    }
   } else if (n < (batch == 1 || key_tiles <= 20 ? 256 : 4 * 256)) {
     const double alone = 2. * key_tiles + 13., parts = std::min(sqrt(40. * key_tiles / n), 256. / n);
     p.least = 4;

@@ -183,6 +183,10 @@ ATTN = [  # dtype, hd, hq, hkv, page, lens, rows
     ("f32", 128, 8, 2, 64, [0, 65, 700], [40, 3, 130]),
     ("f32", 128, 4, 1, 32, [1500], [1]),
     ("f32", 128, 7, 7, 96, [95, 10], [33, 9]),
+    ("bf16", 128, 8, 1, 32, [(37 * i) % 90 for i in range(70)], [(5 * i) % 21 for i in range(70)]),      # more sequences than lanes
+    ("f32", 64, 4, 1, 32, [(29 * i) % 70 for i in range(130)], [1 + i % 2 for i in range(130)]),
+    ("bf16", 64, 1, 1, 32, [10], [700]),                # bitsets of an item that take more than their place in LDS
+    ("f32", 64, 1, 1, 32, [0], [700]),
 ]
 
 
