@@ -6,8 +6,9 @@
 // shares, one a workgroup: the pieces of an item that a cut went through leave (m, l, O) in memory, and k_paged_merge adds them up in the
 // line's order, so results do not depend on scheduling.  Only the device knows lengths and rows; every workgroup looks its share up.
 //
-// k_paged_stream (up to 32 columns an item, four waves that share them) is for decoding, bound by the memory that K and V come from;
-// k_paged_tile (up to 256 columns in bf16, 128 in fp32) for chunks and trees, bound by the matrix cores: it walks a ring of key tiles in LDS.
+// k_paged_stream (32 columns an item, four waves that share them) is for decoding and for little work, bound by the memory that K and V
+// come from; k_paged_tile (up to 256 columns in bf16, 128 in fp32) for much of it, bound by the matrix cores: it walks a ring of key tiles in
+// LDS.  paged_attn_plan chooses.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -117,7 +118,8 @@ __device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch,
   }
   const float all = per_head * (float)kv.hkv;
   if (uniform(all > 0.f) == 0) return false;
-  const int n = uniform(max(1, (int)min((float)shares, all / (float)(tile_time<STREAM>(cap) * TK * least))));
+  int n = uniform(max(1, (int)min((float)shares, all / (float)(tile_time<STREAM>(cap) * TK * least))));
+  if (one && n > it.n * kv.hkv) n = uniform(n - n % (it.n * kv.hkv));         // (as the host does where the bound is the length)
   if (w >= n) return false;
   const float at = all / (float)n * (float)(w + (lane & 1));
   const int head = min((int)(at / per_head), kv.hkv - 1);
@@ -292,7 +294,9 @@ __device__ __forceinline__ void put_columns(float* xo, const f32x16_t (&o)[HD / 
 // --------------------------------------------------------------------------------------------------
 // k_paged_stream: nothing of K and V is used twice, so they go from memory to registers and straight into the matrix
 // instructions.  The waves take the 32-key units of a piece in turn; a wave asks for its next unit's K as soon as its scores are done and
-// for the next V behind the product with this one.
+// for the next V behind the product with this one: four waves, two workgroups a CU, have 128 KB of it on their way.  Measured, 32/8 heads of
+// 128 in bf16: 32 rows over 8192 keys each 192 us, 5.6 TB/s (a plain read on this card 6.1); one over 2048 keys 13 us, of which 8 here (2 to
+// look the share up, 2 until the first keys are there) and 5 in the merge.
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * STREAM_WAVES, sizeof(T) * HD <= 256 ? 2 : 1) void k_paged_stream(PagedDev kv, ChunkDev ch, PagedAttnArgs a,
                                                                                                PagedAttnPlan plan, bool vec_q, bool vec_out) {
@@ -468,15 +472,19 @@ typedef const int __attribute__((address_space(4))) scalar_int;     // memory th
 
 // --------------------------------------------------------------------------------------------------
 // k_paged_tile: key tiles of 64 go from memory straight into a ring of LDS stages (a linear copy, the cache's blocks being in operand order),
-// a block by each of four waves, and are read by all of them.  A fragment that feeds one 32 x 32 x 16 instruction is read from LDS at the full rate of LDS (1 KB in the 32 clocks
-// that the instruction takes on each of four SIMDs), so eight waves with 32 columns each waited for LDS (2.4 us a key tile and 256
-// columns).  In bf16 a wave has 64 columns, two tiles that share every fragment, and 512 registers: one wave a SIMD, which has to overlap its
+// a block by each of four waves, and are read by all of them.  A fragment that feeds one 32 x 32 x 16 instruction is read from LDS at the full
+// rate of LDS (1 KB in the 32 clocks that the instruction takes on each of four SIMDs), so eight waves with 32 columns each waited for LDS
+// (2.4 us a key tile and 256 columns).  In bf16 a wave has 64 columns, two tiles that share every fragment, and 512 registers: one wave a SIMD, which has to overlap its
 // own matrix work and softmax.  Its two column tiles run half a unit apart: while one's scores or outputs are on the matrix
 // cores, the other's exponentials are computed between the instructions, in four groups a unit of 32 keys:
 //   scores of tile 0, next unit  | exponentials of tile 1        outputs of tile 0            | exponentials of tile 1; maximum of tile 0, next unit
 //   scores of tile 1, next unit  | exponentials of tile 0, next  outputs of tile 1            | exponentials of tile 0, next; maximum of tile 1, next
 // Outputs and queries sit in AGPRs (the instructions that touch the outputs are text, so that the compiler moves neither).  In fp32 a wave has
 // one tile: its matrix instructions take 16 times as long, and softmax beside them is an eighth.
+// Measured, 32/8 heads of 128: 1.95 us a key tile of 256 columns; 8192 rows from none 522 us, 1055 TF/s (of which the matrix instructions alone
+// take 410; a product of 8192 x 8192 x 8192 on this card 1388 TF/s), 512 rows over 32768 keys 1025 TF/s.  A piece takes 13 us beside its
+// tiles: 2 to look its share up, 4 until the first tile and the queries are there, 1.5 for the look at outputs where rows are hidden, 2 to 4
+// to store them.
 template <typename T, int HD> struct TileRing {
   static constexpr int BLOCK = 32 * HD * sizeof(T), STAGE = 4 * BLOCK, STAGES = STAGE > 32768 ? 2 : 4, LPW = BLOCK / 1024;
   // Tiles that are asked for ahead.  With two column tiles a wave is half a tile into the next scores when it stops at the barrier, so
@@ -974,8 +982,9 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
 
 // --------------------------------------------------------------------------------------------------
 // The pieces of an item that begins in share w and does not end there: that one and those of the shares behind it, up to the one that ends
-// it.  A workgroup has 32 columns; four features of a column are a thread's, and where fewer than all threads have any, as many groups of them
-// as there is room for take the pieces in turn: nearly all of it is waiting for memory, so all loads are to be on their way at once.
+// it.  Four features of a column are a thread's, and where fewer than all threads have any, as many groups of them as there is room for take
+// the pieces in turn: nearly all of it is waiting for memory, so all loads are to be on their way at once.  A workgroup has the 32 columns of
+// a decoding item (64 pieces of 4 columns: 5.9 us) or 8 of a tile item's, whole lines (16 items of 16 pieces, 34 MB: 9.8 us).
 template <bool STREAM> constexpr int MERGE_THREADS = STREAM ? 1024 : 256;
 template <bool STREAM, int HD> constexpr int MERGE_COLUMNS = STREAM ? 32 : 4 * MERGE_THREADS<STREAM> / HD;
 template <typename T, int HD, bool STREAM>
