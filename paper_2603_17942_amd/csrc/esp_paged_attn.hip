@@ -86,12 +86,19 @@ __device__ __forceinline__ Weights weights_of(const ChunkSeq& s, int G, int per,
   return {(float)start_time<STREAM>() + t * (float)(s.len + (causal ? 0 : s.rows)), causal ? t * (float)(per * 32) / (float)G : 0.f};
 }
 
-// Where share w of `shares` begins and ends.  Order of the line: kv heads, sequences, column groups from the last.  The device may use fewer
+// Share of a workgroup if n of them have work: the ones next to each other on the line, which read the same keys, on one XCD; those that have
+// none behind them.
+__device__ __forceinline__ int share_at(int block, int n) {
+  const int per_xcd = (n + 7) >> 3;
+  return block >> 3 < per_xcd ? (block & 7) * per_xcd + (block >> 3) : block;
+}
+
+// Where a workgroup's share w of `shares` begins and ends.  Order of the line: kv heads, sequences, column groups from the last.  The device may use fewer
 // shares than were launched: none with less than `least` key tiles.  False: no such share.  Every wave finds out for itself: a lane a
 // sequence, 64 at a time, then even lanes for the beginning and odd ones for the end.
 template <bool STREAM>
-__device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch, int G, int cap, bool causal, int w, int shares, int least, Cut& lo,
-                                         Cut& hi) {
+__device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch, int G, int cap, bool causal, int block, int shares, int least, int& w,
+                                         Cut& lo, Cut& hi) {
   constexpr int TK = STREAM ? STREAM_TK : TILE_TK;
   const int lane = threadIdx.x & 63;
   const bool one = kv.batch == 1;                 // (then every lane holds that sequence)
@@ -117,9 +124,11 @@ __device__ __forceinline__ bool share_of(const PagedDev& kv, const ChunkDev& ch,
     per_head += one ? upto : __shfl(upto, 63, 64);
   }
   const float all = per_head * (float)kv.hkv;
+  w = block;
   if (uniform(all > 0.f) == 0) return false;
   int n = uniform(max(1, (int)min((float)shares, all / (float)(tile_time<STREAM>(cap) * TK * least))));
   if (one && n > it.n * kv.hkv) n = uniform(n - n % (it.n * kv.hkv));         // (as the host does where the bound is the length)
+  w = share_at(block, n);
   if (w >= n) return false;
   const float at = all / (float)n * (float)(w + (lane & 1));
   const int head = min((int)(at / per_head), kv.hkv - 1);
@@ -193,9 +202,6 @@ __device__ __forceinline__ Partials partials_of(float* base, int shares, int col
   return {(ShareNote*)base, base + (size_t)shares * sizeof(ShareNote) / 4, cols, hd};
 }
 
-// share of a workgroup: the ones next to each other on the line, which read the same keys, on one XCD
-__device__ __forceinline__ int share_at(int block, int shares) { return (block & 7) * ((shares + 7) >> 3) + (block >> 3); }
-
 // Walks the pieces of a workgroup: run(item, sequence, its items, first and last key tile, slot of the partial or -1 for a whole item).
 template <int NT, bool STREAM, typename RUN>
 __device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, const PagedAttnArgs& a, const PagedAttnPlan& plan, RUN run) {
@@ -219,9 +225,8 @@ __device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, con
     if (blockIdx.x == 0)
       for (int b = threadIdx.x; b < kv.batch; b += NT)
         if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(kv, ch, b));
-    w = share_at(blockIdx.x, shares);
+    if (!share_of<STREAM>(kv, ch, G, CAP, causal, blockIdx.x, shares, plan.least, w, lo, hi)) lo = Cut{{0, kv.hkv, 0}, 0};
     if (w >= shares) return;
-    if (!share_of<STREAM>(kv, ch, G, CAP, causal, w, shares, plan.least, lo, hi)) lo = Cut{{0, kv.hkv, 0}, 0};
   }
   ShareNote note{0, 0, 0, 0, ENDS, {0, 0, 0}};
   Place pl = lo.place;
@@ -993,9 +998,10 @@ __global__ __launch_bounds__(MERGE_THREADS<STREAM>) void k_paged_merge(PagedAttn
   __shared__ int slots[2 * MOST_SHARES];
   __shared__ __align__(16) f32x4_t part[NT];
   __shared__ float part_m[NT], part_l[NT];
-  // a share's workgroups where the share was, which spreads the items over the XCDs however many shares there are to one
-  const int of_share = cols / NC, w = share_at((blockIdx.x / (8 * of_share)) * 8 + (blockIdx.x & 7), shares);
-  const int c0 = (blockIdx.x >> 3) % of_share * NC, tid = threadIdx.x, lane = tid & 63;
+  // The items that began in shares are often a multiple of 8 shares apart: a tile item's workgroups go to all XCDs, decoding items' are spread
+  // over the XCDs as the shares are.  (All on one XCD: 43 us for 9.8.)
+  const int of_share = cols / NC, w = STREAM ? share_at(blockIdx.x, shares) : blockIdx.x / of_share;
+  const int c0 = STREAM ? 0 : blockIdx.x % of_share * NC, tid = threadIdx.x, lane = tid & 63;
   if (w >= shares) return;
   const Partials p = partials_of(a.partials, shares, cols, HD);
   const ShareNote note = p.notes[w];
@@ -1092,7 +1098,7 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((k_paged_tile<T, HD>), g, dim3(64 * TILE_WAVES), bytes, st, kv, ch, a, p, vec_q, vec_out);
     if (p.shares)
-      hipLaunchKernelGGL((k_paged_merge<T, HD, false>), dim3(((p.shares + 7) & ~7) * (32 * p.cap / MERGE_COLUMNS<false, HD>)),
+      hipLaunchKernelGGL((k_paged_merge<T, HD, false>), dim3(p.shares * (32 * p.cap / MERGE_COLUMNS<false, HD>)),
                          dim3(MERGE_THREADS<false>), 0, st, a, kv.hkv, p.shares, 32 * p.cap, vec_out);
   }
   return hipGetLastError();
