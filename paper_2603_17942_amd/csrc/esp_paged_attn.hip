@@ -1110,7 +1110,8 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
 // Stream or tile kernel: the stream kernel begins and ends sooner (7 against 13) and has the work in pieces of 32 columns for every place, but
 // reads every key again for each 32 columns, at best from its XCD's 4 MB of L2.  128 rows over 2048 / 8000 keys: 19 / 42 against 28 / 43;
 // 320 rows over 2048 / 8000: 31 / 78 against 39 / 70; 2048 rows from none: 64 against 72; 2000 in fp32: 332 against 299; 4 x 100 rows over
-// 4000, whose keys are too much for L2: 85 against 58; 32 x 40 over 1000: 115 against 48.
+// 4000, whose keys are too much for L2: 85 against 58; 32 x 40 over 1000: 115 against 48.  Two column tiles each of more pairs than CUs: 64 x 16
+// rows over 200 / 500 / 1000 / 2000: 28 / 48 / 88 / 190 against 35 / 46 / 63 / 122; of fewer, 16 x 16 over 2000: 26 against 30.
 // Stream kernel, shares or an item a workgroup: an item alone takes 7 and 0.57 for 128 keys (64 KB: a CU takes in 110 GB/s, and more waves on
 // an item do not change that); shares with their merge 13.5 and what K and V take.  One row over 1000 / 4000 keys: 11.2 / 25.7 alone,
 // 12.9 / 17.5 in shares; 32 sequences of 2000 / 4000: 45 / 97, 53 / 105 (but alone a batch takes as long as its longest sequence, so a longer
@@ -1129,7 +1130,7 @@ PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int
   };
   const int64_t kv_bytes = ceil_div((int64_t)batch * hkv, 8) * keys * hd * (dtype == ESP_F32 ? 8 : 4);     // of an XCD's sequences and heads
   const int64_t work = items(1) * (len_bound + max_rows / 2) * hd * (dtype == ESP_F32 ? 4 : 2);
-  const bool small = work <= (int64_t)1 << 29 && (tiles <= 2 || kv_bytes <= 5 << 20);
+  const bool small = work <= (int64_t)1 << 29 && (kv_bytes <= 5 << 20 || (tiles <= 2 && (items(1) <= 256 || keys <= 700)));
   p.cap = tiles == 1 || small ? 1 : dtype == ESP_F32 ? TILE_CAP<float> : TILE_CAP<bf16_t>;
   while (p.cap > 2 && p.cap / 2 >= tiles && items(p.cap) < 256) p.cap /= 2;
   const int64_t n = items(p.cap), key_tiles = ceil_div(keys, p.cap == 1 ? STREAM_TK : TILE_TK);
