@@ -615,8 +615,18 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
     // ancestor bitsets of the item's rows in LDS, where they fit
     const int row_lo = col0 / G, n_rows = (min(ncols, col0 + ct * 32) - 1) / G - row_lo + 1;
     const bool anc_here = !causal && (int64_t)n_rows * a.anc_words <= TILE_ANC;
-    if (anc_here)
-      for (int i = opaque(tid); i < n_rows * a.anc_words; i += 64 * TILE_WAVES) anc_lds[i] = a.anc[(size_t)(s.row0 + row_lo) * a.anc_words + i];
+    if (anc_here) {
+      const uint64_t* from = a.anc + (size_t)(s.row0 + row_lo) * a.anc_words;
+      const int words = n_rows * a.anc_words;
+      for (int i = opaque(tid); i < words; i += 4 * 64 * TILE_WAVES) {                       // (four on their way)
+        uint64_t w[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) w[x] = from[min(i + x * 64 * TILE_WAVES, words - 1)];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (i + x * 64 * TILE_WAVES < words) anc_lds[i + x * 64 * TILE_WAVES] = w[x];
+      }
+    }
     auto window_of = [&](int c, int c_lo) {
       const int row = opaque(r[c]);               // (of a dead column: the first)
       if (causal) return attn_low_bits(row + 1 - c_lo);
