@@ -431,7 +431,8 @@ typedef struct {
 
 /* What only the device can see -- len[b] negative, above len_bound or with its rows past the table, row0 or pages out of
  * range -- sets bits in *status.  Of a sequence with bad lengths or rows nothing is read or written; a slot in
- * a page outside the pool is not written (append, commit), and not seen (attention). */
+ * a page outside the pool is not written (append, commit), and not seen (attention).  Where row0 descends, a row may be among those of
+ * several sequences that are each in order: which of them get it, and whose output it holds, is not defined. */
 
 /* Writes K and V of the chunk's rows into their slots of `layer`, K normed and rotated on the way, and the rows' queries,
  * normed and rotated, to q_out [total_rows][n_q_heads][head_dim] (rows q_out_stride elements apart).  rope NULL: no rotation.

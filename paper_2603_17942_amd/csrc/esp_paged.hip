@@ -49,14 +49,20 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
   }
 }
 
-// the sequence that row m belongs to, by the whole wave: the last that begins at or before it; -1 if none holds it
-__device__ __forceinline__ int find_seq(const ChunkDev& ch, int batch, int m, int lane) {
-  int n = 0;
-  for (int b = 0; b < batch; b += 64) {
-    const bool before = b + lane < batch && ch.row0[b + lane] <= m;
-    n += __popcll(__builtin_amdgcn_ballot_w64(before));
+// The sequence that holds row m, by the whole wave: the first that is in order and has it among its rows; -1: none.  (Asked of every sequence, since
+// where row0 descends the one that begins last before a row need not hold it.)
+__device__ __forceinline__ int find_seq(const PagedDev& kv, const ChunkDev& ch, int m, int lane, ChunkSeq& s) {
+  for (int b0 = 0; b0 < kv.batch; b0 += 64) {
+    const int b = b0 + lane;
+    const ChunkSeq x = chunk_seq(kv, ch, min(b, kv.batch - 1));
+    const uint64_t holds = __builtin_amdgcn_ballot_w64(b < kv.batch && x.ok && m >= x.row0 && m - x.row0 < x.rows);
+    if (holds) {
+      const int l = __builtin_ctzll(holds);
+      s = ChunkSeq{__builtin_amdgcn_readlane(x.row0, l), __builtin_amdgcn_readlane(x.rows, l), __builtin_amdgcn_readlane(x.len, l), true};
+      return b0 + l;
+    }
   }
-  return n - 1;
+  return -1;
 }
 
 // Sixteen features of a head in two pieces of eight, one thread: of a part that turns the pieces hold its pairs, so a thread
@@ -120,18 +126,16 @@ __device__ __forceinline__ void rope_rows(const RopeRows& a, const PagedDev& kv,
     int page = -1, slot = 0, pos = 0;
     if (m < a.rows) {
       if (PAGED) {
-        const int seq = find_seq(ch, kv.batch, m, lane);
+        ChunkSeq s;
+        const int seq = find_seq(kv, ch, m, lane, s);
         if (seq >= 0) {
-          const ChunkSeq s = chunk_seq(kv, ch, seq);
-          if (s.ok && m - s.row0 < s.rows) {
-            slot = s.len + (m - s.row0);
-            pos = slot;
-            page = kv.table[(size_t)seq * kv.stride + slot / kv.page_size];
-            slot %= kv.page_size;
-            if ((unsigned)page >= (unsigned)kv.n_pages) {
-              if (lane == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
-              page = -2;                                  // the query is there, the slot is not
-            }
+          slot = s.len + (m - s.row0);
+          pos = slot;
+          page = kv.table[(size_t)seq * kv.stride + slot / kv.page_size];
+          slot %= kv.page_size;
+          if ((unsigned)page >= (unsigned)kv.n_pages) {
+            if (lane == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+            page = -2;                                    // the query is there, the slot is not
           }
         }
       } else {

@@ -654,6 +654,38 @@ def test_append_skips_what_is_malformed(rows):
             assert torch.equal(before[:, pages].view(torch.int16), c.kv.k[:, pages].view(torch.int16))
 
 
+@pytest.mark.parametrize("scale", [1, 10])              # by rows, by blocks of slots
+@pytest.mark.parametrize("starts", [[50, 60, 0, 10, 20], [4, 40, 2, 6, 6], [20, 20, 60, 5, 15], [30, -1, 0, 30, 59]])
+def test_append_of_starts_that_descend(starts, scale):
+    """Rows go to the sequence that holds them, whatever stands in front of it; nothing else in the pool changes."""
+    starts = [scale * s for s in starts]
+    n, most, lens, hkv, hd = max(starts), 40 * scale, [45, 3, 0, 70], 2, 128
+    c = Cache(torch.bfloat16, hkv, hd, 32, lens, [most] * 4, 215, rows_too=False)
+    x = torch.randn((n, 4 + 2 * hkv, hd), generator=gen(216)).to(torch.bfloat16).cuda()
+    q_out = torch.full((n, 4, hd), 9.0, dtype=torch.bfloat16, device="cuda")
+    before = [t.cpu().float().numpy() for t in (c.kv.k, c.kv.v)]
+    B.paged_append(c.kv, 0, B.ChunkRows(i32(starts), n, most), x[:, :4], x[:, 4:4 + hkv], x[:, 4 + hkv:], q_out=q_out)
+    assert c.kv.device_status() == 8
+    held = np.zeros(n, dtype=int)
+    whole = [b for b in range(4) if 0 <= starts[b] <= starts[b + 1] <= starts[b] + most]
+    for b in whole:
+        held[starts[b]:starts[b + 1]] += 1
+    h = torch.from_numpy(held > 0).cuda()
+    assert torch.equal(q_out[h], x[h, :4]) and (q_out[~h] == 9.0).all()
+    after, xs, d = [t.cpu().float().numpy() for t in (c.kv.k, c.kv.v)], x.cpu().float().numpy(), np.arange(hd)
+    touched = [np.zeros(t.shape, dtype=bool) for t in before]
+    for b in whole:
+        for m in range(starts[b], starts[b + 1]):
+            s = lens[b] + m - starts[b]
+            if held[m] == 1:
+                k, v = c.plain(after[0], after[1], b, s)
+                assert (k == xs[m, 4:4 + hkv]).all() and (v == xs[m, 4 + hkv:]).all(), (b, m)
+            for t, place in zip(touched, (k_place, v_place)):
+                t[0, int(c.table[b, s // 32])].reshape(hkv, -1)[:, place(s % 32, d, hd)] = True
+    for t, a, m in zip(before, after, touched):
+        assert ((t == a) | (np.isnan(t) & np.isnan(a)) | m).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows", [3, 300])
 def test_append_at_any_alignment(dtype, rows):
