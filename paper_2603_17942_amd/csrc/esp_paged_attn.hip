@@ -669,19 +669,27 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
         load_pieces<0, R::LPW>(source(), (uint32_t)lane * 16, stage_of(i));
         advance();
       };
-      // The last tile of the sequence: V of keys past its end as zeros (memory there may hold anything).  Safe: infinities and NaN out.
-      const int clean_from = (safe ? s.len : total) / TILE_TK - t0;
+      // The last tile of the sequence: V of keys past its end as zeros (memory there may hold anything), and so V of blocks whose page is not
+      // there (page 0 stands in for it).  Safe: infinities and NaN out of all tiles with rows of the chunk.
+      const int odd_from = s.len / TILE_TK - t0;
+      int clean_from = 0;                         // (set when it is known whether all pages are there)
       auto clean = [&](int i) {
         if (i < clean_from) return;
         const int left = total - (t0 + i) * TILE_TK;
-        const bool tail = left < TILE_TK, odd = safe;
+        const bool odd = safe && i >= odd_from;
+        auto left_of = [&](int b) {               // keys of block b of the tile that are there
+          if (any_bad && (unsigned)table[min(2 * (t0 + i) + b, last_block) / blocks] >= (unsigned)kv.n_pages) return 0;
+          return left - 32 * b;
+        };
+        const int left0 = left_of(0), left1 = left_of(1);
         unsigned char* v = lds + (i % R::STAGES) * R::STAGE + 2 * R::BLOCK;
         constexpr int PIECE = 8 * sizeof(T), IN = R::BLOCK / PIECE;
         for (int x = opaque(tid); x < 2 * IN; x += 64 * TILE_WAVES) {          // piece x: block, fragment (db, u), lane
           const int in_block = x % IN, u = (in_block >> 6) & 1;
           frag_t f = *reinterpret_cast<const frag_t*>(v + x * PIECE);
-          if (tail) f = attn_zero_tail(f, u, in_block & 63, left - (x >= IN ? 32 : 0));
-          if (odd) attn_take_odd(f);              // (safe: of all tiles with rows of the chunk)
+          const int here = x >= IN ? left1 : left0;
+          if (here < 32) f = attn_zero_tail(f, u, in_block & 63, here);
+          if (odd) attn_take_odd(f);
           *reinterpret_cast<frag_t*>(v + x * PIECE) = f;
         }
         __syncthreads();
@@ -716,6 +724,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
       // tile 0 is here for everybody (this wave's loads retire in order, the barrier covers the others')
       wait_tiles_but<R::LPW>(min(R::AHEAD - 1, nt - 1));
       any_bad = any_thread<TILE_WAVES>(bad, said[0]);                          // (with its barrier)
+      clean_from = any_bad ? 0 : (safe ? s.len : total) / TILE_TK - t0;
       clean(0);
       // Tile i + 1 is here, and all are done with tile i (with two column tiles: i - 1), whose stage takes the next that is asked for.
       auto next_tile = [&](int i) {

@@ -1,0 +1,109 @@
+"""Attention over pages where the tile kernel has the work: whole items and shares, one sequence and many, what nobody sees holding no numbers.
+
+References and tolerances are those of test_gpu_paged.py; of long chunks some rows are compared.  Every case says what it is planned as, so that a
+rule that moves it to another kernel fails here."""
+import ctypes as C
+import functools
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_paged import DT, Cache, attention, gen, k_place, pack_anc, queries, random_tree, v_place, visible
+from util import internal
+
+from paper_2603_17942_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+class Plan(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("cap", "q_tiles", "shares", "least")]
+
+
+@functools.lru_cache(None)
+def plans():
+    return internal("paged_attn_plan", *[C.c_int] * 8, restype=Plan)
+
+
+MANY = [(37 * i) % 1001 for i in range(64)], [(i * 5) % 17 for i in range(64)]                       # 0 to 1000 keys, 0 to 16 rows
+BATCH = [(311 * i) % 2001 for i in range(40)], [1 + (i * 7) % 16 for i in range(40)]
+
+# dtype, hd, hq, hkv, page, lens, rows, column tiles of an item at most, in shares
+TILE = {
+    "prompt_bf16_128": ("bf16", 128, 32, 8, 64, [0], [2304], 8, False),
+    "prompt_bf16_64": ("bf16", 64, 64, 16, 32, [0], [2311], 8, False),
+    "prompt_f32_128": ("f32", 128, 32, 8, 64, [0], [2100], 4, False),
+    "prompt_f32_64": ("f32", 64, 32, 16, 96, [100], [2100], 4, False),
+    "many_bf16_128": ("bf16", 128, 32, 8, 32, *MANY, 8, False),
+    "many_bf16_64": ("bf16", 64, 32, 8, 64, *MANY, 8, False),
+    "many_f32_128": ("f32", 128, 32, 8, 32, *MANY, 4, False),
+    "chunk_bf16_128": ("bf16", 128, 32, 8, 64, [9000], [300], 8, True),
+    "chunk_bf16_64": ("bf16", 64, 32, 8, 128, [21001], [333], 8, True),
+    "chunk_f32_128": ("f32", 128, 4, 1, 32, [6000], [200], 4, True),
+    "batch_bf16_128": ("bf16", 128, 32, 8, 64, *BATCH, 8, True),
+    "batch_f32_64": ("f32", 64, 32, 8, 32, *BATCH, 4, True),
+}
+
+
+def make(name, seed, **kw):
+    dtype, hd, hq, hkv, page, lens, rows, cap, shares = TILE[name]
+    c = Cache(DT[dtype], hkv, hd, page, lens, rows, seed, **kw)
+    p = plans()(c.kv.struct.dtype, hd, len(lens), hq, hkv, c.chunk.total_rows, c.chunk.max_rows, c.kv.len_bound)
+    assert (p.cap, p.shares > 0) == (cap, shares), (p.cap, p.shares)
+    return c, queries(c.starts[-1], hq, hd, DT[dtype], seed + 1)
+
+
+def some_rows(r, b):
+    """Of r rows up to 16, the ends among them."""
+    return list(range(r)) if r <= 16 else sorted({0, 1, 31, 32, 33, r - 2, r - 1} | set(np.random.default_rng(b).integers(0, r, 9).tolist()))
+
+
+def check(c, q, out, seen_of):
+    """seen_of(b): [rows, keys] of sequence b, what its rows see."""
+    out = out.cpu().double()
+    for b, (l, r) in enumerate(zip(c.lens, c.rows)):
+        if r == 0:
+            continue
+        pick = torch.tensor(some_rows(r, b))
+        at = c.starts[b] + pick
+        want, tol = attention(q.cpu()[at], c.k[b], c.v[b], seen_of(b)[pick], c.hd ** -0.5)
+        assert torch.isfinite(out[at]).all(), b
+        worst = ((out[at] - want).abs() - tol).max()
+        assert worst <= 0, (b, float(worst))
+    assert torch.isfinite(out).all()
+
+
+def clear_page_0(c):
+    """What is in page 0 moves to a page that is free, and page 0, nobody's then, holds no numbers."""
+    free = next(p for p in range(c.kv.k.shape[1] - 1, 0, -1) if not (c.table == p).any())
+    for pool in (c.kv.k, c.kv.v):
+        pool[:, free] = pool[:, 0]
+        pool[:, 0] = math.nan
+    c.table[c.table == 0] = free
+    c.kv.page_table.copy_(c.table)
+
+
+@pytest.mark.parametrize("name", TILE)
+@pytest.mark.parametrize("tree", [False, True])
+def test_missing_pages_beside_a_page_that_is_not_finite(name, tree):
+    """The slots of pages outside the pool are not seen, whatever the pool's own pages hold."""
+    c, q = make(name, 501)
+    clear_page_0(c)
+    missing = {b: [p for p in (0, 2, (l - 1) // c.page - 1) if 0 <= p < l // c.page] for b, l in enumerate(c.lens) if b % 3 == 0}
+    if len(c.lens) == 1 and c.lens[0] == 0:
+        missing = {0: [0, 2]}
+    for b, pages in missing.items():
+        for i, p in enumerate(pages):
+            c.kv.page_table[b, p] = (-1, 10 ** 6)[i % 2]
+    ancs = [random_tree(r, 510 + b) for b, r in enumerate(c.rows)] if tree else None
+    out = B.paged_attn(c.kv, 0, c.chunk, q, anc=pack_anc(ancs, c.rows, (max(c.rows) + 63) // 64) if tree else None)
+
+    def seen(b):
+        m = visible(c.lens[b], c.rows[b], ancs[b] if tree else None)
+        for p in missing.get(b, []):
+            m[:, p * c.page:(p + 1) * c.page] = False
+        return m
+    check(c, q, out, seen)
+    assert c.kv.device_status() == 16
