@@ -640,7 +640,8 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
 
     const int last_block = (min(keys, t1 * TILE_TK) - 1) >> 5;
     bool any_bad = false;
-    const bool hides = (int64_t)t1 * TILE_TK > s.len && s.rows > 1;           // some key of the piece may be hidden from some column
+    // some key of the piece may be hidden from some column (from a single row only by its own bit)
+    const bool hides = (int64_t)t1 * TILE_TK > s.len && (s.rows > 1 || !causal);
 
     frag_t qf[NT][NS];
     f32x16_t o[NT][DB];

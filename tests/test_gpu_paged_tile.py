@@ -107,3 +107,32 @@ def test_missing_pages_beside_a_page_that_is_not_finite(name, tree):
         return m
     check(c, q, out, seen)
     assert c.kv.device_status() == 16
+
+
+@pytest.mark.parametrize("name", ["many_bf16_128", "many_bf16_64", "many_f32_128", "batch_bf16_128", "batch_f32_64"])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_one_row_that_does_not_see_itself(name, what):
+    """A sequence's only row, hidden from itself, whose K and V are no numbers: zeros where there is nothing before it, else attention to that."""
+    dtype, hd, hq, hkv, page, lens, rows, cap, shares = TILE[name]
+    lens, rows = list(lens), list(rows)
+    for b in range(0, len(rows), 2):
+        rows[b] = 1
+    lens[2] = lens[6] = 0
+    c = Cache(DT[dtype], hkv, hd, page, lens, rows, 521)
+    p = plans()(c.kv.struct.dtype, hd, len(lens), hq, hkv, c.chunk.total_rows, c.chunk.max_rows, c.kv.len_bound)
+    assert (p.cap, p.shares > 0) == (cap, shares)
+    q = queries(c.starts[-1], hq, hd, DT[dtype], 522)
+    d = np.arange(hd)
+    ancs = [random_tree(r, 530 + b) for b, r in enumerate(rows)]
+    for b, r in enumerate(rows):
+        if r != 1:
+            continue
+        ancs[b][0, 0] = False
+        pg, inside = int(c.table[b, lens[b] // page]), lens[b] % page
+        for pool, place in ((c.kv.k, k_place), (c.kv.v, v_place)):
+            pool[0, pg].view(hkv, -1)[:, torch.from_numpy(place(inside, d, hd)).cuda()] = what
+    out = B.paged_attn(c.kv, 0, c.chunk, q, anc=pack_anc(ancs, rows, 1))
+    check(c, q, out, lambda b: visible(lens[b], rows[b], ancs[b]))
+    for b in (2, 6):
+        assert (out[c.starts[b]] == 0).all()
+    assert c.kv.device_status() == 0
