@@ -449,7 +449,8 @@ esp_status esp_paged_append(void *stream, const esp_paged_kv *kv, int32_t layer,
  * [0, len[b]) and, of the chunk, rows 0..r (anc NULL) or the rows c whose bit is set in its ancestor bitset anc
  * [total_rows][anc_words] (as esp_block).  out = softmax(scale q k) v; a row that sees nothing gets zeros.  What a row does
  * not see does not reach it, whatever it holds.  q as in esp_paged_append; out device [total_rows][n_q_heads][head_dim],
- * contiguous, no overlap with q.  A value that is not finite makes the output of the rows that see it not finite.
+ * contiguous, no overlap with q.  An infinity in V makes the output of the rows that see it that infinity, or NaN where its probability
+ * rounds to nothing; NaN in V, and infinities of both signs, make it NaN.
  * scratch: device, 16-byte aligned, esp_paged_attn_scratch_bytes() bytes (0: it may be NULL), which depend on the host's values
  * alone, len_bound among them; calls that overlap in time need one each.  Results do not depend on what it held.
  * Errors: EINVAL (null pointers, scale below 1e-20 or not finite, ...), ESHAPE (n_q_heads not a multiple of n_kv_heads, anc_words * 64

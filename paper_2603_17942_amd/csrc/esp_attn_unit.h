@@ -137,6 +137,25 @@ __device__ __forceinline__ f32x8_t attn_take_odd(f32x8_t& f) {
   }
   return ones;
 }
+// what is in a fragment's places: infinities 1, negative ones 64, NaN 4096, anything else 0, so that up to 63 of each can be told from their sum
+__device__ __forceinline__ float attn_odd_mark(unsigned f32_bits) {
+  if ((f32_bits & 0x7f800000u) != 0x7f800000u) return 0.f;
+  return f32_bits & 0x007fffffu ? 4096.f : f32_bits >> 31 ? 64.f : 1.f;
+}
+__device__ __forceinline__ bf16x8_t attn_odd_marks(bf16x8_t f) {
+  u32x4_t w = __builtin_bit_cast(u32x4_t, f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {                    // (1, 64 and 4096 are bf16 numbers)
+    const unsigned lo = __float_as_uint(attn_odd_mark(w[i] << 16)), hi = __float_as_uint(attn_odd_mark(w[i] & 0xffff0000u));
+    w[i] = lo >> 16 | hi;
+  }
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+__device__ __forceinline__ f32x8_t attn_odd_marks(f32x8_t f) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = attn_odd_mark(__float_as_uint(f[i]));
+  return f;
+}
 __device__ __forceinline__ bool attn_any(bf16x8_t f) {
   const u32x4_t w = __builtin_bit_cast(u32x4_t, f);
   return (w[0] | w[1] | w[2] | w[3]) != 0;
@@ -167,7 +186,8 @@ __device__ __forceinline__ bf16x8_t attn_zero_tail(bf16x8_t f, int u, int lane, 
 
 // In a unit some of whose keys not every column sees, infinities and NaN among the values would reach the columns that do not see them, as 0
 // times them.  So they are taken out there, and where that took any out (odd) the columns that do see them get theirs when all else is
-// done: this adds an infinity for each to the outputs.  v: the unit's fragments in memory; seen: bits of this lane's keys.
+// done: this adds what they see to the outputs, an infinity of its sign, or NaN for a NaN and for infinities of both signs.  v: the unit's
+// fragments in memory; seen: bits of this lane's keys.
 template <typename T, int HD>
 __device__ __forceinline__ void attn_add_odd(const T* v, unsigned seen, int left, int lane, f32x16_t (&o)[HD / 32]) {
   typedef typename AttnFrag<T>::type frag_t;
@@ -181,11 +201,15 @@ __device__ __forceinline__ void attn_add_odd(const T* v, unsigned seen, int left
     for (int i = 0; i < 16; ++i) n[i] = 0.f;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      frag_t f = attn_zero_tail(*reinterpret_cast<const frag_t*>(v + (2 * db + u) * 512 + lane * 8), u, lane, left);
-      n = attn_mma(attn_take_odd(f), s[u], n);
+      const frag_t f = attn_zero_tail(*reinterpret_cast<const frag_t*>(v + (2 * db + u) * 512 + lane * 8), u, lane, left);
+      n = attn_mma(attn_odd_marks(f), s[u], n);
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) o[db][i] += n[i] > 0.f ? __builtin_inff() : 0.f;
+    for (int i = 0; i < 16; ++i) {
+      const int marks = (int)n[i];                 // (32 keys: 32 of a kind at most)
+      const bool up = marks & 63, down = marks >> 6 & 63;
+      if (marks) o[db][i] += marks >> 12 || (up && down) ? __builtin_nanf("") : up ? __builtin_inff() : -__builtin_inff();
+    }
   }
 }
 

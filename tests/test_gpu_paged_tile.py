@@ -56,8 +56,8 @@ def make(name, seed, **kw):
 
 
 def some_rows(r, b):
-    """Of r rows up to 16, the ends among them."""
-    return list(range(r)) if r <= 16 else sorted({0, 1, 31, 32, 33, r - 2, r - 1} | set(np.random.default_rng(b).integers(0, r, 9).tolist()))
+    """Of many rows 16 at most, the ends among them."""
+    return list(range(r)) if r <= 40 else sorted({0, 1, 31, 32, 33, r - 2, r - 1} | set(np.random.default_rng(b).integers(0, r, 9).tolist()))
 
 
 def check(c, q, out, seen_of):
@@ -136,3 +136,51 @@ def test_one_row_that_does_not_see_itself(name, what):
     for b in (2, 6):
         assert (out[c.starts[b]] == 0).all()
     assert c.kv.device_status() == 0
+
+
+SIGNS = dict(TILE, **{      # and of the stream kernel, alone and in shares
+    "stream_bf16_128": ("bf16", 128, 8, 2, 32, [50, 7], [40, 9], 1, False),
+    "stream_bf16_64": ("bf16", 64, 8, 2, 32, [4000, 7], [1, 9], 1, True),
+    "stream_f32_128": ("f32", 128, 8, 2, 64, [40, 90], [33, 5], 1, False),
+    "stream_f32_64": ("f32", 64, 8, 2, 32, [2500, 1], [12, 3], 1, True),
+})
+
+
+@pytest.mark.parametrize("name", SIGNS)
+@pytest.mark.parametrize("tree", [False, True])
+def test_infinities_keep_their_sign(name, tree):
+    """Infinities among the values a row sees make its output that infinity, NaN and infinities of both signs make it NaN, in committed slots and in
+    the chunk's own; who does not see them has its own output.  (The scores are of size 1.5, so no probability comes to nothing.)"""
+    dtype, hd, hq, hkv, page, lens, rows, cap, shares = SIGNS[name]
+    c = Cache(DT[dtype], hkv, hd, page, lens, rows, 541)
+    p = plans()(c.kv.struct.dtype, hd, len(lens), hq, hkv, c.chunk.total_rows, c.chunk.max_rows, c.kv.len_bound)
+    assert (p.cap, p.shares > 0) == (cap, shares)
+    q = queries(c.starts[-1], hq, hd, DT[dtype], 542)
+    kvh, inf, nan = hkv - 1, math.inf, math.nan
+    for b, (l, r) in enumerate(zip(lens, rows)):
+        slots = [s for s, there in ((l // 2, l > 0), (l + r // 3, r > 0), (l + r // 2, r > 3), (l + r - 1, r > 5)) if there]
+        for i, s in enumerate(slots):
+            for d, what in ((1, -inf), (2, inf), (3 if i % 2 else hd - 1, -inf), (4, inf if i else -inf), (5, -inf if i else inf), (6, nan if i == 1 else -inf),
+                            (40, -inf if i == 2 else 0.5), (41, inf if i == 2 else -0.5)):
+                c.v[b][s, kvh, d] = what
+                pg, inside = int(c.table[b, s // page]), s % page
+                c.kv.v[0, pg].view(hkv, -1)[kvh, v_place(inside, d, hd)] = what
+    ancs = [random_tree(r, 550 + b) for b, r in enumerate(rows)] if tree else None
+    out = B.paged_attn(c.kv, 0, c.chunk, q, anc=pack_anc(ancs, rows, (max(rows) + 63) // 64) if tree else None).cpu().double()
+    hit = 0
+    for b, (l, r) in enumerate(zip(lens, rows)):
+        if r == 0:
+            continue
+        pick = torch.tensor(some_rows(r, b))
+        at, seen = c.starts[b] + pick, visible(l, r, ancs[b] if tree else None)[pick]
+        v = c.v[b].double()
+        want, tol = attention(q.cpu()[at], c.k[b], torch.where(torch.isfinite(v), v, 0.0).to(c.dt), seen, hd ** -0.5)
+        s = seen.double()
+        up, down, none = (torch.einsum("rt,thd->rhd", s, m.double()) > 0 for m in (v == inf, v == -inf, v.isnan()))
+        odd = torch.where(none | (up & down), nan, torch.where(up, inf, torch.where(down, -inf, 0.0))).repeat_interleave(hq // hkv, 1)
+        got = out[at]
+        same = (got == odd) | (got.isnan() & odd.isnan())
+        fine = (got - want).abs() <= tol
+        assert torch.where(odd == 0, fine, same).all(), b
+        hit += int((odd != 0).sum())
+    assert hit > 0
