@@ -286,7 +286,7 @@ __global__ __launch_bounds__(256) void k_append_blocks(RopeRows a, PagedDev kv, 
   for (int t = tid; t < HEADS * HD * 4; t += 256) {           // 16-byte pieces of V's block
     const int hv = t / (HD * 4), at = t % (HD * 4), frag = at >> 6, l = at & 63, d = (frag >> 1) * 32 + (l & 31), key0 = (frag & 1) * 16 + 4 * (l >> 5);
     if (kvh0 + hv >= a.hkv) continue;
-    T* dst = (T*)kv.v + page_plane(page, kvh0 + hv, kv.hkv, kv.page_size, HD) + (inside >> 5) * (32 * HD) + at * 8;
+    T* dst = (T*)kv.v + page_plane(page, kvh0 + hv, kv.hkv, kv.page_size, HD) + (size_t)(inside >> 5) * (32 * HD) + at * 8;
     piece_t p;
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[e] = vt[hv][key0 + (e & 3) + 8 * (e >> 2)][d];

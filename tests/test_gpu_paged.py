@@ -686,6 +686,38 @@ def test_append_of_starts_that_descend(starts, scale):
         assert ((t == a) | (np.isnan(t) & np.isnan(a)) | m).all()
 
 
+@pytest.mark.parametrize("rows", [3, 300])
+def test_pages_whose_offsets_pass_31_bits(rows):
+    """A page of 2^24 + 320 slots of 128: its elements number more than 2^31, and so do its bytes and blocks' places in bytes."""
+    hd, page = 128, 2 ** 24 + 320
+    lens = page - 320 - rows // 2
+    kv = B.PagedKv.zeros(1, 1, 1, page, hd, 1, 1, torch.bfloat16)
+    kv.lens.fill_(lens)
+    kv.len_bound = lens
+    x = torch.randn((rows, 3, hd), generator=gen(217)).to(torch.bfloat16).cuda()
+    ch = B.ChunkRows(i32([0, rows]), rows, rows)
+    q = B.paged_append(kv, 0, ch, x[:, :1], x[:, 1:2], x[:, 2:])
+    k, v = B.paged_load(kv, 0, 0, lens, rows)
+    assert torch.equal(k, x[:, 1:2]) and torch.equal(v, x[:, 2:])
+    for pool, n in ((kv.k, x[:, 1:2]), (kv.v, x[:, 2:])):                 # nothing else was written
+        assert sum(int(part.count_nonzero()) for part in pool.view(-1).split(2 ** 28)) == int(n.count_nonzero())
+    out = B.paged_attn(kv, 0, ch, q).cpu().double()
+    # all committed keys are zeros: they have weight e^0 each, and add nothing
+    s = torch.einsum("rhd,thd->rt", x[:, :1].cpu().double(), x[:, 1:2].cpu().double()) * hd ** -0.5
+    p = torch.tril(s.exp())
+    want = (p @ x[:, 2].cpu().double()) / (lens + p.sum(1, keepdim=True))
+    weight = (p @ x[:, 2].cpu().double().abs()) / (lens + p.sum(1, keepdim=True))
+    # p is off by half a step of bf16 and little else (2^-7 for all of it); the ones add up exactly as far as 2^24, and behind that 600 parts
+    # at most are added at half a step of fp32 each, which is below 2^-14
+    assert ((out[:, 0] - want).abs() <= 2.0 ** -8 * want.abs() + weight * (2.0 ** -7 + 2.0 ** -14)).all()
+    assert kv.device_status() == 0
+    kv.lens.fill_(lens - 5)                                              # and a move: row 4 to the second place
+    kv.len_bound = lens
+    B.paged_commit(kv, i32([2]), i32([[0, 6] + [0] * 7]))
+    k, v = B.paged_load(kv, 0, 0, lens - 4, 1)
+    assert torch.equal(k[0], x[1, 1:2]) and torch.equal(v[0], x[1, 2:]) and kv.lens.item() == lens - 3 and kv.device_status() == 0
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows", [3, 300])
 def test_append_at_any_alignment(dtype, rows):
