@@ -397,7 +397,7 @@ esp_status esp_rope_make(int32_t head_dim, int32_t rot_dim, int32_t interleaved,
  * positions device [rows].  Either of q and k may be NULL with its output (its head count is then not looked at).  The
  * arithmetic is fp32 (the angle fp64), rounded once.
  * Errors: EINVAL (null pointers, rows < 0, n_* < 1, eps negative or not finite), ESHAPE (strides below heads * head_dim), EDTYPE,
- * ECAPACITY (more than 2^31 - 1 rows x heads). */
+ * ECAPACITY (more than 2^26 - 4 rows, or than 2^31 - 1 rows x heads, or 2^22 - 1 heads). */
 esp_status esp_rope_qk(void *stream, int32_t dtype, const esp_rope *rope, int32_t rows, int32_t n_q_heads, int32_t n_kv_heads,
                        const void *q, int64_t q_stride, const void *k, int64_t k_stride, const int32_t *positions,
                        const void *q_gain, const void *k_gain, float eps, void *q_out, int64_t q_out_stride, void *k_out,
@@ -438,7 +438,7 @@ typedef struct {
  * normed and rotated, to q_out [total_rows][n_q_heads][head_dim] (rows q_out_stride elements apart).  rope NULL: no rotation.
  * positions device [total_rows], or NULL: a row's position is its slot (a tree's rows have len + depth).  q and q_out may
  * both be NULL, and q_out may be q with the same stride.  len is not advanced.
- * Errors: as esp_rope_qk; EINVAL also for a malformed esp_paged_kv or esp_chunk or a layer outside it; ESHAPE for head_dim other than the
+ * Errors: as esp_rope_qk (heads of q, k and v); EINVAL also for a malformed esp_paged_kv or esp_chunk or a layer outside it; ESHAPE for head_dim other than the
  * rope's. */
 esp_status esp_paged_append(void *stream, const esp_paged_kv *kv, int32_t layer, const esp_chunk *rows, const esp_rope *rope,
                             const int32_t *positions, int32_t n_q_heads, const void *q, int64_t q_stride, const void *k,
@@ -454,7 +454,7 @@ esp_status esp_paged_append(void *stream, const esp_paged_kv *kv, int32_t layer,
  * scratch: device, 16-byte aligned, esp_paged_attn_scratch_bytes() bytes (0: it may be NULL), which depend on the host's values
  * alone, len_bound among them; calls that overlap in time need one each.  Results do not depend on what it held.
  * Errors: EINVAL (null pointers, scale below 1e-20 or not finite, ...), ESHAPE (n_q_heads not a multiple of n_kv_heads, anc_words * 64
- * < max_rows, q_stride), EDTYPE, ECAPACITY (scratch). */
+ * < max_rows, q_stride), EDTYPE, ECAPACITY (scratch; more work than a launch can have, 2^24 workgroups). */
 size_t esp_paged_attn_scratch_bytes(const esp_paged_kv *kv, const esp_chunk *rows, int32_t n_q_heads);
 esp_status esp_paged_attn(void *stream, const esp_paged_kv *kv, int32_t layer, const esp_chunk *rows, int32_t n_q_heads,
                           const void *q, int64_t q_stride, float scale, const uint64_t *anc, int32_t anc_words, void *out,

@@ -37,6 +37,9 @@ __host__ __device__ __forceinline__ size_t page_plane(int page, int kvh, int hkv
   return ((size_t)page * hkv + kvh) * page_size * hd;
 }
 
+// workgroups of 256 threads that a launch can have: threads are counted in 32 bits
+constexpr int64_t MOST_WORKGROUPS = (1 << 24) - 1;
+
 struct RopeRows {             // what the row kernels are told
   const void *q, *k, *v;
   int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
@@ -62,6 +65,7 @@ struct PagedAttnPlan {
   int least = 1;              // key tiles of a share at least
 };
 PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int len_bound);
+int64_t paged_attn_workgroups(const PagedAttnPlan& p, int batch, int hkv);
 size_t paged_attn_partial_floats(const PagedAttnPlan& p, int hd);
 struct PagedAttnArgs {
   const void* q;

@@ -1,5 +1,7 @@
 // Rotary positions with head norms, the append into a paged KV cache, the move of accepted rows, and the way back to
 // plain rows.  The attention over the pages is in esp_paged_attn.hip.
+#include <algorithm>
+
 #include "esp_paged.h"
 
 namespace {
@@ -425,12 +427,11 @@ hipError_t launch_rows(hipStream_t st, const RopeRows& a, const PagedDev& kv, co
 
 template <typename T, int HD>
 hipError_t launch_append(hipStream_t st, const RopeRows& a, const PagedDev& kv, const ChunkDev& ch) {
-  // by rows / by blocks, 32/8 heads of 128 in bf16, us: 64 rows 5.3 / 7.0, 320 7.5 / 7.3, 32 x 8 7.0 / 7.6, 32 x 16 9.0 / 7.6, 8192 61 / 40
-  if (a.rows < 256 || a.rows < 16 * kv.batch) return launch_rows<T, HD, true>(st, a, kv, ch);
-  const bool vec = rows_aligned<T>(a, true);
   const int r = a.rows >= 1024 ? 4 : 1, head_groups = (a.hkv + BLOCK_HEADS<T, HD> - 1) / BLOCK_HEADS<T, HD>;
-  const int64_t block_groups = ((int64_t)a.rows / 32 + 2 * kv.batch) * head_groups, grid = block_groups + (a.hq ? (a.rows + r - 1) / r : 0);
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t block_groups = ((int64_t)a.rows / 32 + 2 * (int64_t)kv.batch) * head_groups, grid = block_groups + (a.hq ? (a.rows + r - 1) / r : 0);
+  // by rows / by blocks, 32/8 heads of 128 in bf16, us: 64 rows 5.3 / 7.0, 320 7.5 / 7.3, 32 x 8 7.0 / 7.6, 32 x 16 9.0 / 7.6, 8192 61 / 40
+  if (a.rows < 256 || a.rows < 16 * kv.batch || grid > MOST_WORKGROUPS) return launch_rows<T, HD, true>(st, a, kv, ch);
+  const bool vec = rows_aligned<T>(a, true);
 #define ESP_APPEND(V_, R_) \
   hipLaunchKernelGGL((k_append_blocks<T, HD, V_, R_>), dim3((unsigned)grid), dim3(256), 0, st, a, kv, ch, (int)block_groups, head_groups)
   if (r == 4) { if (vec) ESP_APPEND(true, 4); else ESP_APPEND(false, 4); }
@@ -447,9 +448,16 @@ hipError_t launch_commit(hipStream_t st, const PagedDev& kv, int layers, const i
   return hipGetLastError();
 }
 template <typename T, int HD>
-hipError_t launch_load(hipStream_t st, const PagedDev& kv, int seq, int first_slot, size_t n, void* k_rows, void* v_rows) {
-  hipLaunchKernelGGL((k_paged_load<T, HD>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, kv, seq, first_slot, n, (T*)k_rows, (T*)v_rows);
-  return hipGetLastError();
+hipError_t launch_load(hipStream_t st, const PagedDev& kv, int seq, int first_slot, int n_slots, void* k_rows, void* v_rows) {
+  const int64_t row = (int64_t)kv.hkv * HD, at_once = 256 * MOST_WORKGROUPS / row;
+  for (int64_t done = 0; done < n_slots; done += at_once) {
+    const size_t n = (size_t)(std::min(at_once, n_slots - done) * row);
+    hipLaunchKernelGGL((k_paged_load<T, HD>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, kv, seq, first_slot + (int)done, n,
+                       (T*)k_rows + done * row, (T*)v_rows + done * row);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
@@ -478,9 +486,7 @@ hipError_t launch_paged_commit(hipStream_t st, int dtype, int hd, const PagedDev
 
 hipError_t launch_paged_load(hipStream_t st, int dtype, int hd, const PagedDev& kv, int seq, int first_slot, int n_slots, void* k_rows,
                              void* v_rows) {
-  const size_t n = (size_t)n_slots * kv.hkv * hd;
-  if (n == 0) return hipSuccess;
-#define ESP_CALL(T_, HD_) (launch_load<T_, HD_>(st, kv, seq, first_slot, n, k_rows, v_rows))
+#define ESP_CALL(T_, HD_) (launch_load<T_, HD_>(st, kv, seq, first_slot, n_slots, k_rows, v_rows))
   return ESP_BY_TYPE(ESP_CALL);
 #undef ESP_CALL
 }

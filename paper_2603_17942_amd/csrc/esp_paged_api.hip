@@ -25,7 +25,7 @@ esp_status check_paged(const esp_paged_kv* kv) {
   // places are counted in blocks of 32 slots, and slots of a sequence, in 31 bits
   if ((int64_t)kv->n_pages * kv->n_kv_heads > INT32_MAX / (kv->page_size / 32)) return ESP_ECAPACITY;
   if ((int64_t)kv->table_stride * kv->page_size > INT32_MAX) return ESP_ECAPACITY;
-  if (kv->n_layers > 65535 || kv->batch > 65535 || (int64_t)kv->n_layers * kv->n_kv_heads > INT32_MAX) return ESP_ECAPACITY;
+  if (kv->n_layers > 65535 || kv->batch > 65535 || (int64_t)kv->n_layers * kv->n_kv_heads > MOST_WORKGROUPS) return ESP_ECAPACITY;
   return ESP_OK;
 }
 esp_status check_chunk(const esp_paged_kv* kv, const esp_chunk* c) {
@@ -38,6 +38,8 @@ PagedDev to_dev(const esp_paged_kv* kv, int layer) {
   return {(char*)kv->k + off, (char*)kv->v + off, kv->page_table, kv->len, kv->status, kv->n_kv_heads, kv->page_size, kv->n_pages,
           kv->batch, kv->table_stride, kv->len_bound};
 }
+// four rows a workgroup; pieces and elements of four rows are counted in 31 bits
+bool too_many(int64_t heads, int64_t rows) { return rows > 4 * MOST_WORKGROUPS || heads * std::max<int64_t>(rows, 512) > INT32_MAX; }
 bool bad_eps(float eps) { return !(eps >= 0.f) || !std::isfinite(eps); }
 // (may be null: no rotation)
 esp_status check_rope(const esp_rope* r) {
@@ -89,7 +91,7 @@ esp_status esp_rope_qk(void* stream, int32_t dtype, const esp_rope* rope, int32_
   if (q && (q_stride < (int64_t)n_q * hd || q_out_stride < (int64_t)n_q * hd)) return ESP_ESHAPE;
   if (k && (k_stride < (int64_t)n_kv * hd || k_out_stride < (int64_t)n_kv * hd)) return ESP_ESHAPE;
   if ((q == q_out && q && q_stride != q_out_stride) || (k == k_out && k && k_stride != k_out_stride)) return ESP_EINVAL;
-  if (((int64_t)(q ? n_q : 0) + (k ? n_kv : 0)) * std::max(rows, 4) > INT32_MAX / 8) return ESP_ECAPACITY;
+  if (too_many((int64_t)(q ? n_q : 0) + (k ? n_kv : 0), rows)) return ESP_ECAPACITY;
   if (rows == 0) return ESP_OK;
   RopeRows a{};
   a.q = q; a.k = k; a.q_stride = q_stride; a.k_stride = k_stride; a.q_out = q_out; a.k_out = k_out;
@@ -116,7 +118,7 @@ esp_status esp_paged_append(void* stream, const esp_paged_kv* kv, int32_t layer,
   if (q && (q_stride < (int64_t)n_q * hd || q_out_stride < (int64_t)n_q * hd)) return ESP_ESHAPE;
   if (k_stride < (int64_t)hkv * hd || v_stride < (int64_t)hkv * hd) return ESP_ESHAPE;
   if (q && q == q_out && q_stride != q_out_stride) return ESP_EINVAL;
-  if (((int64_t)(q ? n_q : 0) + 2 * (int64_t)hkv) * std::max(rows->total_rows, 4) > INT32_MAX / 8) return ESP_ECAPACITY;
+  if (too_many((int64_t)(q ? n_q : 0) + 2 * (int64_t)hkv, rows->total_rows)) return ESP_ECAPACITY;
   if (rows->total_rows == 0 || rows->max_rows == 0) return ESP_OK;
   RopeRows a{};
   a.q = q; a.k = k; a.v = v; a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
@@ -149,6 +151,7 @@ esp_status esp_paged_attn(void* stream, const esp_paged_kv* kv, int32_t layer, c
   if ((int64_t)rows->max_rows * (n_q / kv->n_kv_heads) > INT32_MAX / 2) return ESP_ECAPACITY;
   if (rows->total_rows == 0 || rows->max_rows == 0) return ESP_OK;
   const PagedAttnPlan p = paged_attn_plan(kv->dtype, kv->head_dim, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, kv->len_bound);
+  if (paged_attn_workgroups(p, kv->batch, kv->n_kv_heads) > MOST_WORKGROUPS) return ESP_ECAPACITY;
   const size_t need = paged_attn_partial_floats(p, kv->head_dim) * 4;
   if (need && (!scratch || scratch_bytes < need)) return ESP_ECAPACITY;
   if (need && (uintptr_t)scratch % 16) return ESP_EINVAL;
@@ -171,7 +174,6 @@ esp_status esp_paged_load(void* stream, const esp_paged_kv* kv, int32_t layer, i
   if (st != ESP_OK) return st;
   if (layer < 0 || layer >= kv->n_layers || seq < 0 || seq >= kv->batch || first_slot < 0 || n_slots < 0 || !k_rows || !v_rows) return ESP_EINVAL;
   if ((int64_t)first_slot + n_slots > (int64_t)kv->table_stride * kv->page_size) return ESP_ECAPACITY;
-  if ((int64_t)n_slots * kv->n_kv_heads * kv->head_dim > (int64_t)INT32_MAX * 256) return ESP_ECAPACITY;
   ESP_HIP(launch_paged_load((hipStream_t)stream, kv->dtype, kv->head_dim, to_dev(kv, layer), seq, first_slot, n_slots, k_rows, v_rows));
   return ESP_OK;
 }

@@ -1101,13 +1101,7 @@ hipError_t allow_lds(unsigned bytes) {
 template <typename T, int HD>
 hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const PagedAttnArgs& a, const PagedAttnPlan& p) {
   const bool vec_q = (uintptr_t)a.q % 16 == 0 && a.q_stride * (int64_t)sizeof(T) % 16 == 0, vec_out = (uintptr_t)a.out % 16 == 0;
-  int64_t grid = (p.shares + 7) / 8 * 8;
-  if (p.shares == 0) {
-    const int64_t groups = (int64_t)kv.batch * kv.hkv;
-    grid = (p.q_tiles > 1 && groups >= 8 ? (groups + 7) & ~7ll : groups) * p.q_tiles;
-  }
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
-  const dim3 g((unsigned)grid);
+  const dim3 g((unsigned)paged_attn_workgroups(p, kv.batch, kv.hkv));
   if (p.cap == 1) {
     hipLaunchKernelGGL((k_paged_stream<T, HD>), g, dim3(64 * STREAM_WAVES), 0, st, kv, ch, a, p, vec_q, vec_out);
     if (p.shares)
@@ -1170,6 +1164,11 @@ PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int
     else if (parts >= 2. && 2. * key_tiles / parts + 0.05 * n * parts + 21. < alone) p.shares = (int)(n * std::floor(parts));
   }
   return p;
+}
+int64_t paged_attn_workgroups(const PagedAttnPlan& p, int batch, int hkv) {
+  if (p.shares) return (p.shares + 7) / 8 * 8;
+  const int64_t groups = (int64_t)batch * hkv;
+  return (p.q_tiles > 1 && groups >= 8 ? (groups + 7) & ~7ll : groups) * p.q_tiles;
 }
 size_t paged_attn_partial_floats(const PagedAttnPlan& p, int hd) {
   return p.shares ? notes_floats(p.shares) + 2 * p.shares * slot_floats(32 * p.cap, hd) : 0;

@@ -740,6 +740,24 @@ def test_load_gives_back_what_is_in_the_slots():
             assert torch.equal(k.cpu(), c.k[b][first:first + n]) and torch.equal(v.cpu(), c.v[b][first:first + n])
 
 
+def test_load_of_more_elements_than_a_launch_has_threads():
+    """4.2 million slots of 8 heads of 128, 2^32 elements and some."""
+    hkv, hd, page, n = 8, 128, 1024, 2 ** 22 + 1024
+    kv = B.PagedKv.zeros(1, n // page, hkv, page, hd, 1, n // page, torch.bfloat16)
+    kv.page_table.copy_(torch.arange(n // page, dtype=torch.int32).flip(0)[None])
+    x = torch.randn((5, 3 * hkv, hd), generator=gen(218)).to(torch.bfloat16).cuda()
+    for at in (0, n // 2, n - 5):
+        kv.lens.fill_(at)
+        kv.len_bound = at
+        B.paged_append(kv, 0, B.ChunkRows(i32([0, 5]), 5, 5), None, x[:, hkv:2 * hkv], x[:, 2 * hkv:])
+    k, v = B.paged_load(kv, 0, 0, 0, n)
+    for got, part in ((k, x[:, hkv:2 * hkv]), (v, x[:, 2 * hkv:])):
+        for at in (0, n // 2, n - 5):
+            assert torch.equal(got[at:at + 5], part)
+        assert sum(int(p.count_nonzero()) for p in got.view(-1).split(2 ** 28)) == 3 * int(part.count_nonzero())
+    assert kv.device_status() == 0
+
+
 # ---- commit --------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,hd,page", [("bf16", 128, 64), ("bf16", 64, 32), ("f32", 128, 32), ("f32", 64, 96)])

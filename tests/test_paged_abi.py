@@ -117,6 +117,23 @@ def test_commit_and_load_refusals(lib):
     assert lib.esp_paged_load(None, kv, 0, 0, 50 * 64, 0, P, P) == 0
 
 
+def test_more_than_a_launch_can_have_is_refused(lib):
+    """A launch counts threads in 32 bits: 2^24 - 1 workgroups of 256."""
+    (_, r), many = rope(), 2 ** 26 - 3                                              # four rows a workgroup
+
+    def qk(rows, nq=1):
+        return lib.esp_rope_qk(None, B.ESP_BF16, C.byref(r), rows, nq, 0, P, nq * 128, None, 0, P, None, None, 1e-6, P, nq * 128, None, 0)
+    assert qk(many) == ECAPACITY and qk(2 ** 24, 128) == ECAPACITY and qk(1, 2 ** 22) == ECAPACITY
+    kv = paged(n_kv_heads=1)
+    assert lib.esp_paged_append(None, C.byref(kv), 0, C.byref(chunk(total_rows=many)), None, None, 0, None, 0, P, 128, P, 128, None, None, 1e-6, None,
+                                0) == ECAPACITY
+    kv = paged(batch=65535, len_bound=0)                                             # 65535 x 8 items of a sequence and kv head, 64 each
+    ch = chunk(total_rows=2 ** 28, max_rows=4096)
+    assert lib.esp_paged_attn_scratch_bytes(C.byref(kv), C.byref(ch), 32) == 0
+    assert lib.esp_paged_attn(None, C.byref(kv), 0, C.byref(ch), 32, P, 4096, 0.1, None, 0, P, P, 1 << 30) == ECAPACITY
+    assert lib.esp_paged_commit(None, C.byref(paged(n_layers=40000, n_kv_heads=512)), P, P, P) == ECAPACITY
+
+
 def test_rope_make_refusals():
     for kw, code in ((dict(head_dim=80), ESHAPE), (dict(rot_dim=8), ESHAPE), (dict(rot_dim=130), ESHAPE), (dict(rot_dim=144), ESHAPE), (dict(theta=0.0), EINVAL),
                      (dict(theta=math.inf), EINVAL), (dict(factor=0.0), EINVAL), (dict(factor=math.nan), EINVAL), (dict(orig_len=-1), EINVAL),
