@@ -207,8 +207,8 @@ __device__ __forceinline__ void attn_add_odd(const T* v, unsigned seen, int left
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int marks = (int)n[i];                 // (32 keys: 32 of a kind at most)
-      const bool up = marks & 63, down = marks >> 6 & 63;
-      if (marks) o[db][i] += marks >> 12 || (up && down) ? __builtin_nanf("") : up ? __builtin_inff() : -__builtin_inff();
+      const float up = marks & 63 ? __builtin_inff() : 0.f, down = marks & 63 << 6 ? __builtin_inff() : 0.f, none = marks >> 12 ? __builtin_nanf("") : 0.f;
+      o[db][i] += up - down + none;                // (infinity less infinity is NaN)
     }
   }
 }
