@@ -386,7 +386,7 @@ typedef struct {
  * factor): what turns often keeps its speed, what turns seldom is slowed down.  orig_len 0: all are slowed down
  * (positions divided by factor).
  * Errors: EINVAL (out null, theta or factor not positive and finite, orig_len < 0, low_turns >= high_turns with orig_len > 0,
- * amplitude not finite), ESHAPE (head_dim, rot_dim). */
+ * amplitude not finite, or a speed that comes out of them), ESHAPE (head_dim, rot_dim); *out is then as it was. */
 esp_status esp_rope_make(int32_t head_dim, int32_t rot_dim, int32_t interleaved, double theta, double factor,
                          int32_t orig_len, double low_turns, double high_turns, double amplitude, esp_rope *out);
 

@@ -67,15 +67,17 @@ esp_status esp_rope_make(int32_t head_dim, int32_t rot_dim, int32_t interleaved,
   if (rot_dim < 16 || rot_dim > head_dim || rot_dim % 16) return ESP_ESHAPE;
   if (!(theta > 0) || !std::isfinite(theta) || !(factor > 0) || !std::isfinite(factor) || orig_len < 0 || !std::isfinite((float)amplitude))
     return ESP_EINVAL;
-  if (orig_len > 0 && !(std::isfinite(low_turns) && std::isfinite(high_turns) && low_turns < high_turns)) return ESP_EINVAL;
+  if (orig_len > 0 && !(std::isfinite(low_turns) && std::isfinite(high_turns - low_turns) && low_turns < high_turns)) return ESP_EINVAL;
   const double two_pi = 6.283185307179586476925286766559;
-  *out = esp_rope{};
-  out->head_dim = head_dim; out->rot_dim = rot_dim; out->interleaved = interleaved != 0; out->amplitude = (float)amplitude;
+  esp_rope r{};
+  r.head_dim = head_dim; r.rot_dim = rot_dim; r.interleaved = interleaved != 0; r.amplitude = (float)amplitude;
   for (int i = 0; i < rot_dim / 2; ++i) {
     const double f = std::pow(theta, -2.0 * i / rot_dim) / two_pi;
     const double keep = orig_len > 0 ? std::min(1.0, std::max(0.0, (orig_len * f - low_turns) / (high_turns - low_turns))) : 0.0;
-    out->turns[i] = f * (keep + (1.0 - keep) / factor);
+    r.turns[i] = f * (keep + (1.0 - keep) / factor);
+    if (!std::isfinite(r.turns[i])) return ESP_EINVAL;
   }
+  *out = r;
   return ESP_OK;
 }
 

@@ -142,6 +142,15 @@ def test_rope_make_refusals():
     assert B.load_library().esp_rope_make(128, 128, 0, 1e4, 1.0, 0, 1.0, 32.0, 1.0, None) == EINVAL
 
 
+def test_rope_make_refuses_what_gives_no_speeds():
+    """theta and factor finite, but not the speeds that they make; nothing is written then."""
+    for kw in (dict(theta=5e-324), dict(theta=1e-300, factor=1e-20), dict(factor=1e-320), dict(factor=1e-310, orig_len=4096, low=1.0, high=4.0),
+               dict(orig_len=4096, low=-1e308, high=1e308), dict(theta=5e-324, orig_len=4096)):
+        code, r = rope(**kw)
+        assert code == EINVAL and r.head_dim == 0 and not any(r.turns), kw
+    assert rope(theta=1e-300)[0] == 0 and rope(factor=1e-300)[0] == 0 and rope(theta=1e300)[0] == 0
+
+
 @pytest.mark.parametrize("rot", [16, 64, 96, 128])
 @pytest.mark.parametrize("factor,orig", [(1.0, 0), (4.0, 0), (8.0, 8192), (0.5, 4096)])
 def test_rope_make_frequencies(rot, factor, orig):
