@@ -617,11 +617,21 @@ def rope_qk(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: tor
     return q_out, k_out
 
 
-class PagedKv:
+class _Addresses:
+    """Objects whose tensors' addresses the library holds: an attribute is set once.  Another tensor in its place would not be seen, and the first
+    would be freed under the library's hands."""
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__:
+            raise AttributeError(f"{type(self).__name__}.{name}: copy into the tensor, or make a new {type(self).__name__}")
+        object.__setattr__(self, name, value)
+
+
+class PagedKv(_Addresses):
     """A paged KV cache over the caller's tensors: k and v [n_layers, n_pages, n_kv_heads, page_size, head_dim] (contiguous; the
     slots of a page in the library's block order, so only paged_append writes and paged_load reads them), page_table
-    [batch, pages of a sequence] and lens [batch] int32.  len_bound: upper bound of lens, which the caller advances.  status: one
-    int32 that collects DEV_ bits."""
+    [batch, pages of a sequence] and lens [batch] int32, all of which are the caller's to change in place (len_bound is the one attribute that can
+    be set).  len_bound: upper bound of lens, which the caller advances.  status: one int32 that collects DEV_ bits."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, len_bound: int,
                  status: Optional[torch.Tensor] = None):
@@ -662,7 +672,7 @@ class PagedKv:
         return v
 
 
-class ChunkRows:
+class ChunkRows(_Addresses):
     """New rows of a batch, packed: sequence b has rows row0[b] .. row0[b + 1] - 1.  row0 [batch + 1] int32 on the device; total_rows:
     rows of the buffers, max_rows: upper bound of one sequence's."""
 

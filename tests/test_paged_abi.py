@@ -221,3 +221,19 @@ def test_python_checks_of_tensors():
         B.rope_qk(x, None, torch.zeros(2, dtype=torch.int32), B.rope_spec(64))
     with pytest.raises(B.EspError):
         B.rope_spec(64, rot_dim=20)
+
+
+def test_tensors_whose_addresses_are_held_cannot_be_replaced():
+    k = torch.zeros((1, 4, 2, 32, 64))
+    table, lens = torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    kv, rows = B.PagedKv(k, k.clone(), table, lens, 0), B.ChunkRows(torch.tensor([0, 2], dtype=torch.int32), 2, 2)
+    for name in ("k", "v", "page_table", "lens", "status", "dtype", "struct"):
+        with pytest.raises(AttributeError):
+            setattr(kv, name, getattr(kv, name).clone() if torch.is_tensor(getattr(kv, name)) else None)
+    for name, value in (("row0", rows.row0.clone()), ("total_rows", 3), ("max_rows", 1)):
+        with pytest.raises(AttributeError):
+            setattr(rows, name, value)
+    kv.len_bound = 40                     # the one that may be set, and what is changed in place is seen
+    kv.lens[0] = 33
+    assert kv.struct.len_bound == 40 and C.cast(kv.struct.len, C.POINTER(C.c_int32))[0] == 33
+    assert kv.struct.len == lens.data_ptr() and rows.struct.row0 == rows.row0.data_ptr()
