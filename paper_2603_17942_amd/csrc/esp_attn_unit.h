@@ -46,7 +46,7 @@ __device__ __forceinline__ float attn_max_of_halves(float v) {
 }
 
 // Online softmax of a unit's scores: p = 2^(scale s - scale m) with m the running maximum, followed lazily (the sums hold 2^24 times the
-// largest probability without loss), the probabilities as operand fragments (bf16: rounded to it, 2^-9 of a probability each way, as the
+// largest probability without loss), the probabilities as operand fragments (bf16: rounded to it, 2^-8 of a probability at most, as the
 // matrix product takes them; the sum l is of the unrounded ones).  seen: bits of this lane's keys, at 8 (v / 4) + v % 4.
 template <typename T, int DB>
 __device__ __forceinline__ void attn_softmax(f32x16_t& sc, bool masked, unsigned seen, float scale, f32x16_t (&o)[DB], float& m, float& l,
@@ -213,15 +213,15 @@ __device__ __forceinline__ void attn_add_odd(const T* v, unsigned seen, int left
   }
 }
 
-// One unit out of LDS.  k, v: this lane's share of the unit's first K and first V fragment, fragments FRAG bytes apart, of V (db, u) at
+// One unit out of LDS, in fp32.  k, v: this lane's share of the unit's first K and first V fragment, fragments FRAG bytes apart, of V (db, u) at
 // 2 db + u.  seen: bits of this lane's keys, looked at where `masked`.
-// Fragments are read PF matrix steps ahead and held there (left to itself the compiler reads them all and runs out of registers); the matrix
+// Fragments are read a matrix step ahead and held there (left to itself the compiler reads them all and runs out of registers); the matrix
 // phases run at raised wave priority, so that of the waves of a SIMD one has matrix work and the others fill in with their softmax.
-template <typename T, int HD>
+template <int HD>
 __device__ __forceinline__ void attn_unit(const unsigned char* k, const unsigned char* v, bool masked, unsigned seen, float scale,
-                                          const typename AttnFrag<T>::type (&q)[HD / 16], f32x16_t (&o)[HD / 32], float& m, float& l) {
-  typedef typename AttnFrag<T>::type frag_t;
-  constexpr int NS = HD / 16, DB = HD / 32, FRAG = 512 * sizeof(T), PF = sizeof(T) == 2 ? 3 : 1, NF = PF + 1;
+                                          const f32x8_t (&q)[HD / 16], f32x16_t (&o)[HD / 32], float& m, float& l) {
+  typedef f32x8_t frag_t;
+  constexpr int NS = HD / 16, DB = HD / 32, FRAG = 512 * sizeof(float), PF = 1, NF = PF + 1;
   frag_t fr[NF];
   // fragment j: K steps 0 .. NS - 1, then V in the order (u, db)
   auto frag_at = [&](int j) {
@@ -243,7 +243,7 @@ __device__ __forceinline__ void attn_unit(const unsigned char* k, const unsigned
   }
   __builtin_amdgcn_s_setprio(0);
   frag_t p[2];
-  attn_softmax<T, DB>(sc, masked, seen, scale, o, m, l, p);
+  attn_softmax<float, DB>(sc, masked, seen, scale, o, m, l, p);
   __builtin_amdgcn_s_setprio(2);
 #pragma unroll
   for (int i = 0; i < 2 * DB; ++i) {              // i = u DB + db

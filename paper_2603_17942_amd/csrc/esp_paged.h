@@ -15,19 +15,20 @@ struct ChunkDev {
 };
 // a sequence's rows and length; ok: they fit each other, the buffers and the table
 struct ChunkSeq { int row0, rows, len; bool ok; };
+__device__ __forceinline__ bool chunk_rows_ok(const ChunkDev& ch, int a, int b) {
+  const int64_t rows = (int64_t)b - a;
+  return (a >= 0) & (rows >= 0) & (rows <= ch.max_rows) & (b <= ch.total);
+}
 __device__ __forceinline__ ChunkSeq chunk_seq(const PagedDev& kv, const ChunkDev& ch, int seq) {
   const int a = ch.row0[seq], b = ch.row0[seq + 1], len = kv.len[seq];
   const int64_t rows = (int64_t)b - a;
-  const bool rows_ok = (a >= 0) & (rows >= 0) & (rows <= ch.max_rows) & (b <= ch.total);
+  const bool rows_ok = chunk_rows_ok(ch, a, b);
   const bool len_ok = (len >= 0) & (len <= kv.len_bound) & ((int64_t)len + rows <= (int64_t)kv.stride * kv.page_size);
   return {a, (int)rows, len, rows_ok && len_ok};
 }
 // the bits that belong to a sequence that is not ok
-__device__ __forceinline__ int chunk_fault(const PagedDev& kv, const ChunkDev& ch, int seq) {
-  const int a = ch.row0[seq], b = ch.row0[seq + 1];
-  const int64_t rows = (int64_t)b - a;
-  const bool rows_ok = (a >= 0) & (rows >= 0) & (rows <= ch.max_rows) & (b <= ch.total);
-  return rows_ok ? ESP_DEV_LEN_OVER_BOUND : ESP_DEV_BAD_ROWS;
+__device__ __forceinline__ int chunk_fault(const ChunkDev& ch, int seq) {
+  return chunk_rows_ok(ch, ch.row0[seq], ch.row0[seq + 1]) ? ESP_DEV_LEN_OVER_BOUND : ESP_DEV_BAD_ROWS;
 }
 __device__ __forceinline__ void set_status(int32_t* status, int bits) {
   if (status) atomicOr(status, bits);

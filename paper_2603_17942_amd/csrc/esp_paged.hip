@@ -154,7 +154,7 @@ __device__ __forceinline__ void rope_rows(const RopeRows& a, const PagedDev& kv,
   }
   if (PAGED && block == 0)
     for (int b = tid; b < kv.batch; b += 256)
-      if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(kv, ch, b));
+      if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(ch, b));
   __syncthreads();
   const int heads = a.hq + (PAGED ? 2 : 1) * hkv, per_row = heads * LPH;
   for (int t = tid; t < R * per_row; t += 256) {
@@ -208,10 +208,10 @@ __global__ __launch_bounds__(256) void k_rope_rows(RopeRows a, PagedDev kv, Chun
 // The same for chunks of many rows: K and V go by blocks of the cache, a workgroup takes 32 slots and HEADS kv heads and writes
 // whole 128-byte lines, V turned from rows to columns through LDS; the queries go by rows, in the workgroups behind these.  (By rows
 // a V row is HD stores of one element.)  Four chunks of 700 to 2048 rows: 66 us by rows, 31 by blocks, 4.7 TB/s.
-template <typename T, int HD> constexpr int BLOCK_HEADS = 128 / HD;
+template <int HD> constexpr int BLOCK_HEADS = 128 / HD;
 template <typename T, int HD, bool VEC, int R>
 __global__ __launch_bounds__(256) void k_append_blocks(RopeRows a, PagedDev kv, ChunkDev ch, int block_groups, int head_groups) {
-  constexpr int LPH = HD / 16, HEADS = BLOCK_HEADS<T, HD>;
+  constexpr int LPH = HD / 16, HEADS = BLOCK_HEADS<HD>;
   typedef T piece_t __attribute__((ext_vector_type(8)));
   if ((int)blockIdx.x >= block_groups) {
     rope_rows<T, HD, true, VEC, R>(a, kv, ch, 0, blockIdx.x - block_groups);
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(256) void k_append_blocks(RopeRows a, PagedDev kv, 
   const int x = blockIdx.x / head_groups;
   if (blockIdx.x == 0 && a.hq == 0)
     for (int b = tid; b < kv.batch; b += 256)
-      if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(kv, ch, b));
+      if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(ch, b));
   int seq = -1, block = 0;
   for (int b0 = 0, base = 0; b0 < kv.batch && seq < 0; b0 += 64) {
     const ChunkSeq s = chunk_seq(kv, ch, min(b0 + lane, kv.batch - 1));
@@ -427,7 +427,7 @@ hipError_t launch_rows(hipStream_t st, const RopeRows& a, const PagedDev& kv, co
 
 template <typename T, int HD>
 hipError_t launch_append(hipStream_t st, const RopeRows& a, const PagedDev& kv, const ChunkDev& ch) {
-  const int r = a.rows >= 1024 ? 4 : 1, head_groups = (a.hkv + BLOCK_HEADS<T, HD> - 1) / BLOCK_HEADS<T, HD>;
+  const int r = a.rows >= 1024 ? 4 : 1, head_groups = (a.hkv + BLOCK_HEADS<HD> - 1) / BLOCK_HEADS<HD>;
   const int64_t block_groups = ((int64_t)a.rows / 32 + 2 * (int64_t)kv.batch) * head_groups, grid = block_groups + (a.hq ? (a.rows + r - 1) / r : 0);
   // by rows / by blocks, 32/8 heads of 128 in bf16, us: 64 rows 5.3 / 7.0, 320 7.5 / 7.3, 32 x 8 7.0 / 7.6, 32 x 16 9.0 / 7.6, 8192 61 / 40
   if (a.rows < 256 || a.rows < 16 * kv.batch || grid > MOST_WORKGROUPS) return launch_rows<T, HD, true>(st, a, kv, ch);

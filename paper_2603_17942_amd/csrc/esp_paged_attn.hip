@@ -29,7 +29,7 @@ template <typename T> constexpr int TILE_CAP = TILE_WAVES * TILE_NT<T>;         
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 // a value that the compiler does not see through: what is computed from it stays where it is used.  (Addresses that it takes out of a loop
 // cost registers over all of it, and a register that it saves to memory it has restored in front of the end of a branch, with the
-// branch's lanes only.  The kernels here are to have none that are saved.)
+// branch's lanes only.  The kernels here are to save no vector register; scalar ones, up to 171 of a kernel, are kept in lanes of vector registers.)
 __device__ __forceinline__ int opaque(int x) {
   asm volatile("" : "+v"(x));
   return x;
@@ -220,11 +220,11 @@ __device__ __forceinline__ void walk(const PagedDev& kv, const ChunkDev& ch, con
     lo = Cut{{g / kv.hkv, g % kv.hkv, q_tiles - 1 - (int)(blockIdx.x / step)}, 0};
     hi = Cut{lo.place, INT32_MAX};
     if (lo.place.kvh == 0 && lo.place.at == 0 && threadIdx.x == 0 && !chunk_seq(kv, ch, lo.place.seq).ok)
-      set_status(kv.status, chunk_fault(kv, ch, lo.place.seq));
+      set_status(kv.status, chunk_fault(ch, lo.place.seq));
   } else {
     if (blockIdx.x == 0)
       for (int b = threadIdx.x; b < kv.batch; b += NT)
-        if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(kv, ch, b));
+        if (!chunk_seq(kv, ch, b).ok) set_status(kv.status, chunk_fault(ch, b));
     if (!share_of<STREAM>(kv, ch, G, CAP, causal, blockIdx.x, shares, plan.least, w, lo, hi)) lo = Cut{{0, kv.hkv, 0}, 0};
     if (w >= shares) return;
   }
@@ -872,7 +872,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, 1) void k_paged_tile(PagedDev kv, 
       auto one_tile = [&](int u, const unsigned char* at) {
         const bool masked = u >= hide_at[0];
         if constexpr (NT == 1) {
-          attn_unit<T, HD>(at, at + 2 * R::BLOCK, masked, masked ? seen_of(0, u) : ~0u, a.scale, qf[0], o[0], tile[0].m, tile[0].l);
+          attn_unit<HD>(at, at + 2 * R::BLOCK, masked, masked ? seen_of(0, u) : ~0u, a.scale, qf[0], o[0], tile[0].m, tile[0].l);
         } else {
           bf16x8_t f[NS];
 #pragma unroll
