@@ -449,8 +449,12 @@ esp_status esp_paged_append(void *stream, const esp_paged_kv *kv, int32_t layer,
  * [0, len[b]) and, of the chunk, rows 0..r (anc NULL) or the rows c whose bit is set in its ancestor bitset anc
  * [total_rows][anc_words] (as esp_block).  out = softmax(scale q k) v; a row that sees nothing gets zeros.  What a row does
  * not see does not reach it, whatever it holds.  q as in esp_paged_append; out device [total_rows][n_q_heads][head_dim],
- * contiguous, no overlap with q.  An infinity in V makes the output of the rows that see it that infinity, or NaN where its probability
- * rounds to nothing; NaN in V, and infinities of both signs, make it NaN.
+ * contiguous, no overlap with q.
+ * Scores, sums and the outputs until they are written are fp32; in bf16 the probabilities are rounded to it for the product with V (their
+ * sum is of the unrounded ones), by 2^-8 of each at most: outputs are 2.3e-3 of their size off in the mean, where the rounding of the output alone
+ * makes 1.7e-3.  Scores (scale q k) may be as large as 5e8; beyond that outputs may be NaN or zero.  A key with a score of minus infinity is as one
+ * that is not seen; a score of infinity or NaN makes the row NaN.  An infinity in V makes the output of the rows that see it that
+ * infinity, or NaN where its probability rounds to nothing; NaN in V, and infinities of both signs, make it NaN.
  * scratch: device, 16-byte aligned, esp_paged_attn_scratch_bytes() bytes (0: it may be NULL), which depend on the host's values
  * alone, len_bound among them; calls that overlap in time need one each.  Results do not depend on what it held.
  * Errors: EINVAL (null pointers, scale below 1e-20 or not finite, ...), ESHAPE (n_q_heads not a multiple of n_kv_heads, anc_words * 64
@@ -463,8 +467,9 @@ esp_status esp_paged_attn(void *stream, const esp_paged_kv *kv, int32_t layer, c
 /* After a verified block whose rows were appended: moves K and V of the accepted rows, in every layer, from slots len[b] +
  * accepted_row[b][i] to len[b] + i, i = 1 .. n_emit[b] - 1 (accepted_row[b][0], the root, sits at len[b] already), and writes
  * len_out[b] = len[b] + n_emit[b]; len_out may be kv->len.  accepted_row [batch][ESP_MAX_MASKS + 1] and n_emit [batch] are
- * what esp_verify_accept hands out.  A path is ascending rows from 1 on, n_emit[b] 0 .. ESP_MAX_MASKS + 1; of a sequence with another
- * one nothing moves, len_out[b] = len[b], and ESP_DEV_BAD_PATH is set.
+ * laid out as esp_verify_accept's, which itself walks and moves in the contiguous cache only: over pages the caller finds the path,
+ * from the root to each next row whose token is the choice made at the one before.  A path is ascending rows from 1 on, n_emit[b]
+ * 0 .. ESP_MAX_MASKS + 1; of a sequence with another one nothing moves, len_out[b] = len[b], and ESP_DEV_BAD_PATH is set.
  * Errors: EINVAL. */
 esp_status esp_paged_commit(void *stream, const esp_paged_kv *kv, const int32_t *n_emit, const int32_t *accepted_row,
                             int32_t *len_out);

@@ -365,6 +365,30 @@ def test_large_scores_and_other_scales(dtype, hd, planned):
         check_attention(c, q, B.paged_attn(c.kv, 0, c.chunk, q, scale=scale), scale=scale)
 
 
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+def test_scores_of_hundreds_of_millions(dtype, hd, planned):
+    """The largest score's key has all the weight.  Half a step of fp32 at 2^28 is 16: the exponents' reference is off by as much, the same for a
+    column's keys of a wave, and a score by (hd + 8) steps; rows whose first and second are less than 2000 steps apart are left out."""
+    dt, scale = DT[dtype], 4e6
+    c = Cache(dt, 2, hd, 32, [700, 40], [40, 90], 65)
+    q = queries(130, 6, hd, dt, 66)
+    out = B.paged_attn(c.kv, 0, c.chunk, q, scale=scale).cpu().double()
+    used = 0
+    for b, (l, r) in enumerate(zip(c.lens, c.rows)):
+        a = c.starts[b]
+        k, v = (t[b].double().repeat_interleave(3, 1) for t in (c.k, c.v))
+        x = torch.einsum("rhd,thd->rht", q[a:a + r].cpu().double(), k).mul_(scale).masked_fill_(~visible(l, r)[:, None], -math.inf)
+        top, at = x.topk(2, -1)
+        assert top.abs().max() < 5e8
+        sure = top[..., 0] - top[..., 1] > 2000 * U * x.masked_fill(torch.isinf(x), 0).abs().amax(-1)
+        want = torch.gather(v.permute(1, 0, 2), 1, at[..., :1].expand(-1, -1, hd).permute(1, 0, 2)).permute(1, 0, 2)
+        err = (out[a:a + r] - want).abs()
+        # the weight's own rounding for the product, the output's, the quotient's and the sum's
+        assert (err <= (2 * half(dt) + 8 * U) * want.abs())[sure].all()
+        used += int(sure.sum())
+    assert used > 500
+
+
 @pytest.mark.parametrize("shift", [0, 1, 3])
 def test_queries_at_any_stride_and_alignment(shift, planned):
     for dt in (torch.bfloat16, torch.float32):
