@@ -207,7 +207,8 @@ __global__ __launch_bounds__(256) void k_rope_rows(RopeRows a, PagedDev kv, Chun
 
 // The same for chunks of many rows: K and V go by blocks of the cache, a workgroup takes 32 slots and HEADS kv heads and writes
 // whole 128-byte lines, V turned from rows to columns through LDS; the queries go by rows, in the workgroups behind these.  (By rows
-// a V row is HD stores of one element.)  Four chunks of 700 to 2048 rows: 66 us by rows, 31 by blocks, 4.7 TB/s.
+// a V row is HD stores of one element.)  Four chunks of 700 to 2048 rows, 143 MB: 66 us by rows, 37 by blocks, 3.9 TB/s (31 and 4.7 with
+// the rows in the last cache, as behind a projection)
 template <int HD> constexpr int BLOCK_HEADS = 128 / HD;
 template <typename T, int HD, bool VEC, int R>
 __global__ __launch_bounds__(256) void k_append_blocks(RopeRows a, PagedDev kv, ChunkDev ch, int block_groups, int head_groups) {
