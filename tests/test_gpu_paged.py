@@ -895,6 +895,63 @@ def test_verified_steps_over_a_paged_cache():
     assert kv.device_status() == 0
 
 
+@pytest.mark.parametrize("rows", [[12, 7, 20], [300, 90, 260]])          # by rows, by blocks of slots
+def test_captured_steps_over_a_paged_cache(rows):
+    """Append, attention and commit in one graph, replayed with other rows, trees and paths each time, eager calls on a cache of their own beside
+    them: the same outputs, pools and lengths."""
+    dt, hq, hkv, hd, page, batch, steps = torch.bfloat16, 8, 2, 128, 32, 3, 5
+    g = gen(331)
+    caches = [B.PagedKv.zeros(2, 70, hkv, page, hd, batch, 20, dt) for _ in range(2)]
+    for kv in caches:
+        kv.page_table.copy_(torch.randperm(70, generator=gen(332))[:60].view(3, 20).to(torch.int32))
+        kv.lens.copy_(i32([5, 0, 100]))
+        kv.len_bound = 100 + 9 * steps
+    starts = np.concatenate([[0], np.cumsum(rows)]).tolist()
+    n, words = starts[-1], (max(rows) + 63) // 64
+    ch = B.ChunkRows(i32(starts), n, max(rows))
+    x = torch.zeros((n, hq + 2 * hkv, hd), dtype=dt, device="cuda")
+    pos, anc = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros((n, words), dtype=torch.int64, device="cuda")
+    n_emit, acc = torch.ones(3, dtype=torch.int32, device="cuda"), torch.zeros((3, 9), dtype=torch.int32, device="cuda")
+    spec = B.rope_spec(hd, hd, 1e4)
+    scratch = torch.empty(max(16, B.paged_attn_scratch_bytes(caches[0], ch, hq)), dtype=torch.uint8, device="cuda")
+    q_out, out = (torch.empty((n, hq, hd), dtype=dt, device="cuda") for _ in range(2))
+
+    def step(kv, q_out=None, out=None, scratch=None):
+        for layer in (0, 1):
+            q = B.paged_append(kv, layer, ch, x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], rope=spec, positions=pos, q_out=q_out)
+            out = B.paged_attn(kv, layer, ch, q, anc=anc, out=out, scratch=scratch)
+        B.paged_commit(kv, n_emit, acc)
+        return out
+    before = caches[0].lens.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(caches[0], q_out, out, scratch)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step(caches[0], q_out, out, scratch)
+    torch.cuda.synchronize()
+    caches[0].lens.copy_(before)
+    for kv in caches:
+        kv.k.zero_(), kv.v.zero_()
+    for i in range(steps):
+        trees = [random_tree(r, 340 + 7 * i + b) for b, r in enumerate(rows)]
+        x.copy_(torch.randn(x.shape, generator=g))
+        anc.copy_(pack_anc(trees, rows, words))
+        pos.copy_(torch.cat([t.sum(1) - 1 + l for t, l in zip(trees, caches[1].lens.tolist())]))
+        paths = [torch.nonzero(t[len(t) - 1 - i]).flatten().tolist()[:9] for t in trees]
+        n_emit.copy_(i32([len(p) for p in paths]))
+        acc.copy_(i32([p + [0] * (9 - len(p)) for p in paths]))
+        torch.cuda.synchronize()
+        graph.replay()
+        want = step(caches[1])
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+        a, b = caches
+        assert torch.equal(a.k, b.k) and torch.equal(a.v, b.v) and torch.equal(a.lens, b.lens) and a.lens.tolist() != before.tolist(), i
+    assert caches[0].device_status() == 0 and caches[1].device_status() == 0
+
+
 def test_paged_attention_agrees_with_the_contiguous_cache():
     """The same rows in the framework's contiguous cache and in pages: the two attentions agree to their types."""
     from paper_2603_17942_amd import synth
