@@ -734,8 +734,8 @@ def paged_attn(kv: PagedKv, layer: int, rows: ChunkRows, q: torch.Tensor, scale:
         raise ValueError(f"out: contiguous [{n}, {nq}, {hd}] wanted")
     words = 0
     if anc is not None:
-        if anc.dtype is not torch.int64 or anc.device != dev or anc.dim() != 2 or anc.shape[0] != n or not anc.is_contiguous():
-            raise ValueError(f"anc: contiguous int64 [{n}, words] wanted")
+        if anc.dtype is not torch.int64 or anc.device != dev or anc.dim() != 2 or anc.shape[0] != n or anc.shape[1] == 0 or not anc.is_contiguous():
+            raise ValueError(f"anc: contiguous int64 [{n}, words] wanted")          # (none of no words: its address is null, as of no anc)
         words = anc.shape[1]
     if scratch is None:
         nb = paged_attn_scratch_bytes(kv, rows, nq)

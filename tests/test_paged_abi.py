@@ -237,3 +237,11 @@ def test_tensors_whose_addresses_are_held_cannot_be_replaced():
     kv.lens[0] = 33
     assert kv.struct.len_bound == 40 and C.cast(kv.struct.len, C.POINTER(C.c_int32))[0] == 33
     assert kv.struct.len == lens.data_ptr() and rows.struct.row0 == rows.row0.data_ptr()
+
+
+def test_bitsets_of_no_words_are_not_causal_attention():
+    k = torch.zeros((1, 4, 2, 32, 64))
+    kv = B.PagedKv(k, k.clone(), torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 0)
+    rows, x = B.ChunkRows(torch.tensor([0, 2], dtype=torch.int32), 2, 2), torch.zeros((2, 2, 64))
+    with pytest.raises(ValueError, match="anc"):
+        B.paged_attn(kv, 0, rows, x, anc=torch.zeros((2, 0), dtype=torch.int64))
