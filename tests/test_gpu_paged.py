@@ -582,6 +582,23 @@ def test_rope_many_rows(rows):
         assert ((torch.cat([q, k], 1).cpu().double() - want).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("rows,heads", [(2 ** 26 - 4, 1), (2 ** 22 + 3, 70)])
+def test_rope_of_as_many_rows_as_there_may_be(rows, heads):
+    """In place; elements behind 2^31, and as many workgroups as a launch can have.  Rows repeat after 4099, positions after 1021."""
+    x = torch.randn((4099, heads, 64), generator=gen(61)).to(torch.bfloat16)
+    q = x.cuda().repeat((rows + 4098) // 4099, 1, 1)[:rows]
+    pos = (torch.arange(rows, device="cuda", dtype=torch.int32) % 1021) * 997
+    got, _ = B.rope_qk(q, None, pos, B.rope_spec(64), q_out=q)
+    assert got is q
+    at = torch.cat([torch.arange(5), torch.randint(0, rows, (300,), generator=gen(62)), torch.arange(rows - 5, rows)])
+    want, tol = rotated(x[at % 4099], None, (at % 1021) * 997, 64, 1e4, False, 1.0, 0, 1.0, 4.0, 1.0)
+    assert ((q[at.cuda()].cpu().double() - want).abs() <= tol).all()
+    period = 4099 * 1021                                # and every other row: as the one a whole period before it
+    for lo in range(period, rows, period):
+        n = min(period, rows - lo)
+        assert torch.equal(q[lo:lo + n], q[lo - period:lo - period + n])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rope_at_any_alignment(dtype):
     dt = DT[dtype]
