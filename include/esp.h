@@ -395,7 +395,7 @@ esp_status esp_rope_make(int32_t head_dim, int32_t rot_dim, int32_t interleaved,
  * side by side, rows *_stride elements apart (parts of one projection's rows are taken as they are).  The outputs
  * have strides of their own; an output may be its input with the same stride, and otherwise must not overlap any input.
  * positions device [rows].  Either of q and k may be NULL with its output (its head count is then not looked at).  The
- * arithmetic is fp32 (the angle fp64), rounded once.
+ * arithmetic is fp32 (the angle fp64), rounded once; the squares of a head that is normed have to fit it (features up to 1e18).
  * Errors: EINVAL (null pointers, rows < 0, n_* < 1, eps negative or not finite), ESHAPE (strides below heads * head_dim), EDTYPE,
  * ECAPACITY (more than 2^26 - 4 rows, or than 2^31 - 1 rows x heads, or 2^22 - 1 heads). */
 esp_status esp_rope_qk(void *stream, int32_t dtype, const esp_rope *rope, int32_t rows, int32_t n_q_heads, int32_t n_kv_heads,
@@ -406,7 +406,9 @@ esp_status esp_rope_qk(void *stream, int32_t dtype, const esp_rope *rope, int32_
 /* The pool.  k and v each hold [n_layers][n_pages][n_kv_heads] planes of page_size * head_dim elements in the block order
  * of esp_kv (blocks of 32 slots); 16-byte aligned.  Slot s of sequence b lies in page page_table[b][s / page_size], at slot
  * s % page_size; entries of pages that hold no token of the sequence are never used.  Two sequences may share pages that
- * nobody writes.  Slots [0, len[b]) hold committed tokens. */
+ * nobody writes.  Slots [0, len[b]) hold committed tokens.
+ * ECAPACITY: table_stride * page_size or n_pages * n_kv_heads * page_size / 32 of 2^31 and more, n_layers * n_kv_heads of 2^24 and
+ * more, n_layers or batch above 65535. */
 typedef struct {
   void *k, *v;                /* device                                                                          */
   const int32_t *page_table;  /* device [batch][table_stride]                                                    */
@@ -451,10 +453,11 @@ esp_status esp_paged_append(void *stream, const esp_paged_kv *kv, int32_t layer,
  * not see does not reach it, whatever it holds.  q as in esp_paged_append; out device [total_rows][n_q_heads][head_dim],
  * contiguous, no overlap with q.
  * Scores, sums and the outputs until they are written are fp32; in bf16 the probabilities are rounded to it for the product with V (their
- * sum is of the unrounded ones), by 2^-8 of each at most: outputs are 2.3e-3 of their size off in the mean, where the rounding of the output alone
- * makes 1.7e-3.  Scores (scale q k) may be as large as 5e8; beyond that outputs may be NaN or zero.  A key with a score of minus infinity is as one
- * that is not seen; a score of infinity or NaN makes the row NaN.  An infinity in V makes the output of the rows that see it that
- * infinity, or NaN where its probability rounds to nothing; NaN in V, and infinities of both signs, make it NaN.
+ * sum is of the unrounded ones), by 2^-8 of each at most: outputs are 2.3e-3 of their size off in the mean, where the rounding of the output
+ * alone makes 1.7e-3.  Scores (scale q k) may be as large as 5e8 and values 1e24; beyond that outputs may be infinite, NaN or zero.
+ * A key with a score of minus infinity is as one that is not seen; a score of infinity or NaN makes the row NaN.  An infinity in V makes the
+ * output of the rows that see it that infinity, or NaN where its probability rounds to nothing; NaN in V, and infinities of both signs,
+ * make it NaN.
  * scratch: device, 16-byte aligned, esp_paged_attn_scratch_bytes() bytes (0: it may be NULL), which depend on the host's values
  * alone, len_bound among them; calls that overlap in time need one each.  Results do not depend on what it held.
  * Errors: EINVAL (null pointers, scale below 1e-20 or not finite, ...), ESHAPE (n_q_heads not a multiple of n_kv_heads, anc_words * 64

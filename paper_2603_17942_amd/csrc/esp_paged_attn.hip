@@ -1130,8 +1130,8 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
 // an item do not change that); shares with their merge 13.5 and what K and V take.  One row over 1000 / 4000 keys: 11.2 / 25.7 alone,
 // 12.9 / 17.5 in shares; 32 sequences of 2000 / 4000: 45 / 97, 53 / 105 (but alone a batch takes as long as its longest sequence, so a longer
 // one is shared out).
-// Tile kernel (these times for heads of 64 and fp32 too, whose key tiles take half as long and, by their operations, 3.5 times): 2 for 64 keys, 13 for an item's beginning and end, 8 for the merge and 1/20 for a partial.  With as many items as places, one
-// sequence's go to the places by weight: 4096 rows from none 150 against 190 in shares.  So do a batch's if they are short; else they are
+// Tile kernel: 2 for 64 keys, 13 for an item's beginning and end, 8 for the merge and 1/20 for a partial.  (These are taken for heads of 64 and
+// for fp32 too, whose key tiles take half as long and, by their operations, 3.5 times.)  With as many items as places, one sequence's go to the places by weight: 4096 rows from none 150 against 190 in shares.  So do a batch's if they are short; else they are
 // shared out, since nothing is known here of how their lengths differ (8 chunks of 189 to 512 rows over up to 8192 keys: 215 against 361;
 // 8 x 512 rows over 4096 each: 308 against 296).
 PagedAttnPlan paged_attn_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int len_bound) {
