@@ -364,6 +364,23 @@ esp_status esp_softmax_topk(void *stream, const float *logits, int32_t rows, int
 esp_status esp_softmax_topk_static(void *stream, const float *logits, int32_t rows, int32_t vocab,
                                    int32_t Kp, int32_t *ids, float *probs);
 
+/* The next token of every row from its logits, each row with limits of its own.  In order of their logits (equal ones by id) the tokens weigh
+ * w = exp((logit - largest) / temperature).  Kept are the first top_k; of those, W their weights' sum, each before which less than top_p W lies;
+ * of those, what weighs min_p or more; the first of all in any case.  The token is the lowest id at which the kept weights, added up over the ids to
+ * it, are above u times their sum.  temperature 0: the first of the order.
+ *   logits      device [rows][vocab], fp32 or bf16, rows row_stride elements apart (any alignment of the type)
+ *   temperature, top_p, min_p  device fp32 [rows]; top_k device int32 [rows]; NULL: 1, 1, 0 and none.  top_k below 1, top_p of 1 and more and
+ *               min_p of 0 and less are no limit; top_p below 0 is 0, min_p above 1 is 1
+ *   u           device fp32 [rows], uniform in [0, 1): below (and NaN) 0, above the largest below 1
+ *   ids         device int32 [rows]; probs NULL or device fp32 [rows]: the token's share of the kept weights (temperature 0: 1)
+ * Minus infinity and NaN are tokens that cannot be chosen, plus infinity is as the largest finite fp32 value.  A row without any other, and a row
+ * whose temperature is negative or not finite or whose top_p or min_p is NaN, gets -1 and 0.
+ * Weights are taken in fp64 (7e-12) and added up as integers of 2^-S of the largest, S = min(50, 62 - ceil log2 vocab): what a call chooses
+ * does not depend on the order of the sums, and tokens of less than half of that are not chosen.
+ * Errors: EINVAL (null pointers, rows < 0, vocab < 1), ESHAPE (row_stride < vocab), EDTYPE, ECAPACITY (vocab above 2^24, 2^22 rows and more). */
+esp_status esp_sample(void* stream, int32_t dtype, const void* logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
+                      const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* ids, float* probs);
+
 /* ---- paged KV cache ------------------------------------------------------------------------
  * A cache whose sequences own pages anywhere in a pool, the rotation and the norms that come before it, and the
  * attention that reads it.  The calls take a stream and no context; the device that is current at the call must
@@ -476,6 +493,42 @@ esp_status esp_paged_attn(void *stream, const esp_paged_kv *kv, int32_t layer, c
  * Errors: EINVAL. */
 esp_status esp_paged_commit(void *stream, const esp_paged_kv *kv, const int32_t *n_emit, const int32_t *accepted_row,
                             int32_t *len_out);
+
+/* How much attention the chunk's rows give to each token of their sequences, for esp_paged_evict: with p the softmax of esp_paged_attn (causal; K of
+ * the rows is in its slots already), mass[t] = before[t] + the sum of p_rt over the sequence's counted rows r and the kv head's query heads, for
+ * t < len[b]; the chunk's own tokens get the sum alone, whatever was there.  Slots from len[b] + rows on, and sequences without rows, are not touched.
+ * After a verified tree: the accepted rows alone, packed, with len as it was before them.
+ *   last_rows   0: all rows count; otherwise only the last so many of each sequence's
+ *   before, mass device fp32 [n_layers][batch][n_kv_heads][mass_slots]; before NULL: zeros; it may be mass itself, and otherwise must not overlap it
+ *   scratch     device, 16-byte aligned, esp_paged_weigh_scratch_bytes(), which depend on the host's values alone; calls that overlap in time need
+ *               one each.  Up to 32 counted (row, query head) pairs a kv head it holds their scores: up to 4 bytes a pair, kv head and token of len_bound
+ * Scores, probabilities and sums are fp32, tokens' sums always in the same order.  Scores may be as large as 5e8.  A row with a score of infinity or NaN makes
+ * the tokens it sees NaN; a token in a page outside the pool is not seen (its mass is `before`).  A sequence with len + rows above mass_slots is as one
+ * that is over its bound.
+ * Errors: as esp_paged_attn; EINVAL also for last_rows < 0 and mass_slots < 1; ECAPACITY also for more than 65535 kv heads. */
+size_t esp_paged_weigh_scratch_bytes(const esp_paged_kv* kv, const esp_chunk* rows, int32_t n_q_heads, int32_t last_rows);
+esp_status esp_paged_weigh(void* stream, const esp_paged_kv* kv, int32_t layer, const esp_chunk* rows, int32_t n_q_heads, const void* q,
+                           int64_t q_stride, float scale, int32_t last_rows, const float* before, float* mass, int32_t mass_slots, void* scratch,
+                           size_t scratch_bytes);
+
+/* Bounds what sequences keep: of one with len[b] > keep tokens the first `first`, the last `recent` and of the others those of greatest mass (equal ones: the
+ * earlier; NaN is least) stay, `keep` in all, chosen for every layer and kv head by itself.  They move to slots 0 .. keep - 1 in their order, and
+ * their masses with them; len_out[b] = keep.  Of the other sequences nothing is chosen, and len_out[b] = len[b].  Positions are in the rotated K already and
+ * stay; a row that is appended next has its own position, no longer its slot.
+ *   table_out   device [batch][table_out_stride]: pages that take the kept tokens.  A sequence's entry is either that of kv's page_table in the same place
+ *               (then the block's tokens are moved within the page; page_table itself: all in place) or a page that no sequence reads in this call, for
+ *               instance because the old one is shared.  Pages that are written must belong to one sequence
+ *   mass_out    device fp32 [n_layers][batch][n_kv_heads][mass_out_slots], mass itself with the same mass_slots, or no overlap.  Slots from len_out on
+ *               are left as they were
+ *   len_out     device [batch], may be kv->len
+ *   kept        device int32 [n_layers][batch][n_kv_heads][keep]: the old slots of the tokens, ascending, then -1
+ * A kept token whose old page is outside the pool becomes zeros, one whose new page is is not written; both set ESP_DEV_BAD_PAGE.  A sequence with a length
+ * that is negative, above len_bound, mass_slots or its table is left out: its kept are -1, its len_out its len.
+ * Errors: EINVAL (null pointers, keep < 1, first or recent negative or together above keep, mass_out or table_out the input with other strides), ECAPACITY
+ * (table_out or mass_out too small for keep, more than 4194303 layers x sequences x kv heads). */
+esp_status esp_paged_evict(void* stream, const esp_paged_kv* kv, const float* mass, int32_t mass_slots, int32_t keep, int32_t first, int32_t recent,
+                           const int32_t* table_out, int32_t table_out_stride, float* mass_out, int32_t mass_out_slots, int32_t* len_out,
+                           int32_t* kept);
 
 /* Copies slots first_slot .. of sequence seq, one layer, out of the pool to plain rows [n_slots][n_kv_heads][head_dim].
  * Slots of a page outside the pool come back as zeros.

@@ -76,7 +76,7 @@ EXPORTS = ["esp_status_str", "esp_workspace_bytes", "esp_create", "esp_destroy",
            "esp_gemm_scratch_bytes", "esp_gemm", "esp_gemm_argmax_scratch_bytes", "esp_gemm_argmax", "esp_attn_tree", "esp_softmax_topk_scratch_bytes",
            "esp_softmax_topk", "esp_softmax_topk_static", "esp_profile_enable", "esp_profile_read", "esp_pack_weight", "esp_set_sampling",
            "esp_rope_make", "esp_rope_qk", "esp_paged_append", "esp_paged_attn_scratch_bytes", "esp_paged_attn", "esp_paged_commit",
-           "esp_paged_load"]
+           "esp_paged_load", "esp_sample", "esp_paged_weigh_scratch_bytes", "esp_paged_weigh", "esp_paged_evict"]
 SITES = {"gemm_layer": 0, "attn": 1, "attn_merge": 2, "lm_head": 3, "topk": 4, "tree": 5, "glue": 6}
 
 _lib = None
@@ -143,6 +143,11 @@ def load_library() -> C.CDLL:
     lib.esp_paged_attn.argtypes = [_vp, P(PagedKvStruct), _i32, P(ChunkStruct), _i32, _vp, _i64, _f32, _vp, _i32, _vp, _vp, C.c_size_t]
     lib.esp_paged_commit.argtypes = [_vp, P(PagedKvStruct), _vp, _vp, _vp]
     lib.esp_paged_load.argtypes = [_vp, P(PagedKvStruct), _i32, _i32, _i32, _i32, _vp, _vp]
+    lib.esp_sample.argtypes = [_vp, _i32, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.esp_paged_weigh_scratch_bytes.restype = C.c_size_t
+    lib.esp_paged_weigh_scratch_bytes.argtypes = [P(PagedKvStruct), P(ChunkStruct), _i32, _i32]
+    lib.esp_paged_weigh.argtypes = [_vp, P(PagedKvStruct), _i32, P(ChunkStruct), _i32, _vp, _i64, _f32, _i32, _vp, _vp, _i32, _vp, C.c_size_t]
+    lib.esp_paged_evict.argtypes = [_vp, P(PagedKvStruct), _vp, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _i32, _vp, _vp]
     for name in EXPORTS:
         getattr(lib, name)          # AttributeError here = a declared entry point is not exported
     _lib = lib
@@ -522,7 +527,7 @@ def softmax_topk_static(logits: torch.Tensor, kp: int, ids: torch.Tensor, ps: to
     return ids, ps
 
 
-# ---- paged KV cache -------------------------------------------------------------------------------------
+# ---- sampling, paged KV cache -----------------------------------------------------------------------------
 # Functions on tensors, on the current stream of the tensors' device (which need not be the current one).  Some of the kernels take less
 # time than formatting a message does, so that is done for the call that is refused only.
 
@@ -572,6 +577,39 @@ def _gain(t: Optional[torch.Tensor], name: str, dev, dtype, hd: int) -> Optional
     if t.dtype is not dtype or t.shape != (hd,) or t.device != dev or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous [{hd}] of {dtype} on {dev} wanted")
     return t.data_ptr()
+
+
+def _floats(t: Optional[torch.Tensor], name: str, dev, shape) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous float32 {tuple(shape)} on {dev} wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, ids: Optional[torch.Tensor] = None,
+           probs: Optional[torch.Tensor] = None):
+    """(ids, probs): one token a row of logits [rows, vocab] (rows may lie further apart) and its share of the tokens that were left, by the
+    uniform numbers u [rows] in [0, 1).  temperature, top_k (int32), top_p, min_p [rows]: limits of each row, None for none; temperature 0 is
+    the arg-max.  A row without a token that can be chosen, or with limits that are none, gets -1 and 0."""
+    lib = load_library()
+    if logits.dim() != 2:
+        raise ValueError("logits: [rows, vocab] wanted")
+    (rows, vocab), (s0, s1), dev = logits.shape, logits.stride(), logits.device
+    if s1 != 1 and vocab != 1:
+        raise ValueError("logits: the logits of a row have to lie side by side")
+    if ids is None:
+        ids = torch.empty(rows, dtype=torch.int32, device=dev)
+    if probs is None:
+        probs = torch.empty(rows, dtype=torch.float32, device=dev)
+    n = (rows,)
+    args = (_floats(temperature, "temperature", dev, n), _ints(top_k, "top_k", dev, n), _floats(top_p, "top_p", dev, n),
+            _floats(min_p, "min_p", dev, n), _floats(u, "u", dev, n), _ints(ids, "ids", dev, n), _floats(probs, "probs", dev, n))
+    code = _dtype_of(logits)
+    if rows:
+        _on_device(dev, lib.esp_sample, "esp_sample", code, logits.data_ptr(), s0 if rows > 1 else vocab, rows, vocab, *args)
+    return ids, probs
 
 
 def rope_spec(head_dim: int, rot_dim: Optional[int] = None, theta: float = 1.0e4, interleaved: bool = False, factor: float = 1.0,
@@ -768,3 +806,61 @@ def paged_load(kv: PagedKv, layer: int, seq: int, first_slot: int, n_slots: int)
     if n_slots:
         _on_device(kv.device, lib.esp_paged_load, "esp_paged_load", kv._ref, layer, seq, first_slot, n_slots, k.data_ptr(), v.data_ptr())
     return k, v
+
+
+def _mass(t: torch.Tensor, name: str, kv: PagedKv) -> int:
+    if t.dtype is not torch.float32 or t.dim() != 4 or t.shape[:3] != (kv.k.shape[0], kv.batch, kv.n_kv_heads) or t.device != kv.device or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous float32 [{kv.k.shape[0]}, {kv.batch}, {kv.n_kv_heads}, slots] on {kv.device} wanted")
+    return t.data_ptr()
+
+
+def paged_weigh_scratch_bytes(kv: PagedKv, rows: ChunkRows, n_q_heads: int, last_rows: int = 0) -> int:
+    return load_library().esp_paged_weigh_scratch_bytes(kv._ref, rows._ref, n_q_heads, last_rows)
+
+
+def paged_weigh(kv: PagedKv, layer: int, rows: ChunkRows, q: torch.Tensor, mass: torch.Tensor, before: Optional[torch.Tensor] = None,
+                last_rows: int = 0, scale: Optional[float] = None, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Adds to mass [layers, batch, kv heads, slots] (float32), in `layer`, the attention that the chunk's rows (their K appended before) give to each
+    token, summed over rows and a kv head's queries; the chunk's own tokens get that alone.  before: what it is added to instead of mass.
+    last_rows: only so many of a sequence's rows count, the last ones (0: all).  scratch: uint8, paged_weigh_scratch_bytes."""
+    lib = load_library()
+    _same_batch(kv, rows)
+    dev, dt, hd, n = kv.device, kv.dtype, kv.head_dim, rows.total_rows
+    qp, qs, nq = _heads(q, "q", dev, dt, n, hd)
+    mp = _mass(mass, "mass", kv)
+    bp = mp
+    if before is not None:
+        bp = _mass(before, "before", kv)
+        if before.shape != mass.shape:
+            raise ValueError("before: the shape of mass wanted")
+    if scratch is None:
+        scratch = torch.empty(paged_weigh_scratch_bytes(kv, rows, nq, last_rows), dtype=torch.uint8, device=dev)
+    if scratch.dtype is not torch.uint8 or scratch.device != dev or not scratch.is_contiguous():
+        raise ValueError("scratch: contiguous uint8 wanted")
+    if n:
+        _on_device(dev, lib.esp_paged_weigh, "esp_paged_weigh", kv._ref, layer, rows._ref, nq, qp, qs, hd ** -0.5 if scale is None else scale, last_rows,
+                   bp, mp, mass.shape[3], scratch.data_ptr(), scratch.numel())
+    return mass
+
+
+def paged_evict(kv: PagedKv, mass: torch.Tensor, keep: int, first: int = 0, recent: int = 0, table_out: Optional[torch.Tensor] = None,
+                mass_out: Optional[torch.Tensor] = None, len_out: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Of every sequence with more than `keep` tokens, by layer and kv head, the `first` ones, the last `recent` ones and those of greatest mass move to slots
+    0 .. keep - 1, masses with them; returns their old slots, kept [layers, batch, kv heads, keep] (-1 behind the last).  In place, new lengths to
+    kv.lens, unless other places are given: table_out [batch, pages] (entries that are kv's in the same place or pages that nobody reads)."""
+    lib = load_library()
+    dev, layers = kv.device, kv.k.shape[0]
+    out = kv.lens if len_out is None else len_out
+    table = kv.page_table if table_out is None else table_out
+    to = mass if mass_out is None else mass_out
+    if table.dim() != 2:
+        raise ValueError("table_out: [batch, pages of a sequence] wanted")
+    if keep < 1:
+        raise ValueError("keep: 1 or more wanted")
+    shape = (layers, kv.batch, kv.n_kv_heads, keep)
+    if kept is None:
+        kept = torch.empty(shape, dtype=torch.int32, device=dev)
+    _on_device(dev, lib.esp_paged_evict, "esp_paged_evict", kv._ref, _mass(mass, "mass", kv), mass.shape[3], keep, first, recent,
+               _ints(table, "table_out", dev, (kv.batch, table.shape[1])), table.shape[1], _mass(to, "mass_out", kv), to.shape[3],
+               _ints(out, "len_out", dev, (kv.batch,)), _ints(kept, "kept", dev, shape))
+    return kept

@@ -79,3 +79,35 @@ struct PagedAttnArgs {
 };
 hipError_t launch_paged_attn(hipStream_t st, int dtype, int hd, const PagedDev& kv, const ChunkDev& ch, const PagedAttnArgs& a,
                              const PagedAttnPlan& p);
+
+struct WeighPlan {
+  int width = 0;              // columns that scores are kept for; 0: many, scores are computed twice
+  int share_units = 1, shares = 1;       // units of 32 keys of a share of the statistics
+  int parts = 1;              // many: of the columns, each with sums of its own
+  int most_rows = 0;          // counted rows of a sequence at most
+  bool packed = false;        // many: statistics lie by rows of the chunk, not by most_rows a sequence
+  int64_t tokens = 0;         // of a sequence at most, in whole units
+  int64_t columns = 0;        // many: of a share's statistics
+  int64_t stats_floats = 0, scratch_floats = 0;
+};
+struct WeighArgs {
+  const void* q;
+  int64_t q_stride;
+  const float* before;        // of the layer, as mass; null: nothing
+  float* mass;
+  float* scratch;
+  int hq, last, slots;        // slots: of a sequence and kv head in mass
+  float scale;                // with log2 e
+};
+WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int last, int len_bound);
+int64_t weigh_workgroups(const WeighPlan& p, int batch, int hkv, int G);
+hipError_t launch_paged_weigh(hipStream_t st, int dtype, int hd, const PagedDev& kv, const ChunkDev& ch, const WeighArgs& a, const WeighPlan& p);
+
+struct EvictArgs {
+  const float* mass;
+  float* mass_out;
+  const int32_t* table_out;
+  int32_t *len_out, *kept;
+  int layers, slots, out_slots, out_stride, keep, first, recent;
+};
+hipError_t launch_paged_evict(hipStream_t st, int dtype, int hd, const PagedDev& kv, const EvictArgs& a);

@@ -40,6 +40,8 @@ PagedDev to_dev(const esp_paged_kv* kv, int layer) {
 }
 // four rows a workgroup; pieces and elements of four rows are counted in 31 bits
 bool too_many(int64_t heads, int64_t rows) { return rows > 4 * MOST_WORKGROUPS || heads * std::max<int64_t>(rows, 512) > INT32_MAX; }
+// columns of a sequence and kv head are counted in 31 bits
+bool too_many_columns(const esp_paged_kv* kv, const esp_chunk* c, int n_q) { return (int64_t)c->max_rows * (n_q / kv->n_kv_heads) > INT32_MAX / 2; }
 bool bad_eps(float eps) { return !(eps >= 0.f) || !std::isfinite(eps); }
 // (may be null: no rotation)
 esp_status check_rope(const esp_rope* r) {
@@ -150,7 +152,7 @@ esp_status esp_paged_attn(void* stream, const esp_paged_kv* kv, int32_t layer, c
   if (n_q % kv->n_kv_heads) return ESP_ESHAPE;
   if (q_stride < (int64_t)n_q * kv->head_dim) return ESP_ESHAPE;
   if (anc && (int64_t)anc_words * 64 < rows->max_rows) return ESP_ESHAPE;
-  if ((int64_t)rows->max_rows * (n_q / kv->n_kv_heads) > INT32_MAX / 2) return ESP_ECAPACITY;
+  if (too_many_columns(kv, rows, n_q)) return ESP_ECAPACITY;
   if (rows->total_rows == 0 || rows->max_rows == 0) return ESP_OK;
   const PagedAttnPlan p = paged_attn_plan(kv->dtype, kv->head_dim, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, kv->len_bound);
   if (paged_attn_workgroups(p, kv->batch, kv->n_kv_heads) > MOST_WORKGROUPS) return ESP_ECAPACITY;
@@ -177,6 +179,55 @@ esp_status esp_paged_load(void* stream, const esp_paged_kv* kv, int32_t layer, i
   if (layer < 0 || layer >= kv->n_layers || seq < 0 || seq >= kv->batch || first_slot < 0 || n_slots < 0 || !k_rows || !v_rows) return ESP_EINVAL;
   if ((int64_t)first_slot + n_slots > (int64_t)kv->table_stride * kv->page_size) return ESP_ECAPACITY;
   ESP_HIP(launch_paged_load((hipStream_t)stream, kv->dtype, kv->head_dim, to_dev(kv, layer), seq, first_slot, n_slots, k_rows, v_rows));
+  return ESP_OK;
+}
+
+size_t esp_paged_weigh_scratch_bytes(const esp_paged_kv* kv, const esp_chunk* rows, int32_t n_q, int32_t last_rows) {
+  if (check_paged(kv) != ESP_OK || check_chunk(kv, rows) != ESP_OK || n_q < 1 || n_q % kv->n_kv_heads || last_rows < 0) return 0;
+  if (rows->total_rows == 0 || rows->max_rows == 0 || too_many_columns(kv, rows, n_q)) return 0;
+  const WeighPlan p = weigh_plan(kv->dtype, kv->head_dim, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, last_rows, kv->len_bound);
+  return (size_t)p.scratch_floats * 4;
+}
+
+esp_status esp_paged_weigh(void* stream, const esp_paged_kv* kv, int32_t layer, const esp_chunk* rows, int32_t n_q, const void* q, int64_t q_stride,
+                           float scale, int32_t last_rows, const float* before, float* mass, int32_t mass_slots, void* scratch,
+                           size_t scratch_bytes) {
+  esp_status st = check_paged(kv);
+  if (st != ESP_OK) return st;
+  st = check_chunk(kv, rows);
+  if (st != ESP_OK) return st;
+  if (layer < 0 || layer >= kv->n_layers || n_q < 1 || !q || !mass || mass_slots < 1 || last_rows < 0 || !(scale >= 1e-20f) || !std::isfinite(scale))
+    return ESP_EINVAL;
+  if (n_q % kv->n_kv_heads) return ESP_ESHAPE;
+  if (q_stride < (int64_t)n_q * kv->head_dim) return ESP_ESHAPE;
+  if (kv->n_kv_heads > 65535 || too_many_columns(kv, rows, n_q)) return ESP_ECAPACITY;
+  if (rows->total_rows == 0 || rows->max_rows == 0) return ESP_OK;
+  const WeighPlan p = weigh_plan(kv->dtype, kv->head_dim, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, last_rows, kv->len_bound);
+  if (weigh_workgroups(p, kv->batch, kv->n_kv_heads, n_q / kv->n_kv_heads) > MOST_WORKGROUPS) return ESP_ECAPACITY;
+  const size_t need = (size_t)p.scratch_floats * 4;
+  if (!scratch || scratch_bytes < need) return ESP_ECAPACITY;
+  if ((uintptr_t)scratch % 16) return ESP_EINVAL;
+  const int64_t off = (int64_t)layer * kv->batch * kv->n_kv_heads * mass_slots;
+  const WeighArgs a{q, q_stride, before ? before + off : nullptr, mass + off, (float*)scratch, n_q, last_rows, mass_slots,
+                    (float)((double)scale * 1.4426950408889634)};
+  ESP_HIP(launch_paged_weigh((hipStream_t)stream, kv->dtype, kv->head_dim, to_dev(kv, layer), {rows->row0, rows->total_rows, rows->max_rows}, a, p));
+  return ESP_OK;
+}
+
+esp_status esp_paged_evict(void* stream, const esp_paged_kv* kv, const float* mass, int32_t mass_slots, int32_t keep, int32_t first, int32_t recent,
+                           const int32_t* table_out, int32_t table_out_stride, float* mass_out, int32_t mass_out_slots, int32_t* len_out,
+                           int32_t* kept) {
+  const esp_status st = check_paged(kv);
+  if (st != ESP_OK) return st;
+  if (!mass || !table_out || !mass_out || !len_out || !kept || mass_slots < 1 || mass_out_slots < 1 || table_out_stride < 1 || keep < 1 || first < 0 ||
+      recent < 0 || (int64_t)first + recent > keep)
+    return ESP_EINVAL;
+  if ((mass == mass_out && mass_slots != mass_out_slots) || (table_out == kv->page_table && table_out_stride != kv->table_stride)) return ESP_EINVAL;
+  if (keep > INT32_MAX - 65536 || mass_out_slots < keep || (int64_t)table_out_stride * kv->page_size < keep) return ESP_ECAPACITY;
+  // four times 256 threads a layer, sequence and kv head
+  if (kv->n_kv_heads > 65535 || (int64_t)kv->n_layers * kv->batch * kv->n_kv_heads > MOST_WORKGROUPS / 4) return ESP_ECAPACITY;
+  const EvictArgs a{mass, mass_out, table_out, len_out, kept, kv->n_layers, mass_slots, mass_out_slots, table_out_stride, keep, first, recent};
+  ESP_HIP(launch_paged_evict((hipStream_t)stream, kv->dtype, kv->head_dim, to_dev(kv, 0), a));
   return ESP_OK;
 }
 

@@ -1,0 +1,407 @@
+// How much attention a chunk's rows give to each cached token (esp_paged_weigh): mass[t] = before[t] + sum over counted rows r and the kv
+// head's queries g of softmax_t(scale q_rg . k_t), causal.
+//
+// A token's sum needs every row's largest score and sum of exponentials first, so there are two looks at the scores.  Few columns (row, query
+// head of the kv head: up to 32, a decode step's): K is what has to be read, once; the scores, 4 bytes each, go to scratch with the share's
+// statistics, and a second kernel adds up their exponentials, a thread a token.  Many columns (a prompt's): the products are what costs, and are
+// taken twice.  First a wave has 32 columns and goes over the keys, for the statistics; then a wave has 32 or 64 keys and goes over the columns,
+// whose tiles four waves share through LDS, so that a token's sum stays in a lane and nothing is added by atomics: the same bits every time.
+//
+// Scores are S = Q K^T on 32 x 32 matrix instructions.  With keys as the second operand a lane has one key and the columns
+// 8 (v / 4) + 4 half + v % 4 in its 16 registers; with keys first (the statistics of many columns) one column and those keys.
+#include <algorithm>
+
+#include "esp_attn_unit.h"
+#include "esp_paged.h"
+
+namespace {
+
+constexpr int WAVES = 4, THREADS = 64 * WAVES;
+
+struct WeighSeq {            // a sequence's counted rows: the last `rows` of its chunk
+  int first_row;             // in the chunk
+  int first, rows, len, total;       // total: len and all rows
+  bool ok;
+};
+__device__ __forceinline__ WeighSeq weigh_seq(const PagedDev& kv, const ChunkDev& ch, int seq, int last, int slots) {
+  const ChunkSeq c = chunk_seq(kv, ch, seq);
+  const bool ok = c.ok && (int64_t)c.len + c.rows <= slots;
+  const int n = last > 0 ? min(c.rows, last) : c.rows;
+  return {c.row0, c.rows - n, n, c.len, c.len + c.rows, ok};
+}
+
+// first element of a unit of 32 keys; null: its page is outside the pool
+template <typename T>
+__device__ __forceinline__ const T* unit_at(const PagedDev& kv, int seq, int kvh, int unit, int hd) {
+  const int slot = 32 * unit, at = slot / kv.page_size;
+  const int page = kv.table[(size_t)seq * kv.stride + at];
+  if (page < 0 || page >= kv.n_pages) return nullptr;
+  return (const T*)kv.k + page_plane(page, kvh, kv.hkv, kv.page_size, hd) + (size_t)(slot - at * kv.page_size) * hd;
+}
+template <typename T, int HD>
+__device__ __forceinline__ void load_unit(const T* p, int lane, typename AttnFrag<T>::type (&k)[HD / 16]) {
+  typedef typename AttnFrag<T>::type F;
+#pragma unroll
+  for (int s = 0; s < HD / 16; ++s) k[s] = *reinterpret_cast<const F*>(p + (s * 64 + lane) * 8);
+}
+// features of one column as operand: 16 s + 8 half + 0..7
+template <typename T, int HD>
+__device__ __forceinline__ void load_column(const T* p, int half, typename AttnFrag<T>::type (&q)[HD / 16]) {
+#pragma unroll
+  for (int s = 0; s < HD / 16; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[s][e] = p ? p[16 * s + 8 * half + e] : from_f32<T>(0.f);
+}
+
+// (reference, sum of exponentials against it).  The reference is the largest score times the scale, rounded, and is the same number
+// wherever it is taken away: scale times a difference of two scores is not, by 2^-24 of the references.
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+  const float m = fmaxf(a.x, b.x);
+  return {m, a.y * __builtin_amdgcn_exp2f(a.x - m) + b.y * __builtin_amdgcn_exp2f(b.x - m)};
+}
+// (reference, 1 / sum): a row that saw nothing gives nothing
+__device__ __forceinline__ float2 finish(float2 a) { return {a.x, a.y == 0.f ? 0.f : 1.f / a.y}; }
+
+// ---- few columns ---------------------------------------------------------------------------------------------
+
+// scores [seq][kvh][t][width] of columns below `width`; stats [seq][kvh][share][width]
+template <typename T, int HD, int NV>      // NV: groups of eight columns
+__global__ __launch_bounds__(THREADS) void k_weigh_scores(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
+  typedef typename AttnFrag<T>::type F;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const int share = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z;
+  const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
+  if (!c.ok) {
+    if (share == 0 && kvh == 0 && tid == 0) set_status(kv.status, chunk_fault(ch, seq));
+    return;
+  }
+  const int units = (c.total + 31) / 32, begin = share * p.share_units, end = min(begin + p.share_units, units);
+  if (c.rows == 0 || begin >= end) return;
+  const int G = a.hq / kv.hkv, cols = c.rows * G;
+  F q[HD / 16], k[HD / 16], next[HD / 16] = {};
+  const int mine = lane & 31;
+  load_column<T, HD>(mine < cols ? (const T*)a.q + (int64_t)(c.first_row + c.first + mine / G) * a.q_stride + (int64_t)(kvh * G + mine % G) * HD : nullptr, half, q);
+  int sees[4 * NV];                    // last slot that a column sees
+  float m[4 * NV], l[4 * NV];
+#pragma unroll
+  for (int v = 0; v < 4 * NV; ++v) {
+    const int col = 8 * (v >> 2) + 4 * half + (v & 3);
+    sees[v] = col < cols ? c.len + c.first + col / G : -1;
+    m[v] = ATTN_UNSEEN;
+    l[v] = 0.f;
+  }
+  float* scores = a.scratch + p.stats_floats + ((int64_t)seq * kv.hkv + kvh) * p.tokens * p.width;
+  const T* at = begin + wave < end ? unit_at<T>(kv, seq, kvh, begin + wave, HD) : nullptr;
+  if (at) load_unit<T, HD>(at, lane, next);
+  for (int u = begin + wave; u < end; u += WAVES) {
+    const bool there = at != nullptr;
+    if (!there && lane == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) k[s] = next[s];
+    if (u + WAVES < end) {
+      at = unit_at<T>(kv, seq, kvh, u + WAVES, HD);
+      if (at) load_unit<T, HD>(at, lane, next);
+    }
+    f32x16_t x = {};
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) x = attn_mma(q[s], k[s], x);
+    const int slot = 32 * u + mine;
+#pragma unroll
+    for (int v = 0; v < 4 * NV; ++v) {
+      const bool seen = there && slot <= sees[v];
+      const float top = seen ? fmaxf(m[v], x[v] * a.scale) : m[v];
+      const float e = seen ? __builtin_amdgcn_exp2f(fmaf(x[v], a.scale, -top)) : 0.f;
+      l[v] = l[v] * __builtin_amdgcn_exp2f(m[v] - top) + e;
+      m[v] = top;
+      x[v] = seen ? x[v] : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (8 * i + 4 * half < p.width && slot < c.total)
+        *reinterpret_cast<f32x4_t*>(scores + (int64_t)slot * p.width + 8 * i + 4 * half) = f32x4_t{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+  }
+  __shared__ float2 part[WAVES][32];
+#pragma unroll
+  for (int v = 0; v < 4 * NV; ++v) {
+    float2 r = {m[v], l[v]};
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) r = join(r, float2{__shfl_xor(r.x, o, 64), __shfl_xor(r.y, o, 64)});
+    if (mine == 0) part[wave][8 * (v >> 2) + 4 * half + (v & 3)] = r;
+  }
+  __syncthreads();
+  if (tid < p.width) {
+    float2 r = part[0][tid];
+    for (int w = 1; w < WAVES; ++w) r = join(r, part[w][tid]);
+    reinterpret_cast<float2*>(a.scratch)[(((int64_t)seq * kv.hkv + kvh) * p.shares + share) * p.width + tid] = r;
+  }
+}
+
+__global__ __launch_bounds__(THREADS) void k_weigh_sum(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
+  const int tid = threadIdx.x, kvh = blockIdx.y, seq = blockIdx.z, slot = blockIdx.x * THREADS + tid;
+  const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
+  if (!c.ok || c.rows == 0 || (int)blockIdx.x * THREADS >= c.total) return;
+  __shared__ float2 col[32];
+  const int64_t head = (int64_t)seq * kv.hkv + kvh;
+  if (tid < p.width) {
+    const int shares = ((c.total + 31) / 32 + p.share_units - 1) / p.share_units;
+    const float2* s = reinterpret_cast<const float2*>(a.scratch) + head * p.shares * p.width + tid;
+    float2 r = s[0];
+    for (int i = 1; i < shares; ++i) r = join(r, s[(int64_t)i * p.width]);
+    col[tid] = finish(r);
+  }
+  __syncthreads();
+  if (slot >= c.total) return;
+  const float* x = a.scratch + p.stats_floats + (head * p.tokens + slot) * p.width;
+  float sum = 0.f;
+  for (int i = 0; i < p.width; i += 4) {
+    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(x + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)        // (minus infinity: not seen, also by a row that is NaN)
+      sum = v[e] == -INFINITY ? sum : fmaf(__builtin_amdgcn_exp2f(fmaf(v[e], a.scale, -col[i + e].x)), col[i + e].y, sum);
+  }
+  const int64_t at = head * a.slots + slot;
+  a.mass[at] = (a.before && slot < c.len ? a.before[at] : 0.f) + sum;
+}
+
+// ---- many columns --------------------------------------------------------------------------------------------
+
+// columns of a sequence and kv head begin at this one of the statistics
+__device__ __forceinline__ int64_t first_column(const WeighPlan& p, const WeighSeq& c, const PagedDev& kv, int G, int seq, int kvh) {
+  return p.packed ? ((int64_t)c.first_row * kv.hkv + (int64_t)kvh * (c.total - c.len)) * G : ((int64_t)seq * kv.hkv + kvh) * p.most_rows * G;
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(THREADS) void k_weigh_stats(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
+  typedef typename AttnFrag<T>::type F;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const int share = blockIdx.x % p.shares, tile = blockIdx.x / p.shares * WAVES + wave, kvh = blockIdx.y, seq = blockIdx.z;
+  const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
+  if (!c.ok) {
+    if (blockIdx.x == 0 && kvh == 0 && tid == 0) set_status(kv.status, chunk_fault(ch, seq));
+    return;
+  }
+  const int G = a.hq / kv.hkv, cols = c.rows * G, col = 32 * tile + (lane & 31);
+  if (32 * tile >= cols) return;       // (no barrier below)
+  const int row = c.first + min(col, cols - 1) / G;
+  const int low_row = c.first + 32 * tile / G, top_row = c.first + min(32 * tile + 31, cols - 1) / G;
+  const int begin = share * p.share_units, end = min(begin + p.share_units, (c.len + top_row) / 32 + 1);
+  F q[HD / 16], k[HD / 16], next[HD / 16] = {};
+  load_column<T, HD>(col < cols ? (const T*)a.q + (int64_t)(c.first_row + row) * a.q_stride + (int64_t)(kvh * G + col % G) * HD : nullptr, half, q);
+  float m = ATTN_UNSEEN, l = 0.f;
+  const T* at = begin < end ? unit_at<T>(kv, seq, kvh, begin, HD) : nullptr;
+  if (at) load_unit<T, HD>(at, lane, next);
+  for (int u = begin; u < end; ++u) {
+    const bool there = at != nullptr;
+    if (!there && lane == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) k[s] = next[s];
+    if (u + 1 < end) {
+      at = unit_at<T>(kv, seq, kvh, u + 1, HD);
+      if (at) load_unit<T, HD>(at, lane, next);
+    }
+    if (!there) continue;
+    f32x16_t x = {};
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) x = attn_mma(k[s], q[s], x);
+    const bool whole = 32 * u + 31 <= c.len + low_row;
+    if (!whole) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[v] = 32 * u + 8 * (v >> 2) + 4 * half + (v & 3) <= c.len + row ? x[v] : -INFINITY;
+    }
+    float top = attn_max3(x[0], x[1], x[2]);
+#pragma unroll
+    for (int v = 3; v < 15; v += 2) top = attn_max3(top, x[v], x[v + 1]);
+    const float ref = fmaxf(m, fmaxf(top, x[15]) * a.scale);
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(fmaf(x[v], a.scale, -ref));
+    l = fmaf(l, __builtin_amdgcn_exp2f(m - ref), sum);
+    m = ref;
+  }
+  const float2 r = join(float2{m, l}, float2{__shfl_xor(m, 32, 64), __shfl_xor(l, 32, 64)});
+  if (half == 0 && col < cols) {
+    float2* out = reinterpret_cast<float2*>(a.scratch) + share * p.columns + first_column(p, c, kv, G, seq, kvh) + col;
+    *out = p.shares > 1 ? r : finish(r);
+  }
+}
+
+// the shares' statistics together, in the first one's place
+__global__ __launch_bounds__(THREADS) void k_weigh_join(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
+  const int kvh = blockIdx.y, seq = blockIdx.z, col = blockIdx.x * THREADS + threadIdx.x;
+  const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
+  const int G = a.hq / kv.hkv;
+  if (!c.ok || col >= c.rows * G) return;
+  float2* s = reinterpret_cast<float2*>(a.scratch) + first_column(p, c, kv, G, seq, kvh) + col;
+  const int shares = (c.total + 31) / 32;
+  float2 r = s[0];
+  for (int i = 1; i < p.shares && i * p.share_units < shares; ++i) r = join(r, s[i * p.columns]);
+  *s = finish(r);
+}
+
+// KU units of 32 keys a wave
+template <typename T, int HD, int KU>
+__global__ __launch_bounds__(THREADS) void k_weigh_add(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
+  typedef typename AttnFrag<T>::type F;
+  __shared__ __align__(16) F tile_q[HD / 16 * 64];
+  __shared__ __align__(16) float ref[32], inv[32];
+  __shared__ int sees[32];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const int part = blockIdx.x % p.parts, tile = blockIdx.x / p.parts, kvh = blockIdx.y, seq = blockIdx.z;
+  const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
+  const int tile0 = tile * WAVES * KU * 32;
+  if (!c.ok || c.rows == 0 || tile0 >= c.total) return;
+  const int G = a.hq / kv.hkv, cols = c.rows * G;
+  F k[KU][HD / 16];
+  bool there[KU];
+  float sum[KU];
+  const int unit0 = tile0 / 32 + wave * KU;
+#pragma unroll
+  for (int i = 0; i < KU; ++i) {
+    const T* at = 32 * (unit0 + i) < c.total ? unit_at<T>(kv, seq, kvh, unit0 + i, HD) : nullptr;
+    there[i] = at != nullptr;
+    sum[i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) k[i][s] = F{};
+    if (at) load_unit<T, HD>(at, lane, k[i]);
+  }
+  const float2* stats = reinterpret_cast<const float2*>(a.scratch) + first_column(p, c, kv, G, seq, kvh);
+  // column tiles of this part, less those whose rows all end before the first key
+  const int tiles = (cols + 31) / 32, each = (tiles + p.parts - 1) / p.parts;
+  const int first_needed = max(0, tile0 - c.len - c.first) * G / 32;
+  const int t0 = max(part * each, first_needed), t1 = min((part + 1) * each, tiles);
+  for (int t = t0; t < t1; ++t) {
+    __syncthreads();
+    for (int i = tid; i < HD / 8 * 32; i += THREADS) {                           // eight features of a column
+      const int col = 32 * t + i / (HD / 8), f = i % (HD / 8);
+      F v = {};
+      if (col < cols) {
+        const T* src = (const T*)a.q + (int64_t)(c.first_row + c.first + col / G) * a.q_stride + (int64_t)(kvh * G + col % G) * HD + 8 * f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = src[e];
+      }
+      tile_q[(f >> 1) * 64 + (f & 1) * 32 + i / (HD / 8)] = v;
+    }
+    if (tid < 32) {
+      const int col = 32 * t + tid;
+      const float2 s = col < cols ? stats[col] : float2{0.f, 0.f};
+      ref[tid] = s.x; inv[tid] = s.y;
+      sees[tid] = col < cols ? c.len + c.first + col / G : -1;
+    }
+    __syncthreads();
+    f32x16_t x[KU] = {};
+    float of_tile[KU] = {};            // (tiles by themselves: 16 and then hundreds of additions in a row, not thousands)
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) {
+      const F q = tile_q[s * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < KU; ++i) x[i] = attn_mma(q, k[i][s], x[i]);
+    }
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int col = 8 * (v >> 2) + 4 * half + (v & 3);
+      const float r = ref[col], w = inv[col];
+      const int last = sees[col];
+#pragma unroll
+      for (int i = 0; i < KU; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(x[i][v], a.scale, -r));
+        of_tile[i] = 32 * (unit0 + i) + (lane & 31) <= last ? fmaf(e, w, of_tile[i]) : of_tile[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < KU; ++i) sum[i] += of_tile[i];
+  }
+  const int64_t head = (int64_t)seq * kv.hkv + kvh;
+#pragma unroll
+  for (int i = 0; i < KU; ++i) {
+    const float all = there[i] ? attn_sum_of_halves(sum[i]) : 0.f;
+    const int slot = 32 * (unit0 + i) + (lane & 31);
+    if (half == 0 && slot < c.total) {
+      const int64_t at = head * a.slots + slot;
+      if (p.parts > 1) a.scratch[p.stats_floats + (part * (int64_t)kv.batch * kv.hkv + head) * p.tokens + slot] = all;
+      else a.mass[at] = (a.before && slot < c.len ? a.before[at] : 0.f) + all;
+    }
+  }
+}
+
+__global__ __launch_bounds__(THREADS) void k_weigh_parts(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
+  const int kvh = blockIdx.y, seq = blockIdx.z, slot = blockIdx.x * THREADS + threadIdx.x;
+  const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
+  if (!c.ok || c.rows == 0 || slot >= c.total) return;
+  const int64_t head = (int64_t)seq * kv.hkv + kvh, at = head * a.slots + slot;
+  const float* s = a.scratch + p.stats_floats + head * p.tokens + slot;
+  float sum = 0.f;
+  for (int i = 0; i < p.parts; ++i) sum += s[i * (int64_t)kv.batch * kv.hkv * p.tokens];
+  a.mass[at] = (a.before && slot < c.len ? a.before[at] : 0.f) + sum;
+}
+
+template <typename T, int HD>
+hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const WeighArgs& a, const WeighPlan& p) {
+  const dim3 tokens((unsigned)((p.tokens + THREADS - 1) / THREADS), kv.hkv, kv.batch), wg(THREADS);
+  if (p.width) {
+    const dim3 grid(p.shares, kv.hkv, kv.batch);
+    if (p.width <= 8) hipLaunchKernelGGL((k_weigh_scores<T, HD, 1>), grid, wg, 0, st, kv, ch, a, p);
+    else if (p.width <= 16) hipLaunchKernelGGL((k_weigh_scores<T, HD, 2>), grid, wg, 0, st, kv, ch, a, p);
+    else hipLaunchKernelGGL((k_weigh_scores<T, HD, 4>), grid, wg, 0, st, kv, ch, a, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_weigh_sum, tokens, wg, 0, st, kv, ch, a, p);
+    return hipGetLastError();
+  }
+  const int G = a.hq / kv.hkv, tiles = (int)(((int64_t)p.most_rows * G + 31) / 32);
+  hipLaunchKernelGGL((k_weigh_stats<T, HD>), dim3((tiles + WAVES - 1) / WAVES * p.shares, kv.hkv, kv.batch), wg, 0, st, kv, ch, a, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (p.shares > 1) {
+    hipLaunchKernelGGL(k_weigh_join, dim3((32 * tiles + THREADS - 1) / THREADS, kv.hkv, kv.batch), wg, 0, st, kv, ch, a, p);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  constexpr int KU = sizeof(T) == 2 ? 2 : 1, KEYS = WAVES * KU * 32;
+  hipLaunchKernelGGL((k_weigh_add<T, HD, KU>), dim3((unsigned)((p.tokens + KEYS - 1) / KEYS) * p.parts, kv.hkv, kv.batch), wg, 0, st, kv, ch, a, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.parts == 1) return e;
+  hipLaunchKernelGGL(k_weigh_parts, tokens, wg, 0, st, kv, ch, a, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int last, int len_bound) {
+  WeighPlan p{};
+  const int G = hq / hkv, rows = std::min(std::min(max_rows, total_rows), last > 0 ? last : max_rows);
+  const int64_t cols = (int64_t)rows * G, heads = (int64_t)batch * hkv;
+  p.most_rows = rows;
+  p.tokens = ((int64_t)len_bound + std::min(max_rows, total_rows) + 31) / 32 * 32;
+  const int units = (int)(p.tokens / 32);
+  if (cols <= 32) {
+    p.width = cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 16 ? 16 : 32;
+    const int64_t most = std::max<int64_t>(1, 2048 / heads);                     // shares of a sequence and kv head
+    p.share_units = (int)std::max<int64_t>(4, (units + most - 1) / most);
+    p.shares = (units + p.share_units - 1) / p.share_units;
+    p.stats_floats = 2 * heads * p.shares * p.width;
+    p.scratch_floats = p.stats_floats + heads * p.tokens * p.width;
+    return p;
+  }
+  p.packed = (int64_t)total_rows < (int64_t)batch * rows;
+  p.columns = (p.packed ? (int64_t)total_rows : (int64_t)batch * rows) * hq;
+  const int64_t groups = ((cols + 31) / 32 + WAVES - 1) / WAVES * heads;
+  const int64_t most = std::max<int64_t>(1, 1024 / groups);
+  p.share_units = (int)std::max<int64_t>(16, (units + most - 1) / most);
+  p.shares = (units + p.share_units - 1) / p.share_units;
+  p.stats_floats = 2 * p.columns * p.shares;
+  const int keys = WAVES * 32 * (dtype == ESP_BF16 ? 2 : 1);
+  const int64_t key_groups = (p.tokens + keys - 1) / keys * heads;
+  p.parts = (int)std::max<int64_t>(1, std::min<int64_t>((cols + 255) / 256, 1024 / key_groups));
+  p.scratch_floats = p.stats_floats + (p.parts > 1 ? p.parts * heads * p.tokens : 0);
+  return p;
+}
+
+int64_t weigh_workgroups(const WeighPlan& p, int batch, int hkv, int G) {
+  const int64_t tiles = ((int64_t)p.most_rows * G + 31) / 32, heads = (int64_t)batch * hkv;
+  return std::max<int64_t>({p.tokens / 128 + 1, (tiles / WAVES + 1) * p.shares, (p.tokens / 128 + 1) * std::max(1, p.parts)}) * heads;
+}
+
+hipError_t launch_paged_weigh(hipStream_t st, int dtype, int hd, const PagedDev& kv, const ChunkDev& ch, const WeighArgs& a, const WeighPlan& p) {
+  if (dtype == ESP_BF16) return hd == 128 ? launch<bf16_t, 128>(st, kv, ch, a, p) : launch<bf16_t, 64>(st, kv, ch, a, p);
+  return hd == 128 ? launch<float, 128>(st, kv, ch, a, p) : launch<float, 64>(st, kv, ch, a, p);
+}

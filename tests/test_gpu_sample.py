@@ -1,0 +1,264 @@
+"""The choice of tokens from logits (sample) against its definition in 64 bits.
+
+Whole numbers have to be equal.  The kernel's weights are off by 7e-12 of themselves (what its series leaves out) and by half of 2^-S, S = min(50, 62 - ceil
+log2 vocab), where the largest weighs 1.  A sum of n of them is off by n times that at most, a border's place among all, W, by twice (7e-12 + n 2^-S-1 / W);
+beside it 1e-13 for the reference's own sums.  Where the number u, or a limit, is nearer to a border than that, both sides of it are right and the row
+says nothing; a test says how many such rows it may have.  probs: the quotient rounded to fp32, and those errors."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from util import ROOT  # noqa: F401
+
+from paper_2603_17942_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def choose(x, T, k, p, m, u):
+    """(id, share, nearest border) of one row x (float64 numpy) by the definition."""
+    x = np.where(np.isnan(x), -np.inf, np.minimum(x, float(np.finfo(np.float32).max)))
+    alive = np.flatnonzero(x > -np.inf)
+    if len(alive) == 0 or not (0 <= T < math.inf) or math.isnan(p) or math.isnan(m):
+        return -1, 0.0, math.inf
+    order = alive[np.lexsort((alive, -x[alive]))]
+    if T == 0:
+        return int(order[0]), 1.0, math.inf
+    w = np.exp((x[order] - x[order[0]]) / T)
+    near = math.inf                                    # nearest border, in units of what it may be off by
+    half_step = 2.0 ** -(min(50, 62 - math.ceil(math.log2(len(x)))) + 1)
+    allowed = lambda n, total: 2 * (7e-12 + n * half_step / total) + 1e-13          # noqa: E731
+    if k > 0:
+        w = w[:k]
+    if p < 1:
+        before = np.concatenate([[0.0], np.cumsum(w)])
+        goal = max(p, 0.0) * before[-1]
+        if goal > 0:
+            near = min(near, np.abs(before[1:-1] - goal).min(initial=math.inf) / before[-1] / allowed(len(w), before[-1]))
+        w = w[:max(1, int(np.count_nonzero(before[:-1] < goal)))]
+    if m > 0:
+        # (what weighs less than 1e-9 makes no difference that the other errors do not make)
+        near = min(near, (np.abs(w - min(m, 1.0)) / (7e-12 * w + 2 * half_step))[(w < 1) & (w > 1e-9)].min(initial=math.inf))
+        w = w[:max(1, int(np.count_nonzero(w >= min(m, 1.0))))]
+    by_id = np.argsort(order[:len(w)])
+    run, total = np.cumsum(w[by_id]), math.fsum(w)
+    goal = min(max(u, 0.0), 1 - 2.0 ** -24) * total if u == u else 0.0
+    at = min(int(np.count_nonzero(run <= goal)), len(w) - 1)
+    if goal > 0:
+        near = min(near, np.abs(run - goal).min() / total / allowed(len(w), total))
+    return int(order[by_id[at]]), float(w[by_id[at]] / total), near
+
+
+def dev(t):
+    return None if t is None else t.cuda()
+
+
+def check(x, u, T=None, k=None, p=None, m=None, silent=0):
+    """x: CPU logits; returns ids.  silent: rows that may be too near a border."""
+    ids, probs = B.sample(x.cuda(), u.cuda(), dev(T), dev(k), dev(p), dev(m))
+    n, quiet = x.shape[0], 0
+    for r in range(n):
+        want, share, near = choose(x[r].double().numpy(), 1.0 if T is None else float(T[r]), 0 if k is None else int(k[r]), 1.0 if p is None else float(p[r]),
+                                   0.0 if m is None else float(m[r]), float(u[r]))
+        if near < 1:
+            quiet += 1
+            continue
+        assert int(ids[r]) == want, (r, int(ids[r]), want, share)
+        assert abs(float(probs[r]) - share) <= 2.0 ** -23 * share + 1e-9, (r, float(probs[r]), share)
+    assert quiet <= silent
+    again, _ = B.sample(x.cuda(), u.cuda(), dev(T), dev(k), dev(p), dev(m))
+    assert torch.equal(ids, again)
+    return ids
+
+
+def limits(n, seed):
+    """Every combination of limits, a greedy row in eight."""
+    g = gen(seed)
+    has = torch.arange(n) % 8
+    T = torch.where(has == 0, 0.0, 0.3 + 1.2 * torch.rand(n, generator=g))
+    k = torch.where((has & 1) == 1, torch.randint(1, 200, (n,), generator=g), 0).to(torch.int32)
+    p = torch.where((has & 2) == 2, torch.rand(n, generator=g), 1.0)
+    m = torch.where((has & 4) == 4, torch.rand(n, generator=g) ** 3, 0.0)
+    return T, k, p, m
+
+
+def logits(n, vocab, seed, spread=2.0, dtype=torch.float32):
+    g = gen(seed)
+    x = spread * torch.randn((n, vocab), generator=g)
+    # some rows are sure of a few tokens
+    for r in range(0, n, 2):
+        at = torch.randint(0, vocab, (min(20, vocab),), generator=g)
+        x[r, at] += 12 * torch.rand(len(at), generator=g)
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [1, 2, 3, 63, 64, 255, 257, 1000, 4096, 4097, 8197, 50001, 128256])
+def test_every_combination_of_limits(vocab, dtype):
+    n = 48 if vocab < 10000 else 24
+    check(logits(n, vocab, vocab, dtype=dtype), torch.rand(n, generator=gen(vocab + 1)), *limits(n, vocab + 2))
+
+
+@pytest.mark.parametrize("vocab", [151936, 200003])
+def test_large_vocabularies_without_limits(vocab):
+    check(logits(12, vocab, 5), torch.rand(12, generator=gen(6)))
+    check(logits(12, vocab, 7, dtype=torch.bfloat16), torch.rand(12, generator=gen(8)), T=torch.full((12,), 0.7))
+
+
+@pytest.mark.parametrize("spread", [1e-4, 1e-2, 0.3, 8.0, 60.0])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_flat_and_steep_rows(spread, dtype):
+    """1e-4 and 1e-2: far more tokens in one step of the first division than LDS holds."""
+    n, vocab = 16, 40000
+    x = (spread * torch.randn((n, vocab), generator=gen(1))).to(dtype)
+    T, k, p, m = limits(n, 2)
+    k = torch.where(torch.arange(n) % 3 == 0, k * 150, k).to(torch.int32)
+    check(x, torch.rand(n, generator=gen(3)), T, k, p, m, silent=1)
+    check(x + 50.0, torch.rand(n, generator=gen(4)), T, k, p, m, silent=1)
+
+
+@pytest.mark.parametrize("vocab", [7, 5000, 60000])
+@pytest.mark.parametrize("values", [1, 2, 5, 70])
+def test_equal_logits_go_by_id(vocab, values):
+    n = 24
+    g = gen(values)
+    table = torch.randn(values, generator=g)
+    x = table[torch.randint(0, values, (n, vocab), generator=g)]
+    T, k, p, m = limits(n, 4)
+    k[1], k[3] = 1, vocab // 2 + 1
+    check(x, torch.rand(n, generator=g), T, k, p, m, silent=1)
+    if values == 1:                                    # one value: the lowest ids, evenly
+        k = torch.full((n,), min(vocab, 5), dtype=torch.int32)
+        ids = check(x, (torch.arange(n) % 5 + 0.5) / 5, k=k)
+        if vocab >= 5:
+            assert ids.tolist() == [i % 5 for i in range(n)]
+        p = torch.full((n,), 0.5)
+        ids = check(torch.zeros((n, 64)), torch.full((n,), 0.99999), p=p, silent=n)
+        assert ids.tolist() == [31] * n                # before the 33rd lies half of all, not less
+
+
+def test_zeros_of_both_signs_are_equal():
+    x = torch.full((2, 300), -0.0)
+    x[0, 5], x[1, 200] = 0.0, 0.0
+    assert B.sample(x.cuda(), torch.zeros(2).cuda(), temperature=torch.zeros(2).cuda())[0].tolist() == [0, 0]
+    assert check(x, torch.full((2,), 0.99), k=torch.tensor([3, 3], dtype=torch.int32)).tolist() == [2, 2]
+
+
+def test_masks_infinities_and_nan():
+    vocab, low = 9000, float(torch.finfo(torch.float32).min)
+    x = logits(12, vocab, 9)
+    mask = torch.rand((12, vocab), generator=gen(10)) < 0.7
+    x[0:3] = x[0:3].masked_fill(mask[0:3], -math.inf)
+    x[3:5] = x[3:5].masked_fill(mask[3:5], low)
+    x[5:7] = x[5:7].masked_fill(mask[5:7], math.nan)
+    x[7] = -math.inf                                   # nothing left
+    x[8] = math.nan
+    x[9] = low                                         # all masked alike: all alike
+    x[10, [17, 4000, 8999]] = math.inf
+    x[11] = -math.inf
+    x[11, 8998] = -3.0
+    for T, k, p, m in ((None,) * 4, limits(12, 11), (torch.zeros(12), None, None, None), (None, torch.full((12,), 2, dtype=torch.int32), torch.full((12,), 0.9), None)):
+        ids = check(x, torch.rand(12, generator=gen(12)), T, k, p, m)
+        assert ids[7] == -1 and ids[8] == -1 and ids[11] == 8998 and int(ids[10]) in (17, 4000, 8999)
+        assert all(not bool(mask[r, int(ids[r])]) for r in range(7))
+
+
+def test_limits_at_their_ends():
+    x = logits(8, 3000, 20)
+    u = torch.rand(8, generator=gen(21))
+    ones = torch.ones(8)
+    for T in (1e-30, 1e-45, 1e-3, 100.0, 3e38):
+        check(x, u, T=T * ones, silent=1)
+    for k in (-5, 0, 1, 2999, 3000, 3001, 2 ** 31 - 1):
+        check(x, u, k=torch.full((8,), k, dtype=torch.int32))
+    for p in (-1.0, 0.0, 1e-30, 0.999999, 1.0, 7.0):
+        check(x, u, p=p * ones, silent=1)
+    for m in (-1.0, 0.0, 1e-30, 1e-12, 1.0, 7.0):
+        check(x, u, m=m * ones)
+    for v in (0.0, -1.0, 1.0, 2.0, math.nan, 1 - 2.0 ** -24, 1e-38):
+        check(x, torch.full((8,), v))
+        check(x, torch.full((8,), v), k=torch.full((8,), 40, dtype=torch.int32))
+    for bad in (dict(T=-ones), dict(T=math.inf * ones), dict(T=math.nan * ones), dict(p=math.nan * ones), dict(m=math.nan * ones)):
+        assert check(x, u, **bad).tolist() == [-1] * 8
+
+
+def test_even_numbers_give_every_token_its_share():
+    """u on a grid of n: the inverse of a distribution function, so a token of share s is chosen n s times, one more or less."""
+    vocab, n = 37, 20000
+    x = 1.5 * torch.randn((1, vocab), generator=gen(30))
+    u = ((torch.arange(n) + 0.5) / n)
+    ids, _ = B.sample(x.cuda().expand(n, vocab).contiguous(), u.cuda(), temperature=torch.full((n,), 0.8).cuda())
+    share = torch.softmax(x[0].double() / 0.8, 0)
+    got = torch.bincount(ids.cpu().long(), minlength=vocab).double()
+    assert (got - n * share).abs().max() <= 1.0 + 1e-3
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("off,pad", [(0, 0), (1, 3), (8, 8), (3, 5)])
+def test_rows_that_lie_apart(off, pad, dtype):
+    n, vocab = 9, 5003
+    big = torch.full((n, off + vocab + pad), math.inf, dtype=dtype)          # what is around would be chosen
+    big[:, off:off + vocab] = logits(n, vocab, 40, dtype=dtype)
+    u, lim = torch.rand(n, generator=gen(41)), limits(n, 42)
+    want = check(big[:, off:off + vocab].contiguous(), u, *lim)
+    got, _ = B.sample(big.cuda()[:, off:off + vocab], u.cuda(), *(t.cuda() for t in lim))
+    assert torch.equal(got, want)
+
+
+def test_outputs_without_probs_and_no_rows():
+    x, u = logits(5, 700, 50).cuda(), torch.rand(5, generator=gen(51)).cuda()
+    ids, probs = torch.full((5,), -7, dtype=torch.int32).cuda(), torch.full((5,), -7.0).cuda()
+    a, b = B.sample(x, u, ids=ids, probs=probs)
+    assert a is ids and b is probs and (ids >= 0).all() and (probs > 0).all()
+    lib, only = B.load_library(), torch.full((6,), -7, dtype=torch.int32).cuda()
+    assert lib.esp_sample(B._stream_ptr(), B.ESP_F32, x.data_ptr(), 700, 5, 700, None, None, None, None, u.data_ptr(), only.data_ptr(), None) == 0
+    assert torch.equal(only[:5], ids) and int(only[5]) == -7
+    assert B.sample(x[:0], u[:0])[0].numel() == 0
+
+
+def test_a_captured_call_follows_its_inputs():
+    n, vocab = 6, 20000
+    x, u = torch.empty((n, vocab)).cuda(), torch.empty(n).cuda()
+    T, k, p, m = (torch.empty_like(t).cuda() for t in limits(n, 1))
+    ids, probs = torch.empty(n, dtype=torch.int32).cuda(), torch.empty(n).cuda()
+    B.sample(x.zero_(), u.zero_(), T.fill_(1), k.zero_(), p.fill_(1), m.zero_(), ids=ids, probs=probs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.sample(x, u, T, k, p, m, ids=ids, probs=probs)
+    for i in range(4):
+        new = [logits(n, vocab, 60 + i), torch.rand(n, generator=gen(70 + i)), *limits(n, 80 + i)]
+        for t, v in zip((x, u, T, k, p, m), new):
+            t.copy_(v)
+        ids.fill_(-9)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = check(*new)
+        assert torch.equal(ids, want)
+
+
+def test_two_streams_at_once():
+    n, vocab = 40, 60000
+    x, u, lim = logits(n, vocab, 90).cuda(), torch.rand(n, generator=gen(91)).cuda(), [t.cuda() for t in limits(n, 92)]
+    want = B.sample(x, u, *lim)[0]
+    torch.cuda.synchronize()
+    streams, out = [torch.cuda.Stream() for _ in range(2)], []
+    for i in range(6):
+        with torch.cuda.stream(streams[i % 2]):
+            out.append(B.sample(x, u, *lim)[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in out)
+
+
+def test_rows_behind_31_bits_of_elements():
+    vocab, n = 131072, 16390                           # the last rows' first elements lie behind 2^31
+    x = torch.zeros((n, vocab), dtype=torch.bfloat16, device="cuda")
+    at = (torch.arange(n, device="cuda") * 7919) % vocab
+    x[torch.arange(n, device="cuda"), at] = 30.0       # weight of all others: 1.2e-8
+    ids, _ = B.sample(x, torch.full((n,), 0.5, device="cuda"))
+    assert torch.equal(ids, at.int())
