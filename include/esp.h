@@ -375,11 +375,15 @@ esp_status esp_softmax_topk_static(void *stream, const float *logits, int32_t ro
  *   ids         device int32 [rows]; probs NULL or device fp32 [rows]: the token's share of the kept weights (temperature 0: 1)
  * Minus infinity and NaN are tokens that cannot be chosen, plus infinity is as the largest finite fp32 value.  A row without any other, and a row
  * whose temperature is negative or not finite or whose top_p or min_p is NaN, gets -1 and 0.
- * Weights are taken in fp64 (7e-12) and added up as integers of 2^-S of the largest, S = min(50, 62 - ceil log2 vocab): what a call chooses
- * does not depend on the order of the sums, and tokens of less than half of that are not chosen.
- * Errors: EINVAL (null pointers, rows < 0, vocab < 1), ESHAPE (row_stride < vocab), EDTYPE, ECAPACITY (vocab above 2^24, 2^22 rows and more). */
+ * Temperatures between 0 and 1e-20 are as 1e-20, above 1e20 as 1e20.  Weights are taken in fp64 (1.1e-12 of themselves) and added up in units of 2^-S of
+ * the largest, S = min(45, 62 - ceil log2 vocab); tokens of less than half a unit are not chosen.  The same call chooses the same tokens.
+ *   scratch     device, 16-byte aligned, esp_sample_scratch_bytes() (up to 185 KB a row of 128256, of up to 1024 rows: more are done in lots); calls that
+ *               overlap in time need one each.  Results do not depend on what it held
+ * Errors: EINVAL (null pointers, rows < 0, vocab < 1), ESHAPE (row_stride < vocab), EDTYPE, ECAPACITY (scratch; vocab above 2^22). */
+size_t esp_sample_scratch_bytes(int32_t rows, int32_t vocab);
 esp_status esp_sample(void* stream, int32_t dtype, const void* logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
-                      const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* ids, float* probs);
+                      const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* ids, float* probs, void* scratch,
+                      size_t scratch_bytes);
 
 /* ---- paged KV cache ------------------------------------------------------------------------
  * A cache whose sequences own pages anywhere in a pool, the rotation and the norms that come before it, and the

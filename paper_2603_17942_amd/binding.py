@@ -76,7 +76,7 @@ EXPORTS = ["esp_status_str", "esp_workspace_bytes", "esp_create", "esp_destroy",
            "esp_gemm_scratch_bytes", "esp_gemm", "esp_gemm_argmax_scratch_bytes", "esp_gemm_argmax", "esp_attn_tree", "esp_softmax_topk_scratch_bytes",
            "esp_softmax_topk", "esp_softmax_topk_static", "esp_profile_enable", "esp_profile_read", "esp_pack_weight", "esp_set_sampling",
            "esp_rope_make", "esp_rope_qk", "esp_paged_append", "esp_paged_attn_scratch_bytes", "esp_paged_attn", "esp_paged_commit",
-           "esp_paged_load", "esp_sample", "esp_paged_weigh_scratch_bytes", "esp_paged_weigh", "esp_paged_evict"]
+           "esp_paged_load", "esp_sample_scratch_bytes", "esp_sample", "esp_paged_weigh_scratch_bytes", "esp_paged_weigh", "esp_paged_evict"]
 SITES = {"gemm_layer": 0, "attn": 1, "attn_merge": 2, "lm_head": 3, "topk": 4, "tree": 5, "glue": 6}
 
 _lib = None
@@ -143,7 +143,9 @@ def load_library() -> C.CDLL:
     lib.esp_paged_attn.argtypes = [_vp, P(PagedKvStruct), _i32, P(ChunkStruct), _i32, _vp, _i64, _f32, _vp, _i32, _vp, _vp, C.c_size_t]
     lib.esp_paged_commit.argtypes = [_vp, P(PagedKvStruct), _vp, _vp, _vp]
     lib.esp_paged_load.argtypes = [_vp, P(PagedKvStruct), _i32, _i32, _i32, _i32, _vp, _vp]
-    lib.esp_sample.argtypes = [_vp, _i32, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.esp_sample_scratch_bytes.restype = C.c_size_t
+    lib.esp_sample_scratch_bytes.argtypes = [_i32, _i32]
+    lib.esp_sample.argtypes = [_vp, _i32, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t]
     lib.esp_paged_weigh_scratch_bytes.restype = C.c_size_t
     lib.esp_paged_weigh_scratch_bytes.argtypes = [P(PagedKvStruct), P(ChunkStruct), _i32, _i32]
     lib.esp_paged_weigh.argtypes = [_vp, P(PagedKvStruct), _i32, P(ChunkStruct), _i32, _vp, _i64, _f32, _i32, _vp, _vp, _i32, _vp, C.c_size_t]
@@ -587,12 +589,17 @@ def _floats(t: Optional[torch.Tensor], name: str, dev, shape) -> Optional[int]:
     return t.data_ptr()
 
 
+def sample_scratch_bytes(rows: int, vocab: int) -> int:
+    return load_library().esp_sample_scratch_bytes(rows, vocab)
+
+
 def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
            top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, ids: Optional[torch.Tensor] = None,
-           probs: Optional[torch.Tensor] = None):
+           probs: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None):
     """(ids, probs): one token a row of logits [rows, vocab] (rows may lie further apart) and its share of the tokens that were left, by the
     uniform numbers u [rows] in [0, 1).  temperature, top_k (int32), top_p, min_p [rows]: limits of each row, None for none; temperature 0 is
-    the arg-max.  A row without a token that can be chosen, or with limits that are none, gets -1 and 0."""
+    the arg-max.  A row without a token that can be chosen, or with limits that are none, gets -1 and 0.
+    scratch: uint8, sample_scratch_bytes."""
     lib = load_library()
     if logits.dim() != 2:
         raise ValueError("logits: [rows, vocab] wanted")
@@ -607,8 +614,13 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
     args = (_floats(temperature, "temperature", dev, n), _ints(top_k, "top_k", dev, n), _floats(top_p, "top_p", dev, n),
             _floats(min_p, "min_p", dev, n), _floats(u, "u", dev, n), _ints(ids, "ids", dev, n), _floats(probs, "probs", dev, n))
     code = _dtype_of(logits)
+    if scratch is None:
+        scratch = torch.empty(lib.esp_sample_scratch_bytes(rows, vocab), dtype=torch.uint8, device=dev)
+    if scratch.dtype is not torch.uint8 or scratch.device != dev or not scratch.is_contiguous():
+        raise ValueError("scratch: contiguous uint8 wanted")
     if rows:
-        _on_device(dev, lib.esp_sample, "esp_sample", code, logits.data_ptr(), s0 if rows > 1 else vocab, rows, vocab, *args)
+        _on_device(dev, lib.esp_sample, "esp_sample", code, logits.data_ptr(), s0 if rows > 1 else vocab, rows, vocab, *args, scratch.data_ptr(),
+                   scratch.numel())
     return ids, probs
 
 

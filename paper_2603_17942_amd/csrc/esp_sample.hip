@@ -1,16 +1,19 @@
 // One token a row from its logits: temperature, top-k, top-p, min-p, inverse distribution function over ids (esp_sample).
 //
-// Weights are integers: q_i = rint(2^S exp((l_i - max) / T)), the exponential in fp64, S as large as leaves room for the sum of a row's in 63
-// bits (50 at most).  Sums of them are the same in any order, so neither the histogram's atomics nor the division of the row among lanes
-// can move a border between two tokens.  fp32 weights would: with 1e-7 each, the borders of 128256 tokens of which a few thousand count
-// move by 1e-4 of all draws together.
+// w = exp((l - largest) / T) is computed in fp64 (1.1e-12 of itself) and added up in integers or, within a part of a row, in fp64 in a fixed order.
+// fp32 would not do: with 1e-7 for each weight the borders of 128256 tokens of which a few thousand count move by 1e-4 of all draws together.
 //
-// A workgroup has a row, a wave a sixteenth of it that lies in one piece, so that what waves add up is in the order of ids.  Passes over the row (the
-// first from memory, the others from the caches): the largest; then, where top-k or top-p can cut, a histogram of counts and sums over 4096
-// equal steps of log w, which says in what step the cut lies and with what count and sum before it.  The step's tokens go to LDS and are
-// divided further, by the bits of their logits, until a few (ranked by comparing all with all) or equal ones (arithmetic) are left: the cut is
-// a logit and how many of those equal to it are in.  Top-k first, as top-p is of its sum.  A last pass adds up what is in, by waves; the wave's
-// piece in which the target lies is looked through by all.
+// What goes over logits has them in registers, 4096 or 8192 a workgroup (a part of a row), so that one row is spread over many CUs; what decides has a
+// workgroup a row and looks at what the parts left.
+//   k_sample_parts  a part's largest logit and the first id that has it; where all tokens' weights count (no limit, or top-p without top-k) their sum
+//                   against that largest one; for top-k and top-p a histogram over equal steps of log w: how many tokens, and where in the step they lie
+//   k_sample_edges  the histograms together say in which steps the cut lies, for certain: counts are exact, weights known to 1e-3 from the places
+//   k_sample_collect the tokens of these steps to a list, what lies before them added up by parts (threads whose largest logit is below do not look again)
+//   k_sample_pick   the list is divided by the bits of its logits until a few tokens (ranked by comparing all with all) or equal ones (arithmetic) are left:
+//                   the cut is a logit and how many of those equal to it are in.  Top-k first, as top-p is of what it leaves.  The part in which the
+//                   target lies is looked through.
+// The two in the middle are launched where there are limits.  Rows that they cannot narrow down (more than 4096 tokens in the steps of the cut, or
+// logits above 2^20 steps) are divided in k_sample_pick by going over the row again and again, some 100 us.
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
@@ -19,22 +22,76 @@
 
 namespace {
 
-constexpr int WAVES = 16, THREADS = 64 * WAVES;
-constexpr int BINS = 4096;             // of the first division, 12 bytes each
-constexpr int SUB = THREADS;           // of the further ones: a thread each
-constexpr int LIST = 4096;             // tokens of one bin that go to LDS
+constexpr int PART_THREADS = 256;      // of what goes over logits
+constexpr int THREADS = 1024, WAVES = THREADS / 64;    // of what decides
+constexpr int BINS = 1024;             // steps of log w, 47 powers of two at most
+constexpr int PLACES = 512;            // that are told apart in a step.  A bin: tokens (up to 8192) << 44 | sum of places << 22 | of their squares / PLACES
+constexpr int LIST = 4096;             // tokens that may be listed
 constexpr int FEW = 64;                // that are ranked by comparing all with all
+constexpr int MOST_PARTS = THREADS;
+constexpr int ROWS_AT_ONCE = 1024;     // that the workspace is for; more are done one lot after the other
+constexpr float FAR_STEPS = 0x1p20f;   // logits of more steps than that have no place in one
+
+struct Part {
+  float top;                           // largest logit (infinity: as the largest finite value), and the first id that has it (-1: none)
+  int at;
+  double sum;                          // of the weights against it
+};
+struct PartSums { uint64_t all, in; }; // of what is before the list; less what min-p takes
+enum { AS_IT_IS = 0, COLLECT = 1, DIVIDE = 2 };        // without list; with it; by going over the row
+struct RowState {
+  int mode, first, last;               // steps of the list; what is before `first` is added up
+  unsigned before;                     // tokens before the list
+  int list_n;
+  float base;                          // step of the largest logit
+};
 
 struct SampleArgs {
   const void* logits;
   int64_t stride;
-  int rows, vocab, shift;              // shift: S
+  int vocab, shift;                    // shift: of the integers, S
+  int part, parts;                     // logits of a part, parts of a row
   const float* temperature;
   const int32_t* top_k;
   const float *top_p, *min_p, *u;
   int32_t* ids;
   float* probs;
+  // workspace: [rows][parts] and [rows]
+  Part* tops;
+  PartSums* sums;
+  uint64_t* bins;                      // [BINS]
+  float* maxima;                       // [PART_THREADS]
+  RowState* state;
+  uint64_t* list;                      // [LIST]  key << 32 | ~id: larger is earlier in the order
 };
+
+struct Limits {
+  float temperature, top_p, min_p;
+  int top_k;
+  bool valid, by_count, by_sum, by_part;
+};
+__device__ __forceinline__ Limits limits(const SampleArgs& a, int row) {
+  Limits m;
+  const float t = a.temperature ? a.temperature[row] : 1.f;
+  m.top_p = a.top_p ? a.top_p[row] : 1.f;
+  m.min_p = a.min_p ? a.min_p[row] : 0.f;
+  m.top_k = a.top_k ? a.top_k[row] : 0;
+  m.valid = t >= 0.f && t < INFINITY && m.top_p == m.top_p && m.min_p == m.min_p;
+  m.temperature = t > 0.f ? fminf(fmaxf(t, 1e-20f), 1e20f) : t;
+  m.by_count = m.top_k > 0 && m.top_k < a.vocab;
+  m.by_sum = m.top_p < 1.f;
+  m.by_part = m.min_p > 0.f;
+  return m;
+}
+__device__ __forceinline__ bool draws(const Limits& m) { return m.valid && m.temperature > 0.f; }
+__device__ __forceinline__ bool limited(const Limits& m) { return m.by_count || m.by_sum || m.by_part; }
+// do the weights of all tokens count
+__device__ __forceinline__ bool all_count(const Limits& m) { return !m.by_count && (m.by_sum || !m.by_part); }
+
+// powers of two, and steps of log w, that a unit of the logits is
+__device__ __forceinline__ double octaves(const Limits& m) { return 1.4426950408889634 / (double)m.temperature; }
+__device__ __forceinline__ float steps(const SampleArgs& a, const Limits& m) { return (float)(octaves(m) * (BINS / (double)(a.shift + 2))); }
+__device__ __forceinline__ float step_of(float x, float per) { return floorf(x * per); }
 
 // fp32 order as unsigned order; both zeros are one
 __device__ __forceinline__ unsigned key_of(float x) {
@@ -43,76 +100,68 @@ __device__ __forceinline__ unsigned key_of(float x) {
 }
 __device__ __forceinline__ float of_key(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// rint(2^shift 2^t), t <= 0: 2^t = 2^n 2^f, |f| <= 1/2, the series of exp(f ln 2) up to f^9 (7e-12 is left out), the integer from the low bits of
-// its sum with 2^52
+// Weights against a largest logit.  2^t = 2^n 2^f with |f| <= 1/2: n and the fraction by adding 1.5 2^52, 2^f = 1 + f p(f) with p of degree 7
+// (equal ripples of the relative error, 1.1e-12, found by exchange), n into the exponent.
 struct Weigher {
   double top, scale;                   // of (l - top) scale: log2 of the weight
-  float floor_t;                       // from here down there is nothing
-  int shift;
-  __device__ __forceinline__ double log2w(float l) const { return ((double)l - top) * scale; }
-  __device__ __forceinline__ uint64_t of_log(double t) const {
-    const double n = __builtin_rint(t), f = t - n;
-    double p = 1.01780860092396997e-7;                  // (ln 2)^i / i!
-    p = __builtin_fma(p, f, 1.32154867901443095e-6);
-    p = __builtin_fma(p, f, 1.52527338040598403e-5);
-    p = __builtin_fma(p, f, 1.54035303933816099e-4);
-    p = __builtin_fma(p, f, 1.33335581464284434e-3);
-    p = __builtin_fma(p, f, 9.61812910762847716e-3);
-    p = __builtin_fma(p, f, 5.55041086648215800e-2);
-    p = __builtin_fma(p, f, 2.40226506959100712e-1);
-    p = __builtin_fma(p, f, 6.93147180559945309e-1);
+  // 2^up w, up >= 0; what is no number, minus infinity or below 2^-900 weighs 2^-900
+  __device__ __forceinline__ double real(float l, int up) const {
+    const double t = __builtin_fmax(((double)l - top) * scale, -900.0);
+    const double k = t + 0x1.8p52, f = t - (k - 0x1.8p52);
+    double p = 1.3344183709045696e-06;
+    p = __builtin_fma(p, f, 1.5314209233228402e-05);
+    p = __builtin_fma(p, f, 0.00015403098285429032);
+    p = __builtin_fma(p, f, 0.001333343415751413);
+    p = __builtin_fma(p, f, 0.009618129558840711);
+    p = __builtin_fma(p, f, 0.05550410959228873);
+    p = __builtin_fma(p, f, 0.24022650694742584);
+    p = __builtin_fma(p, f, 0.6931471805412327);
     p = __builtin_fma(p, f, 1.0);
-    const double w = __builtin_ldexp(p, (int)n + shift) + 0x1p52;
-    return (uint64_t)__double_as_longlong(w) & 0xfffffffffffffull;
+    const int n = (int)__double_as_longlong(k) + up;
+    return __longlong_as_double(__double_as_longlong(p) + ((int64_t)n << 52));
   }
-  // 0 for what is no number, minus infinity, or too far down
-  __device__ __forceinline__ uint64_t operator()(float l) const {
-    const double t = log2w(l);
-    return t > (double)floor_t ? of_log(t) : 0ull;
+  // rint(2^up w), up <= 50: the low bits of its sum with 2^52
+  __device__ __forceinline__ uint64_t whole(float l, int up) const {
+    return (uint64_t)__double_as_longlong(real(l, up) + 0x1p52) & 0xfffffffffffffull;
   }
 };
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int by) {
-  const unsigned lo = __shfl_up((unsigned)v, by, 64), hi = __shfl_up((unsigned)(v >> 32), by, 64);
-  return (uint64_t)hi << 32 | lo;
+// A wave's running sums and reductions by data-parallel-primitive moves (a dozen cycles each; exchanges through LDS take ten times that, and these
+// chains are most of what the deciding kernels do): lanes 1, 2, 4, 8 back in a row of 16, then the last of a row to the next one, of two to the others.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned moved(unsigned v, unsigned idle) {
+  return (unsigned)__builtin_amdgcn_update_dpp((int)idle, (int)v, CTRL, ROWS, 0xf, false);
 }
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int by) {
-  const unsigned lo = __shfl_xor((unsigned)v, by, 64), hi = __shfl_xor((unsigned)(v >> 32), by, 64);
-  return (uint64_t)hi << 32 | lo;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t moved(uint64_t v, unsigned) {
+  return (uint64_t)moved<CTRL, ROWS>((unsigned)(v >> 32), 0u) << 32 | moved<CTRL, ROWS>((unsigned)v, 0u);
 }
-
-struct Shared {
-  uint64_t sum[BINS];
-  uint64_t sub_sum[SUB];
-  uint64_t list[LIST];                 // key << 32 | ~id: larger is earlier in the order
-  unsigned cnt[BINS];
-  unsigned sub_cnt[SUB];
-  uint64_t wave_sum[WAVES];
-  unsigned wave_cnt[WAVES];
-  float wave_max[WAVES];
-  int wave_id[WAVES];
-  // what one thread found
-  uint64_t found_sum, few_sum;
-  unsigned found_cnt, found_n, key_lo, key_hi, list_n, few_n, few_key, few_ties;
-  int found_bin;
-};
-
-// sums of the threads before this one
-__device__ __forceinline__ void before(Shared& s, unsigned& cnt, uint64_t& sum) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const unsigned own_c = cnt;
-  const uint64_t own_s = sum;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned c = __shfl_up(cnt, o, 64);
-    const uint64_t q = shfl_up64(sum, o);
-    if (lane >= o) { cnt += c; sum += q; }
-  }
-  __syncthreads();
-  if (lane == 63) { s.wave_cnt[wave] = cnt; s.wave_sum[wave] = sum; }
-  __syncthreads();
-  cnt -= own_c; sum -= own_s;
-  for (int w = 0; w < wave; ++w) { cnt += s.wave_cnt[w]; sum += s.wave_sum[w]; }
+template <typename V, typename OP>
+__device__ __forceinline__ V running(V v, unsigned idle, OP op) {
+  v = op(v, moved<0x111, 0xf>(v, idle));
+  v = op(v, moved<0x112, 0xf>(v, idle));
+  v = op(v, moved<0x114, 0xf>(v, idle));
+  v = op(v, moved<0x118, 0xf>(v, idle));
+  v = op(v, moved<0x142, 0xa>(v, idle));
+  return op(v, moved<0x143, 0xc>(v, idle));
+}
+template <typename V>
+__device__ __forceinline__ V running_sum(V v) { return running(v, 0u, [](V a, V b) { return a + b; }); }
+__device__ __forceinline__ unsigned lane_of(unsigned v, int l) { return __builtin_amdgcn_readlane(v, l); }
+__device__ __forceinline__ uint64_t lane_of(uint64_t v, int l) { return (uint64_t)lane_of((unsigned)(v >> 32), l) << 32 | lane_of((unsigned)v, l); }
+template <typename V>
+__device__ __forceinline__ V wave_total(V v) { return lane_of(running_sum(v), 63); }
+// the larger of two logits, the lower id of equal ones
+__device__ __forceinline__ void take_larger(float& top, int& at, float other, int other_at) {
+  if (other > top || (other == top && (unsigned)other_at < (unsigned)at)) { top = other; at = other_at; }
+}
+__device__ __forceinline__ void wave_largest(float& top, int& at) {
+  const unsigned low = __float_as_uint(-INFINITY);
+  const float m = __uint_as_float(lane_of(running(__float_as_uint(top), low, [](unsigned a, unsigned b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }), 63));
+  at = (int)lane_of(running(top == m ? (unsigned)at : ~0u, ~0u, [](unsigned a, unsigned b) { return min(a, b); }), 63);
+  top = m;
 }
 
 template <typename T> struct Piece;
@@ -127,13 +176,13 @@ template <> struct Piece<bf16_t> {
   __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
 };
 
-// A row; a lane takes pieces of N consecutive logits, 16 bytes.
+// A row; a thread takes pieces of N consecutive logits, 16 bytes.
 template <typename T, bool ALIGNED>
 struct Row {
   static constexpr int N = Piece<T>::N;
   const T* p;
   int vocab;
-  bool has_inf;                        // (then infinity is as the largest finite value)
+  __device__ __forceinline__ Row(const SampleArgs& a, int row) : p((const T*)a.logits + (int64_t)row * a.stride), vocab(a.vocab) {}
   __device__ __forceinline__ void load(int at, float (&x)[N]) const {
     if (ALIGNED && at + N <= vocab) {
       Piece<T> q;
@@ -145,350 +194,633 @@ struct Row {
       for (int i = 0; i < N; ++i) x[i] = at + i < vocab ? to_f32(p[at + i]) : -INFINITY;
     }
   }
-  // f(id of the first, N logits) for this wave's pieces of [lo, hi), in ascending order for each lane; lo a multiple of N
-  template <typename F> __device__ __forceinline__ void each(int lo, int hi, F f) const {
-    constexpr int AHEAD = 32 / N;      // pieces on their way at once
-    const int lane = threadIdx.x & 63;
-    for (int b = lo; b < hi; b += 64 * N * AHEAD) {
-      float x[AHEAD][N];
+};
+// infinity is as the largest finite value
+__device__ __forceinline__ float tame(float x) { return x == INFINITY ? FLT_MAX : x; }
+
+template <typename T, bool ALIGNED, int PER>           // PER logits a thread
+__global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
+  constexpr int N = Piece<T>::N, PIECES = PER / N;
+  __shared__ float wave_top[4];
+  __shared__ int wave_at[4];
+  __shared__ double wave_sum[4];
+  __shared__ uint64_t bins[BINS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = blockIdx.x, row = blockIdx.y;
+  const int64_t mine = (int64_t)row * a.parts + part;
+  const Limits m = limits(a, row);
+  const Row<T, ALIGNED> r(a, row);
+  const int lo = part * (PART_THREADS * PER);
+  float x[PIECES][N];
+  float own = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < AHEAD; ++j) {
-        const int at = b + (j * 64 + lane) * N;
-        load(at < hi ? at : vocab, x[j]);
-      }
+  for (int j = 0; j < PIECES; ++j) r.load(min(lo + (j * PART_THREADS + tid) * N, a.vocab), x[j]);
 #pragma unroll
-      for (int j = 0; j < AHEAD; ++j) {
-        const int at = b + (j * 64 + lane) * N;
-        if (at >= hi) break;
-        if (has_inf) {
+  for (int j = 0; j < PIECES; ++j)
 #pragma unroll
-          for (int i = 0; i < N; ++i) x[j][i] = x[j][i] == INFINITY ? FLT_MAX : x[j][i];
+    for (int i = 0; i < N; ++i) own = fmaxf(own, x[j][i]);
+  if (own == INFINITY) {
+    own = FLT_MAX;
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[j][i] = tame(x[j][i]);
+  }
+  float top = own;
+  int at = -1;
+  if (top > -INFINITY) {
+#pragma unroll
+    for (int j = PIECES - 1; j >= 0; --j)
+#pragma unroll
+      for (int i = N - 1; i >= 0; --i) at = x[j][i] == top ? lo + (j * PART_THREADS + tid) * N + i : at;
+  }
+  wave_largest(top, at);
+  if (lane == 0) { wave_top[wave] = top; wave_at[wave] = at; }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) take_larger(top, at, wave_top[w], wave_at[w]);
+  double sum = 0.0;
+  if (draws(m) && at >= 0) {
+    if (all_count(m)) {
+      const Weigher weight{(double)top, octaves(m)};
+      double s[2] = {0.0, 0.0};
+#pragma unroll
+      for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i & 1] += weight.real(x[j][i], 0);
+      sum = s[0] + s[1];
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      if (lane == 0) wave_sum[wave] = sum;
+      __syncthreads();
+      sum = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
+    }
+    if (limited(m)) a.maxima[mine * PART_THREADS + tid] = own;
+    if (m.by_count || m.by_sum) {
+      for (int i = tid; i < BINS; i += PART_THREADS) bins[i] = 0;
+      __syncthreads();
+      const float per = steps(a, m), base = step_of(top, per);
+#pragma unroll
+      for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float s = x[j][i] * per, step = base - floorf(s);
+          if (step < (float)BINS) {
+            const unsigned f = (unsigned)((s - floorf(s)) * PLACES);
+            atomicAdd((unsigned long long*)&bins[(int)step], 1ull << 44 | (uint64_t)f << 22 | (f * f / PLACES));
+          }
         }
-        f(at, x[j]);
+      __syncthreads();
+      for (int i = tid; i < BINS; i += PART_THREADS) a.bins[mine * BINS + i] = bins[i];
+    }
+  }
+  if (tid == 0) a.tops[mine] = {top, at, sum};
+}
+
+// ---- a workgroup a row -----------------------------------------------------------------------------------------
+
+struct Sums {                          // of a workgroup's waves
+  uint64_t sum[WAVES];
+  unsigned cnt[WAVES];
+};
+// sums of the threads before this one, in place; all threads'
+__device__ __forceinline__ void before(Sums& s, unsigned& cnt, uint64_t& sum, unsigned& all_cnt, uint64_t& all_sum) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const unsigned c = running_sum(cnt);
+  const uint64_t q = running_sum(sum);
+  __syncthreads();
+  if (lane == 63) { s.cnt[wave] = c; s.sum[wave] = q; }
+  __syncthreads();
+  const unsigned of_c = running_sum(lane < WAVES ? s.cnt[lane & (WAVES - 1)] : 0u);
+  const uint64_t of_q = running_sum(lane < WAVES ? s.sum[lane & (WAVES - 1)] : (uint64_t)0);
+  all_cnt = lane_of(of_c, WAVES - 1);
+  all_sum = lane_of(of_q, WAVES - 1);
+  const int last = __builtin_amdgcn_readfirstlane(wave) - 1;
+  cnt = c - cnt + (last >= 0 ? lane_of(of_c, max(last, 0)) : 0u);
+  sum = q - sum + (last >= 0 ? lane_of(of_q, max(last, 0)) : (uint64_t)0);
+}
+__device__ __forceinline__ uint64_t total_of(Sums& s, uint64_t sum) {
+  unsigned none = 0, c;
+  uint64_t all;
+  before(s, none, sum, c, all);
+  return all;
+}
+
+// The parts of a row: a thread's own, the largest logit of all and its first id.
+struct Joined { Part mine; float top; int at; };
+__device__ __forceinline__ Joined join_parts(const SampleArgs& a, int row, float (&wave_top)[WAVES], int (&wave_at)[WAVES]) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  Joined j;
+  j.mine = tid < a.parts ? a.tops[(int64_t)row * a.parts + tid] : Part{-INFINITY, -1, 0.0};
+  j.top = j.mine.top; j.at = j.mine.at;
+  wave_largest(j.top, j.at);
+  if (lane == 0) { wave_top[wave] = j.top; wave_at[wave] = j.at; }
+  __syncthreads();
+  j.top = lane < WAVES ? wave_top[lane & (WAVES - 1)] : -INFINITY;
+  j.at = lane < WAVES ? wave_at[lane & (WAVES - 1)] : -1;
+  wave_largest(j.top, j.at);
+  return j;
+}
+// a part's weights in units of 2^-shift of the largest logit's
+__device__ __forceinline__ uint64_t part_weight(const Part& p, const Weigher& weight, int shift) {
+  return p.at >= 0 ? (uint64_t)__builtin_rint(p.sum * weight.real(p.top, shift)) : 0ull;
+}
+__device__ __forceinline__ uint64_t sum_goal(float top_p, uint64_t sum) {        // (the first is in)
+  return max(1ull, (uint64_t)__builtin_ceil((double)fmaxf(top_p, 0.f) * (double)sum));
+}
+
+static_assert(BINS == THREADS, "k_sample_edges: a thread a step");
+__global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
+  __shared__ Sums s;
+  __shared__ float wave_top[WAVES];
+  __shared__ int wave_at[WAVES], offset[MOST_PARTS];
+  __shared__ int found[4];
+  const int tid = threadIdx.x, row = blockIdx.x;
+  const Limits m = limits(a, row);
+  RowState& out = a.state[row];
+  if (!draws(m) || !limited(m)) {
+    if (tid == 0) out.mode = AS_IT_IS;
+    return;
+  }
+  const Joined j = join_parts(a, row, wave_top, wave_at);
+  const float per = steps(a, m), base = step_of(j.top, per);
+  const double octave = (double)(a.shift + 2) / BINS;  // of a step
+  RowState st{COLLECT, 0, -1, 0u, 0, base};
+  // (largest logits between which the parts' differ by 2^20 steps and more differ by more than 47 powers of two: nothing there counts)
+  if (j.at < 0 || !(fabsf(j.top * per) < FAR_STEPS)) {
+    if (tid == 0) { st.mode = j.at < 0 ? AS_IT_IS : DIVIDE; out = st; }
+    return;
+  }
+  if (!m.by_count && !m.by_sum) {      // min-p: what can weigh that much, a step more and the one that the largest is in
+    st.first = (int)fminf(-__builtin_amdgcn_logf(fminf(m.min_p, 1.f)) * (float)(1.0 / octave) * 1.001f + 3.f, (float)BINS);
+    if (tid == 0) out = st;
+    return;
+  }
+  if (tid < a.parts) {
+    const float d = j.mine.at < 0 ? (float)BINS : base - step_of(j.mine.top, per);
+    offset[tid] = d < (float)BINS ? (int)d : BINS;
+  }
+  if (tid < 4) found[tid] = tid == 1 ? BINS - 1 : 0;
+  __syncthreads();
+  unsigned n = 0, places = 0, squares = 0;
+#pragma unroll 4
+  for (int p = 0; p < a.parts; ++p) {
+    const int i = tid - offset[p];
+    const uint64_t v = i >= 0 ? a.bins[((int64_t)row * a.parts + p) * BINS + i] : 0ull;
+    n += (unsigned)(v >> 44); places += (unsigned)(v >> 22) & 0x3fffffu; squares += (unsigned)v & 0x3fffffu;
+  }
+  // Sums of weights in units of 2^-40.  A token at place f of a step weighs 1 + k f + (k f)^2 / 2 + up to k^3 / 5 times what one at its lower end does,
+  // k = ln 2 octave = 0.032: 6.6e-6 for the last, k / PLACES = 6e-5 for the place, k^2 / PLACES = 2e-6 for its square; the first two taken at their
+  // middle, sums are off by 4e-5, by what the step's number is off, and by 1e-6 for the exponential.
+  const double k = 0.6931471805599453 * octave, up = j.top * per - base;
+  const double middle = (double)n * (1 + 0.5 * k / PLACES) + k / PLACES * ((double)places + 0.5 * k * (double)squares);
+  const uint64_t w = (uint64_t)(middle * (double)__builtin_amdgcn_exp2f((float)(40.0 - (tid + up) * octave)));
+  unsigned c0 = n;
+  uint64_t q0 = w;
+  unsigned alive;
+  uint64_t unused;
+  before(s, c0, q0, alive, unused);
+  if (m.by_count) {                    // (no cut, if fewer weigh anything: the last step)
+    const unsigned want = min((unsigned)m.top_k, alive);
+    if (c0 < want && want <= c0 + n) found[0] = found[1] = tid;
+  } else {
+    const uint64_t goal = sum_goal(m.top_p, total_of(s, part_weight(j.mine, Weigher{(double)j.top, octaves(m)}, a.shift)));
+    const double g = __builtin_ldexp((double)goal, 40 - a.shift), off = 1e-4 + 0.1 * 0x1p-23 * fabsf(j.top * per);
+    const uint64_t reach = max(1ull, (uint64_t)(g * (1 - off))), surely = (uint64_t)(g * (1 + off)) + BINS;
+    if (q0 < reach && reach <= q0 + w) found[0] = tid;
+    if (q0 < surely && surely <= q0 + w) found[1] = tid;
+  }
+  __syncthreads();
+  const int first = found[0], last = found[1];
+  __syncthreads();
+  if (tid == first) found[2] = (int)c0;
+  if (tid == last) found[3] = (int)(c0 + n);
+  __syncthreads();
+  if (tid == 0) {
+    const unsigned ahead = (unsigned)found[2], end = (unsigned)found[3];
+    // All tokens from the first on, if there is room: top-p after top-k needs that, and so does top-k where all that weighs anything is in.
+    st.last = last;
+    if (end > LIST) {
+      st.first = first; st.before = ahead;
+      if (end - ahead > LIST || (m.by_count && (m.by_sum || (unsigned)m.top_k >= alive))) st.mode = DIVIDE;
+    }
+    out = st;
+  }
+}
+
+template <typename T, bool ALIGNED, int PER>
+__global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
+  constexpr int N = Piece<T>::N, PIECES = PER / N;
+  __shared__ uint64_t list[LIST];
+  __shared__ uint64_t wave_sum[4][2];
+  __shared__ unsigned list_n, place;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = blockIdx.x, row = blockIdx.y;
+  const int64_t mine = (int64_t)row * a.parts + part;
+  const RowState st = a.state[row];
+  if (st.mode != COLLECT) return;
+  const Limits m = limits(a, row);
+  const Row<T, ALIGNED> r(a, row);
+  const float per = steps(a, m), first = (float)st.first, end = (float)max(st.first, st.last + 1);
+  // the largest logit has the step st.base: its weight's reference is found as its own part found it
+  __shared__ float tops[4];
+  float top = -INFINITY;
+  for (int i = tid; i < a.parts; i += PART_THREADS) top = fmaxf(top, a.tops[(int64_t)row * a.parts + i].top);
+  top = wave_max(top);
+  if (lane == 0) tops[wave] = top;
+  if (tid == 0) list_n = 0;
+  __syncthreads();
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  const Weigher weight{(double)top, octaves(m)};
+  const uint64_t least = m.by_part ? max(1ull, (uint64_t)__builtin_rint(__builtin_ldexp((double)fminf(m.min_p, 1.f), a.shift))) : 1ull;
+  uint64_t all = 0, in = 0;
+  const float own = a.tops[mine].at < 0 ? -INFINITY : a.maxima[mine * PART_THREADS + tid];
+  if (st.base - step_of(own, per) < end) {
+    float x[PIECES][N];
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) r.load(min(part * (PART_THREADS * PER) + (j * PART_THREADS + tid) * N, a.vocab), x[j]);
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) {
+      float most = x[j][0] = tame(x[j][0]);
+#pragma unroll
+      for (int i = 1; i < N; ++i) { x[j][i] = tame(x[j][i]); most = fmaxf(most, x[j][i]); }
+      const float nearest = st.base - step_of(most, per);
+      if (nearest < first) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {  // (of the piece's others too: side by side they take less time than branches do)
+          const uint64_t q = st.base - step_of(x[j][i], per) < first ? weight.whole(x[j][i], a.shift) : 0ull;
+          all += q;
+          in += q >= least ? q : 0ull;
+        }
+      }
+      if (nearest < end && first < end) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float step = st.base - step_of(x[j][i], per);
+          if (step >= first && step < end) {
+            const unsigned n = atomicAdd(&list_n, 1u);
+            if (n < LIST) list[n] = (uint64_t)key_of(x[j][i]) << 32 | (unsigned)~(part * (PART_THREADS * PER) + (j * PART_THREADS + tid) * N + i);
+          }
+        }
       }
     }
   }
-};
+  all = wave_total(all); in = wave_total(in);
+  if (lane == 0) { wave_sum[wave][0] = all; wave_sum[wave][1] = in; }
+  __syncthreads();
+  if (tid == 0) {
+    a.sums[mine] = {wave_sum[0][0] + wave_sum[1][0] + wave_sum[2][0] + wave_sum[3][0], wave_sum[0][1] + wave_sum[1][1] + wave_sum[2][1] + wave_sum[3][1]};
+    place = list_n ? atomicAdd((unsigned*)&a.state[row].list_n, list_n) : 0u;
+  }
+  __syncthreads();
+  for (unsigned i = tid; i < min(list_n, (unsigned)LIST); i += PART_THREADS)
+    if (place + i < LIST) a.list[(int64_t)row * LIST + place + i] = list[i];
+}
 
+struct Shared {
+  Sums sums;
+  uint64_t sub_sum[THREADS];           // a division: a thread a bin
+  unsigned sub_cnt[THREADS];
+  uint64_t part_sum[MOST_PARTS];       // what is in
+  unsigned part_ties[MOST_PARTS];
+  uint64_t list[LIST];
+  float wave_top[WAVES];
+  int wave_at[WAVES];
+  // what one thread found
+  uint64_t found_sum, ahead_sum;
+  unsigned found_cnt, found_n, key_lo, key_hi, few_n, few_key, few_ties, ahead_ties;
+  int found_part;
+  float found_top;
+};
 struct Cut {
   unsigned key;                        // what is above it is in
   unsigned ties;                       // and so many of those at it, by id
-  uint64_t sum;                        // of all that is in
+  uint64_t sum;                        // of all that is in, min-p aside
 };
 
 template <typename T, bool ALIGNED>
-__global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a) {
+__global__ __launch_bounds__(THREADS) void k_sample_pick(SampleArgs a) {
   __shared__ Shared s;
   constexpr int N = Piece<T>::N;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x;
-  const int vocab = a.vocab;
-  Row<T, ALIGNED> r{(const T*)a.logits + (int64_t)row * a.stride, vocab, false};
-  const int piece = ((vocab + WAVES - 1) / WAVES + 64 * N - 1) / (64 * N) * (64 * N);       // a wave's
-  const int lo = min(wave * piece, vocab), hi = min(lo + piece, vocab);
-
-  const float temperature = a.temperature ? a.temperature[row] : 1.f;
-  const float top_p = a.top_p ? a.top_p[row] : 1.f;
-  const float min_p = a.min_p ? a.min_p[row] : 0.f;
-  const int top_k = a.top_k ? a.top_k[row] : 0;
-  const bool valid = temperature >= 0.f && temperature < INFINITY && top_p == top_p && min_p == min_p;
-
-  // the largest, and where it is first
-  float best = -INFINITY;
-  int best_at = -1;
-  if (valid)
-    r.each(lo, hi, [&](int at, const float (&x)[N]) {
-      float m = x[0];
-#pragma unroll
-      for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
-      if (m > best) { best = m; best_at = at; }
-    });
-  if (best_at >= 0) {
-    float x[N];
-    r.load(best_at, x);
-    int e = 0;
-#pragma unroll
-    for (int i = N - 1; i >= 0; --i) e = x[i] == best ? i : e;
-    best_at += e;
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float m = __shfl_xor(best, o, 64);
-    const int at = __shfl_xor(best_at, o, 64);
-    if (m > best || (m == best && at >= 0 && (unsigned)at < (unsigned)best_at)) { best = m; best_at = at; }
-  }
-  if (lane == 0) { s.wave_max[wave] = best; s.wave_id[wave] = best_at; }
-  __syncthreads();
-  for (int w = 0; w < WAVES; ++w)      // (waves have ascending ids)
-    if (s.wave_max[w] > best || (s.wave_max[w] == best && (unsigned)s.wave_id[w] < (unsigned)best_at)) { best = s.wave_max[w]; best_at = s.wave_id[w]; }
-  if (best_at < 0 || temperature == 0.f) {             // nothing to choose, or the first of the order
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, vocab = a.vocab, shift = a.shift;
+  const Limits lim = limits(a, row);
+  const Row<T, ALIGNED> r(a, row);
+  const Joined j = join_parts(a, row, s.wave_top, s.wave_at);
+  if (!draws(lim) || j.at < 0) {       // nothing to choose, or the first of the order
     if (tid == 0) {
-      a.ids[row] = best_at;
-      if (a.probs) a.probs[row] = best_at < 0 ? 0.f : 1.f;
+      const bool none = !lim.valid || j.at < 0;
+      a.ids[row] = none ? -1 : j.at;
+      if (a.probs) a.probs[row] = none ? 0.f : 1.f;
     }
     return;
   }
-  if (best == INFINITY) { r.has_inf = true; best = FLT_MAX; }
-
-  const Weigher weight{(double)best, 1.4426950408889634 / (double)temperature, -(float)(a.shift + 2), a.shift};
-  const uint64_t least = min_p > 0.f ? max(1ull, (uint64_t)__builtin_rint(__builtin_ldexp((double)fminf(min_p, 1.f), a.shift))) : 1ull;
+  const Weigher weight{(double)j.top, octaves(lim)};
+  const float u = a.u[row];
+  const double uu = u > 0.f ? (double)fminf(u, 0.99999994f) : 0.0;
+  const uint64_t least = lim.by_part ? max(1ull, (uint64_t)__builtin_rint(__builtin_ldexp((double)fminf(lim.min_p, 1.f), shift))) : 1ull;
   Cut cut{0u, 0u, 0ull};               // all is in
-  const bool by_count = top_k > 0 && top_k < vocab, by_sum = top_p < 1.f;
+  uint64_t own = part_weight(j.mine, weight, shift);             // this thread's part: what is in
+  unsigned own_ties = 0;
+  const bool narrow = limited(lim);
 
-  if (by_count || by_sum) {
-    const double steps = (double)BINS / (a.shift + 2);
-    auto bin_of = [&](double t) { return min((int)(-t * steps), BINS - 1); };
-    for (int i = tid; i < BINS; i += THREADS) { s.cnt[i] = 0; s.sum[i] = 0; }
-    __syncthreads();
-    r.each(lo, hi, [&](int, const float (&x)[N]) {
+  if (narrow) {
+    const RowState st = a.state[row];
+    const bool listed = st.mode == COLLECT;
+    const unsigned listed_n = listed ? min((unsigned)st.list_n, (unsigned)LIST) : 0u;
+    const bool from_top = listed && st.first == 0;
+    PartSums mine{0, 0};
+    if (listed && tid < a.parts) mine = a.sums[(int64_t)row * a.parts + tid];
+    const uint64_t all = lim.by_sum ? total_of(s.sums, own) : 0ull;            // of all tokens (top-p without top-k)
+    const uint64_t q0 = from_top ? 0ull : total_of(s.sums, mine.all);          // of those before the list
+    own = mine.in;
+    // f(key, id) for the listed tokens, or all of the row
+    auto tokens = [&](auto f) {
+      if (listed) {
+#pragma unroll 1
+        for (unsigned i = tid; i < listed_n; i += THREADS) f((unsigned)(s.list[i] >> 32), (int)~(unsigned)s.list[i]);
+      } else {
+#pragma unroll 1
+        for (int at = tid * N; at < vocab; at += THREADS * N) {
+          float x[N];
+          r.load(at, x);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const double t = weight.log2w(x[i]);
-        if (t > (double)weight.floor_t) {
-          const uint64_t q = weight.of_log(t);
-          if (q) {
-            const int b = bin_of(t);
-            atomicAdd(&s.cnt[b], 1u);
-            atomicAdd((unsigned long long*)&s.sum[b], (unsigned long long)q);
-          }
+          for (int i = 0; i < N; ++i)
+            if (x[i] > -INFINITY) f(key_of(tame(x[i])), at + i);
         }
       }
+    };
+    if (tid == 0) { s.key_lo = ~0u; s.key_hi = 0u; }
+    s.part_sum[tid] = own;
+    s.part_ties[tid] = 0;
+#pragma unroll 1
+    for (unsigned i = tid; i < listed_n; i += THREADS) s.list[i] = a.list[(int64_t)row * LIST + i];
+    __syncthreads();
+    unsigned k_min = ~0u, k_max = 0u, here = 0;
+    uint64_t weights = 0;
+    tokens([&](unsigned k, int) {
+      const uint64_t q = weight.whole(of_key(k), shift);
+      if (q) { k_min = min(k_min, k); k_max = max(k_max, k); ++here; weights += q; }
     });
-    __syncthreads();
-    constexpr int EACH = BINS / THREADS;
-    unsigned total_c = 0;
-    uint64_t total_s = 0;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) { total_c += s.cnt[tid * EACH + i]; total_s += s.sum[tid * EACH + i]; }
-    unsigned before_c = total_c;
-    uint64_t before_s = total_s;
-    before(s, before_c, before_s);
-    if (tid == THREADS - 1) { s.found_cnt = before_c + total_c; s.found_sum = before_s + total_s; }
-    __syncthreads();
-    const unsigned alive = s.found_cnt;
-    cut.sum = s.found_sum;
-    __syncthreads();
-
-    // The cut after `count` tokens, or before the first one with `sum` or more before it, whichever comes first; it is there.
-    auto find = [&](unsigned count, uint64_t sum) {
-      unsigned c = before_c;
-      uint64_t q = before_s;
-#pragma unroll
-      for (int i = 0; i < EACH; ++i) {
-        const unsigned n = s.cnt[tid * EACH + i];
-        const uint64_t w = s.sum[tid * EACH + i];
-        if (n && c < count && q < sum && (c + n >= count || q + w >= sum)) { s.found_bin = tid * EACH + i; s.found_cnt = c; s.found_sum = q; s.found_n = n; }
-        c += n; q += w;
+    if (here) { atomicMin(&s.key_lo, k_min); atomicMax(&s.key_hi, k_max); }
+    unsigned list_cnt;
+    uint64_t list_sum;
+    before(s.sums, here, weights, list_cnt, list_sum);
+    const unsigned list_lo = s.key_lo, list_hi = s.key_hi, ahead_cnt = listed && !from_top ? st.before : 0u;
+    cut.sum = lim.by_count || !listed ? q0 + list_sum : all;
+#pragma unroll 1
+    for (int stage = 0; stage < 2; ++stage) {          // by count, by sum
+      unsigned count = ~0u, n = list_cnt, c0 = ahead_cnt, k_lo = list_lo, k_hi = list_hi;
+      uint64_t goal = ~0ull, q = q0;
+      if (stage == 0) {
+        if (!lim.by_count || (unsigned)lim.top_k > ahead_cnt + list_cnt) continue;        // (no more than that weigh anything)
+        count = (unsigned)lim.top_k;
+      } else {
+        if (!lim.by_sum) break;
+        goal = sum_goal(lim.top_p, cut.sum);
       }
-      if (tid == 0) { s.key_lo = ~0u; s.key_hi = 0u; s.list_n = 0; }
-      __syncthreads();
-      const int bin = s.found_bin;
-      r.each(lo, hi, [&](int at, const float (&x)[N]) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const double t = weight.log2w(x[i]);
-          if (t > (double)weight.floor_t && bin_of(t) == bin && weight.of_log(t)) {
-            const unsigned k = key_of(x[i]), place = atomicAdd(&s.list_n, 1u);
-            if (place < LIST) s.list[place] = (uint64_t)k << 32 | (unsigned)~(at + i);
-            atomicMin(&s.key_lo, k);
-            atomicMax(&s.key_hi, k);
-          }
-        }
-      });
-      __syncthreads();
-      const bool listed = s.list_n <= LIST;
-      const unsigned listed_n = s.list_n;
+      // The cut among n tokens with keys between the two, after `count` tokens, or before the first one with `goal` or more before it.  c0, q: tokens
+      // and weights before them.
+#pragma unroll 1
       for (int level = 0; level < 6; ++level) {        // (32 bits, ten at a time, and the last look)
-        const unsigned k_lo = s.key_lo, k_hi = s.key_hi, n = s.found_n, c0 = s.found_cnt;
-        const uint64_t q0 = s.found_sum;
         if (k_lo == k_hi) {            // equal ones: as many as there is room for
-          const uint64_t q = weight(of_key(k_lo));
+          const uint64_t w = max(1ull, weight.whole(of_key(k_lo), shift));
           uint64_t m = min((uint64_t)n, (uint64_t)(count - c0));
-          m = min(m, (sum - q0 - 1) / q + 1);
-          cut = {k_lo, (unsigned)m, q0 + m * q};
-          __syncthreads();
-          return;
+          m = min(m, (goal - q - 1) / w + 1);
+          cut = {k_lo, (unsigned)m, q + m * w};
+          break;
         }
-        auto members = [&](auto f) {   // f(key, id) for what is between the two keys
-          if (listed) {
-            for (unsigned i = tid; i < listed_n; i += THREADS) {
-              const unsigned k = (unsigned)(s.list[i] >> 32);
-              if (k >= k_lo && k <= k_hi) f(k, (int)~(unsigned)s.list[i]);
-            }
-          } else {
-            r.each(lo, hi, [&](int at, const float (&x)[N]) {
-#pragma unroll
-              for (int i = 0; i < N; ++i) {
-                if (x[i] > -INFINITY) {
-                  const unsigned k = key_of(x[i]);
-                  if (k >= k_lo && k <= k_hi) f(k, at + i);
-                }
-              }
-            });
-          }
-        };
+        __syncthreads();
         if (n <= FEW) {                // (their places in sub_sum)
-          if (tid == 0) { s.few_n = 0; s.few_sum = 0; }
+          if (tid == 0) s.few_n = 0;
           __syncthreads();
-          members([&](unsigned k, int id) { s.sub_sum[atomicAdd(&s.few_n, 1u)] = (uint64_t)k << 32 | (unsigned)~id; });
+          tokens([&](unsigned k, int id) {
+            if (k >= k_lo && k <= k_hi && weight.whole(of_key(k), shift)) s.sub_sum[atomicAdd(&s.few_n, 1u) & (THREADS - 1)] = (uint64_t)k << 32 | (unsigned)~id;
+          });
           __syncthreads();
           if (wave == 0) {
-            const uint64_t mine = lane < (int)n ? s.sub_sum[lane] : 0ull;
-            const unsigned k = (unsigned)(mine >> 32);
-            const uint64_t w = lane < (int)n ? weight(of_key(k)) : 0ull;
+            const uint64_t token = lane < (int)n ? s.sub_sum[lane] : 0ull;
+            const unsigned k = (unsigned)(token >> 32);
+            const uint64_t w = lane < (int)n ? weight.whole(of_key(k), shift) : 0ull;
             unsigned rank = 0;
             uint64_t ahead = 0;
-            for (int j = 0; j < (int)n; ++j) {
-              const uint64_t other = s.sub_sum[j];
-              const unsigned lo_w = __shfl((unsigned)w, j, 64), hi_w = __shfl((unsigned)(w >> 32), j, 64);
-              const uint64_t wj = (uint64_t)hi_w << 32 | lo_w;
-              if (other > mine) { ++rank; ahead += wj; }
+#pragma unroll 1
+            for (int i = 0; i < (int)n; ++i) {
+              const uint64_t other = s.sub_sum[i];
+              const unsigned w_lo = __builtin_amdgcn_readlane((unsigned)w, i), w_hi = __builtin_amdgcn_readlane((unsigned)(w >> 32), i);
+              if (other > token) { ++rank; ahead += (uint64_t)w_hi << 32 | w_lo; }
             }
-            const bool in = lane < (int)n && c0 + rank < count && q0 + ahead < sum;
+            const bool in = lane < (int)n && c0 + rank < count && q + ahead < goal;
             const int last = __popcll(__builtin_amdgcn_ballot_w64(in)) - 1;      // (what is in is a prefix of the ranking)
-            if (in && (int)rank == last) { s.few_key = k; s.few_sum = q0 + ahead + w; }
+            if (in && (int)rank == last) { s.few_key = k; s.found_sum = q + ahead + w; }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             const int ties = __popcll(__builtin_amdgcn_ballot_w64(in && k == s.few_key));
             if (lane == 0) s.few_ties = ties;
           }
           __syncthreads();
-          cut = {s.few_key, s.few_ties, s.few_sum};
-          __syncthreads();
-          return;
+          cut = {s.few_key, s.few_ties, s.found_sum};
+          break;
         }
-        const int bits = 32 - __clz(k_hi - k_lo), by = max(0, bits - 10);          // SUB = 2^10 of them
+        const int bits = 32 - __clz(k_hi - k_lo), by = max(0, bits - 10);        // THREADS = 2^10 bins
         s.sub_cnt[tid] = 0; s.sub_sum[tid] = 0;
         __syncthreads();
-        members([&](unsigned k, int) {
-          const unsigned b = (k_hi - k) >> by;
-          atomicAdd(&s.sub_cnt[b], 1u);
-          atomicAdd((unsigned long long*)&s.sub_sum[b], (unsigned long long)weight(of_key(k)));
+        tokens([&](unsigned k, int) {
+          const uint64_t w = k >= k_lo && k <= k_hi ? weight.whole(of_key(k), shift) : 0ull;
+          if (w) {
+            const unsigned b = (k_hi - k) >> by;
+            atomicAdd(&s.sub_cnt[b], 1u);
+            atomicAdd((unsigned long long*)&s.sub_sum[b], (unsigned long long)w);
+          }
         });
         __syncthreads();
         const unsigned m = s.sub_cnt[tid];
         const uint64_t w = s.sub_sum[tid];
         unsigned c1 = m;
         uint64_t q1 = w;
-        before(s, c1, q1);
-        c1 += c0; q1 += q0;
-        __syncthreads();
-        if (m && c1 < count && q1 < sum && (c1 + m >= count || q1 + w >= sum)) {
+        unsigned all_c;
+        uint64_t all_q;
+        before(s.sums, c1, q1, all_c, all_q);
+        c1 += c0; q1 += q;
+        if (m && c1 < count && q1 < goal && (c1 + m >= count || q1 + w >= goal)) {
           s.found_cnt = c1; s.found_sum = q1; s.found_n = m;
           s.key_hi = k_hi - ((unsigned)tid << by);
           const uint64_t down = ((uint64_t)tid + 1) << by;
           s.key_lo = down - 1 >= (uint64_t)(k_hi - k_lo) ? k_lo : k_hi - (unsigned)(down - 1);
         }
         __syncthreads();
+        k_lo = s.key_lo; k_hi = s.key_hi; n = s.found_n; c0 = s.found_cnt; q = s.found_sum;
       }
-    };
-    if (by_count && (unsigned)top_k < alive) find((unsigned)top_k, ~0ull);
-    if (by_sum) {
-      const double p = fmaxf(top_p, 0.f) * (double)cut.sum;
-      const uint64_t goal = max(1ull, (uint64_t)__builtin_ceil(p));            // (the first is in)
-      if (goal <= cut.sum) find(~0u, goal);
     }
+    // what of the list is in, by parts
+    __syncthreads();
+    tokens([&](unsigned k, int id) {
+      const uint64_t q = k >= cut.key ? weight.whole(of_key(k), shift) : 0ull;
+      if (q >= least) {
+        if (k > cut.key) atomicAdd((unsigned long long*)&s.part_sum[id / a.part], (unsigned long long)q);
+        else atomicAdd(&s.part_ties[id / a.part], 1u);
+      }
+    });
+    __syncthreads();
+    own = s.part_sum[tid];
+    own_ties = s.part_ties[tid];
   }
 
-  // what is in, by waves
+  // the part in which the target lies; of tokens at the cut's logit the first by id are in
+  const uint64_t tie_q = cut.key ? weight.whole(of_key(cut.key), shift) : 0ull;
+  unsigned ties_ahead = own_ties, none = 0, all_c;
+  uint64_t unused = 0, total;
+  if (cut.key) before(s.sums, ties_ahead, unused, all_c, total);
+  own += tie_q * min(own_ties, cut.ties - min(ties_ahead, cut.ties));
+  uint64_t ahead = own;
+  before(s.sums, none, ahead, all_c, total);
+  const uint64_t target = min((uint64_t)(uu * (double)total), total - 1);
+  if (target >= ahead && target < ahead + own) {
+    s.found_part = tid; s.found_sum = own; s.ahead_sum = ahead; s.ahead_ties = ties_ahead;
+    s.found_top = j.mine.top;
+  }
+  __syncthreads();
+  // A run of its logits for every thread.  Without limits weights are taken against the part's largest, as its sum was.
+  const Weigher local{narrow ? (double)j.top : (double)s.found_top, weight.scale};
+  constexpr int RUN = 8;               // (a part has up to THREADS times as many)
+  const int from = s.found_part * a.part + tid * RUN, to = min(min(from + RUN, (s.found_part + 1) * a.part), vocab);
+  float x[RUN];
+  if (from < to) {
+#pragma unroll
+    for (int i = 0; i < RUN; i += N) {
+      float v[N];
+      r.load(min(from + i, vocab), v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[i + e] = v[e];
+    }
+  }
+  // the weight of what is in for certain, and whether it is one of the equal ones at the cut
+  auto take = [&](float v, int i, bool& tie) {
+    v = tame(v);
+    const unsigned k = key_of(v);
+    const uint64_t q = from + i < to && v > -INFINITY && k >= cut.key ? local.whole(v, shift) : 0ull;
+    tie = q >= least && k == cut.key;
+    return q >= least && k > cut.key ? q : 0ull;
+  };
   uint64_t sum = 0;
   unsigned ties = 0;
-  auto take = [&](float x, uint64_t& q_in, unsigned& tie) {
-    const uint64_t q = weight(x);
-    const unsigned k = key_of(x);
-    q_in = q >= least && k > cut.key ? q : 0ull;
-    tie = q >= least && k == cut.key ? 1u : 0u;
-  };
-  r.each(lo, hi, [&](int, const float (&x)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      uint64_t q; unsigned t;
-      take(x[i], q, t);
-      sum += q; ties += t;
-    }
-  });
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { sum += shfl_xor64(sum, o); ties += __shfl_xor(ties, o, 64); }
-  __syncthreads();
-  if (lane == 0) { s.wave_sum[wave] = sum; s.wave_cnt[wave] = ties; }
-  __syncthreads();
-  const uint64_t tie_q = cut.key ? weight(of_key(cut.key)) : 0ull;
-  uint64_t all = 0;
-  unsigned tied = 0;
-  for (int w = 0; w < WAVES; ++w) { all += s.wave_sum[w]; tied += s.wave_cnt[w]; }
-  all += tie_q * min(tied, cut.ties);
-  const float u = a.u[row];
-  const double uu = u > 0.f ? (double)fminf(u, 0.99999994f) : 0.0;
-  const uint64_t target = min((uint64_t)(uu * (double)all), all - 1);
-  int in_wave = WAVES - 1;
-  uint64_t ahead = 0;
-  unsigned ties_ahead = 0;
-  for (int w = 0; w < WAVES; ++w) {
-    const unsigned left = cut.ties - min(ties_ahead, cut.ties);
-    const uint64_t q = s.wave_sum[w] + tie_q * min(s.wave_cnt[w], left);
-    if (target < ahead + q) { in_wave = w; break; }
-    ahead += q; ties_ahead += s.wave_cnt[w];
+  for (int i = 0; i < RUN; ++i) {
+    bool tie;
+    sum += take(x[i], i, tie);
+    ties += tie;
   }
-  // that piece, a run of consecutive ids for every thread
-  const int start = min(in_wave * piece, vocab), end = min(start + piece, vocab);
-  const int run = (piece / THREADS + N) / N * N;
-  const int mine = min(start + tid * run, end), mine_end = min(mine + run, end);
-  sum = 0; ties = 0;
-  for (int at = mine; at < mine_end; at += N) {
-    float x[N];
-    r.load(at, x);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      uint64_t q; unsigned t;
-      if (r.has_inf && x[i] == INFINITY) x[i] = FLT_MAX;
-      take(x[i], q, t);
-      if (at + i < mine_end) { sum += q; ties += t; }
-    }
+  const uint64_t own_sum = sum;
+  const unsigned own_count = ties;
+  uint64_t of_part;
+  before(s.sums, ties, sum, all_c, of_part);           // of the threads before
+  const unsigned left0 = cut.ties - min(s.ahead_ties, cut.ties), left = cut.ties - min(s.ahead_ties + ties, cut.ties);
+  uint64_t goal = target - s.ahead_sum, at_q = sum + tie_q * (left0 - left);
+  double share = 1.0 / (double)total;
+  if (!narrow) {                       // (of the part's sum in these units)
+    goal = min((uint64_t)((double)goal / (double)s.found_sum * (double)of_part), of_part - 1);
+    share = (double)s.found_sum / (double)of_part / (double)total;
   }
-  uint64_t q1 = sum;
-  unsigned c1 = ties;
-  before(s, c1, q1);
-  c1 += ties_ahead;
-  const unsigned left0 = cut.ties - min(ties_ahead, cut.ties), left1 = cut.ties - min(c1, cut.ties);
-  uint64_t at_q = ahead + q1 + tie_q * (left0 - left1);
-  if (target >= at_q && target < at_q + sum + tie_q * min(ties, left1)) {
-    unsigned left = left1;
-    for (int at = mine; at < mine_end; ++at) {
-      float x = to_f32(r.p[at]);
-      if (r.has_inf && x == INFINITY) x = FLT_MAX;
-      uint64_t q; unsigned t;
-      take(x, q, t);
-      if (t && left) { q = tie_q; --left; }
-      if (target < at_q + q) {
-        a.ids[row] = at;
-        if (a.probs) a.probs[row] = (float)((double)q / (double)all);
-        break;
+  if (goal >= at_q && goal < at_q + own_sum + tie_q * min(own_count, left)) {
+    unsigned more = left;
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) {
+      bool tie;
+      uint64_t q = take(x[i], i, tie);
+      if (tie && more) { q = tie_q; --more; }
+      if (goal >= at_q && goal < at_q + q) {
+        a.ids[row] = from + i;
+        if (a.probs) a.probs[row] = (float)((double)q * share);
       }
       at_q += q;
     }
   }
 }
 
-template <typename T>
-hipError_t launch(hipStream_t st, const SampleArgs& a) {
-  const bool aligned = (uintptr_t)a.logits % 16 == 0 && a.stride * sizeof(T) % 16 == 0;
-  auto* f = aligned ? k_sample<T, true> : k_sample<T, false>;
-  hipLaunchKernelGGL(f, dim3(a.rows), dim3(THREADS), 0, st, a);
+// Logits of a part: as many as a thread's registers hold with ease (32) where there are many; half of them where a short launch is spread over more CUs.
+int part_logits(int rows, int vocab) { return (int64_t)rows * ((vocab + 4095) / 4096) > 2048 ? 8192 : 4096; }
+
+// the workspace's arrays for so many rows, behind one another; its bytes
+size_t place(SampleArgs& a, int rows, char* base) {
+  const size_t parts = (size_t)rows * a.parts;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { char* p = base + at; at += (bytes + 15) / 16 * 16; return p; };
+  a.tops = (Part*)take(parts * sizeof(Part));
+  a.sums = (PartSums*)take(parts * sizeof(PartSums));
+  a.bins = (uint64_t*)take(parts * BINS * 8);
+  a.maxima = (float*)take(parts * PART_THREADS * 4);
+  a.state = (RowState*)take(rows * sizeof(RowState));
+  a.list = (uint64_t*)take((size_t)rows * LIST * 8);
+  return at;
+}
+
+template <typename T, bool ALIGNED>
+hipError_t launch(hipStream_t st, const SampleArgs& a, int rows) {
+  const dim3 grid(a.parts, rows), wg(PART_THREADS);
+  const bool wide = a.part == 8192;
+  if (wide) hipLaunchKernelGGL((k_sample_parts<T, ALIGNED, 32>), grid, wg, 0, st, a);
+  else hipLaunchKernelGGL((k_sample_parts<T, ALIGNED, 16>), grid, wg, 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.top_k || a.top_p || a.min_p) {
+    hipLaunchKernelGGL(k_sample_edges, dim3(rows), dim3(THREADS), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (wide) hipLaunchKernelGGL((k_sample_collect<T, ALIGNED, 32>), grid, wg, 0, st, a);
+    else hipLaunchKernelGGL((k_sample_collect<T, ALIGNED, 16>), grid, wg, 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((k_sample_pick<T, ALIGNED>), dim3(rows), dim3(THREADS), 0, st, a);
   return hipGetLastError();
 }
 
+// A lot of rows at a time; the rows' arrays move along.
+template <typename T>
+hipError_t launch_rows(hipStream_t st, SampleArgs a, int rows) {
+  const bool aligned = (uintptr_t)a.logits % 16 == 0 && a.stride * sizeof(T) % 16 == 0;
+  for (int done = 0; done < rows; done += ROWS_AT_ONCE) {
+    SampleArgs b = a;
+    b.logits = (const T*)a.logits + (int64_t)done * a.stride;
+    if (a.temperature) b.temperature += done;
+    if (a.top_k) b.top_k += done;
+    if (a.top_p) b.top_p += done;
+    if (a.min_p) b.min_p += done;
+    b.u += done; b.ids += done;
+    if (a.probs) b.probs += done;
+    const int n = std::min(rows - done, ROWS_AT_ONCE);
+    const hipError_t e = aligned ? launch<T, true>(st, b, n) : launch<T, false>(st, b, n);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+bool too_large(int vocab) { return vocab > MOST_PARTS * 4096; }
+
 }  // namespace
+
+extern "C" size_t esp_sample_scratch_bytes(int32_t rows, int32_t vocab) {
+  if (rows < 1 || vocab < 1 || too_large(vocab)) return 0;
+  SampleArgs a{};
+  const int n = std::min(rows, ROWS_AT_ONCE);
+  a.part = part_logits(n, vocab);
+  a.parts = (vocab + a.part - 1) / a.part;
+  return place(a, n, nullptr);
+}
 
 extern "C" esp_status esp_sample(void* stream, int32_t dtype, const void* logits, int64_t row_stride, int32_t rows, int32_t vocab,
                                  const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
-                                 int32_t* ids, float* probs) {
+                                 int32_t* ids, float* probs, void* scratch, size_t scratch_bytes) {
   if (!logits || !u || !ids || rows < 0 || vocab < 1) return ESP_EINVAL;
   if (dtype != ESP_F32 && dtype != ESP_BF16) return ESP_EDTYPE;
   if (row_stride < vocab) return ESP_ESHAPE;
-  // ids are counted in 31 bits with room for a workgroup's pieces behind the last; a launch counts threads in 32
-  if (vocab > (1 << 24) || rows >= (1 << 22)) return ESP_ECAPACITY;
+  if (too_large(vocab)) return ESP_ECAPACITY;
   if (rows == 0) return ESP_OK;
+  if (!scratch || scratch_bytes < esp_sample_scratch_bytes(rows, vocab)) return ESP_ECAPACITY;
+  if ((uintptr_t)scratch % 16) return ESP_EINVAL;
   int log2_vocab = 0;
   while ((1 << log2_vocab) < vocab) ++log2_vocab;
-  const SampleArgs a{logits, row_stride, rows, vocab, std::min(50, 62 - log2_vocab), temperature, top_k, top_p, min_p, u, ids, probs};
-  const hipError_t e = dtype == ESP_F32 ? launch<float>((hipStream_t)stream, a) : launch<bf16_t>((hipStream_t)stream, a);
+  SampleArgs a{};
+  a.logits = logits; a.stride = row_stride; a.vocab = vocab;
+  a.shift = std::min(45, 62 - log2_vocab);
+  a.part = part_logits(std::min(rows, ROWS_AT_ONCE), vocab);
+  a.parts = (vocab + a.part - 1) / a.part;
+  a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.u = u; a.ids = ids; a.probs = probs;
+  place(a, std::min(rows, ROWS_AT_ONCE), (char*)scratch);
+  const hipError_t e = dtype == ESP_F32 ? launch_rows<float>((hipStream_t)stream, a, rows) : launch_rows<bf16_t>((hipStream_t)stream, a, rows);
   return e == hipSuccess ? ESP_OK : ESP_EDEVICE;
 }

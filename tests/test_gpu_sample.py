@@ -1,7 +1,7 @@
 """The choice of tokens from logits (sample) against its definition in 64 bits.
 
-Whole numbers have to be equal.  The kernel's weights are off by 7e-12 of themselves (what its series leaves out) and by half of 2^-S, S = min(50, 62 - ceil
-log2 vocab), where the largest weighs 1.  A sum of n of them is off by n times that at most, a border's place among all, W, by twice (7e-12 + n 2^-S-1 / W);
+Whole numbers have to be equal.  The kernel's weights are off by 1.1e-12 of themselves (its polynomial; 3e-12 with the roundings) and by half of 2^-S, S = min(45, 62 - ceil
+log2 vocab), where the largest weighs 1.  A sum of n of them is off by n times that at most, a border's place among all, W, by twice (3e-12 + n 2^-S-1 / W);
 beside it 1e-13 for the reference's own sums.  Where the number u, or a limit, is nearer to a border than that, both sides of it are right and the row
 says nothing; a test says how many such rows it may have.  probs: the quotient rounded to fp32, and those errors."""
 import math
@@ -31,8 +31,8 @@ def choose(x, T, k, p, m, u):
         return int(order[0]), 1.0, math.inf
     w = np.exp((x[order] - x[order[0]]) / T)
     near = math.inf                                    # nearest border, in units of what it may be off by
-    half_step = 2.0 ** -(min(50, 62 - math.ceil(math.log2(len(x)))) + 1)
-    allowed = lambda n, total: 2 * (7e-12 + n * half_step / total) + 1e-13          # noqa: E731
+    half_step = 2.0 ** -(min(45, 62 - math.ceil(math.log2(len(x)))) + 1)
+    allowed = lambda n, total: 2 * (3e-12 + n * half_step / total) + 1e-13          # noqa: E731
     if k > 0:
         w = w[:k]
     if p < 1:
@@ -43,7 +43,7 @@ def choose(x, T, k, p, m, u):
         w = w[:max(1, int(np.count_nonzero(before[:-1] < goal)))]
     if m > 0:
         # (what weighs less than 1e-9 makes no difference that the other errors do not make)
-        near = min(near, (np.abs(w - min(m, 1.0)) / (7e-12 * w + 2 * half_step))[(w < 1) & (w > 1e-9)].min(initial=math.inf))
+        near = min(near, (np.abs(w - min(m, 1.0)) / (3e-12 * w + 2 * half_step))[(w < 1) & (w > 1e-9)].min(initial=math.inf))
         w = w[:max(1, int(np.count_nonzero(w >= min(m, 1.0))))]
     by_id = np.argsort(order[:len(w)])
     run, total = np.cumsum(w[by_id]), math.fsum(w)
@@ -215,8 +215,10 @@ def test_outputs_without_probs_and_no_rows():
     ids, probs = torch.full((5,), -7, dtype=torch.int32).cuda(), torch.full((5,), -7.0).cuda()
     a, b = B.sample(x, u, ids=ids, probs=probs)
     assert a is ids and b is probs and (ids >= 0).all() and (probs > 0).all()
+    scratch = torch.full((B.sample_scratch_bytes(5, 700),), 255, dtype=torch.uint8).cuda()
     lib, only = B.load_library(), torch.full((6,), -7, dtype=torch.int32).cuda()
-    assert lib.esp_sample(B._stream_ptr(), B.ESP_F32, x.data_ptr(), 700, 5, 700, None, None, None, None, u.data_ptr(), only.data_ptr(), None) == 0
+    assert lib.esp_sample(B._stream_ptr(), B.ESP_F32, x.data_ptr(), 700, 5, 700, None, None, None, None, u.data_ptr(), only.data_ptr(), None, scratch.data_ptr(),
+                          scratch.numel()) == 0
     assert torch.equal(only[:5], ids) and int(only[5]) == -7
     assert B.sample(x[:0], u[:0])[0].numel() == 0
 

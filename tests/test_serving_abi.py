@@ -16,14 +16,21 @@ def lib():
 
 
 def test_sample_refusals(lib):
-    def call(dtype=B.ESP_F32, logits=P, stride=100, rows=3, vocab=100, u=P, ids=P):
-        return lib.esp_sample(None, dtype, logits, stride, rows, vocab, None, None, None, None, u, ids, None)
+    def call(dtype=B.ESP_F32, logits=P, stride=100, rows=3, vocab=100, u=P, ids=P, scratch=P, n=1 << 30):
+        return lib.esp_sample(None, dtype, logits, stride, rows, vocab, None, None, None, None, u, ids, None, scratch, n)
     assert call(logits=None) == EINVAL and call(u=None) == EINVAL and call(ids=None) == EINVAL
     assert call(rows=-1) == EINVAL and call(vocab=0) == EINVAL and call(vocab=-5) == EINVAL
     assert call(dtype=2) == EDTYPE and call(dtype=-1) == EDTYPE
     assert call(stride=99) == ESHAPE and call(stride=0) == ESHAPE
-    assert call(vocab=2 ** 24 + 1, stride=2 ** 25) == ECAPACITY and call(rows=2 ** 22) == ECAPACITY
+    assert call(vocab=2 ** 22 + 1, stride=2 ** 25) == ECAPACITY
     assert call(rows=0) == 0
+    for rows, vocab in ((1, 1), (3, 4097), (64, 128256), (320, 151936), (2 ** 31 - 1, 2 ** 22)):
+        need, lot = lib.esp_sample_scratch_bytes(rows, vocab), min(rows, 1024)
+        parts = [lot * ((vocab + n - 1) // n) for n in (8192, 4096)]
+        assert parts[0] * 9248 <= need - lot * (4096 * 8 + 24) <= parts[1] * 9248 + 16
+        assert call(rows=rows, vocab=vocab, stride=vocab, n=need - 1) == ECAPACITY and call(rows=rows, vocab=vocab, stride=vocab, scratch=None) == ECAPACITY
+        assert call(rows=rows, vocab=vocab, stride=vocab, scratch=P + 8, n=need) == EINVAL
+    assert lib.esp_sample_scratch_bytes(0, 10) == 0 and lib.esp_sample_scratch_bytes(10, 0) == 0 and lib.esp_sample_scratch_bytes(1, 2 ** 22 + 1) == 0
 
 
 @pytest.mark.parametrize("change,code", BAD_CACHE)
@@ -86,7 +93,7 @@ def test_python_checks_of_tensors():
         with pytest.raises(ValueError):
             B.sample(bad, u)
     for kw in (dict(temperature=torch.zeros(2)), dict(temperature=u.double()), dict(top_k=u), dict(top_k=torch.zeros(3, dtype=torch.int64)), dict(top_p=u.half()),
-               dict(min_p=torch.zeros((3, 1))), dict(ids=torch.zeros(3)), dict(probs=torch.zeros(3, dtype=torch.float64)), dict(temperature=torch.zeros(6)[::2])):
+               dict(min_p=torch.zeros((3, 1))), dict(scratch=torch.zeros(1000)), dict(ids=torch.zeros(3)), dict(probs=torch.zeros(3, dtype=torch.float64)), dict(temperature=torch.zeros(6)[::2])):
         with pytest.raises(ValueError):
             B.sample(x, u, **kw)
     with pytest.raises(ValueError):
