@@ -16,6 +16,7 @@
 // logits above 2^20 steps) are divided in k_sample_pick by going over the row again and again, some 100 us.
 #include <algorithm>
 #include <cfloat>
+#include <climits>
 #include <cmath>
 
 #include "esp_internal.h"
@@ -43,7 +44,7 @@ struct RowState {
   int mode, first, last;               // steps of the list; what is before `first` is added up
   unsigned before;                     // tokens before the list
   int list_n;
-  float base;                          // step of the largest logit
+  float top, base;                     // the largest logit, its step
 };
 
 struct SampleArgs {
@@ -151,15 +152,14 @@ __device__ __forceinline__ unsigned lane_of(unsigned v, int l) { return __builti
 __device__ __forceinline__ uint64_t lane_of(uint64_t v, int l) { return (uint64_t)lane_of((unsigned)(v >> 32), l) << 32 | lane_of((unsigned)v, l); }
 template <typename V>
 __device__ __forceinline__ V wave_total(V v) { return lane_of(running_sum(v), 63); }
-// the larger of two logits, the lower id of equal ones
-__device__ __forceinline__ void take_larger(float& top, int& at, float other, int other_at) {
-  if (other > top || (other == top && (unsigned)other_at < (unsigned)at)) { top = other; at = other_at; }
-}
-__device__ __forceinline__ void wave_largest(float& top, int& at) {
-  const unsigned low = __float_as_uint(-INFINITY);
-  const float m = __uint_as_float(lane_of(running(__float_as_uint(top), low, [](unsigned a, unsigned b) {
+__device__ __forceinline__ unsigned wave_most(unsigned float_bits) {
+  return lane_of(running(float_bits, __float_as_uint(-INFINITY), [](unsigned a, unsigned b) {
     return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
-  }), 63));
+  }), 63);
+}
+// the largest of a wave's logits, the lowest id of equal ones
+__device__ __forceinline__ void wave_largest(float& top, int& at) {
+  const float m = __uint_as_float(wave_most(__float_as_uint(top)));
   at = (int)lane_of(running(top == m ? (unsigned)at : ~0u, ~0u, [](unsigned a, unsigned b) { return min(a, b); }), 63);
   top = m;
 }
@@ -202,7 +202,7 @@ template <typename T, bool ALIGNED, int PER>           // PER logits a thread
 __global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
   constexpr int N = Piece<T>::N, PIECES = PER / N;
   __shared__ float wave_top[4];
-  __shared__ int wave_at[4];
+  __shared__ int first_at;
   __shared__ double wave_sum[4];
   __shared__ uint64_t bins[BINS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = blockIdx.x, row = blockIdx.y;
@@ -225,21 +225,23 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
 #pragma unroll
       for (int i = 0; i < N; ++i) x[j][i] = tame(x[j][i]);
   }
-  float top = own;
-  int at = -1;
-  if (top > -INFINITY) {
+  // the largest of all, then its first id among the few threads that have it
+  const float of_wave = __uint_as_float(wave_most(__float_as_uint(own)));
+  if (lane == 0) wave_top[wave] = of_wave;
+  if (tid == 0) first_at = INT_MAX;
+  __syncthreads();
+  const float top = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
+  if (own == top && top > -INFINITY) {
+    int at = INT_MAX;
 #pragma unroll
     for (int j = PIECES - 1; j >= 0; --j)
 #pragma unroll
       for (int i = N - 1; i >= 0; --i) at = x[j][i] == top ? lo + (j * PART_THREADS + tid) * N + i : at;
+    atomicMin(&first_at, at);
   }
-  wave_largest(top, at);
-  if (lane == 0) { wave_top[wave] = top; wave_at[wave] = at; }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 4; ++w) take_larger(top, at, wave_top[w], wave_at[w]);
+  if (draws(m) && limited(m)) a.maxima[mine * PART_THREADS + tid] = own;
   double sum = 0.0;
-  if (draws(m) && at >= 0) {
+  if (draws(m) && top > -INFINITY) {
     if (all_count(m)) {
       const Weigher weight{(double)top, octaves(m)};
       double s[2] = {0.0, 0.0};
@@ -254,7 +256,6 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
       __syncthreads();
       sum = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
     }
-    if (limited(m)) a.maxima[mine * PART_THREADS + tid] = own;
     if (m.by_count || m.by_sum) {
       for (int i = tid; i < BINS; i += PART_THREADS) bins[i] = 0;
       __syncthreads();
@@ -273,7 +274,8 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
       for (int i = tid; i < BINS; i += PART_THREADS) a.bins[mine * BINS + i] = bins[i];
     }
   }
-  if (tid == 0) a.tops[mine] = {top, at, sum};
+  __syncthreads();
+  if (tid == 0) a.tops[mine] = {top, top > -INFINITY ? first_at : -1, sum};
 }
 
 // ---- a workgroup a row -----------------------------------------------------------------------------------------
@@ -282,28 +284,31 @@ struct Sums {                          // of a workgroup's waves
   uint64_t sum[WAVES];
   unsigned cnt[WAVES];
 };
-// sums of the threads before this one, in place; all threads'
-__device__ __forceinline__ void before(Sums& s, unsigned& cnt, uint64_t& sum, unsigned& all_cnt, uint64_t& all_sum) {
+// sums of the threads before this one, in place; returns all threads'
+__device__ __forceinline__ uint64_t before(Sums& s, uint64_t& sum) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const unsigned c = running_sum(cnt);
   const uint64_t q = running_sum(sum);
   __syncthreads();
-  if (lane == 63) { s.cnt[wave] = c; s.sum[wave] = q; }
+  if (lane == 63) s.sum[wave] = q;
   __syncthreads();
-  const unsigned of_c = running_sum(lane < WAVES ? s.cnt[lane & (WAVES - 1)] : 0u);
-  const uint64_t of_q = running_sum(lane < WAVES ? s.sum[lane & (WAVES - 1)] : (uint64_t)0);
-  all_cnt = lane_of(of_c, WAVES - 1);
-  all_sum = lane_of(of_q, WAVES - 1);
+  const uint64_t of = running_sum(lane < WAVES ? s.sum[lane & (WAVES - 1)] : (uint64_t)0);
   const int last = __builtin_amdgcn_readfirstlane(wave) - 1;
-  cnt = c - cnt + (last >= 0 ? lane_of(of_c, max(last, 0)) : 0u);
-  sum = q - sum + (last >= 0 ? lane_of(of_q, max(last, 0)) : (uint64_t)0);
+  sum = q - sum + (last >= 0 ? lane_of(of, max(last, 0)) : (uint64_t)0);
+  return lane_of(of, WAVES - 1);
 }
-__device__ __forceinline__ uint64_t total_of(Sums& s, uint64_t sum) {
-  unsigned none = 0, c;
-  uint64_t all;
-  before(s, none, sum, c, all);
-  return all;
+__device__ __forceinline__ unsigned before(Sums& s, unsigned& cnt) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const unsigned c = running_sum(cnt);
+  __syncthreads();
+  if (lane == 63) s.cnt[wave] = c;
+  __syncthreads();
+  const unsigned of = running_sum(lane < WAVES ? s.cnt[lane & (WAVES - 1)] : 0u);
+  const int last = __builtin_amdgcn_readfirstlane(wave) - 1;
+  cnt = c - cnt + (last >= 0 ? lane_of(of, max(last, 0)) : 0u);
+  return lane_of(of, WAVES - 1);
 }
+template <typename V>
+__device__ __forceinline__ V total_of(Sums& s, V v) { return before(s, v); }
 
 // The parts of a row: a thread's own, the largest logit of all and its first id.
 struct Joined { Part mine; float top; int at; };
@@ -332,7 +337,7 @@ static_assert(BINS == THREADS, "k_sample_edges: a thread a step");
 __global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
   __shared__ Sums s;
   __shared__ float wave_top[WAVES];
-  __shared__ int wave_at[WAVES], offset[MOST_PARTS];
+  __shared__ int wave_at[WAVES];
   __shared__ int found[4];
   const int tid = threadIdx.x, row = blockIdx.x;
   const Limits m = limits(a, row);
@@ -344,7 +349,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
   const Joined j = join_parts(a, row, wave_top, wave_at);
   const float per = steps(a, m), base = step_of(j.top, per);
   const double octave = (double)(a.shift + 2) / BINS;  // of a step
-  RowState st{COLLECT, 0, -1, 0u, 0, base};
+  RowState st{COLLECT, 0, -1, 0u, 0, j.top, base};
   // (largest logits between which the parts' differ by 2^20 steps and more differ by more than 47 powers of two: nothing there counts)
   if (j.at < 0 || !(fabsf(j.top * per) < FAR_STEPS)) {
     if (tid == 0) { st.mode = j.at < 0 ? AS_IT_IS : DIVIDE; out = st; }
@@ -355,18 +360,24 @@ __global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
     if (tid == 0) out = st;
     return;
   }
-  if (tid < a.parts) {
-    const float d = j.mine.at < 0 ? (float)BINS : base - step_of(j.mine.top, per);
-    offset[tid] = d < (float)BINS ? (int)d : BINS;
-  }
   if (tid < 4) found[tid] = tid == 1 ? BINS - 1 : 0;
-  __syncthreads();
   unsigned n = 0, places = 0, squares = 0;
-#pragma unroll 4
-  for (int p = 0; p < a.parts; ++p) {
-    const int i = tid - offset[p];
-    const uint64_t v = i >= 0 ? a.bins[((int64_t)row * a.parts + p) * BINS + i] : 0ull;
-    n += (unsigned)(v >> 44); places += (unsigned)(v >> 22) & 0x3fffffu; squares += (unsigned)v & 0x3fffffu;
+  for (int p0 = 0; p0 < a.parts; p0 += 64) {
+    // lane l: by how many steps part p0 + l begins below the row's largest (BINS: by all of them)
+    const int p = p0 + (tid & 63);
+    const Part of = p < a.parts ? a.tops[(int64_t)row * a.parts + p] : Part{0.f, -1, 0.0};
+    const float d = of.at < 0 ? (float)BINS : fminf(base - step_of(of.top, per), (float)BINS);
+    const int by = (int)d;
+    for (int e0 = 0; e0 < min(64, a.parts - p0); e0 += 16) {       // (sixteen parts' on their way at once)
+      uint64_t v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int i = tid - __builtin_amdgcn_readlane(by, e0 + e);
+        v[e] = i >= 0 ? a.bins[((int64_t)row * a.parts + p0 + e0 + e) * BINS + i] : 0ull;
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) { n += (unsigned)(v[e] >> 44); places += (unsigned)(v[e] >> 22) & 0x3fffffu; squares += (unsigned)v[e] & 0x3fffffu; }
+    }
   }
   // Sums of weights in units of 2^-40.  A token at place f of a step weighs 1 + k f + (k f)^2 / 2 + up to k^3 / 5 times what one at its lower end does,
   // k = ln 2 octave = 0.032: 6.6e-6 for the last, k / PLACES = 6e-5 for the place, k^2 / PLACES = 2e-6 for its square; the first two taken at their
@@ -376,9 +387,8 @@ __global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
   const uint64_t w = (uint64_t)(middle * (double)__builtin_amdgcn_exp2f((float)(40.0 - (tid + up) * octave)));
   unsigned c0 = n;
   uint64_t q0 = w;
-  unsigned alive;
-  uint64_t unused;
-  before(s, c0, q0, alive, unused);
+  const unsigned alive = before(s, c0);
+  if (!m.by_count) before(s, q0);
   if (m.by_count) {                    // (no cut, if fewer weigh anything: the last step)
     const unsigned want = min((unsigned)m.top_k, alive);
     if (c0 < want && want <= c0 + n) found[0] = found[1] = tid;
@@ -410,8 +420,8 @@ __global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
 template <typename T, bool ALIGNED, int PER>
 __global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
   constexpr int N = Piece<T>::N, PIECES = PER / N;
-  __shared__ uint64_t list[LIST];
-  __shared__ uint64_t wave_sum[4][2];
+  __shared__ unsigned short list[LIST];                // places in the part
+  __shared__ double wave_sum[4][2];
   __shared__ unsigned list_n, place;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = blockIdx.x, row = blockIdx.y;
   const int64_t mine = (int64_t)row * a.parts + part;
@@ -419,21 +429,15 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
   if (st.mode != COLLECT) return;
   const Limits m = limits(a, row);
   const Row<T, ALIGNED> r(a, row);
-  const float per = steps(a, m), first = (float)st.first, end = (float)max(st.first, st.last + 1);
-  // the largest logit has the step st.base: its weight's reference is found as its own part found it
-  __shared__ float tops[4];
-  float top = -INFINITY;
-  for (int i = tid; i < a.parts; i += PART_THREADS) top = fmaxf(top, a.tops[(int64_t)row * a.parts + i].top);
-  top = wave_max(top);
-  if (lane == 0) tops[wave] = top;
+  // step < n is x per >= base - n + 1
+  const float per = steps(a, m), ahead = st.base - (float)st.first + 1.f, listed = st.base - (float)max(st.first, st.last + 1) + 1.f;
   if (tid == 0) list_n = 0;
+  const float own = a.maxima[mine * PART_THREADS + tid];
+  const Weigher weight{(double)st.top, octaves(m)};
   __syncthreads();
-  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  const Weigher weight{(double)top, octaves(m)};
-  const uint64_t least = m.by_part ? max(1ull, (uint64_t)__builtin_rint(__builtin_ldexp((double)fminf(m.min_p, 1.f), a.shift))) : 1ull;
-  uint64_t all = 0, in = 0;
-  const float own = a.tops[mine].at < 0 ? -INFINITY : a.maxima[mine * PART_THREADS + tid];
-  if (st.base - step_of(own, per) < end) {
+  const double least = m.by_part ? __builtin_rint(__builtin_ldexp((double)fminf(m.min_p, 1.f), a.shift)) - 0.5 : 0.0;
+  double all = 0.0, in = 0.0;
+  if (own * per >= listed) {
     float x[PIECES][N];
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) r.load(min(part * (PART_THREADS * PER) + (j * PART_THREADS + tid) * N, a.vocab), x[j]);
@@ -442,37 +446,41 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
       float most = x[j][0] = tame(x[j][0]);
 #pragma unroll
       for (int i = 1; i < N; ++i) { x[j][i] = tame(x[j][i]); most = fmaxf(most, x[j][i]); }
-      const float nearest = st.base - step_of(most, per);
-      if (nearest < first) {
+      if (most * per >= ahead) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {  // (of the piece's others too: side by side they take less time than branches do)
-          const uint64_t q = st.base - step_of(x[j][i], per) < first ? weight.whole(x[j][i], a.shift) : 0ull;
-          all += q;
-          in += q >= least ? q : 0ull;
+        for (int i = 0; i < N; ++i) {  // (the piece's others weigh 2^-900: side by side they take less time than branches do)
+          const double w = weight.real(x[j][i] * per >= ahead ? x[j][i] : -INFINITY, a.shift);
+          all += w;
+          if (m.by_part) in += w >= least ? w : 0.0;
         }
       }
-      if (nearest < end && first < end) {
+      if (most * per >= listed && st.first <= st.last) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const float step = st.base - step_of(x[j][i], per);
-          if (step >= first && step < end) {
+          const float t = x[j][i] * per;
+          if (t >= listed && t < ahead) {
             const unsigned n = atomicAdd(&list_n, 1u);
-            if (n < LIST) list[n] = (uint64_t)key_of(x[j][i]) << 32 | (unsigned)~(part * (PART_THREADS * PER) + (j * PART_THREADS + tid) * N + i);
+            if (n < LIST) list[n] = (unsigned short)((j * PART_THREADS + tid) * N + i);
           }
         }
       }
     }
   }
-  all = wave_total(all); in = wave_total(in);
-  if (lane == 0) { wave_sum[wave][0] = all; wave_sum[wave][1] = in; }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) { all += __shfl_xor(all, o); if (m.by_part) in += __shfl_xor(in, o); }
+  if (lane == 0) { wave_sum[wave][0] = all; wave_sum[wave][1] = m.by_part ? in : all; }
   __syncthreads();
   if (tid == 0) {
-    a.sums[mine] = {wave_sum[0][0] + wave_sum[1][0] + wave_sum[2][0] + wave_sum[3][0], wave_sum[0][1] + wave_sum[1][1] + wave_sum[2][1] + wave_sum[3][1]};
+    a.sums[mine] = {(uint64_t)__builtin_rint((wave_sum[0][0] + wave_sum[1][0]) + (wave_sum[2][0] + wave_sum[3][0])),
+                    (uint64_t)__builtin_rint((wave_sum[0][1] + wave_sum[1][1]) + (wave_sum[2][1] + wave_sum[3][1]))};
     place = list_n ? atomicAdd((unsigned*)&a.state[row].list_n, list_n) : 0u;
   }
   __syncthreads();
   for (unsigned i = tid; i < min(list_n, (unsigned)LIST); i += PART_THREADS)
-    if (place + i < LIST) a.list[(int64_t)row * LIST + place + i] = list[i];
+    if (place + i < LIST) {
+      const int id = part * (PART_THREADS * PER) + list[i];
+      a.list[(int64_t)row * LIST + place + i] = (uint64_t)key_of(tame(to_f32(r.p[id]))) << 32 | (unsigned)~id;
+    }
 }
 
 struct Shared {
@@ -497,12 +505,23 @@ struct Cut {
 };
 
 template <typename T, bool ALIGNED>
-__global__ __launch_bounds__(THREADS) void k_sample_pick(SampleArgs a) {
+__global__ __launch_bounds__(THREADS, 8) void k_sample_pick(SampleArgs a) {
   __shared__ Shared s;
   constexpr int N = Piece<T>::N;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, vocab = a.vocab, shift = a.shift;
   const Limits lim = limits(a, row);
   const Row<T, ALIGNED> r(a, row);
+  // all that may be wanted is asked for at once
+  const bool narrow = draws(lim) && limited(lim);
+  const float u = a.u[row];
+  RowState st{AS_IT_IS, 0, -1, 0u, 0, 0.f, 0.f};
+  PartSums mine{0, 0};
+  uint64_t listed_first = 0;
+  if (narrow) {
+    st = a.state[row];
+    if (tid < a.parts) mine = a.sums[(int64_t)row * a.parts + tid];
+    listed_first = a.list[(int64_t)row * LIST + tid];
+  }
   const Joined j = join_parts(a, row, s.wave_top, s.wave_at);
   if (!draws(lim) || j.at < 0) {       // nothing to choose, or the first of the order
     if (tid == 0) {
@@ -513,21 +532,17 @@ __global__ __launch_bounds__(THREADS) void k_sample_pick(SampleArgs a) {
     return;
   }
   const Weigher weight{(double)j.top, octaves(lim)};
-  const float u = a.u[row];
   const double uu = u > 0.f ? (double)fminf(u, 0.99999994f) : 0.0;
   const uint64_t least = lim.by_part ? max(1ull, (uint64_t)__builtin_rint(__builtin_ldexp((double)fminf(lim.min_p, 1.f), shift))) : 1ull;
   Cut cut{0u, 0u, 0ull};               // all is in
   uint64_t own = part_weight(j.mine, weight, shift);             // this thread's part: what is in
   unsigned own_ties = 0;
-  const bool narrow = limited(lim);
 
   if (narrow) {
-    const RowState st = a.state[row];
     const bool listed = st.mode == COLLECT;
     const unsigned listed_n = listed ? min((unsigned)st.list_n, (unsigned)LIST) : 0u;
     const bool from_top = listed && st.first == 0;
-    PartSums mine{0, 0};
-    if (listed && tid < a.parts) mine = a.sums[(int64_t)row * a.parts + tid];
+    if (!listed) mine = {0, 0};
     const uint64_t all = lim.by_sum ? total_of(s.sums, own) : 0ull;            // of all tokens (top-p without top-k)
     const uint64_t q0 = from_top ? 0ull : total_of(s.sums, mine.all);          // of those before the list
     own = mine.in;
@@ -551,7 +566,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_pick(SampleArgs a) {
     s.part_sum[tid] = own;
     s.part_ties[tid] = 0;
 #pragma unroll 1
-    for (unsigned i = tid; i < listed_n; i += THREADS) s.list[i] = a.list[(int64_t)row * LIST + i];
+    for (unsigned i = tid; i < listed_n; i += THREADS) s.list[i] = i < THREADS ? listed_first : a.list[(int64_t)row * LIST + i];
     __syncthreads();
     unsigned k_min = ~0u, k_max = 0u, here = 0;
     uint64_t weights = 0;
@@ -559,10 +574,12 @@ __global__ __launch_bounds__(THREADS) void k_sample_pick(SampleArgs a) {
       const uint64_t q = weight.whole(of_key(k), shift);
       if (q) { k_min = min(k_min, k); k_max = max(k_max, k); ++here; weights += q; }
     });
-    if (here) { atomicMin(&s.key_lo, k_min); atomicMax(&s.key_hi, k_max); }
-    unsigned list_cnt;
-    uint64_t list_sum;
-    before(s.sums, here, weights, list_cnt, list_sum);
+    // (an atomic of a wave's lanes on one word is a loop over them)
+    k_min = lane_of(running(k_min, ~0u, [](unsigned x, unsigned y) { return min(x, y); }), 63);
+    k_max = lane_of(running(k_max, 0u, [](unsigned x, unsigned y) { return max(x, y); }), 63);
+    if (lane == 0 && k_max) { atomicMin(&s.key_lo, k_min); atomicMax(&s.key_hi, k_max); }
+    const unsigned list_cnt = total_of(s.sums, here);
+    const uint64_t list_sum = total_of(s.sums, weights);
     const unsigned list_lo = s.key_lo, list_hi = s.key_hi, ahead_cnt = listed && !from_top ? st.before : 0u;
     cut.sum = lim.by_count || !listed ? q0 + list_sum : all;
 #pragma unroll 1
@@ -590,23 +607,27 @@ __global__ __launch_bounds__(THREADS) void k_sample_pick(SampleArgs a) {
         __syncthreads();
         if (n <= FEW) {                // (their places in sub_sum)
           if (tid == 0) s.few_n = 0;
+          if (tid < FEW) { s.sub_cnt[tid] = 0; s.sub_sum[FEW + tid] = 0; }
           __syncthreads();
           tokens([&](unsigned k, int id) {
-            if (k >= k_lo && k <= k_hi && weight.whole(of_key(k), shift)) s.sub_sum[atomicAdd(&s.few_n, 1u) & (THREADS - 1)] = (uint64_t)k << 32 | (unsigned)~id;
+            if (k >= k_lo && k <= k_hi && weight.whole(of_key(k), shift)) s.sub_sum[atomicAdd(&s.few_n, 1u) & (FEW - 1)] = (uint64_t)k << 32 | (unsigned)~id;
           });
           __syncthreads();
+          // A lane has a token, a wave compares all with four of them: how many come before it, and what they weigh
+          const uint64_t token = lane < (int)n ? s.sub_sum[lane] : 0ull;
+          const unsigned k = (unsigned)(token >> 32);
+          const uint64_t w = lane < (int)n ? weight.whole(of_key(k), shift) : 0ull;
+          unsigned rank = 0;
+          uint64_t ahead = 0;
+#pragma unroll
+          for (int e = 0; e < FEW / WAVES; ++e) {
+            const int i = __builtin_amdgcn_readfirstlane(wave) * (FEW / WAVES) + e;
+            if (lane_of(token, i) > token) { ++rank; ahead += lane_of(w, i); }
+          }
+          if (lane < (int)n && rank) { atomicAdd(&s.sub_cnt[lane], rank); atomicAdd((unsigned long long*)&s.sub_sum[FEW + lane], (unsigned long long)ahead); }
+          __syncthreads();
           if (wave == 0) {
-            const uint64_t token = lane < (int)n ? s.sub_sum[lane] : 0ull;
-            const unsigned k = (unsigned)(token >> 32);
-            const uint64_t w = lane < (int)n ? weight.whole(of_key(k), shift) : 0ull;
-            unsigned rank = 0;
-            uint64_t ahead = 0;
-#pragma unroll 1
-            for (int i = 0; i < (int)n; ++i) {
-              const uint64_t other = s.sub_sum[i];
-              const unsigned w_lo = __builtin_amdgcn_readlane((unsigned)w, i), w_hi = __builtin_amdgcn_readlane((unsigned)(w >> 32), i);
-              if (other > token) { ++rank; ahead += (uint64_t)w_hi << 32 | w_lo; }
-            }
+            rank = s.sub_cnt[lane]; ahead = s.sub_sum[FEW + lane];
             const bool in = lane < (int)n && c0 + rank < count && q + ahead < goal;
             const int last = __popcll(__builtin_amdgcn_ballot_w64(in)) - 1;      // (what is in is a prefix of the ranking)
             if (in && (int)rank == last) { s.few_key = k; s.found_sum = q + ahead + w; }
@@ -634,9 +655,8 @@ __global__ __launch_bounds__(THREADS) void k_sample_pick(SampleArgs a) {
         const uint64_t w = s.sub_sum[tid];
         unsigned c1 = m;
         uint64_t q1 = w;
-        unsigned all_c;
-        uint64_t all_q;
-        before(s.sums, c1, q1, all_c, all_q);
+        before(s.sums, c1);
+        before(s.sums, q1);
         c1 += c0; q1 += q;
         if (m && c1 < count && q1 < goal && (c1 + m >= count || q1 + w >= goal)) {
           s.found_cnt = c1; s.found_sum = q1; s.found_n = m;
@@ -664,13 +684,11 @@ __global__ __launch_bounds__(THREADS) void k_sample_pick(SampleArgs a) {
 
   // the part in which the target lies; of tokens at the cut's logit the first by id are in
   const uint64_t tie_q = cut.key ? weight.whole(of_key(cut.key), shift) : 0ull;
-  unsigned ties_ahead = own_ties, none = 0, all_c;
-  uint64_t unused = 0, total;
-  if (cut.key) before(s.sums, ties_ahead, unused, all_c, total);
+  unsigned ties_ahead = own_ties;
+  if (cut.key) before(s.sums, ties_ahead);
   own += tie_q * min(own_ties, cut.ties - min(ties_ahead, cut.ties));
   uint64_t ahead = own;
-  before(s.sums, none, ahead, all_c, total);
-  const uint64_t target = min((uint64_t)(uu * (double)total), total - 1);
+  const uint64_t total = before(s.sums, ahead), target = min((uint64_t)(uu * (double)total), total - 1);
   if (target >= ahead && target < ahead + own) {
     s.found_part = tid; s.found_sum = own; s.ahead_sum = ahead; s.ahead_ties = ties_ahead;
     s.found_top = j.mine.top;
@@ -708,15 +726,21 @@ __global__ __launch_bounds__(THREADS) void k_sample_pick(SampleArgs a) {
   }
   const uint64_t own_sum = sum;
   const unsigned own_count = ties;
-  uint64_t of_part;
-  before(s.sums, ties, sum, all_c, of_part);           // of the threads before
+  uint64_t of_part = before(s.sums, sum);              // of the threads before
+  const unsigned all_c = cut.key ? before(s.sums, ties) : 0u;
   const unsigned left0 = cut.ties - min(s.ahead_ties, cut.ties), left = cut.ties - min(s.ahead_ties + ties, cut.ties);
-  uint64_t goal = target - s.ahead_sum, at_q = sum + tie_q * (left0 - left);
-  double share = 1.0 / (double)total;
-  if (!narrow) {                       // (of the part's sum in these units)
-    goal = min((uint64_t)((double)goal / (double)s.found_sum * (double)of_part), of_part - 1);
-    share = (double)s.found_sum / (double)of_part / (double)total;
+  // The part's sum was of weights before they were rounded, or against its own largest: the target in the units of this one.
+  of_part += tie_q * min(all_c, left0);
+  if (of_part == 0) {                  // (a part of nothing but less than half units: the largest stands for it)
+    if (tid == 0) {
+      a.ids[row] = j.at;
+      if (a.probs) a.probs[row] = (float)(__builtin_ldexp(1.0, shift) / (double)total);
+    }
+    return;
   }
+  const uint64_t goal = min((uint64_t)((double)(target - s.ahead_sum) / (double)s.found_sum * (double)of_part), of_part - 1);
+  const double share = (double)s.found_sum / (double)of_part / (double)total;
+  uint64_t at_q = sum + tie_q * (left0 - left);
   if (goal >= at_q && goal < at_q + own_sum + tie_q * min(own_count, left)) {
     unsigned more = left;
 #pragma unroll
