@@ -7,10 +7,11 @@
 // k_evict_move: the list's tokens go to slots 0, 1, ...; a token never moves back, so a plane's blocks of 32 new slots are filled one after the other and what
 // is still to be read lies behind what is written, also where old and new pages are the same.
 #include "esp_paged.h"
+#include "esp_scan.h"
 
 namespace {
 
-constexpr int CHOOSERS = 1024, DIGIT_BINS = 4096;
+constexpr int CHOOSERS = 512, DIGIT_BINS = 4096, EACH = DIGIT_BINS / CHOOSERS;
 
 // larger weights have larger keys; NaN has the least of all
 __device__ __forceinline__ unsigned weight_key(float x) {
@@ -18,31 +19,9 @@ __device__ __forceinline__ unsigned weight_key(float x) {
   return x != x ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// sums over the threads before this one, and of all
-__device__ __forceinline__ uint2 sums_before(uint2 v, uint2& all, uint2* of_wave) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint2 at = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned x = __shfl_up(at.x, o, 64), y = __shfl_up(at.y, o, 64);
-    if (lane >= o) { at.x += x; at.y += y; }
-  }
-  __syncthreads();
-  if (lane == 63) of_wave[wave] = at;
-  __syncthreads();
-  all = {0, 0};
-  uint2 r = {at.x - v.x, at.y - v.y};
-  for (int w = 0; w < CHOOSERS / 64; ++w) {
-    const uint2 t = of_wave[w];
-    if (w < wave) { r.x += t.x; r.y += t.y; }
-    all.x += t.x; all.y += t.y;
-  }
-  return r;
-}
-
 __global__ __launch_bounds__(CHOOSERS) void k_evict_choose(PagedDev kv, EvictArgs a) {
   __shared__ unsigned bins[DIGIT_BINS];
-  __shared__ uint2 of_wave[CHOOSERS / 64];
+  __shared__ WaveSums<CHOOSERS / 64> sums;
   __shared__ unsigned found[2];
   const int tid = threadIdx.x, kvh = blockIdx.x, seq = blockIdx.y, layer = blockIdx.z;
   const int64_t head = ((int64_t)layer * kv.batch + seq) * kv.hkv + kvh;
@@ -73,15 +52,14 @@ __global__ __launch_bounds__(CHOOSERS) void k_evict_choose(PagedDev kv, EvictArg
         if (step == 0 || (k >> (shift + bits)) == (cut >> (shift + bits))) atomicAdd(&bins[(k >> shift) & ((1u << bits) - 1u)], 1u);
       }
       __syncthreads();
-      // thread t has the bins 4 t .. from the largest down
-      unsigned n[4], mine = 0;
+      // thread t has EACH bins, from the largest down
+      unsigned n[EACH], at = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { n[i] = bins[DIGIT_BINS - 1 - (4 * tid + i)]; mine += n[i]; }
-      uint2 all;
-      unsigned at = sums_before({mine, 0}, all, of_wave).x;
+      for (int i = 0; i < EACH; ++i) { n[i] = bins[DIGIT_BINS - 1 - (EACH * tid + i)]; at += n[i]; }
+      before(sums, at);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (at < want && want <= at + n[i]) { found[0] = DIGIT_BINS - 1 - (4 * tid + i); found[1] = at; }
+      for (int i = 0; i < EACH; ++i) {
+        if (at < want && want <= at + n[i]) { found[0] = DIGIT_BINS - 1 - (EACH * tid + i); found[1] = at; }
         at += n[i];
       }
       __syncthreads();
@@ -95,17 +73,17 @@ __global__ __launch_bounds__(CHOOSERS) void k_evict_choose(PagedDev kv, EvictArg
   // `want` of those at the cut are in
   const int run = (len + CHOOSERS - 1) / CHOOSERS, begin = min(tid * run, len), end = min(begin + run, len);
   const bool none = a.keep == a.first + a.recent;
-  uint2 mine = {0, 0};                 // in for certain, at the cut
+  unsigned certain = 0, equal = 0;     // in, and at the cut
   for (int i = begin; i < end; ++i) {
-    if (i < lo || i >= hi) { ++mine.x; continue; }
-    const unsigned k = weight_key(mass[i]);
+    if (i < lo || i >= hi) { ++certain; continue; }
     if (none) continue;
-    mine.x += k > cut;
-    mine.y += k == cut;
+    const unsigned k = weight_key(mass[i]);
+    certain += k > cut;
+    equal += k == cut;
   }
-  uint2 all;
-  const uint2 before = sums_before(mine, all, of_wave);
-  unsigned ties = before.y, place = before.x + min(before.y, want);
+  before(sums, certain);
+  before(sums, equal);
+  unsigned ties = equal, place = certain + min(equal, want);
   for (int i = begin; i < end; ++i) {
     bool in = i < lo || i >= hi;
     if (!in && !none) {
@@ -124,83 +102,160 @@ __global__ __launch_bounds__(CHOOSERS) void k_evict_choose(PagedDev kv, EvictArg
   }
 }
 
+// Tokens in batches of 64 (two blocks), a thread HD / 64 pieces of eight elements of K and of V each.  The next batch is on its way while one is written, and
+// where a token of the one after lies is looked up meanwhile.  A piece of V has eight tokens' elements of one feature: eight loads whose lanes have
+// neighbouring features, 16 bytes (of the type's size, eight elements) apart, so a wave's loads of a block come from lines that they share.
+constexpr int MOVERS = 512, BATCH = 64;
+// an empty statement that takes a value, which therefore has arrived
+template <typename V> __device__ __forceinline__ void wait_for(const V& v) {
+  typedef __attribute__((ext_vector_type(sizeof(V) / 4))) uint32_t words;
+  const words w = __builtin_bit_cast(words, v);
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(V) / 4; ++i) { const uint32_t x = w[i]; asm volatile("" ::"v"(x)); }
+}
+template <typename T> struct Raw { typedef uint32_t type; };
+template <> struct Raw<bf16_t> { typedef uint16_t type; };
+struct Source { int64_t at; int key; };                // first element of the block (-1: outside the pool), place in it
+
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_evict_move(PagedDev kv, EvictArgs a) {
+__global__ __launch_bounds__(MOVERS) void k_evict_move(PagedDev kv, EvictArgs a) {
   typedef __attribute__((ext_vector_type(8))) T vec;
-  constexpr int PIECES = HD / 8;                       // of eight features, of a slot of K
-  constexpr int KN = 32 * PIECES / 256, VN = 32 * HD / 256;
-  __shared__ int from[32];
+  typedef typename Raw<T>::type raw;                   // (loads into halves of a register would wait for one another)
+  constexpr int PIECES = HD / 64;                      // of K, and of V
+  __shared__ Source src[4][BATCH];                     // of the batch that is written, the one on its way, the one after, and one that others may still read
+  __shared__ int64_t dst[4][2];                        // of the batch's blocks; -1: not to be written
+  __shared__ int bad[4];                               // tokens of it lie outside the pool
+  __shared__ int counted[MOVERS / 64];
   const int tid = threadIdx.x, kvh = blockIdx.x, seq = blockIdx.y, layer = blockIdx.z;
   const int32_t* kept = a.kept + (((int64_t)layer * kv.batch + seq) * kv.hkv + kvh) * a.keep;
   const size_t of_layer = (size_t)layer * kv.n_pages * kv.hkv * kv.page_size * HD;
   T* kp = (T*)kv.k + of_layer;
   T* vp = (T*)kv.v + of_layer;
+  const int32_t* table = kv.table + (size_t)seq * kv.stride;
+  const int32_t* table_out = a.table_out + (size_t)seq * a.out_stride;
+
   int n = 0;
-  for (int b = 0; b < a.keep; b += 32) {
-    __syncthreads();
-    if (tid < 32) from[tid] = b + tid < a.keep ? kept[b + tid] : -1;
-    __syncthreads();
-    if (from[0] < 0) break;
-    const int last = 31 - __clz((int)__builtin_amdgcn_ballot_w64((threadIdx.x & 63) < 32 && from[threadIdx.x & 31] >= 0));
-    n = b + last + 1;
-    const int to_page = a.table_out[(size_t)seq * a.out_stride + b / kv.page_size], inside = b % kv.page_size;
-    const bool to_ok = to_page >= 0 && to_page < kv.n_pages;
-    if (!to_ok) {
-      if (tid == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
-      continue;
-    }
-    if (from[last] == b + last && kv.table[(size_t)seq * kv.stride + b / kv.page_size] == to_page) continue;     // (all where they are)
-    auto plane_of = [&](int slot, int& in_page) -> int64_t {
-      const int at = slot / kv.page_size, page = kv.table[(size_t)seq * kv.stride + at];
-      in_page = slot - at * kv.page_size;
-      if (page < 0 || page >= kv.n_pages) return -1;
-      return (int64_t)page_plane(page, kvh, kv.hkv, kv.page_size, HD);
-    };
-    vec k[KN];
-    T v[VN];
-    bool bad = false;
+  for (int i = tid; i < a.keep; i += MOVERS) n += kept[i] >= 0;
+  n = (int)wave_sum((float)n);                         // (a thread has less than 2^13 of them, a wave less than 2^19)
+  if ((tid & 63) == 0) counted[tid >> 6] = n;
+  __syncthreads();
+  n = 0;
 #pragma unroll
-    for (int i = 0; i < KN; ++i) {
-      const int piece = i * 256 + tid, slot = from[piece % 32];
-      k[i] = vec{};
-      if (slot >= 0) {
-        int in;
-        const int64_t plane = plane_of(slot, in);
-        if (plane >= 0) k[i] = *reinterpret_cast<const vec*>(kp + plane + k_off(in, piece / 32 * 8, HD));
-        bad |= plane < 0;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < VN; ++i) {
-      const int e = i * 256 + tid, slot = from[e % 32];
-      v[i] = from_f32<T>(0.f);
-      if (slot >= 0) {
-        int in;
-        const int64_t plane = plane_of(slot, in);
-        if (plane >= 0) v[i] = vp[plane + v_off(in, e / 32, HD)];
-      }
-    }
-    if (bad) set_status(kv.status, ESP_DEV_BAD_PAGE);
-    __syncthreads();
-    const size_t to = page_plane(to_page, kvh, kv.hkv, kv.page_size, HD);
-#pragma unroll
-    for (int i = 0; i < KN; ++i) {
-      const int piece = i * 256 + tid, s = piece % 32;
-      if (s <= last) *reinterpret_cast<vec*>(kp + to + k_off(inside + s, piece / 32 * 8, HD)) = k[i];
-    }
-#pragma unroll
-    for (int i = 0; i < VN; ++i) {
-      const int e = i * 256 + tid, s = e % 32;
-      if (s <= last) vp[to + v_off(inside + s, e / 32, HD)] = v[i];
-    }
-  }
+  for (int w = 0; w < MOVERS / 64; ++w) n += counted[w];
   // (of the workgroups here only this one looks at the length, so len_out may be where it came from)
   if (tid == 0 && kvh == 0 && layer == 0) a.len_out[seq] = n > 0 ? n : kv.len[seq];
+  if (n == 0 || (a.table_out == kv.table && kept[n - 1] == n - 1)) return;       // (all where they are)
+
+  auto block_at = [&](int page, int slot_in_page) {
+    return page < 0 || page >= kv.n_pages ? (int64_t)-1
+                                          : (int64_t)(page_plane(page, kvh, kv.hkv, kv.page_size, HD) + (size_t)(slot_in_page >> 5) * 32 * HD);
+  };
+  // lane l < 64: old slot of token l of a batch; its page; and so on one step later each
+  auto old_slot = [&](int batch) {
+    const int i = batch * BATCH + tid;
+    return tid < BATCH && i < n ? kept[i] : -1;
+  };
+  auto page_of = [&](int slot) { return slot >= 0 ? table[slot / kv.page_size] : 0; };
+  auto put = [&](int batch, int slot, int page) {
+    if (tid >= BATCH) return;
+    const int buf = batch & 3;
+    int64_t at = -1;
+    if (slot >= 0) {
+      at = block_at(page, slot % kv.page_size);
+      if (at < 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+    }
+    src[buf][tid] = {at, slot & 31};
+    const bool outside = __builtin_amdgcn_ballot_w64(slot >= 0 && at < 0) != 0ull;
+    if (tid == 0) bad[buf] = outside;
+    if ((tid & 31) == 0) {
+      const int first = batch * BATCH + tid, last = min(first + 31, n - 1);
+      int64_t to = -1;
+      if (first < n) {
+        const int new_page = table_out[first / kv.page_size];
+        to = block_at(new_page, first % kv.page_size);
+        if (to < 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+        else if (kept[last] == last && table[first / kv.page_size] == new_page) to = -1;       // (all where they are)
+      }
+      dst[buf][tid >> 5] = to;
+    }
+  };
+  // K: piece p of a block is features 8 (p / 32) .. of token p % 32.  V: feature 32 (p / 128) + p % 32, tokens 16 (p / 64 % 2) + 4 (p / 32 % 2) + 0..3 and 8 more.
+  // (what is not there is read at the pool's beginning)
+  auto fetch = [&](int batch, vec (&k)[PIECES], raw (&v)[PIECES][8]) {
+    const int buf = batch & 3;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int piece = i * MOVERS + tid, block = piece / (4 * HD), p = piece % (4 * HD);
+      const Source s = src[buf][32 * block + p % 32];
+      k[i] = *reinterpret_cast<const vec*>(kp + max(s.at, (int64_t)0) + (p / 32 * 32 + s.key) * 8);
+      const int d = 32 * (p / 128) + p % 32, first = 16 * (p / 64 % 2) + 4 * (p / 32 % 2);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const Source t = src[buf][32 * block + first + 8 * (e >> 2) + (e & 3)];
+        v[i][e] = reinterpret_cast<const raw*>(vp)[max(t.at, (int64_t)0) + v_off(t.key, d, HD)];
+      }
+    }
+  };
+  auto store = [&](int batch, const vec (&k)[PIECES], const vec (&v)[PIECES]) {
+    const int buf = batch & 3;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int piece = i * MOVERS + tid, block = piece / (4 * HD), p = piece % (4 * HD);
+      const int64_t to = dst[buf][block];
+      if (to < 0) continue;
+      const int left = n - batch * BATCH - 32 * block, first = 16 * (p / 64 % 2) + 4 * (p / 32 % 2);
+      if (p % 32 < left) *reinterpret_cast<vec*>(kp + to + p * 8) = k[i];
+      if (first + 11 < left) {
+        *reinterpret_cast<vec*>(vp + to + p * 8) = v[i];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (first + 8 * (e >> 2) + (e & 3) < left) vp[to + p * 8 + e] = v[i][e];
+      }
+    }
+  };
+
+  const int batches = (n + BATCH - 1) / BATCH;
+  put(0, old_slot(0), page_of(old_slot(0)));
+  put(1, old_slot(1), page_of(old_slot(1)));
+  int slot2 = old_slot(2), page2 = page_of(slot2), slot3 = old_slot(3);
+  vec k[PIECES], v[PIECES], next_k[PIECES];
+  raw next_v[PIECES][8];
+  __syncthreads();
+  fetch(0, next_k, next_v);
+  for (int b = 0; b < batches; ++b) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      k[i] = next_k[i];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = __builtin_bit_cast(T, next_v[i][e]);
+    }
+    if (bad[b & 3]) {                  // zeros in their place
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const int piece = i * MOVERS + tid, block = piece / (4 * HD), p = piece % (4 * HD), first = 16 * (p / 64 % 2) + 4 * (p / 32 % 2);
+        if (src[b & 3][32 * block + p % 32].at < 0) k[i] = vec{};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (src[b & 3][32 * block + first + 8 * (e >> 2) + (e & 3)].at < 0) v[i][e] = from_f32<T>(0.f);
+      }
+    }
+    if (b + 1 < batches) fetch(b + 1, next_k, next_v);
+    put(b + 2, slot2, page2);
+    slot2 = slot3;
+    page2 = page_of(slot2);
+    slot3 = old_slot(b + 4);
+    // what anybody reads of this batch has arrived (k and v are made of it) before anything of it is written
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) { wait_for(k[i]); wait_for(v[i]); }
+    __syncthreads();
+    store(b, k, v);
+  }
 }
 
 template <typename T, int HD>
 void move(hipStream_t st, const PagedDev& kv, const EvictArgs& a) {
-  hipLaunchKernelGGL((k_evict_move<T, HD>), dim3(kv.hkv, kv.batch, a.layers), dim3(256), 0, st, kv, a);
+  hipLaunchKernelGGL((k_evict_move<T, HD>), dim3(kv.hkv, kv.batch, a.layers), dim3(MOVERS), 0, st, kv, a);
 }
 
 }  // namespace
