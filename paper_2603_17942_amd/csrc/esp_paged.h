@@ -98,6 +98,7 @@ struct WeighArgs {
   float* scratch;
   int hq, last, slots;        // slots: of a sequence and kv head in mass
   float scale;                // with log2 e
+  bool whole;                 // q can be read 16 bytes at a time
 };
 WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int last, int len_bound);
 int64_t weigh_workgroups(const WeighPlan& p, int batch, int hkv, int G);

@@ -209,7 +209,7 @@ esp_status esp_paged_weigh(void* stream, const esp_paged_kv* kv, int32_t layer, 
   if ((uintptr_t)scratch % 16) return ESP_EINVAL;
   const int64_t off = (int64_t)layer * kv->batch * kv->n_kv_heads * mass_slots;
   const WeighArgs a{q, q_stride, before ? before + off : nullptr, mass + off, (float*)scratch, n_q, last_rows, mass_slots,
-                    (float)((double)scale * 1.4426950408889634)};
+                    (float)((double)scale * 1.4426950408889634), (uintptr_t)q % 16 == 0 && q_stride * (int64_t)elt(kv->dtype) % 16 == 0};
   ESP_HIP(launch_paged_weigh((hipStream_t)stream, kv->dtype, kv->head_dim, to_dev(kv, layer), {rows->row0, rows->total_rows, rows->max_rows}, a, p));
   return ESP_OK;
 }

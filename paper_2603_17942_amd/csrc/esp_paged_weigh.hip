@@ -17,6 +17,7 @@
 namespace {
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES;
+constexpr int stat_tiles(bool bf16) { return bf16 ? 2 : 1; }      // column tiles of a wave of the statistics
 
 struct WeighSeq {            // a sequence's counted rows: the last `rows` of its chunk
   int first_row;             // in the chunk
@@ -44,13 +45,24 @@ __device__ __forceinline__ void load_unit(const T* p, int lane, typename AttnFra
 #pragma unroll
   for (int s = 0; s < HD / 16; ++s) k[s] = *reinterpret_cast<const F*>(p + (s * 64 + lane) * 8);
 }
+// eight features of q (null: zeros); WHOLE: 16-byte loads
+template <typename T>
+__device__ __forceinline__ typename AttnFrag<T>::type load_eight(const T* p, bool whole) {
+  typedef typename AttnFrag<T>::type F;
+  F f = {};
+  if (p && whole) {
+    f = *reinterpret_cast<const F*>(p);
+  } else if (p) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = p[e];
+  }
+  return f;
+}
 // features of one column as operand: 16 s + 8 half + 0..7
 template <typename T, int HD>
-__device__ __forceinline__ void load_column(const T* p, int half, typename AttnFrag<T>::type (&q)[HD / 16]) {
+__device__ __forceinline__ void load_column(const T* p, int half, bool whole, typename AttnFrag<T>::type (&q)[HD / 16]) {
 #pragma unroll
-  for (int s = 0; s < HD / 16; ++s)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q[s][e] = p ? p[16 * s + 8 * half + e] : from_f32<T>(0.f);
+  for (int s = 0; s < HD / 16; ++s) q[s] = load_eight<T>(p ? p + 16 * s + 8 * half : nullptr, whole);
 }
 
 // (reference, sum of exponentials against it).  The reference is the largest score times the scale, rounded, and is the same number
@@ -80,7 +92,7 @@ __global__ __launch_bounds__(THREADS) void k_weigh_scores(PagedDev kv, ChunkDev 
   const int G = a.hq / kv.hkv, cols = c.rows * G;
   F q[HD / 16], k[HD / 16], next[HD / 16] = {};
   const int mine = lane & 31;
-  load_column<T, HD>(mine < cols ? (const T*)a.q + (int64_t)(c.first_row + c.first + mine / G) * a.q_stride + (int64_t)(kvh * G + mine % G) * HD : nullptr, half, q);
+  load_column<T, HD>(mine < cols ? (const T*)a.q + (int64_t)(c.first_row + c.first + mine / G) * a.q_stride + (int64_t)(kvh * G + mine % G) * HD : nullptr, half, a.whole, q);
   int sees[4 * NV];                    // last slot that a column sees
   float m[4 * NV], l[4 * NV];
 #pragma unroll
@@ -136,31 +148,41 @@ __global__ __launch_bounds__(THREADS) void k_weigh_scores(PagedDev kv, ChunkDev 
   }
 }
 
+template <int EACH>                     // tokens of a thread
 __global__ __launch_bounds__(THREADS) void k_weigh_sum(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
-  const int tid = threadIdx.x, kvh = blockIdx.y, seq = blockIdx.z, slot = blockIdx.x * THREADS + tid;
+  const int tid = threadIdx.x, kvh = blockIdx.y, seq = blockIdx.z, slot0 = blockIdx.x * THREADS * EACH;
   const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
-  if (!c.ok || c.rows == 0 || (int)blockIdx.x * THREADS >= c.total) return;
-  __shared__ float2 col[32];
+  if (!c.ok || c.rows == 0 || slot0 >= c.total) return;
+  __shared__ float2 col[THREADS];
   const int64_t head = (int64_t)seq * kv.hkv + kvh;
-  if (tid < p.width) {
-    const int shares = ((c.total + 31) / 32 + p.share_units - 1) / p.share_units;
-    const float2* s = reinterpret_cast<const float2*>(a.scratch) + head * p.shares * p.width + tid;
-    float2 r = s[0];
-    for (int i = 1; i < shares; ++i) r = join(r, s[(int64_t)i * p.width]);
-    col[tid] = finish(r);
+  // thread: column tid % width, shares tid / width and every THREADS / width on
+  const int shares = ((c.total + 31) / 32 + p.share_units - 1) / p.share_units;
+  const float2* s = reinterpret_cast<const float2*>(a.scratch) + head * p.shares * p.width;
+  float2 r = {ATTN_UNSEEN, 0.f};
+  for (int i = tid / p.width; i < shares; i += THREADS / p.width) r = join(r, s[i * p.width + tid % p.width]);
+  col[tid] = r;
+  for (int n = THREADS / 2; n >= p.width; n /= 2) {
+    __syncthreads();
+    if (tid < n) col[tid] = join(col[tid], col[tid + n]);
   }
+  if (tid < p.width) col[tid] = finish(col[tid]);
   __syncthreads();
-  if (slot >= c.total) return;
-  const float* x = a.scratch + p.stats_floats + (head * p.tokens + slot) * p.width;
-  float sum = 0.f;
-  for (int i = 0; i < p.width; i += 4) {
-    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(x + i);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)        // (minus infinity: not seen, also by a row that is NaN)
-      sum = v[e] == -INFINITY ? sum : fmaf(__builtin_amdgcn_exp2f(fmaf(v[e], a.scale, -col[i + e].x)), col[i + e].y, sum);
+  for (int j = 0; j < EACH; ++j) {
+    const int slot = slot0 + j * THREADS + tid;
+    if (slot >= c.total) return;
+    const float* x = a.scratch + p.stats_floats + (head * p.tokens + slot) * p.width;
+    const int64_t at = head * a.slots + slot;
+    const float old = a.before && slot < c.len ? a.before[at] : 0.f;
+    float sum = 0.f;
+    for (int i = 0; i < p.width; i += 4) {
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>(x + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)      // (minus infinity: not seen, also by a row that is NaN)
+        sum = v[e] == -INFINITY ? sum : fmaf(__builtin_amdgcn_exp2f(fmaf(v[e], a.scale, -col[i + e].x)), col[i + e].y, sum);
+    }
+    a.mass[at] = old + sum;
   }
-  const int64_t at = head * a.slots + slot;
-  a.mass[at] = (a.before && slot < c.len ? a.before[at] : 0.f) + sum;
 }
 
 // ---- many columns --------------------------------------------------------------------------------------------
@@ -170,24 +192,33 @@ __device__ __forceinline__ int64_t first_column(const WeighPlan& p, const WeighS
   return p.packed ? ((int64_t)c.first_row * kv.hkv + (int64_t)kvh * (c.total - c.len)) * G : ((int64_t)seq * kv.hkv + kvh) * p.most_rows * G;
 }
 
-template <typename T, int HD>
-__global__ __launch_bounds__(THREADS) void k_weigh_stats(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
+// CT column tiles a wave: what it loads of K serves them all
+template <typename T, int HD, int CT>
+__global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
   typedef typename AttnFrag<T>::type F;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-  const int share = blockIdx.x % p.shares, tile = blockIdx.x / p.shares * WAVES + wave, kvh = blockIdx.y, seq = blockIdx.z;
+  const int share = blockIdx.x % p.shares, tile = (blockIdx.x / p.shares * WAVES + wave) * CT, kvh = blockIdx.y, seq = blockIdx.z;
   const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
   if (!c.ok) {
     if (blockIdx.x == 0 && kvh == 0 && tid == 0) set_status(kv.status, chunk_fault(ch, seq));
     return;
   }
-  const int G = a.hq / kv.hkv, cols = c.rows * G, col = 32 * tile + (lane & 31);
+  const int G = a.hq / kv.hkv, cols = c.rows * G;
   if (32 * tile >= cols) return;       // (no barrier below)
-  const int row = c.first + min(col, cols - 1) / G;
-  const int low_row = c.first + 32 * tile / G, top_row = c.first + min(32 * tile + 31, cols - 1) / G;
+  const int low_row = c.first + 32 * tile / G, top_row = c.first + min(32 * (tile + CT) - 1, cols - 1) / G;
   const int begin = share * p.share_units, end = min(begin + p.share_units, (c.len + top_row) / 32 + 1);
-  F q[HD / 16], k[HD / 16], next[HD / 16] = {};
-  load_column<T, HD>(col < cols ? (const T*)a.q + (int64_t)(c.first_row + row) * a.q_stride + (int64_t)(kvh * G + col % G) * HD : nullptr, half, q);
-  float m = ATTN_UNSEEN, l = 0.f;
+  F q[CT][HD / 16], k[HD / 16], next[HD / 16] = {};
+  int sees[CT];
+  float m[CT], l[CT];
+#pragma unroll
+  for (int i = 0; i < CT; ++i) {
+    const int col = 32 * (tile + i) + (lane & 31), row = c.first + min(col, cols - 1) / G;
+    load_column<T, HD>(col < cols ? (const T*)a.q + (int64_t)(c.first_row + row) * a.q_stride + (int64_t)(kvh * G + col % G) * HD : nullptr, half,
+                       a.whole, q[i]);
+    sees[i] = c.len + row;
+    m[i] = ATTN_UNSEEN;
+    l[i] = 0.f;
+  }
   const T* at = begin < end ? unit_at<T>(kv, seq, kvh, begin, HD) : nullptr;
   if (at) load_unit<T, HD>(at, lane, next);
   for (int u = begin; u < end; ++u) {
@@ -200,28 +231,35 @@ __global__ __launch_bounds__(THREADS) void k_weigh_stats(PagedDev kv, ChunkDev c
       if (at) load_unit<T, HD>(at, lane, next);
     }
     if (!there) continue;
-    f32x16_t x = {};
+    f32x16_t x[CT] = {};
 #pragma unroll
-    for (int s = 0; s < HD / 16; ++s) x = attn_mma(k[s], q[s], x);
+    for (int s = 0; s < HD / 16; ++s)
+#pragma unroll
+      for (int i = 0; i < CT; ++i) x[i] = attn_mma(k[s], q[i][s], x[i]);
     const bool whole = 32 * u + 31 <= c.len + low_row;
-    if (!whole) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) x[v] = 32 * u + 8 * (v >> 2) + 4 * half + (v & 3) <= c.len + row ? x[v] : -INFINITY;
+    for (int i = 0; i < CT; ++i) {
+      if (!whole) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[i][v] = 32 * u + 8 * (v >> 2) + 4 * half + (v & 3) <= sees[i] ? x[i][v] : -INFINITY;
+      }
+      float top = attn_max3(x[i][0], x[i][1], x[i][2]);
+#pragma unroll
+      for (int v = 3; v < 15; v += 2) top = attn_max3(top, x[i][v], x[i][v + 1]);
+      const float ref = fmaxf(m[i], fmaxf(top, x[i][15]) * a.scale);
+      float sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(fmaf(x[i][v], a.scale, -ref));
+      l[i] = fmaf(l[i], __builtin_amdgcn_exp2f(m[i] - ref), sum);
+      m[i] = ref;
     }
-    float top = attn_max3(x[0], x[1], x[2]);
-#pragma unroll
-    for (int v = 3; v < 15; v += 2) top = attn_max3(top, x[v], x[v + 1]);
-    const float ref = fmaxf(m, fmaxf(top, x[15]) * a.scale);
-    float sum = 0.f;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(fmaf(x[v], a.scale, -ref));
-    l = fmaf(l, __builtin_amdgcn_exp2f(m - ref), sum);
-    m = ref;
   }
-  const float2 r = join(float2{m, l}, float2{__shfl_xor(m, 32, 64), __shfl_xor(l, 32, 64)});
-  if (half == 0 && col < cols) {
-    float2* out = reinterpret_cast<float2*>(a.scratch) + share * p.columns + first_column(p, c, kv, G, seq, kvh) + col;
-    *out = p.shares > 1 ? r : finish(r);
+  float2* out = reinterpret_cast<float2*>(a.scratch) + share * p.columns + first_column(p, c, kv, G, seq, kvh);
+#pragma unroll
+  for (int i = 0; i < CT; ++i) {
+    const float2 r = join(float2{m[i], l[i]}, float2{__shfl_xor(m[i], 32, 64), __shfl_xor(l[i], 32, 64)});
+    const int col = 32 * (tile + i) + (lane & 31);
+    if (half == 0 && col < cols) out[col] = p.shares > 1 ? r : finish(r);
   }
 }
 
@@ -238,13 +276,14 @@ __global__ __launch_bounds__(THREADS) void k_weigh_join(PagedDev kv, ChunkDev ch
   *s = finish(r);
 }
 
-// KU units of 32 keys a wave
+// KU units of 32 keys a wave.  Column tiles go through two places in LDS: the next one is on its way while this one is used.
 template <typename T, int HD, int KU>
-__global__ __launch_bounds__(THREADS) void k_weigh_add(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
+__global__ __launch_bounds__(THREADS, 2) void k_weigh_add(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
   typedef typename AttnFrag<T>::type F;
-  __shared__ __align__(16) F tile_q[HD / 16 * 64];
-  __shared__ __align__(16) float ref[32], inv[32];
-  __shared__ int sees[32];
+  constexpr int EIGHTS = HD / 8 * 32 / THREADS;        // of eight features, a thread's of a tile
+  __shared__ __align__(16) F tile_q[2][HD / 16 * 64];
+  __shared__ __align__(16) float ref[2][32], inv[2][32];
+  __shared__ int sees[2][32];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int part = blockIdx.x % p.parts, tile = blockIdx.x / p.parts, kvh = blockIdx.y, seq = blockIdx.z;
   const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
@@ -265,50 +304,72 @@ __global__ __launch_bounds__(THREADS) void k_weigh_add(PagedDev kv, ChunkDev ch,
     if (at) load_unit<T, HD>(at, lane, k[i]);
   }
   const float2* stats = reinterpret_cast<const float2*>(a.scratch) + first_column(p, c, kv, G, seq, kvh);
+  const T* q0 = (const T*)a.q + (int64_t)(c.first_row + c.first) * a.q_stride + (int64_t)kvh * G * HD;
   // column tiles of this part, less those whose rows all end before the first key
   const int tiles = (cols + 31) / 32, each = (tiles + p.parts - 1) / p.parts;
-  const int first_needed = max(0, tile0 - c.len - c.first) * G / 32;
+  const int first_needed = (int)((int64_t)max(0, tile0 - c.len - c.first) * G / 32);
   const int t0 = max(part * each, first_needed), t1 = min((part + 1) * each, tiles);
-  for (int t = t0; t < t1; ++t) {
-    __syncthreads();
-    for (int i = tid; i < HD / 8 * 32; i += THREADS) {                           // eight features of a column
-      const int col = 32 * t + i / (HD / 8), f = i % (HD / 8);
-      F v = {};
-      if (col < cols) {
-        const T* src = (const T*)a.q + (int64_t)(c.first_row + c.first + col / G) * a.q_stride + (int64_t)(kvh * G + col % G) * HD + 8 * f;
+  F q_next[EIGHTS];
+  float2 s_next = {0.f, 0.f};
+  auto fetch = [&](int t) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = src[e];
-      }
-      tile_q[(f >> 1) * 64 + (f & 1) * 32 + i / (HD / 8)] = v;
+    for (int i = 0; i < EIGHTS; ++i) {
+      const int e = i * THREADS + tid, col = 32 * t + e / (HD / 8), f = e % (HD / 8), row = col / G;
+      q_next[i] = load_eight<T>(col < cols ? q0 + row * a.q_stride + (col - row * G) * HD + 8 * f : nullptr, a.whole);
+    }
+    if (tid < 32) s_next = 32 * t + tid < cols ? stats[32 * t + tid] : float2{0.f, 0.f};
+  };
+  auto put = [&](int t, int buf) {
+#pragma unroll
+    for (int i = 0; i < EIGHTS; ++i) {
+      const int e = i * THREADS + tid, f = e % (HD / 8);
+      tile_q[buf][(f >> 1) * 64 + (f & 1) * 32 + e / (HD / 8)] = q_next[i];
     }
     if (tid < 32) {
       const int col = 32 * t + tid;
-      const float2 s = col < cols ? stats[col] : float2{0.f, 0.f};
-      ref[tid] = s.x; inv[tid] = s.y;
-      sees[tid] = col < cols ? c.len + c.first + col / G : -1;
+      ref[buf][tid] = s_next.x; inv[buf][tid] = s_next.y;
+      sees[buf][tid] = col < cols ? c.len + c.first + col / G : -1;
     }
-    __syncthreads();
+  };
+  if (t0 < t1) { fetch(t0); put(t0, 0); }
+  __syncthreads();
+  for (int t = t0; t < t1; ++t) {
+    const int buf = (t - t0) & 1;
+    if (t + 1 < t1) fetch(t + 1);
     f32x16_t x[KU] = {};
     float of_tile[KU] = {};            // (tiles by themselves: 16 and then hundreds of additions in a row, not thousands)
 #pragma unroll
     for (int s = 0; s < HD / 16; ++s) {
-      const F q = tile_q[s * 64 + lane];
+      const F q = tile_q[buf][s * 64 + lane];
 #pragma unroll
       for (int i = 0; i < KU; ++i) x[i] = attn_mma(q, k[i][s], x[i]);
     }
+    // (whole: all columns of the tile see all keys of the wave; the last tile's columns past the end have a weight of zero)
+    const bool whole = 32 * t + 32 <= cols && 32 * (unit0 + KU) - 1 <= c.len + c.first + 32 * t / G;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int col = 8 * (v >> 2) + 4 * half + (v & 3);
-      const float r = ref[col], w = inv[col];
-      const int last = sees[col];
+    for (int g = 0; g < 4; ++g) {
+      const f32x4_t r = *reinterpret_cast<const f32x4_t*>(&ref[buf][8 * g + 4 * half]), w = *reinterpret_cast<const f32x4_t*>(&inv[buf][8 * g + 4 * half]);
+      if (whole) {
 #pragma unroll
-      for (int i = 0; i < KU; ++i) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(x[i][v], a.scale, -r));
-        of_tile[i] = 32 * (unit0 + i) + (lane & 31) <= last ? fmaf(e, w, of_tile[i]) : of_tile[i];
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int i = 0; i < KU; ++i) of_tile[i] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[i][4 * g + e], a.scale, -r[e])), w[e], of_tile[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int last = sees[buf][8 * g + 4 * half + e];
+#pragma unroll
+          for (int i = 0; i < KU; ++i) {
+            const float y = fmaf(__builtin_amdgcn_exp2f(fmaf(x[i][4 * g + e], a.scale, -r[e])), w[e], of_tile[i]);
+            of_tile[i] = 32 * (unit0 + i) + (lane & 31) <= last ? y : of_tile[i];
+          }
+        }
       }
     }
 #pragma unroll
     for (int i = 0; i < KU; ++i) sum[i] += of_tile[i];
+    if (t + 1 < t1) put(t + 1, buf ^ 1);               // (nobody reads that one: all have passed the barrier behind its tile)
+    __syncthreads();
   }
   const int64_t head = (int64_t)seq * kv.hkv + kvh;
 #pragma unroll
@@ -344,11 +405,14 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
     else hipLaunchKernelGGL((k_weigh_scores<T, HD, 4>), grid, wg, 0, st, kv, ch, a, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_weigh_sum, tokens, wg, 0, st, kv, ch, a, p);
+    // (four tokens a thread where there are many: the shares are joined by every workgroup)
+    if (p.tokens * kv.hkv * kv.batch >= (1 << 20)) hipLaunchKernelGGL(k_weigh_sum<4>, dim3((tokens.x + 3) / 4, tokens.y, tokens.z), wg, 0, st, kv, ch, a, p);
+    else hipLaunchKernelGGL(k_weigh_sum<1>, tokens, wg, 0, st, kv, ch, a, p);
     return hipGetLastError();
   }
   const int G = a.hq / kv.hkv, tiles = (int)(((int64_t)p.most_rows * G + 31) / 32);
-  hipLaunchKernelGGL((k_weigh_stats<T, HD>), dim3((tiles + WAVES - 1) / WAVES * p.shares, kv.hkv, kv.batch), wg, 0, st, kv, ch, a, p);
+  constexpr int CT = stat_tiles(sizeof(T) == 2);
+  hipLaunchKernelGGL((k_weigh_stats<T, HD, CT>), dim3((tiles + WAVES * CT - 1) / (WAVES * CT) * p.shares, kv.hkv, kv.batch), wg, 0, st, kv, ch, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (p.shares > 1) {
@@ -375,7 +439,7 @@ WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_ro
   const int units = (int)(p.tokens / 32);
   if (cols <= 32) {
     p.width = cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 16 ? 16 : 32;
-    const int64_t most = std::max<int64_t>(1, 2048 / heads);                     // shares of a sequence and kv head
+    const int64_t most = std::max<int64_t>(1, 8192 / heads);                     // shares of a sequence and kv head
     p.share_units = (int)std::max<int64_t>(4, (units + most - 1) / most);
     p.shares = (units + p.share_units - 1) / p.share_units;
     p.stats_floats = 2 * heads * p.shares * p.width;
@@ -384,7 +448,8 @@ WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_ro
   }
   p.packed = (int64_t)total_rows < (int64_t)batch * rows;
   p.columns = (p.packed ? (int64_t)total_rows : (int64_t)batch * rows) * hq;
-  const int64_t groups = ((cols + 31) / 32 + WAVES - 1) / WAVES * heads;
+  const int of_group = WAVES * stat_tiles(dtype == ESP_BF16);
+  const int64_t groups = ((cols + 31) / 32 + of_group - 1) / of_group * heads;
   const int64_t most = std::max<int64_t>(1, 1024 / groups);
   p.share_units = (int)std::max<int64_t>(16, (units + most - 1) / most);
   p.shares = (units + p.share_units - 1) / p.share_units;
