@@ -84,6 +84,7 @@ struct WeighPlan {
   int width = 0;              // columns that scores are kept for; 0: many, scores are computed twice
   int share_units = 1, shares = 1;       // units of 32 keys of a share of the statistics
   int parts = 1;              // many: of the columns, each with sums of its own
+  bool join_here = false;     // many: the shares' statistics are joined where they are used
   int most_rows = 0;          // counted rows of a sequence at most
   bool packed = false;        // many: statistics lie by rows of the chunk, not by most_rows a sequence
   int64_t tokens = 0;         // of a sequence at most, in whole units

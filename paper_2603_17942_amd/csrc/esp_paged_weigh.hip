@@ -31,14 +31,30 @@ __device__ __forceinline__ WeighSeq weigh_seq(const PagedDev& kv, const ChunkDev
   return {c.row0, c.rows - n, n, c.len, c.len + c.rows, ok};
 }
 
-// first element of a unit of 32 keys; null: its page is outside the pool
+// Units of 32 keys of a sequence and kv head, one after the other: a lane has the page of one of 64 pages ahead, so that a unit's address takes no look
+// into the table of its own.
 template <typename T>
-__device__ __forceinline__ const T* unit_at(const PagedDev& kv, int seq, int kvh, int unit, int hd) {
-  const int slot = 32 * unit, at = slot / kv.page_size;
-  const int page = kv.table[(size_t)seq * kv.stride + at];
-  if (page < 0 || page >= kv.n_pages) return nullptr;
-  return (const T*)kv.k + page_plane(page, kvh, kv.hkv, kv.page_size, hd) + (size_t)(slot - at * kv.page_size) * hd;
-}
+struct Units {
+  const int32_t* table;
+  const T* k;                          // of the layer
+  size_t plane;                        // elements of a page and kv head, before it those of the page's other heads
+  int hkv, kvh, n_pages, pages_end, of_page, first_page, pages;
+  __device__ __forceinline__ Units(const PagedDev& kv, int seq, int kvh_, int hd)
+      : table(kv.table + (size_t)seq * kv.stride), k((const T*)kv.k), plane((size_t)kv.page_size * hd), hkv(kv.hkv), kvh(kvh_), n_pages(kv.n_pages),
+        pages_end(kv.stride), of_page(kv.page_size / 32), first_page(-64), pages(0) {}
+  // first element of a unit; null: its page is outside the pool
+  __device__ __forceinline__ const T* at(int unit, int page, int hd) {
+    if (page >= first_page + 64 || page < first_page) {
+      first_page = page;
+      const int i = page + (int)(threadIdx.x & 63);
+      pages = i < pages_end ? table[i] : -1;
+    }
+    const int id = __builtin_amdgcn_readlane(pages, page - first_page);
+    if (id < 0 || id >= n_pages) return nullptr;
+    return k + ((size_t)id * hkv + kvh) * plane + (size_t)(unit - page * of_page) * 32 * hd;
+  }
+  __device__ __forceinline__ const T* at(int unit, int hd) { return at(unit, unit / of_page, hd); }
+};
 template <typename T, int HD>
 __device__ __forceinline__ void load_unit(const T* p, int lane, typename AttnFrag<T>::type (&k)[HD / 16]) {
   typedef typename AttnFrag<T>::type F;
@@ -103,15 +119,17 @@ __global__ __launch_bounds__(THREADS) void k_weigh_scores(PagedDev kv, ChunkDev 
     l[v] = 0.f;
   }
   float* scores = a.scratch + p.stats_floats + ((int64_t)seq * kv.hkv + kvh) * p.tokens * p.width;
-  const T* at = begin + wave < end ? unit_at<T>(kv, seq, kvh, begin + wave, HD) : nullptr;
+  Units<T> units_of(kv, seq, kvh, HD);
+  const int w0 = __builtin_amdgcn_readfirstlane(wave);
+  const T* at = begin + w0 < end ? units_of.at(begin + w0, HD) : nullptr;
   if (at) load_unit<T, HD>(at, lane, next);
-  for (int u = begin + wave; u < end; u += WAVES) {
+  for (int u = begin + w0; u < end; u += WAVES) {
     const bool there = at != nullptr;
     if (!there && lane == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
 #pragma unroll
     for (int s = 0; s < HD / 16; ++s) k[s] = next[s];
     if (u + WAVES < end) {
-      at = unit_at<T>(kv, seq, kvh, u + WAVES, HD);
+      at = units_of.at(u + WAVES, HD);
       if (at) load_unit<T, HD>(at, lane, next);
     }
     f32x16_t x = {};
@@ -197,7 +215,10 @@ template <typename T, int HD, int CT>
 __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
   typedef typename AttnFrag<T>::type F;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-  const int share = blockIdx.x % p.shares, tile = (blockIdx.x / p.shares * WAVES + wave) * CT, kvh = blockIdx.y, seq = blockIdx.z;
+  // Late columns have the most to do and come first.  Column groups lie next to each other, shares far apart: workgroups go to the XCDs in turn, and early
+  // columns have no last shares (eight shares next to each other: 204 us for a prompt of 4096, half of the XCDs idle most of the time; so 117).
+  const int block = gridDim.x - 1 - blockIdx.x, groups = gridDim.x / p.shares;
+  const int share = block / groups, tile = (block % groups * WAVES + wave) * CT, kvh = blockIdx.y, seq = blockIdx.z;
   const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
   if (!c.ok) {
     if (blockIdx.x == 0 && kvh == 0 && tid == 0) set_status(kv.status, chunk_fault(ch, seq));
@@ -207,7 +228,17 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDe
   if (32 * tile >= cols) return;       // (no barrier below)
   const int low_row = c.first + 32 * tile / G, top_row = c.first + min(32 * (tile + CT) - 1, cols - 1) / G;
   const int begin = share * p.share_units, end = min(begin + p.share_units, (c.len + top_row) / 32 + 1);
-  F q[CT][HD / 16], k[HD / 16], next[HD / 16] = {};
+  F q[CT][HD / 16], k[HD / 16] = {}, next[HD / 16] = {};
+  Units<T> units(kv, seq, kvh, HD);
+  // (two turns apart in the code, so that the next unit's registers need not be copied)
+  bool there = false, next_there = false;
+  auto fetch = [&](int u, F (&key)[HD / 16], bool& is_there) {
+    const T* at = u < end ? units.at(u, HD) : nullptr;
+    is_there = at != nullptr;
+    if (at) load_unit<T, HD>(at, lane, key);
+    else if (u < end && lane == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
+  };
+  fetch(begin, k, there);
   int sees[CT];
   float m[CT], l[CT];
 #pragma unroll
@@ -219,23 +250,13 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDe
     m[i] = ATTN_UNSEEN;
     l[i] = 0.f;
   }
-  const T* at = begin < end ? unit_at<T>(kv, seq, kvh, begin, HD) : nullptr;
-  if (at) load_unit<T, HD>(at, lane, next);
-  for (int u = begin; u < end; ++u) {
-    const bool there = at != nullptr;
-    if (!there && lane == 0) set_status(kv.status, ESP_DEV_BAD_PAGE);
-#pragma unroll
-    for (int s = 0; s < HD / 16; ++s) k[s] = next[s];
-    if (u + 1 < end) {
-      at = unit_at<T>(kv, seq, kvh, u + 1, HD);
-      if (at) load_unit<T, HD>(at, lane, next);
-    }
-    if (!there) continue;
+  // what a unit adds to the statistics
+  auto use = [&](int u, const F (&key)[HD / 16]) {
     f32x16_t x[CT] = {};
 #pragma unroll
     for (int s = 0; s < HD / 16; ++s)
 #pragma unroll
-      for (int i = 0; i < CT; ++i) x[i] = attn_mma(k[s], q[i][s], x[i]);
+      for (int i = 0; i < CT; ++i) x[i] = attn_mma(key[s], q[i][s], x[i]);
     const bool whole = 32 * u + 31 <= c.len + low_row;
 #pragma unroll
     for (int i = 0; i < CT; ++i) {
@@ -253,6 +274,12 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDe
       l[i] = fmaf(l[i], __builtin_amdgcn_exp2f(m[i] - ref), sum);
       m[i] = ref;
     }
+  };
+  for (int u = begin; u < end; u += 2) {
+    fetch(u + 1, next, next_there);
+    if (there) use(u, k);
+    fetch(u + 2, k, there);
+    if (next_there) use(u + 1, next);
   }
   float2* out = reinterpret_cast<float2*>(a.scratch) + share * p.columns + first_column(p, c, kv, G, seq, kvh);
 #pragma unroll
@@ -281,11 +308,13 @@ template <typename T, int HD, int KU>
 __global__ __launch_bounds__(THREADS, 2) void k_weigh_add(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
   typedef typename AttnFrag<T>::type F;
   constexpr int EIGHTS = HD / 8 * 32 / THREADS;        // of eight features, a thread's of a tile
+  // (columns of a step and half exchanged by the step's number: rows are written eight features a lane, and would all meet in the same banks)
   __shared__ __align__(16) F tile_q[2][HD / 16 * 64];
   __shared__ __align__(16) float ref[2][32], inv[2][32];
   __shared__ int sees[2][32];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-  const int part = blockIdx.x % p.parts, tile = blockIdx.x / p.parts, kvh = blockIdx.y, seq = blockIdx.z;
+  // (parts turned by one from key tile to key tile: workgroups go to the XCDs in turn, and a tile's first parts may have nothing to do)
+  const int tile = blockIdx.x / p.parts, part = p.parts - 1 - (blockIdx.x + tile) % p.parts, kvh = blockIdx.y, seq = blockIdx.z;
   const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
   const int tile0 = tile * WAVES * KU * 32;
   if (!c.ok || c.rows == 0 || tile0 >= c.total) return;
@@ -293,10 +322,11 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_add(PagedDev kv, ChunkDev 
   F k[KU][HD / 16];
   bool there[KU];
   float sum[KU];
-  const int unit0 = tile0 / 32 + wave * KU;
+  const int unit0 = tile0 / 32 + __builtin_amdgcn_readfirstlane(wave) * KU;
+  Units<T> units(kv, seq, kvh, HD);
 #pragma unroll
   for (int i = 0; i < KU; ++i) {
-    const T* at = 32 * (unit0 + i) < c.total ? unit_at<T>(kv, seq, kvh, unit0 + i, HD) : nullptr;
+    const T* at = 32 * (unit0 + i) < c.total ? units.at(unit0 + i, HD) : nullptr;
     there[i] = at != nullptr;
     sum[i] = 0.f;
 #pragma unroll
@@ -311,27 +341,50 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_add(PagedDev kv, ChunkDev 
   const int t0 = max(part * each, first_needed), t1 = min((part + 1) * each, tiles);
   F q_next[EIGHTS];
   float2 s_next = {0.f, 0.f};
+  // row and query head of this thread's columns of the next tile to be asked for, tile after tile without dividing
+  int row[EIGHTS], g[EIGHTS], stat_row = (32 * t0 + (tid & 31)) / G, stat_g = (32 * t0 + (tid & 31)) % G;
+  const int more_rows = 32 / G, more_g = 32 % G;
+  auto step = [&](int& r, int& h) {
+    r += more_rows; h += more_g;
+    if (h >= G) { h -= G; ++r; }
+  };
+#pragma unroll
+  for (int i = 0; i < EIGHTS; ++i) {
+    const int col = 32 * t0 + (i * THREADS + tid) / (HD / 8);
+    row[i] = col / G; g[i] = col % G;
+  }
   auto fetch = [&](int t) {
 #pragma unroll
     for (int i = 0; i < EIGHTS; ++i) {
-      const int e = i * THREADS + tid, col = 32 * t + e / (HD / 8), f = e % (HD / 8), row = col / G;
-      q_next[i] = load_eight<T>(col < cols ? q0 + row * a.q_stride + (col - row * G) * HD + 8 * f : nullptr, a.whole);
-    }
-    if (tid < 32) s_next = 32 * t + tid < cols ? stats[32 * t + tid] : float2{0.f, 0.f};
-  };
-  auto put = [&](int t, int buf) {
-#pragma unroll
-    for (int i = 0; i < EIGHTS; ++i) {
       const int e = i * THREADS + tid, f = e % (HD / 8);
-      tile_q[buf][(f >> 1) * 64 + (f & 1) * 32 + e / (HD / 8)] = q_next[i];
+      q_next[i] = load_eight<T>(row[i] < c.rows ? q0 + row[i] * a.q_stride + g[i] * HD + 8 * f : nullptr, a.whole);
+      step(row[i], g[i]);
     }
     if (tid < 32) {
       const int col = 32 * t + tid;
-      ref[buf][tid] = s_next.x; inv[buf][tid] = s_next.y;
-      sees[buf][tid] = col < cols ? c.len + c.first + col / G : -1;
+      s_next = {0.f, 0.f};
+      if (col < cols && !p.join_here) s_next = stats[col];
+      if (col < cols && p.join_here) {
+        s_next = stats[col];
+        for (int i = 1; i < p.shares; ++i) s_next = join(s_next, stats[i * p.columns + col]);
+        s_next = finish(s_next);
+      }
     }
   };
-  if (t0 < t1) { fetch(t0); put(t0, 0); }
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < EIGHTS; ++i) {
+      const int e = i * THREADS + tid, f = e % (HD / 8);
+      tile_q[buf][(f >> 1) * 64 + (f & 1) * 32 + ((e / (HD / 8)) ^ (f & 7))] = q_next[i];
+    }
+    if (tid < 32) {
+      ref[buf][tid] = s_next.x; inv[buf][tid] = s_next.y;
+      sees[buf][tid] = stat_row < c.rows ? c.len + c.first + stat_row : -1;
+      step(stat_row, stat_g);
+    }
+  };
+  int low_row = 32 * t0 / G, low_g = 32 * t0 % G;      // of a tile's first column
+  if (t0 < t1) { fetch(t0); put(0); }
   __syncthreads();
   for (int t = t0; t < t1; ++t) {
     const int buf = (t - t0) & 1;
@@ -340,12 +393,13 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_add(PagedDev kv, ChunkDev 
     float of_tile[KU] = {};            // (tiles by themselves: 16 and then hundreds of additions in a row, not thousands)
 #pragma unroll
     for (int s = 0; s < HD / 16; ++s) {
-      const F q = tile_q[buf][s * 64 + lane];
+      const F q = tile_q[buf][s * 64 + 32 * half + ((lane & 31) ^ ((2 * s + half) & 7))];
 #pragma unroll
       for (int i = 0; i < KU; ++i) x[i] = attn_mma(q, k[i][s], x[i]);
     }
     // (whole: all columns of the tile see all keys of the wave; the last tile's columns past the end have a weight of zero)
-    const bool whole = 32 * t + 32 <= cols && 32 * (unit0 + KU) - 1 <= c.len + c.first + 32 * t / G;
+    const bool whole = 32 * t + 32 <= cols && 32 * (unit0 + KU) - 1 <= c.len + c.first + low_row;
+    step(low_row, low_g);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const f32x4_t r = *reinterpret_cast<const f32x4_t*>(&ref[buf][8 * g + 4 * half]), w = *reinterpret_cast<const f32x4_t*>(&inv[buf][8 * g + 4 * half]);
@@ -368,7 +422,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_add(PagedDev kv, ChunkDev 
     }
 #pragma unroll
     for (int i = 0; i < KU; ++i) sum[i] += of_tile[i];
-    if (t + 1 < t1) put(t + 1, buf ^ 1);               // (nobody reads that one: all have passed the barrier behind its tile)
+    if (t + 1 < t1) put(buf ^ 1);               // (nobody reads that one: all have passed the barrier behind its tile)
     __syncthreads();
   }
   const int64_t head = (int64_t)seq * kv.hkv + kvh;
@@ -415,7 +469,7 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
   hipLaunchKernelGGL((k_weigh_stats<T, HD, CT>), dim3((tiles + WAVES * CT - 1) / (WAVES * CT) * p.shares, kv.hkv, kv.batch), wg, 0, st, kv, ch, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (p.shares > 1) {
+  if (p.shares > 1 && !p.join_here) {
     hipLaunchKernelGGL(k_weigh_join, dim3((32 * tiles + THREADS - 1) / THREADS, kv.hkv, kv.batch), wg, 0, st, kv, ch, a, p);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -450,13 +504,17 @@ WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_ro
   p.columns = (p.packed ? (int64_t)total_rows : (int64_t)batch * rows) * hq;
   const int of_group = WAVES * stat_tiles(dtype == ESP_BF16);
   const int64_t groups = ((cols + 31) / 32 + of_group - 1) / of_group * heads;
-  const int64_t most = std::max<int64_t>(1, 1024 / groups);
-  p.share_units = (int)std::max<int64_t>(16, (units + most - 1) / most);
+  // About 2048 workgroups for the statistics, of 16 units at least where there are many; four shares at most where there are few, which the sums then
+  // join themselves.
+  const int64_t most = std::max<int64_t>(1, 2048 / groups);
+  if (most <= 4 || units <= 64) p.share_units = (int)std::max<int64_t>(2, (units + std::min<int64_t>(4, most) - 1) / std::min<int64_t>(4, most));
+  else p.share_units = (int)std::max<int64_t>(16, (units + most - 1) / most);
   p.shares = (units + p.share_units - 1) / p.share_units;
+  p.join_here = p.shares > 1 && p.shares <= 4 && cols <= 256;
   p.stats_floats = 2 * p.columns * p.shares;
   const int keys = WAVES * 32 * (dtype == ESP_BF16 ? 2 : 1);
   const int64_t key_groups = (p.tokens + keys - 1) / keys * heads;
-  p.parts = (int)std::max<int64_t>(1, std::min<int64_t>((cols + 255) / 256, 1024 / key_groups));
+  p.parts = (int)std::max<int64_t>(1, std::min<int64_t>((cols + 255) / 256, 2048 / key_groups));
   p.scratch_floats = p.stats_floats + (p.parts > 1 ? p.parts * heads * p.tokens : 0);
   return p;
 }

@@ -12,7 +12,8 @@
 //   k_sample_pick   the list is divided by the bits of its logits until a few tokens (ranked by comparing all with all) or equal ones (arithmetic) are left:
 //                   the cut is a logit and how many of those equal to it are in.  Top-k first, as top-p is of what it leaves.  The part in which the
 //                   target lies is looked through.
-// The two in the middle are launched where there are limits.  Rows that they cannot narrow down (more than 4096 tokens in the steps of the cut, or
+// The two in the middle are launched where there are limits and more than 4096 tokens: so many are a list by themselves (a row of 4096 with top-k: 25 us
+// with all four, 17 with two).  Rows that they cannot narrow down (more than 4096 tokens in the steps of the cut, or
 // logits above 2^20 steps) are divided in k_sample_pick by going over the row again and again, some 100 us.
 #include <algorithm>
 #include <cfloat>
@@ -85,6 +86,8 @@ __device__ __forceinline__ Limits limits(const SampleArgs& a, int row) {
   m.by_part = m.min_p > 0.f;
   return m;
 }
+// all tokens are the list
+__device__ __forceinline__ bool one_list(const SampleArgs& a) { return a.vocab <= LIST; }
 __device__ __forceinline__ bool draws(const Limits& m) { return m.valid && m.temperature > 0.f; }
 __device__ __forceinline__ bool limited(const Limits& m) { return m.by_count || m.by_sum || m.by_part; }
 // do the weights of all tokens count
@@ -215,7 +218,7 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
       for (int i = N - 1; i >= 0; --i) at = x[j][i] == top ? lo + (j * PART_THREADS + tid) * N + i : at;
     atomicMin(&first_at, at);
   }
-  if (draws(m) && limited(m)) a.maxima[mine * PART_THREADS + tid] = own;
+  if (draws(m) && limited(m) && !one_list(a)) a.maxima[mine * PART_THREADS + tid] = own;
   double sum = 0.0;
   if (draws(m) && top > -INFINITY) {
     if (all_count(m)) {
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
       __syncthreads();
       sum = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
     }
-    if (m.by_count || m.by_sum) {
+    if ((m.by_count || m.by_sum) && !one_list(a)) {
       for (int i = tid; i < BINS; i += PART_THREADS) bins[i] = 0;
       __syncthreads();
       const float per = steps(a, m), base = step_of(top, per);
@@ -467,7 +470,10 @@ __global__ __launch_bounds__(THREADS, 8) void k_sample_pick(SampleArgs a) {
   RowState st{AS_IT_IS, 0, -1, 0u, 0, 0.f, 0.f};
   PartSums mine{0, 0};
   uint64_t listed_first = 0;
-  if (narrow) {
+  if (narrow && one_list(a)) {
+    st.mode = COLLECT;
+    st.list_n = vocab;
+  } else if (narrow) {
     st = a.state[row];
     if (tid < a.parts) mine = a.sums[(int64_t)row * a.parts + tid];
     listed_first = a.list[(int64_t)row * LIST + tid];
@@ -516,7 +522,10 @@ __global__ __launch_bounds__(THREADS, 8) void k_sample_pick(SampleArgs a) {
     s.part_sum[tid] = own;
     s.part_ties[tid] = 0;
 #pragma unroll 1
-    for (unsigned i = tid; i < listed_n; i += THREADS) s.list[i] = i < THREADS ? listed_first : a.list[(int64_t)row * LIST + i];
+    for (unsigned i = tid; i < listed_n; i += THREADS) {
+      if (one_list(a)) s.list[i] = (uint64_t)key_of(tame(to_f32(r.p[i]))) << 32 | (unsigned)~i;            // (what is no number weighs nothing)
+      else s.list[i] = i < THREADS ? listed_first : a.list[(int64_t)row * LIST + i];
+    }
     __syncthreads();
     unsigned k_min = ~0u, k_max = 0u, here = 0;
     uint64_t weights = 0;
@@ -716,6 +725,7 @@ size_t place(SampleArgs& a, int rows, char* base) {
   size_t at = 0;
   auto take = [&](size_t bytes) { char* p = base + at; at += (bytes + 15) / 16 * 16; return p; };
   a.tops = (Part*)take(parts * sizeof(Part));
+  if (a.vocab <= LIST) return at;
   a.sums = (PartSums*)take(parts * sizeof(PartSums));
   a.bins = (uint64_t*)take(parts * BINS * 8);
   a.maxima = (float*)take(parts * PART_THREADS * 4);
@@ -732,7 +742,7 @@ hipError_t launch(hipStream_t st, const SampleArgs& a, int rows) {
   else hipLaunchKernelGGL((k_sample_parts<T, ALIGNED, 16>), grid, wg, 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.top_k || a.top_p || a.min_p) {
+  if ((a.top_k || a.top_p || a.min_p) && a.vocab > LIST) {
     hipLaunchKernelGGL(k_sample_edges, dim3(rows), dim3(THREADS), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (wide) hipLaunchKernelGGL((k_sample_collect<T, ALIGNED, 32>), grid, wg, 0, st, a);
@@ -771,6 +781,7 @@ extern "C" size_t esp_sample_scratch_bytes(int32_t rows, int32_t vocab) {
   if (rows < 1 || vocab < 1 || too_large(vocab)) return 0;
   SampleArgs a{};
   const int n = std::min(rows, ROWS_AT_ONCE);
+  a.vocab = vocab;
   a.part = part_logits(n, vocab);
   a.parts = (vocab + a.part - 1) / a.part;
   return place(a, n, nullptr);
