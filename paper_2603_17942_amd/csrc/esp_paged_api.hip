@@ -223,7 +223,7 @@ esp_status esp_paged_evict(void* stream, const esp_paged_kv* kv, const float* ma
       recent < 0 || (int64_t)first + recent > keep)
     return ESP_EINVAL;
   if ((mass == mass_out && mass_slots != mass_out_slots) || (table_out == kv->page_table && table_out_stride != kv->table_stride)) return ESP_EINVAL;
-  if (keep > INT32_MAX - 65536 || mass_out_slots < keep || (int64_t)table_out_stride * kv->page_size < keep) return ESP_ECAPACITY;
+  if (keep > INT32_MAX - 65536 || kv->len_bound > INT32_MAX - 65536 || mass_out_slots < keep || (int64_t)table_out_stride * kv->page_size < keep) return ESP_ECAPACITY;
   // four times 256 threads a layer, sequence and kv head
   if (kv->n_kv_heads > 65535 || (int64_t)kv->n_layers * kv->batch * kv->n_kv_heads > MOST_WORKGROUPS / 4) return ESP_ECAPACITY;
   const EvictArgs a{mass, mass_out, table_out, len_out, kept, kv->n_layers, mass_slots, mass_out_slots, table_out_stride, keep, first, recent};

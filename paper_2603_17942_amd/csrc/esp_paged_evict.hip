@@ -136,7 +136,7 @@ __global__ __launch_bounds__(MOVERS) void k_evict_move(PagedDev kv, EvictArgs a)
 
   int n = 0;
   for (int i = tid; i < a.keep; i += MOVERS) n += kept[i] >= 0;
-  n = (int)wave_sum((float)n);                         // (a thread has less than 2^13 of them, a wave less than 2^19)
+  n = (int)wave_total((unsigned)n);
   if ((tid & 63) == 0) counted[tid >> 6] = n;
   __syncthreads();
   n = 0;

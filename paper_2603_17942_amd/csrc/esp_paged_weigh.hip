@@ -226,11 +226,10 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDe
   }
   const int G = a.hq / kv.hkv, cols = c.rows * G;
   if (32 * tile >= cols) return;       // (no barrier below)
-  const int low_row = c.first + 32 * tile / G, top_row = c.first + min(32 * (tile + CT) - 1, cols - 1) / G;
+  const int top_row = c.first + min(32 * (tile + CT) - 1, cols - 1) / G;
   const int begin = share * p.share_units, end = min(begin + p.share_units, (c.len + top_row) / 32 + 1);
   F q[CT][HD / 16], k[HD / 16] = {}, next[HD / 16] = {};
   Units<T> units(kv, seq, kvh, HD);
-  // (two turns apart in the code, so that the next unit's registers need not be copied)
   bool there = false, next_there = false;
   auto fetch = [&](int u, F (&key)[HD / 16], bool& is_there) {
     const T* at = u < end ? units.at(u, HD) : nullptr;
@@ -250,20 +249,18 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDe
     m[i] = ATTN_UNSEEN;
     l[i] = 0.f;
   }
-  // what a unit adds to the statistics
-  auto use = [&](int u, const F (&key)[HD / 16]) {
-    f32x16_t x[CT] = {};
+  auto scores = [&](const F (&key)[HD / 16], f32x16_t (&x)[CT]) {
+#pragma unroll
+    for (int i = 0; i < CT; ++i) x[i] = f32x16_t{};
 #pragma unroll
     for (int s = 0; s < HD / 16; ++s)
 #pragma unroll
       for (int i = 0; i < CT; ++i) x[i] = attn_mma(key[s], q[i][s], x[i]);
-    const bool whole = 32 * u + 31 <= c.len + low_row;
+  };
+  // what a unit's scores add to the statistics
+  auto add = [&](const f32x16_t (&x)[CT]) {
 #pragma unroll
     for (int i = 0; i < CT; ++i) {
-      if (!whole) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) x[i][v] = 32 * u + 8 * (v >> 2) + 4 * half + (v & 3) <= sees[i] ? x[i][v] : -INFINITY;
-      }
       float top = attn_max3(x[i][0], x[i][1], x[i][2]);
 #pragma unroll
       for (int v = 3; v < 15; v += 2) top = attn_max3(top, x[i][v], x[i][v + 1]);
@@ -275,11 +272,56 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDe
       m[i] = ref;
     }
   };
-  for (int u = begin; u < end; u += 2) {
+  // Units that all columns see whole, as long as their pages are there: one's scores among the other's exponentials (a wave has its SIMD to itself much of the
+  // time, and the matrix core would wait for the exponentials and they for it).
+  auto both = [&](const F (&key)[HD / 16], f32x16_t (&next_x)[CT], const f32x16_t (&x)[CT]) {
+    scores(key, next_x);
+    add(x);
+#pragma unroll
+    for (int i = 0; i < CT * HD / 16 * (sizeof(T) == 2 ? 1 : 8); ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       // a matrix instruction
+      __builtin_amdgcn_sched_group_barrier(0x002, sizeof(T) == 2 ? 8 : 1, 0);
+    }
+  };
+  int u = begin;
+  const int end_whole = min(end, (c.len + c.first + 32 * tile / G + 1) / 32);
+  f32x16_t x[CT], y[CT];
+  if (there && u + 1 < end_whole) {
     fetch(u + 1, next, next_there);
-    if (there) use(u, k);
-    fetch(u + 2, k, there);
-    if (next_there) use(u + 1, next);
+    scores(k, x);
+    while (next_there && u + 2 < end_whole) {          // x: scores of unit u; next: keys of the one after
+      fetch(u + 2, k, there);
+      both(next, y, x);
+      ++u;
+      if (!there || u + 2 >= end_whole) {
+#pragma unroll
+        for (int i = 0; i < CT; ++i) x[i] = y[i];
+#pragma unroll
+        for (int s = 0; s < HD / 16; ++s) next[s] = k[s];
+        next_there = there;
+        break;
+      }
+      fetch(u + 2, next, next_there);
+      both(k, x, y);
+      ++u;
+    }
+    add(x);
+    ++u;
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) k[s] = next[s];
+    there = next_there;
+  }
+  for (; u < end; ++u) {
+    if (there) {
+      scores(k, x);
+#pragma unroll
+      for (int i = 0; i < CT; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[i][v] = 32 * u + 8 * (v >> 2) + 4 * half + (v & 3) <= sees[i] ? x[i][v] : -INFINITY;
+    }
+    const bool was_there = there;
+    fetch(u + 1, k, there);
+    if (was_there) add(x);
   }
   float2* out = reinterpret_cast<float2*>(a.scratch) + share * p.columns + first_column(p, c, kv, G, seq, kvh);
 #pragma unroll

@@ -86,7 +86,7 @@ def test_evict_refusals(lib):
     assert call(keep=0) == EINVAL and call(keep=-1) == EINVAL and call(first=-1) == EINVAL and call(recent=-1) == EINVAL
     assert call(first=60, recent=41) == EINVAL and call(keep=2 ** 31 - 1, first=2 ** 31 - 1, recent=2 ** 31 - 1) == EINVAL
     assert call(mass_out=P, out_slots=4000) == EINVAL and call(table=P, stride=49) == EINVAL
-    assert call(out_slots=99) == ECAPACITY and call(stride=1) == ECAPACITY
+    assert call(out_slots=99) == ECAPACITY and call(stride=1) == ECAPACITY and call(kv=paged(len_bound=2 ** 31 - 1)) == ECAPACITY
     assert call(kv=paged(batch=60000, n_layers=100)) == ECAPACITY
 
 
