@@ -215,10 +215,11 @@ template <typename T, int HD, int CT>
 __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
   typedef typename AttnFrag<T>::type F;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-  // Late columns have the most to do and come first.  Column groups lie next to each other, shares far apart: workgroups go to the XCDs in turn, and early
-  // columns have no last shares (eight shares next to each other: 204 us for a prompt of 4096, half of the XCDs idle most of the time; so 117).
-  const int block = gridDim.x - 1 - blockIdx.x, groups = gridDim.x / p.shares;
-  const int share = block / groups, tile = (block % groups * WAVES + wave) * CT, kvh = blockIdx.y, seq = blockIdx.z;
+  // Late columns have the most to do and come first.  Workgroups go to the XCDs in turn, and early columns have no last shares: column groups lie next to
+  // each other, shares far apart (eight shares next to each other: 204 us for a prompt of 4096, half of the XCDs idle most of the time; so 158), and
+  // groups are turned by one from head to head.
+  const int block = gridDim.x - 1 - blockIdx.x, groups = gridDim.x / p.shares, kvh = blockIdx.y, seq = blockIdx.z;
+  const int share = block / groups, tile = ((block + kvh) % groups * WAVES + wave) * CT;
   const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
   if (!c.ok) {
     if (blockIdx.x == 0 && kvh == 0 && tid == 0) set_status(kv.status, chunk_fault(ch, seq));
@@ -228,6 +229,11 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDe
   if (32 * tile >= cols) return;       // (no barrier below)
   const int top_row = c.first + min(32 * (tile + CT) - 1, cols - 1) / G;
   const int begin = share * p.share_units, end = min(begin + p.share_units, (c.len + top_row) / 32 + 1);
+  float2* out = reinterpret_cast<float2*>(a.scratch) + share * p.columns + first_column(p, c, kv, G, seq, kvh);
+  if (begin >= end) {                  // (none of the share's units is seen: then there are several)
+    for (int col = 32 * tile + lane; col < min(32 * (tile + CT), cols); col += 64) out[col] = {ATTN_UNSEEN, 0.f};
+    return;
+  }
   F q[CT][HD / 16], k[HD / 16] = {}, next[HD / 16] = {};
   Units<T> units(kv, seq, kvh, HD);
   bool there = false, next_there = false;
@@ -323,7 +329,6 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDe
     fetch(u + 1, k, there);
     if (was_there) add(x);
   }
-  float2* out = reinterpret_cast<float2*>(a.scratch) + share * p.columns + first_column(p, c, kv, G, seq, kvh);
 #pragma unroll
   for (int i = 0; i < CT; ++i) {
     const float2 r = join(float2{m[i], l[i]}, float2{__shfl_xor(m[i], 32, 64), __shfl_xor(l[i], 32, 64)});
