@@ -447,23 +447,24 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_add(PagedDev kv, ChunkDev 
     // (whole: all columns of the tile see all keys of the wave; the last tile's columns past the end have a weight of zero)
     const bool whole = 32 * t + 32 <= cols && 32 * (unit0 + KU) - 1 <= c.len + c.first + low_row;
     step(low_row, low_g);
+    if (whole) {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4_t r = *reinterpret_cast<const f32x4_t*>(&ref[buf][8 * g + 4 * half]), w = *reinterpret_cast<const f32x4_t*>(&inv[buf][8 * g + 4 * half]);
-      if (whole) {
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const f32x4_t r = *reinterpret_cast<const f32x4_t*>(&ref[buf][8 * g4 + 4 * half]), w = *reinterpret_cast<const f32x4_t*>(&inv[buf][8 * g4 + 4 * half]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int i = 0; i < KU; ++i) of_tile[i] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[i][4 * g + e], a.scale, -r[e])), w[e], of_tile[i]);
-      } else {
+          for (int i = 0; i < KU; ++i) of_tile[i] = fmaf(__builtin_amdgcn_exp2f(fmaf(x[i][4 * g4 + e], a.scale, -r[e])), w[e], of_tile[i]);
+      }
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int last = sees[buf][8 * g + 4 * half + e];
+      for (int v = 0; v < 16; ++v) {
+        const int col = 8 * (v >> 2) + 4 * half + (v & 3), last = sees[buf][col];
+        const float r = ref[buf][col], w = inv[buf][col];
 #pragma unroll
-          for (int i = 0; i < KU; ++i) {
-            const float y = fmaf(__builtin_amdgcn_exp2f(fmaf(x[i][4 * g + e], a.scale, -r[e])), w[e], of_tile[i]);
-            of_tile[i] = 32 * (unit0 + i) + (lane & 31) <= last ? y : of_tile[i];
-          }
+        for (int i = 0; i < KU; ++i) {
+          const float y = fmaf(__builtin_amdgcn_exp2f(fmaf(x[i][v], a.scale, -r)), w, of_tile[i]);
+          of_tile[i] = 32 * (unit0 + i) + (lane & 31) <= last ? y : of_tile[i];
         }
       }
     }
