@@ -345,6 +345,7 @@ EVICT = [  # dtype, hd, hkv, page, layers, lens, keep, first, recent
     ("f32", 128, 4, 32, 1, [321, 65], 64, 0, 64),
     ("f32", 128, 1, 128, 3, [130, 500], 129, 128, 1),
     ("bf16", 128, 2, 32, 1, [(53 * i) % 200 for i in range(40)], 70, 3, 10),
+    ("bf16", 64, 1, 128, 1, [20001, 7000], 6999, 5, 700),
 ]
 
 
@@ -437,6 +438,66 @@ def test_captured_eviction_follows_the_lengths():
     for a, b in zip(runs[:4], runs[4:]):
         for x, y in zip(a, b):
             assert same(x.float(), y.float())
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_pools_behind_31_and_32_bits(rows):
+    """A sequence whose pages and layer lie behind 2^31 and 2^32 elements of a pool does what the same does in a small one."""
+    small = Plain(torch.bfloat16, 1, 8, 128, 64, [400, 90], [rows, rows], 111, keep=128)
+    pages, layers = 50000, 2                           # 3.3e9 elements a layer
+    shape = (layers, pages, 8, 64, 128)
+    kv = B.PagedKv(torch.zeros(shape, dtype=torch.bfloat16, device="cuda"), torch.zeros(shape, dtype=torch.bfloat16, device="cuda"),
+                   torch.zeros_like(small.kv.page_table), i32([400, 90]), 400)
+    n = small.pages
+    base = pages - n - 3
+    kv.k[1, base:base + n] = small.kv.k[0]
+    kv.v[1, base:base + n] = small.kv.v[0]
+    kv.page_table.copy_(torch.where(small.table < n, small.table + base, small.table))
+    q = queries(2 * rows, 32, 128, torch.bfloat16, 112)
+    mass, far = torch.zeros((1, 2, 8, 500), device="cuda"), torch.zeros((2, 2, 8, 500), device="cuda")
+    B.paged_weigh(small.kv, 0, small.chunk, q, mass)
+    B.paged_weigh(kv, 1, small.chunk, q, far)
+    assert torch.equal(mass[0], far[1]) and (far[0] == 0).all() and float(mass[0, 0, :, 400].min()) > 0
+    far[0] = far[1]
+    fresh = small.fresh.cuda()
+    a = B.paged_evict(small.kv, mass, 128, 4, 16, table_out=fresh)
+    b = B.paged_evict(kv, far, 128, 4, 16, table_out=(fresh + base).to(torch.int32))
+    assert torch.equal(a[0], b[1]) and torch.equal(mass[0], far[1]) and kv.lens.tolist() == [128, 90]
+    assert same(kv.k[1, base:base + n].float(), small.kv.k[0].float()) and same(kv.v[1, base:base + n].float(), small.kv.v[0].float())
+    assert (kv.k[0, base:base + n] == 0).all() and (kv.k[1, :base] == 0).all() and (kv.v[1, base + n:] == 0).all()
+    assert kv.device_status() == 0 and small.kv.device_status() == 0
+
+
+def test_queries_that_lie_apart_and_at_any_place():
+    """Rows of a projection, and rows whose addresses 16-byte loads cannot take."""
+    for rows in (1, 40):
+        c = Plain(torch.bfloat16, 1, 2, 128, 32, [70, 9], [rows, rows], 121)
+        q = queries(2 * rows, 8, 128, torch.bfloat16, 122)
+        want = torch.zeros((1, 2, 2, 128), device="cuda")
+        B.paged_weigh(c.kv, 0, c.chunk, q, want)
+        for off, pad in ((0, 256), (8, 8), (1, 0), (3, 5)):
+            big = torch.full((2 * rows, off + 1024 + pad), math.nan, dtype=torch.bfloat16, device="cuda")
+            big[:, off:off + 1024] = q.reshape(2 * rows, 1024)
+            got = torch.zeros_like(want)
+            B.paged_weigh(c.kv, 0, c.chunk, big[:, off:off + 1024].unflatten(1, (8, 128)), got)
+            assert torch.equal(got, want)
+
+
+def test_two_streams_with_a_workspace_each():
+    c = Plain(torch.bfloat16, 1, 4, 128, 32, [900, 400, 30], [20, 20, 20], 131)
+    q = queries(60, 16, 128, torch.bfloat16, 132)
+    want = torch.zeros((1, 3, 4, 1000), device="cuda")
+    B.paged_weigh(c.kv, 0, c.chunk, q, want)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.zeros_like(want) for _ in range(6)]
+    scratch = [torch.empty(B.paged_weigh_scratch_bytes(c.kv, c.chunk, 16), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for i, o in enumerate(outs):
+        with torch.cuda.stream(streams[i % 2]):
+            B.paged_weigh(c.kv, 0, c.chunk, q, o, scratch=scratch[i % 2])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
 
 
 # ---- a run of them together ------------------------------------------------------------------------------------

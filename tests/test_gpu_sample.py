@@ -264,3 +264,53 @@ def test_rows_behind_31_bits_of_elements():
     x[torch.arange(n, device="cuda"), at] = 30.0       # weight of all others: 1.2e-8
     ids, _ = B.sample(x, torch.full((n,), 0.5, device="cuda"))
     assert torch.equal(ids, at.int())
+
+
+def test_more_rows_than_are_done_at_once_and_a_workspace_of_anything():
+    n, vocab = 2100, 5003                              # three lots
+    x, u, lim = logits(n, vocab, 110), torch.rand(n, generator=gen(111)), limits(n, 112)
+    rows = torch.tensor([0, 1, 2, 3, 1022, 1023, 1024, 1025, 2047, 2048, 2049, 2097, 2098, 2099])
+    want = check(x[rows], u[rows], *(t[rows] for t in lim))
+    args = [x.cuda(), u.cuda(), *(t.cuda() for t in lim)]
+    ids = B.sample(*args)[0]
+    assert torch.equal(ids[rows.cuda()], want)
+    scratch = torch.empty(B.sample_scratch_bytes(n, vocab), dtype=torch.uint8, device="cuda")
+    for fill in (0, 255, 127):
+        scratch.fill_(fill)
+        assert torch.equal(B.sample(*args, scratch=scratch)[0], ids)
+
+
+@pytest.mark.parametrize("vocab,k", [(30000, 5000), (30000, 29999), (140000, 20000), (140000, 3)])
+def test_more_tokens_left_than_are_listed(vocab, k):
+    n = 8
+    x = logits(n, vocab, 120)
+    u = torch.rand(n, generator=gen(121))
+    ks = torch.full((n,), k, dtype=torch.int32)
+    check(x, u, k=ks)
+    check(x, u, k=ks, p=torch.full((n,), 0.97), T=torch.full((n,), 1.3))
+    # (the rows that are sure of a few: at 0.9999 the sum's border lies among tokens that weigh some 1e-8 of W each, and it may be off
+    # by 2 (3e-12 + 140000 2^-45 / W) = 8e-9 at W = 1: whatever the kernel does, up to these four say nothing)
+    check(x, u, p=torch.full((n,), 0.9999), m=torch.full((n,), 1e-4), silent=4 if vocab == 140000 else 0)
+    check(x.bfloat16(), u, k=ks, m=torch.full((n,), 1e-3))
+
+
+def test_logits_far_from_zero():
+    """Steps of log w are counted from zero: far from it logits are divided another way."""
+    n, vocab = 6, 20000
+    x = logits(n, vocab, 130)
+    u, lim = torch.rand(n, generator=gen(131)), limits(n, 132)
+    lim[0][0] = 0.9
+    for shift in (300.0, -300.0, 4.0e4, -4.0e4, 1.0e6):         # (1e6: a sixteenth apart at least)
+        check(x + shift, u, *lim)
+    check(x * 1e6, u, lim[0] * 1e6, *lim[1:])
+    check(x * 1e-30, u, lim[0] * 1e-10, *lim[1:])
+
+
+def test_outputs_and_inputs_of_others_are_left_alone():
+    n, vocab = 5, 6000
+    x, u, lim = logits(n, vocab, 140).cuda(), torch.rand(n, generator=gen(141)).cuda(), [t.cuda() for t in limits(n, 142)]
+    before = [t.clone() for t in (x, u, *lim)]
+    ids, probs = torch.full((n + 2,), -7, dtype=torch.int32).cuda(), torch.full((n + 2,), -7.0).cuda()
+    B.sample(x, u, *lim, ids=ids[1:-1], probs=probs[1:-1])
+    assert ids[0] == -7 and ids[-1] == -7 and probs[0] == -7 and probs[-1] == -7 and (ids[1:-1] >= 0).all()
+    assert all(torch.equal(a, b) for a, b in zip(before, (x, u, *lim)))
