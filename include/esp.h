@@ -377,8 +377,9 @@ esp_status esp_softmax_topk_static(void *stream, const float *logits, int32_t ro
  * whose temperature is negative or not finite or whose top_p or min_p is NaN, gets -1 and 0.
  * Temperatures between 0 and 1e-20 are as 1e-20, above 1e20 as 1e20.  Weights are taken in fp64 (1.1e-12 of themselves) and added up in units of 2^-S of
  * the largest, S = min(45, 62 - ceil log2 vocab); tokens of less than half a unit are not chosen.  The same call chooses the same tokens.
- *   scratch     device, 16-byte aligned, esp_sample_scratch_bytes() (up to 185 KB a row of 128256, of up to 1024 rows: more are done in lots); calls that
- *               overlap in time need one each.  Results do not depend on what it held
+ *   scratch     device, 16-byte aligned, esp_sample_scratch_bytes(): what is enough for so many rows and for fewer (of a row of 128256 up to 329 KB for 64 rows,
+ *               181 KB where there are more; of up to 4096 tokens 16 bytes; of up to 1024 rows: more are done in lots).  Calls that overlap in time need one
+ *               each.  Results do not depend on what it held
  * Errors: EINVAL (null pointers, rows < 0, vocab < 1), ESHAPE (row_stride < vocab), EDTYPE, ECAPACITY (scratch; vocab above 2^22). */
 size_t esp_sample_scratch_bytes(int32_t rows, int32_t vocab);
 esp_status esp_sample(void* stream, int32_t dtype, const void* logits, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
@@ -505,10 +506,11 @@ esp_status esp_paged_commit(void *stream, const esp_paged_kv *kv, const int32_t 
  *   last_rows   0: all rows count; otherwise only the last so many of each sequence's
  *   before, mass device fp32 [n_layers][batch][n_kv_heads][mass_slots]; before NULL: zeros; it may be mass itself, and otherwise must not overlap it
  *   scratch     device, 16-byte aligned, esp_paged_weigh_scratch_bytes(), which depend on the host's values alone; calls that overlap in time need
- *               one each.  Up to 32 counted (row, query head) pairs a kv head it holds their scores: up to 4 bytes a pair, kv head and token of len_bound
- * Scores, probabilities and sums are fp32, tokens' sums always in the same order.  Scores may be as large as 5e8.  A row with a score of infinity or NaN makes
- * the tokens it sees NaN; a token in a page outside the pool is not seen (its mass is `before`).  A sequence with len + rows above mass_slots is as one
- * that is over its bound.
+ *               one each.  Up to 32 counted (row, query head) pairs a kv head it holds their scores, 4 bytes a pair (in fours), kv head and token of
+ *               len_bound: a call with more rows can want less
+ * Scores, probabilities and sums are fp32, tokens' sums always in the same order.  Scores may be as large as 5e8.  A row with a score of plus infinity or NaN makes
+ * the tokens it sees NaN, a score of minus infinity weighs nothing; a token in a page outside the pool is not seen (its mass is `before`).  A sequence
+ * with len + rows above mass_slots is as one that is over its bound.
  * Errors: as esp_paged_attn; EINVAL also for last_rows < 0 and mass_slots < 1; ECAPACITY also for more than 65535 kv heads. */
 size_t esp_paged_weigh_scratch_bytes(const esp_paged_kv* kv, const esp_chunk* rows, int32_t n_q_heads, int32_t last_rows);
 esp_status esp_paged_weigh(void* stream, const esp_paged_kv* kv, int32_t layer, const esp_chunk* rows, int32_t n_q_heads, const void* q,
@@ -529,7 +531,7 @@ esp_status esp_paged_weigh(void* stream, const esp_paged_kv* kv, int32_t layer, 
  * A kept token whose old page is outside the pool becomes zeros, one whose new page is is not written; both set ESP_DEV_BAD_PAGE.  A sequence with a length
  * that is negative, above len_bound, mass_slots or its table is left out: its kept are -1, its len_out its len.
  * Errors: EINVAL (null pointers, keep < 1, first or recent negative or together above keep, mass_out or table_out the input with other strides), ECAPACITY
- * (table_out or mass_out too small for keep, more than 4194303 layers x sequences x kv heads). */
+ * (table_out or mass_out too small for keep, more than 4194303 layers x sequences x kv heads, keep or len_bound above 2^31 - 65537). */
 esp_status esp_paged_evict(void* stream, const esp_paged_kv* kv, const float* mass, int32_t mass_slots, int32_t keep, int32_t first, int32_t recent,
                            const int32_t* table_out, int32_t table_out_stride, float* mass_out, int32_t mass_out_slots, int32_t* len_out,
                            int32_t* kept);

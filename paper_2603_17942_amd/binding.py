@@ -838,6 +838,7 @@ def paged_weigh(kv: PagedKv, layer: int, rows: ChunkRows, q: torch.Tensor, mass:
     lib = load_library()
     _same_batch(kv, rows)
     dev, dt, hd, n = kv.device, kv.dtype, kv.head_dim, rows.total_rows
+    last_rows = max(-1, min(last_rows, 2 ** 31 - 1))
     qp, qs, nq = _heads(q, "q", dev, dt, n, hd)
     mp = _mass(mass, "mass", kv)
     bp = mp
@@ -867,8 +868,8 @@ def paged_evict(kv: PagedKv, mass: torch.Tensor, keep: int, first: int = 0, rece
     to = mass if mass_out is None else mass_out
     if table.dim() != 2:
         raise ValueError("table_out: [batch, pages of a sequence] wanted")
-    if keep < 1:
-        raise ValueError("keep: 1 or more wanted")
+    if not (1 <= keep < 2 ** 31 and first >= 0 and recent >= 0 and first + recent <= keep):
+        raise ValueError("keep: 1 or more wanted, and room for first and recent")
     shape = (layers, kv.batch, kv.n_kv_heads, keep)
     if kept is None:
         kept = torch.empty(shape, dtype=torch.int32, device=dev)

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
         for (int i = 0; i < N; ++i) {
           const float s = x[j][i] * per, step = base - floorf(s);
           if (step < (float)BINS) {
-            const unsigned f = (unsigned)((s - floorf(s)) * PLACES);
+            const unsigned f = (unsigned)(__builtin_amdgcn_fractf(s) * PLACES);         // (below 1, which s - floor(s) is not for a little less than 0)
             atomicAdd((unsigned long long*)&bins[(int)step], 1ull << 44 | (uint64_t)f << 22 | (f * f / PLACES));
           }
         }
@@ -550,7 +550,7 @@ __global__ __launch_bounds__(THREADS, 8) void k_sample_pick(SampleArgs a) {
         count = (unsigned)lim.top_k;
       } else {
         if (!lim.by_sum) break;
-        goal = sum_goal(lim.top_p, cut.sum);
+        goal = min(sum_goal(lim.top_p, cut.sum), q0 + list_sum);       // (tokens of less than half a unit count in the parts' sums: nothing behind the list)
       }
       // The cut among n tokens with keys between the two, after `count` tokens, or before the first one with `goal` or more before it.  c0, q: tokens
       // and weights before them.
@@ -717,7 +717,11 @@ __global__ __launch_bounds__(THREADS, 8) void k_sample_pick(SampleArgs a) {
 }
 
 // Logits of a part: as many as a thread's registers hold with ease (32) where there are many; half of them where a short launch is spread over more CUs.
-int part_logits(int rows, int vocab) { return (int64_t)rows * ((vocab + 4095) / 4096) > 2048 ? 8192 : 4096; }
+constexpr int SMALL_PARTS = 2048;
+void divide(SampleArgs& a, int rows) {
+  a.part = (int64_t)rows * ((a.vocab + 4095) / 4096) > SMALL_PARTS ? 8192 : 4096;
+  a.parts = (a.vocab + a.part - 1) / a.part;
+}
 
 // the workspace's arrays for so many rows, behind one another; its bytes
 size_t place(SampleArgs& a, int rows, char* base) {
@@ -779,12 +783,16 @@ bool too_large(int vocab) { return vocab > MOST_PARTS * 4096; }
 
 extern "C" size_t esp_sample_scratch_bytes(int32_t rows, int32_t vocab) {
   if (rows < 1 || vocab < 1 || too_large(vocab)) return 0;
-  SampleArgs a{};
-  const int n = std::min(rows, ROWS_AT_ONCE);
-  a.vocab = vocab;
-  a.part = part_logits(n, vocab);
-  a.parts = (vocab + a.part - 1) / a.part;
-  return place(a, n, nullptr);
+  // (what the most rows with small parts want can be more than what more rows do: enough for those also)
+  const int small = std::min(rows, SMALL_PARTS / ((vocab + 4095) / 4096));
+  size_t most = 0;
+  for (const int n : {std::min(rows, ROWS_AT_ONCE), std::min(std::max(small, 1), ROWS_AT_ONCE)}) {
+    SampleArgs a{};
+    a.vocab = vocab;
+    divide(a, n);
+    most = std::max(most, place(a, n, nullptr));
+  }
+  return most;
 }
 
 extern "C" esp_status esp_sample(void* stream, int32_t dtype, const void* logits, int64_t row_stride, int32_t rows, int32_t vocab,
@@ -802,8 +810,7 @@ extern "C" esp_status esp_sample(void* stream, int32_t dtype, const void* logits
   SampleArgs a{};
   a.logits = logits; a.stride = row_stride; a.vocab = vocab;
   a.shift = std::min(45, 62 - log2_vocab);
-  a.part = part_logits(std::min(rows, ROWS_AT_ONCE), vocab);
-  a.parts = (vocab + a.part - 1) / a.part;
+  divide(a, std::min(rows, ROWS_AT_ONCE));
   a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.u = u; a.ids = ids; a.probs = probs;
   place(a, std::min(rows, ROWS_AT_ONCE), (char*)scratch);
   const hipError_t e = dtype == ESP_F32 ? launch_rows<float>((hipStream_t)stream, a, rows) : launch_rows<bf16_t>((hipStream_t)stream, a, rows);

@@ -314,3 +314,32 @@ def test_outputs_and_inputs_of_others_are_left_alone():
     B.sample(x, u, *lim, ids=ids[1:-1], probs=probs[1:-1])
     assert ids[0] == -7 and ids[-1] == -7 and probs[0] == -7 and probs[-1] == -7 and (ids[1:-1] >= 0).all()
     assert all(torch.equal(a, b) for a, b in zip(before, (x, u, *lim)))
+
+
+@pytest.mark.parametrize("value", [-1e-10, -1e-30, -2.0 ** -149, 0.0])
+def test_a_part_of_equal_logits_a_little_below_zero(value):
+    """8192 of them lie at the very end of their step."""
+    n, vocab = 64, 140000
+    x = torch.full((n, vocab), -math.inf)
+    x[:, 8192:16384] = value
+    x[:, 20000:23000] = -0.04 - 0.3 * torch.rand((n, 3000), generator=gen(150))
+    x[:, 139999] = 0.0
+    check(x, torch.rand(n, generator=gen(151)), p=torch.linspace(0.70, 0.99, n))
+    check(x, torch.rand(n, generator=gen(152)), k=torch.linspace(8180, 8210, n).to(torch.int32))
+
+
+@pytest.mark.parametrize("vocab", [5000, 2 ** 22])
+def test_the_largest_top_p_below_one(vocab):
+    """Weights that are none in integers and much more than 1 - top_p of all together are tokens that are not chosen."""
+    for octaves in (42.5, 41.2, 47.0, 60.0):
+        x = torch.full((2, vocab), -octaves * math.log(2))
+        x[:, 1234] = 0.0
+        x[:, 4321] = -1.0
+        p, u = torch.full((2,), 1 - 2.0 ** -24), torch.tensor([0.5, 0.9])
+        ids, probs = B.sample(x.cuda(), u.cuda(), top_p=p.cuda())
+        share = 1 / (1 + math.exp(-1))
+        assert ids.tolist() == [1234, 4321], octaves
+        # 2^22 tokens of 2^-41.2 at most weigh 1.7e-6; fp32
+        assert torch.allclose(probs.cpu(), torch.tensor([share, 1 - share]), rtol=0, atol=2e-6 + 2.0 ** -24)
+        ids, _ = B.sample(x.cuda(), u.cuda(), top_p=p.cuda(), top_k=torch.full((2,), 4000, dtype=torch.int32).cuda(), min_p=torch.full((2,), 1e-12).cuda())
+        assert ids.tolist() == [1234, 4321], octaves

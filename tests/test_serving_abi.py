@@ -126,3 +126,20 @@ def test_python_checks_of_tensors():
             B.paged_evict(kv, mass, **kw)
     with pytest.raises(ValueError, match="no CPU fallback"):
         B.paged_evict(kv, mass, 8)
+
+
+@pytest.mark.parametrize("vocab", [1, 4096, 4097, 32000, 128256, 2 ** 22])
+def test_a_workspace_for_more_rows_is_enough_for_fewer(vocab):
+    lib = B.load_library()
+    need = [lib.esp_sample_scratch_bytes(n, vocab) for n in range(1, 2100)]
+    assert all(a <= b for a, b in zip(need, need[1:]))
+    assert need[-1] == need[1023]
+
+
+def test_python_numbers_beyond_32_bits():
+    k = torch.zeros((1, 4, 2, 32, 64))
+    kv = B.PagedKv(k, k.clone(), torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 0)
+    mass = torch.zeros((1, 1, 2, 64))
+    for kw in (dict(keep=2 ** 32 + 8), dict(keep=8, first=2 ** 32), dict(keep=8, recent=2 ** 32 + 1), dict(keep=8, first=-2 ** 32), dict(keep=8, first=5, recent=4)):
+        with pytest.raises(ValueError, match="keep: 1 or more wanted"):
+            B.paged_evict(kv, mass, **kw)
