@@ -23,6 +23,7 @@ __global__ __launch_bounds__(CHOOSERS) void k_evict_choose(PagedDev kv, EvictArg
   __shared__ unsigned bins[DIGIT_BINS];
   __shared__ WaveSums<CHOOSERS / 64> sums;
   __shared__ unsigned found[2];
+  int turn = 0;
   const int tid = threadIdx.x, kvh = blockIdx.x, seq = blockIdx.y, layer = blockIdx.z;
   const int64_t head = ((int64_t)layer * kv.batch + seq) * kv.hkv + kvh;
   const float* mass = a.mass + head * a.slots;
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(CHOOSERS) void k_evict_choose(PagedDev kv, EvictArg
       unsigned n[EACH], at = 0;
 #pragma unroll
       for (int i = 0; i < EACH; ++i) { n[i] = bins[DIGIT_BINS - 1 - (EACH * tid + i)]; at += n[i]; }
-      before(sums, at);
+      before(sums, turn, at);
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         if (at < want && want <= at + n[i]) { found[0] = DIGIT_BINS - 1 - (EACH * tid + i); found[1] = at; }
@@ -81,8 +82,8 @@ __global__ __launch_bounds__(CHOOSERS) void k_evict_choose(PagedDev kv, EvictArg
     certain += k > cut;
     equal += k == cut;
   }
-  before(sums, certain);
-  before(sums, equal);
+  before(sums, turn, certain);
+  before(sums, turn, equal);
   unsigned ties = equal, place = certain + min(equal, want);
   for (int i = begin; i < end; ++i) {
     bool in = i < lo || i >= hi;

@@ -139,38 +139,27 @@ __device__ __forceinline__ unsigned wave_most(unsigned float_bits) {
 // the largest of a wave's logits, the lowest id of equal ones
 __device__ __forceinline__ void wave_largest(float& top, int& at) {
   const float m = __uint_as_float(wave_most(__float_as_uint(top)));
-  at = (int)lane_of(running(top == m ? (unsigned)at : ~0u, ~0u, [](unsigned a, unsigned b) { return min(a, b); }), 63);
+  at = (int)lane_of(running(top == m ? (unsigned)at : ~0u, ~0u, Least()), 63);
   top = m;
 }
-
-template <typename T> struct Piece;
-template <> struct Piece<float> {
-  static constexpr int N = 4;
-  f32x4_t v;
-  __device__ __forceinline__ float operator[](int i) const { return v[i]; }
-};
-template <> struct Piece<bf16_t> {
-  static constexpr int N = 8;
-  bf16x8_t v;
-  __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
-};
 
 // A row; a thread takes pieces of N consecutive logits, 16 bytes.
 template <typename T, bool ALIGNED>
 struct Row {
-  static constexpr int N = Piece<T>::N;
+  static constexpr int N = 16 / sizeof(T);
   const T* p;
   int vocab;
   __device__ __forceinline__ Row(const SampleArgs& a, int row) : p((const T*)a.logits + (int64_t)row * a.stride), vocab(a.vocab) {}
-  __device__ __forceinline__ void load(int at, float (&x)[N]) const {
-    if (ALIGNED && at + N <= vocab) {
-      Piece<T> q;
-      q.v = *reinterpret_cast<const decltype(q.v)*>(p + at);
+  template <int M>                     // a divisor of N; `at` is divided by it
+  __device__ __forceinline__ void load(int at, float (&x)[M]) const {
+    typedef __attribute__((ext_vector_type(M))) T vec;
+    if (ALIGNED && at + M <= vocab) {
+      const vec v = *reinterpret_cast<const vec*>(p + at);
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = q[i];
+      for (int i = 0; i < M; ++i) x[i] = (float)v[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = at + i < vocab ? to_f32(p[at + i]) : -INFINITY;
+      for (int i = 0; i < M; ++i) x[i] = at + i < vocab ? to_f32(p[at + i]) : -INFINITY;
     }
   }
 };
@@ -179,7 +168,7 @@ __device__ __forceinline__ float tame(float x) { return x == INFINITY ? FLT_MAX 
 
 template <typename T, bool ALIGNED, int PER>           // PER logits a thread
 __global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
-  constexpr int N = Piece<T>::N, PIECES = PER / N;
+  constexpr int N = Row<T, ALIGNED>::N, PIECES = PER / N;
   __shared__ float wave_top[4];
   __shared__ int first_at;
   __shared__ double wave_sum[4];
@@ -260,24 +249,29 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_parts(SampleArgs a) {
 // ---- a workgroup a row -----------------------------------------------------------------------------------------
 
 typedef WaveSums<WAVES> Sums;
-template <typename V>
-__device__ __forceinline__ V total_of(Sums& s, V v) { return before(s, v); }
 
-// The parts of a row: a thread's own, the largest logit of all and its first id.
-struct Joined { Part mine; float top; int at; };
-__device__ __forceinline__ Joined join_parts(const SampleArgs& a, int row, float (&wave_top)[WAVES], int (&wave_at)[WAVES]) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  Joined j;
-  j.mine = tid < a.parts ? a.tops[(int64_t)row * a.parts + tid] : Part{-INFINITY, -1, 0.0};
-  j.top = j.mine.top; j.at = j.mine.at;
-  wave_largest(j.top, j.at);
-  if (lane == 0) { wave_top[wave] = j.top; wave_at[wave] = j.at; }
-  __syncthreads();
-  j.top = lane < WAVES ? wave_top[lane & (WAVES - 1)] : -INFINITY;
-  j.at = lane < WAVES ? wave_at[lane & (WAVES - 1)] : -1;
-  wave_largest(j.top, j.at);
-  return j;
-}
+// The parts of a row.  Every wave looks at all of them, a lane at `each` consecutive ones (as a rule one), so nothing is exchanged between waves: an exchange with its
+// barrier and two rounds of running sums takes half a microsecond, and there were ten of them.
+struct Parts {
+  const Part* p;
+  int n, each, first;
+  Part mine;                           // this lane's first
+  __device__ __forceinline__ Parts(const SampleArgs& a, int row)
+      : p(a.tops + (int64_t)row * a.parts), n(a.parts), each((a.parts + 63) / 64), first((int)(threadIdx.x & 63) * each) {
+    mine = first < n ? p[first] : Part{-INFINITY, -1, 0.0};
+  }
+  template <typename F>
+  __device__ __forceinline__ void all(F f) const {     // of this lane
+    f(first, mine);
+    for (int i = 1; i < each; ++i)
+      if (first + i < n) f(first + i, p[first + i]);
+  }
+  __device__ __forceinline__ void largest(float& top, int& at) const {
+    top = -INFINITY; at = -1;
+    all([&](int, const Part& q) { if (q.top > top) { top = q.top; at = q.at; } });
+    wave_largest(top, at);
+  }
+};
 // a part's weights in units of 2^-shift of the largest logit's
 __device__ __forceinline__ uint64_t part_weight(const Part& p, const Weigher& weight, int shift) {
   return p.at >= 0 ? (uint64_t)__builtin_rint(p.sum * weight.real(p.top, shift)) : 0ull;
@@ -289,23 +283,25 @@ __device__ __forceinline__ uint64_t sum_goal(float top_p, uint64_t sum) {       
 static_assert(BINS == THREADS, "k_sample_edges: a thread a step");
 __global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
   __shared__ Sums s;
-  __shared__ float wave_top[WAVES];
-  __shared__ int wave_at[WAVES];
   __shared__ int found[4];
+  int turn = 0;
   const int tid = threadIdx.x, row = blockIdx.x;
+  const Parts parts(a, row);
   const Limits m = limits(a, row);
   RowState& out = a.state[row];
   if (!draws(m) || !limited(m)) {
     if (tid == 0) out.mode = AS_IT_IS;
     return;
   }
-  const Joined j = join_parts(a, row, wave_top, wave_at);
-  const float per = steps(a, m), base = step_of(j.top, per);
+  float top;
+  int top_at;
+  parts.largest(top, top_at);
+  const float per = steps(a, m), base = step_of(top, per);
   const double octave = (double)(a.shift + 2) / BINS;  // of a step
-  RowState st{COLLECT, 0, -1, 0u, 0, j.top, base};
+  RowState st{COLLECT, 0, -1, 0u, 0, top, base};
   // (largest logits between which the parts' differ by 2^20 steps and more differ by more than 47 powers of two: nothing there counts)
-  if (j.at < 0 || !(fabsf(j.top * per) < FAR_STEPS)) {
-    if (tid == 0) { st.mode = j.at < 0 ? AS_IT_IS : DIVIDE; out = st; }
+  if (top_at < 0 || !(fabsf(top * per) < FAR_STEPS)) {
+    if (tid == 0) { st.mode = top_at < 0 ? AS_IT_IS : DIVIDE; out = st; }
     return;
   }
   if (!m.by_count && !m.by_sum) {      // min-p: what can weigh that much, a step more and the one that the largest is in
@@ -318,7 +314,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
   for (int p0 = 0; p0 < a.parts; p0 += 64) {
     // lane l: by how many steps part p0 + l begins below the row's largest (BINS: by all of them)
     const int p = p0 + (tid & 63);
-    const Part of = p < a.parts ? a.tops[(int64_t)row * a.parts + p] : Part{0.f, -1, 0.0};
+    const Part of = parts.each == 1 ? parts.mine : p < a.parts ? parts.p[p] : Part{0.f, -1, 0.0};
     const float d = of.at < 0 ? (float)BINS : fminf(base - step_of(of.top, per), (float)BINS);
     const int by = (int)d;
     for (int e0 = 0; e0 < min(64, a.parts - p0); e0 += 16) {       // (sixteen parts' on their way at once)
@@ -335,19 +331,21 @@ __global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
   // Sums of weights in units of 2^-40.  A token at place f of a step weighs 1 + k f + (k f)^2 / 2 + up to k^3 / 5 times what one at its lower end does,
   // k = ln 2 octave = 0.032: 6.6e-6 for the last, k / PLACES = 6e-5 for the place, k^2 / PLACES = 2e-6 for its square; the first two taken at their
   // middle, sums are off by 4e-5, by what the step's number is off, and by 1e-6 for the exponential.
-  const double k = 0.6931471805599453 * octave, up = j.top * per - base;
+  const double k = 0.6931471805599453 * octave, up = top * per - base;
   const double middle = (double)n * (1 + 0.5 * k / PLACES) + k / PLACES * ((double)places + 0.5 * k * (double)squares);
   const uint64_t w = (uint64_t)(middle * (double)__builtin_amdgcn_exp2f((float)(40.0 - (tid + up) * octave)));
   unsigned c0 = n;
   uint64_t q0 = w;
-  const unsigned alive = before(s, c0);
-  if (!m.by_count) before(s, q0);
+  const unsigned alive = before(s, turn, c0);
+  if (!m.by_count) before(s, turn, q0);
   if (m.by_count) {                    // (no cut, if fewer weigh anything: the last step)
     const unsigned want = min((unsigned)m.top_k, alive);
     if (c0 < want && want <= c0 + n) found[0] = found[1] = tid;
   } else {
-    const uint64_t goal = sum_goal(m.top_p, total_of(s, part_weight(j.mine, Weigher{(double)j.top, octaves(m)}, a.shift)));
-    const double g = __builtin_ldexp((double)goal, 40 - a.shift), off = 1e-4 + 0.1 * 0x1p-23 * fabsf(j.top * per);
+    uint64_t all = 0;
+    parts.all([&](int, const Part& q) { all += part_weight(q, Weigher{(double)top, octaves(m)}, a.shift); });
+    const uint64_t goal = sum_goal(m.top_p, wave_total(all));
+    const double g = __builtin_ldexp((double)goal, 40 - a.shift), off = 1e-4 + 0.1 * 0x1p-23 * fabsf(top * per);
     const uint64_t reach = max(1ull, (uint64_t)(g * (1 - off))), surely = (uint64_t)(g * (1 + off)) + BINS;
     if (q0 < reach && reach <= q0 + w) found[0] = tid;
     if (q0 < surely && surely <= q0 + w) found[1] = tid;
@@ -372,7 +370,7 @@ __global__ __launch_bounds__(THREADS) void k_sample_edges(SampleArgs a) {
 
 template <typename T, bool ALIGNED, int PER>
 __global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
-  constexpr int N = Piece<T>::N, PIECES = PER / N;
+  constexpr int N = Row<T, ALIGNED>::N, PIECES = PER / N;
   __shared__ unsigned short list[LIST];                // places in the part
   __shared__ double wave_sum[4][2];
   __shared__ unsigned list_n, place;
@@ -436,236 +434,302 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
     }
 }
 
+struct Survey { uint64_t sum; unsigned cnt, lo, hi; };          // of tokens: what they weigh, how many, least and largest key
 struct Shared {
   Sums sums;
+  Survey surveys[2][WAVES];
   uint64_t sub_sum[THREADS];           // a division: a thread a bin
   unsigned sub_cnt[THREADS];
   uint64_t part_sum[MOST_PARTS];       // what is in
   unsigned part_ties[MOST_PARTS];
-  uint64_t list[LIST];
-  float wave_top[WAVES];
-  int wave_at[WAVES];
+  uint64_t few[FEW], few_weight[FEW], ranked[FEW], ranked_weight[FEW];
   // what one thread found
-  uint64_t found_sum, ahead_sum;
-  unsigned found_cnt, found_n, key_lo, key_hi, few_n, few_key, few_ties, ahead_ties;
-  int found_part;
-  float found_top;
+  uint64_t found_sum;
+  unsigned found_cnt, found_n, found_bin, few_n;
 };
 struct Cut {
   unsigned key;                        // what is above it is in
   unsigned ties;                       // and so many of those at it, by id
-  uint64_t sum;                        // of all that is in, min-p aside
 };
 
-template <typename T, bool ALIGNED>
-__global__ __launch_bounds__(THREADS, 8) void k_sample_pick(SampleArgs a) {
+// LIMITS: of some row.  The list's tokens and their weights are in registers, EACH a thread.
+template <typename T, bool ALIGNED, bool LIMITS>
+__global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
   __shared__ Shared s;
-  constexpr int N = Piece<T>::N;
+  constexpr int N = Row<T, ALIGNED>::N, EACH = LIST / THREADS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, vocab = a.vocab, shift = a.shift;
+  int turn = 0, survey_turn = 0;
+  // all that may be wanted is asked for at once
   const Limits lim = limits(a, row);
   const Row<T, ALIGNED> r(a, row);
-  // all that may be wanted is asked for at once
-  const bool narrow = draws(lim) && limited(lim);
+  const Parts parts(a, row);
   const float u = a.u[row];
-  RowState st{AS_IT_IS, 0, -1, 0u, 0, 0.f, 0.f};
+  RowState st{COLLECT, 0, -1, 0u, vocab, 0.f, 0.f};
   PartSums mine{0, 0};
   uint64_t listed_first = 0;
-  if (narrow && one_list(a)) {
-    st.mode = COLLECT;
-    st.list_n = vocab;
-  } else if (narrow) {
+  if (LIMITS && !one_list(a)) {
     st = a.state[row];
     if (tid < a.parts) mine = a.sums[(int64_t)row * a.parts + tid];
     listed_first = a.list[(int64_t)row * LIST + tid];
   }
-  const Joined j = join_parts(a, row, s.wave_top, s.wave_at);
-  if (!draws(lim) || j.at < 0) {       // nothing to choose, or the first of the order
+  float top;
+  int top_at;
+  parts.largest(top, top_at);
+  if (!draws(lim) || top_at < 0) {     // nothing to choose, or the first of the order
     if (tid == 0) {
-      const bool none = !lim.valid || j.at < 0;
-      a.ids[row] = none ? -1 : j.at;
+      const bool none = !lim.valid || top_at < 0;
+      a.ids[row] = none ? -1 : top_at;
       if (a.probs) a.probs[row] = none ? 0.f : 1.f;
     }
     return;
   }
-  const Weigher weight{(double)j.top, octaves(lim)};
+  const bool narrow = LIMITS && limited(lim);
+  const Weigher weight{(double)top, octaves(lim)};
   const double uu = u > 0.f ? (double)fminf(u, 0.99999994f) : 0.0;
   const uint64_t least = lim.by_part ? max(1ull, (uint64_t)__builtin_rint(__builtin_ldexp((double)fminf(lim.min_p, 1.f), shift))) : 1ull;
-  Cut cut{0u, 0u, 0ull};               // all is in
-  uint64_t own = part_weight(j.mine, weight, shift);             // this thread's part: what is in
+  Cut cut{0u, 0u};                     // all is in
+  uint64_t own = 0;                    // of this lane's parts: what is in
   unsigned own_ties = 0;
 
   if (narrow) {
     const bool listed = st.mode == COLLECT;
     const unsigned listed_n = listed ? min((unsigned)st.list_n, (unsigned)LIST) : 0u;
     const bool from_top = listed && st.first == 0;
-    if (!listed) mine = {0, 0};
-    const uint64_t all = lim.by_sum ? total_of(s.sums, own) : 0ull;            // of all tokens (top-p without top-k)
-    const uint64_t q0 = from_top ? 0ull : total_of(s.sums, mine.all);          // of those before the list
-    own = mine.in;
-    // f(key, id) for the listed tokens, or all of the row
-    auto tokens = [&](auto f) {
+    unsigned key[EACH];
+    int id[EACH];
+    uint64_t q_of[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const unsigned i = tid + e * THREADS;
+      key[e] = 0; id[e] = 0; q_of[e] = 0;
+      if (i < listed_n) {
+        if (one_list(a)) {
+          key[e] = key_of(tame(to_f32(r.p[i])));
+          id[e] = (int)i;
+        } else {
+          const uint64_t l = e == 0 ? listed_first : a.list[(int64_t)row * LIST + i];
+          key[e] = (unsigned)(l >> 32);
+          id[e] = (int)~(unsigned)l;
+        }
+        q_of[e] = weight.whole(of_key(key[e]), shift);
+      }
+    }
+    // f(key, id, weight) for the listed tokens, or all of the row, that weigh anything and whose key passes
+    auto tokens = [&](auto pass, auto f) {
       if (listed) {
-#pragma unroll 1
-        for (unsigned i = tid; i < listed_n; i += THREADS) f((unsigned)(s.list[i] >> 32), (int)~(unsigned)s.list[i]);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+          if (q_of[e] && pass(key[e])) f(key[e], id[e], q_of[e]);
       } else {
 #pragma unroll 1
         for (int at = tid * N; at < vocab; at += THREADS * N) {
           float x[N];
           r.load(at, x);
 #pragma unroll
-          for (int i = 0; i < N; ++i)
-            if (x[i] > -INFINITY) f(key_of(tame(x[i])), at + i);
+          for (int i = 0; i < N; ++i) {
+            const unsigned k = key_of(tame(x[i]));
+            const uint64_t q = x[i] > -INFINITY && pass(k) ? weight.whole(of_key(k), shift) : 0ull;
+            if (q) f(k, at + i, q);
+          }
         }
       }
     };
-    if (tid == 0) { s.key_lo = ~0u; s.key_hi = 0u; }
-    s.part_sum[tid] = own;
+    auto survey = [&](auto pass) {
+      Survey v{0, 0u, ~0u, 0u};
+      tokens(pass, [&](unsigned k, int, uint64_t q) { v.sum += q; ++v.cnt; v.lo = min(v.lo, k); v.hi = max(v.hi, k); });
+      v = {wave_total(v.sum), wave_total(v.cnt), lane_of(running(v.lo, ~0u, Least()), 63), lane_of(running(v.hi, 0u, Most()), 63)};
+      survey_turn ^= 1;
+      if (lane == 0) s.surveys[survey_turn][wave] = v;
+      __syncthreads();
+      v = s.surveys[survey_turn][lane & (WAVES - 1)];
+      constexpr int LAST = WAVES - 1;
+      return Survey{lane_of(running_row(v.sum, 0u, Plus()), LAST), lane_of(running_row(v.cnt, 0u, Plus()), LAST),
+                    lane_of(running_row(v.lo, ~0u, Least()), LAST), lane_of(running_row(v.hi, 0u, Most()), LAST)};
+    };
+    if (tid == 0) s.few_n = 0;
+    s.part_sum[tid] = listed ? mine.in : 0ull;
     s.part_ties[tid] = 0;
+    const uint64_t q0 = from_top || !listed ? 0ull : before(s.sums, turn, mine.all);         // of those before the list
+    const unsigned c0 = listed && !from_top ? st.before : 0u;
+    Survey left = survey([](unsigned) { return true; });       // (its barrier: all of the above is there)
+    const uint64_t all_in = q0 + left.sum;
+    // Among the tokens of `left`, c0 and q0 before them: the cut after `count` tokens (by_sum: before the first one with `goal` or more before it).
+    auto find = [&](const bool by_sum, unsigned count, uint64_t goal) {
+      unsigned n = left.cnt, c = c0, k_lo = left.lo, k_hi = left.hi, bin = 0;
+      uint64_t q = q0;
+      // Equal steps of the logits first, as what is listed is spread over them.  Then, where more than a few lie in one of them, the keys' bits, ten at a time.
+      bool equal_steps = true, in_step = false;
+      const float hi = of_key(k_hi), per = ((float)THREADS - 0.1f) / (hi - of_key(k_lo));
+      auto step = [&](unsigned k) { return min((unsigned)((hi - of_key(k)) * per), (unsigned)THREADS - 1u); };
 #pragma unroll 1
-    for (unsigned i = tid; i < listed_n; i += THREADS) {
-      if (one_list(a)) s.list[i] = (uint64_t)key_of(tame(to_f32(r.p[i]))) << 32 | (unsigned)~i;            // (what is no number weighs nothing)
-      else s.list[i] = i < THREADS ? listed_first : a.list[(int64_t)row * LIST + i];
-    }
-    __syncthreads();
-    unsigned k_min = ~0u, k_max = 0u, here = 0;
-    uint64_t weights = 0;
-    tokens([&](unsigned k, int) {
-      const uint64_t q = weight.whole(of_key(k), shift);
-      if (q) { k_min = min(k_min, k); k_max = max(k_max, k); ++here; weights += q; }
-    });
-    // (an atomic of a wave's lanes on one word is a loop over them)
-    k_min = lane_of(running(k_min, ~0u, [](unsigned x, unsigned y) { return min(x, y); }), 63);
-    k_max = lane_of(running(k_max, 0u, [](unsigned x, unsigned y) { return max(x, y); }), 63);
-    if (lane == 0 && k_max) { atomicMin(&s.key_lo, k_min); atomicMax(&s.key_hi, k_max); }
-    const unsigned list_cnt = total_of(s.sums, here);
-    const uint64_t list_sum = total_of(s.sums, weights);
-    const unsigned list_lo = s.key_lo, list_hi = s.key_hi, ahead_cnt = listed && !from_top ? st.before : 0u;
-    cut.sum = lim.by_count || !listed ? q0 + list_sum : all;
-#pragma unroll 1
-    for (int stage = 0; stage < 2; ++stage) {          // by count, by sum
-      unsigned count = ~0u, n = list_cnt, c0 = ahead_cnt, k_lo = list_lo, k_hi = list_hi;
-      uint64_t goal = ~0ull, q = q0;
-      if (stage == 0) {
-        if (!lim.by_count || (unsigned)lim.top_k > ahead_cnt + list_cnt) continue;        // (no more than that weigh anything)
-        count = (unsigned)lim.top_k;
-      } else {
-        if (!lim.by_sum) break;
-        goal = min(sum_goal(lim.top_p, cut.sum), q0 + list_sum);       // (tokens of less than half a unit count in the parts' sums: nothing behind the list)
-      }
-      // The cut among n tokens with keys between the two, after `count` tokens, or before the first one with `goal` or more before it.  c0, q: tokens
-      // and weights before them.
-#pragma unroll 1
-      for (int level = 0; level < 6; ++level) {        // (32 bits, ten at a time, and the last look)
+      for (int level = 0; level < 8; ++level) {
         if (k_lo == k_hi) {            // equal ones: as many as there is room for
           const uint64_t w = max(1ull, weight.whole(of_key(k_lo), shift));
-          uint64_t m = min((uint64_t)n, (uint64_t)(count - c0));
-          m = min(m, (goal - q - 1) / w + 1);
-          cut = {k_lo, (unsigned)m, q + m * w};
-          break;
+          cut = {k_lo, (unsigned)(by_sum ? min((uint64_t)n, (goal - q - 1) / w + 1) : (uint64_t)min(n, count - c))};
+          return;
         }
-        __syncthreads();
-        if (n <= FEW) {                // (their places in sub_sum)
-          if (tid == 0) s.few_n = 0;
-          if (tid < FEW) { s.sub_cnt[tid] = 0; s.sub_sum[FEW + tid] = 0; }
-          __syncthreads();
-          tokens([&](unsigned k, int id) {
-            if (k >= k_lo && k <= k_hi && weight.whole(of_key(k), shift)) s.sub_sum[atomicAdd(&s.few_n, 1u) & (FEW - 1)] = (uint64_t)k << 32 | (unsigned)~id;
+        auto pass = [&](unsigned k) { return k >= k_lo && k <= k_hi && (!in_step || step(k) == bin); };
+        if (n <= FEW) {                // each one's rank by comparing it with all
+          tokens(pass, [&](unsigned k, int i, uint64_t w) {
+            const unsigned at = atomicAdd(&s.few_n, 1u) & (FEW - 1);
+            s.few[at] = (uint64_t)k << 32 | (unsigned)~i;
+            s.few_weight[at] = w;
           });
           __syncthreads();
-          // A lane has a token, a wave compares all with four of them: how many come before it, and what they weigh
-          const uint64_t token = lane < (int)n ? s.sub_sum[lane] : 0ull;
-          const unsigned k = (unsigned)(token >> 32);
-          const uint64_t w = lane < (int)n ? weight.whole(of_key(k), shift) : 0ull;
-          unsigned rank = 0;
-          uint64_t ahead = 0;
+          if (tid == 0) s.few_n = 0;
+          const uint64_t token = lane < (int)n ? s.few[lane] : 0ull;
 #pragma unroll
           for (int e = 0; e < FEW / WAVES; ++e) {
             const int i = __builtin_amdgcn_readfirstlane(wave) * (FEW / WAVES) + e;
-            if (lane_of(token, i) > token) { ++rank; ahead += lane_of(w, i); }
-          }
-          if (lane < (int)n && rank) { atomicAdd(&s.sub_cnt[lane], rank); atomicAdd((unsigned long long*)&s.sub_sum[FEW + lane], (unsigned long long)ahead); }
-          __syncthreads();
-          if (wave == 0) {
-            rank = s.sub_cnt[lane]; ahead = s.sub_sum[FEW + lane];
-            const bool in = lane < (int)n && c0 + rank < count && q + ahead < goal;
-            const int last = __popcll(__builtin_amdgcn_ballot_w64(in)) - 1;      // (what is in is a prefix of the ranking)
-            if (in && (int)rank == last) { s.few_key = k; s.found_sum = q + ahead + w; }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            const int ties = __popcll(__builtin_amdgcn_ballot_w64(in && k == s.few_key));
-            if (lane == 0) s.few_ties = ties;
+            const int rank = __popcll(__builtin_amdgcn_ballot_w64(token > lane_of(token, i)));
+            if (lane == i && i < (int)n) { s.ranked[rank] = token; s.ranked_weight[rank] = s.few_weight[i]; }
           }
           __syncthreads();
-          cut = {s.few_key, s.few_ties, s.found_sum};
-          break;
+          const unsigned k = lane < (int)n ? (unsigned)(s.ranked[lane] >> 32) : 0u;
+          bool in = lane < (int)n;
+          if (by_sum) {
+            const uint64_t w = in ? s.ranked_weight[lane] : 0ull;
+            in = in && q + running_sum(w) - w < goal;
+          } else {
+            in = in && c + lane < count;
+          }
+          const unsigned last = lane_of(k, max(__popcll(__builtin_amdgcn_ballot_w64(in)) - 1, 0));          // (what is in is a prefix of the ranking)
+          cut = {last, (unsigned)__popcll(__builtin_amdgcn_ballot_w64(in && k == last))};
+          return;
         }
-        const int bits = 32 - __clz(k_hi - k_lo), by = max(0, bits - 10);        // THREADS = 2^10 bins
-        s.sub_cnt[tid] = 0; s.sub_sum[tid] = 0;
+        if (in_step) {                 // more than a few in one step: their keys
+          left = survey(pass);
+          k_lo = left.lo; k_hi = left.hi;
+          in_step = false;
+          continue;
+        }
+        const int by = max(0, 32 - __clz(k_hi - k_lo) - 10);   // THREADS = 2^10 bins
+        s.sub_cnt[tid] = 0;
+        if (by_sum) s.sub_sum[tid] = 0;
         __syncthreads();
-        tokens([&](unsigned k, int) {
-          const uint64_t w = k >= k_lo && k <= k_hi ? weight.whole(of_key(k), shift) : 0ull;
-          if (w) {
-            const unsigned b = (k_hi - k) >> by;
-            atomicAdd(&s.sub_cnt[b], 1u);
-            atomicAdd((unsigned long long*)&s.sub_sum[b], (unsigned long long)w);
-          }
+        tokens(pass, [&](unsigned k, int, uint64_t w) {
+          const unsigned b = equal_steps ? step(k) : (k_hi - k) >> by;
+          atomicAdd(&s.sub_cnt[b], 1u);
+          if (by_sum) atomicAdd((unsigned long long*)&s.sub_sum[b], (unsigned long long)w);
         });
         __syncthreads();
         const unsigned m = s.sub_cnt[tid];
-        const uint64_t w = s.sub_sum[tid];
-        unsigned c1 = m;
-        uint64_t q1 = w;
-        before(s.sums, c1);
-        before(s.sums, q1);
-        c1 += c0; q1 += q;
-        if (m && c1 < count && q1 < goal && (c1 + m >= count || q1 + w >= goal)) {
-          s.found_cnt = c1; s.found_sum = q1; s.found_n = m;
-          s.key_hi = k_hi - ((unsigned)tid << by);
-          const uint64_t down = ((uint64_t)tid + 1) << by;
-          s.key_lo = down - 1 >= (uint64_t)(k_hi - k_lo) ? k_lo : k_hi - (unsigned)(down - 1);
+        if (by_sum) {
+          const uint64_t w = s.sub_sum[tid];
+          uint64_t ahead = w;
+          before(s.sums, turn, ahead);
+          ahead += q;
+          if (m && ahead < goal && goal <= ahead + w) { s.found_sum = ahead; s.found_n = m; s.found_bin = tid; }
+        } else {
+          unsigned ahead = m;
+          before(s.sums, turn, ahead);
+          ahead += c;
+          if (m && ahead < count && count <= ahead + m) { s.found_cnt = ahead; s.found_n = m; s.found_bin = tid; }
         }
         __syncthreads();
-        k_lo = s.key_lo; k_hi = s.key_hi; n = s.found_n; c0 = s.found_cnt; q = s.found_sum;
+        bin = s.found_bin; n = s.found_n;
+        if (by_sum) q = s.found_sum;
+        else c = s.found_cnt;
+        if (equal_steps) {
+          equal_steps = false;
+          in_step = true;
+        } else {
+          const uint64_t down = ((uint64_t)bin + 1) << by;
+          const unsigned below = down - 1 >= (uint64_t)(k_hi - k_lo) ? k_lo : k_hi - (unsigned)(down - 1);
+          k_hi -= bin << by;
+          k_lo = below;
+        }
+      }
+    };
+    uint64_t to_cut = all_in;          // what is in by count
+    if (lim.by_count && (unsigned)lim.top_k <= c0 + left.cnt) {        // (otherwise no more than that weigh anything)
+      find(false, (unsigned)lim.top_k, 0);
+      if (lim.by_sum) {                // (all that weighs anything is in the list)
+        const unsigned in = cut.key;
+        left = survey([&](unsigned k) { return k >= in; });
+        to_cut = left.sum - (left.cnt - (unsigned)lim.top_k) * weight.whole(of_key(in), shift);
       }
     }
+    if (lim.by_sum) {
+      uint64_t of = to_cut;
+      if (!lim.by_count && listed) {   // of all tokens, by the parts' sums
+        of = 0;
+        parts.all([&](int, const Part& p) { of += part_weight(p, weight, shift); });
+        of = wave_total(of);
+      }
+      // (tokens of less than half a unit count in the parts' sums: nothing behind the list)
+      find(true, ~0u, min(sum_goal(lim.top_p, of), to_cut));
+    }
     // what of the list is in, by parts
-    __syncthreads();
-    tokens([&](unsigned k, int id) {
-      const uint64_t q = k >= cut.key ? weight.whole(of_key(k), shift) : 0ull;
-      if (q >= least) {
-        if (k > cut.key) atomicAdd((unsigned long long*)&s.part_sum[id / a.part], (unsigned long long)q);
-        else atomicAdd(&s.part_ties[id / a.part], 1u);
+    const int log2_part = 31 - __clz(a.part);
+    uint64_t in = 0;
+    unsigned ties = 0;
+    tokens([&](unsigned k) { return k >= cut.key; }, [&](unsigned k, int i, uint64_t q) {
+      if (q < least) return;
+      if (a.parts == 1) {
+        if (k > cut.key) in += q;
+        else ++ties;
+      } else if (k > cut.key) {
+        atomicAdd((unsigned long long*)&s.part_sum[i >> log2_part], (unsigned long long)q);
+      } else {
+        atomicAdd(&s.part_ties[i >> log2_part], 1u);
       }
     });
+    if (a.parts == 1) {                // (all atomics would meet in one place)
+      in = wave_total(in);
+      ties = wave_total(ties);
+      if (lane == 0 && in) atomicAdd((unsigned long long*)&s.part_sum[0], (unsigned long long)in);
+      if (lane == 0 && ties) atomicAdd(&s.part_ties[0], ties);
+    }
     __syncthreads();
-    own = s.part_sum[tid];
-    own_ties = s.part_ties[tid];
   }
 
   // the part in which the target lies; of tokens at the cut's logit the first by id are in
   const uint64_t tie_q = cut.key ? weight.whole(of_key(cut.key), shift) : 0ull;
-  unsigned ties_ahead = own_ties;
-  if (cut.key) before(s.sums, ties_ahead);
-  own += tie_q * min(own_ties, cut.ties - min(ties_ahead, cut.ties));
-  uint64_t ahead = own;
-  const uint64_t total = before(s.sums, ahead), target = min((uint64_t)(uu * (double)total), total - 1);
-  if (target >= ahead && target < ahead + own) {
-    s.found_part = tid; s.found_sum = own; s.ahead_sum = ahead; s.ahead_ties = ties_ahead;
-    s.found_top = j.mine.top;
-  }
-  __syncthreads();
-  // A run of its logits for every thread.  Without limits weights are taken against the part's largest, as its sum was.
-  const Weigher local{narrow ? (double)j.top : (double)s.found_top, weight.scale};
-  constexpr int RUN = 8;               // (a part has up to THREADS times as many)
-  const int from = s.found_part * a.part + tid * RUN, to = min(min(from + RUN, (s.found_part + 1) * a.part), vocab);
-  float x[RUN];
-  if (from < to) {
-#pragma unroll
-    for (int i = 0; i < RUN; i += N) {
-      float v[N];
-      r.load(min(from + i, vocab), v);
-#pragma unroll
-      for (int e = 0; e < N; ++e) x[i + e] = v[e];
+  auto of_part = [&](int p, const Part& part, unsigned& ties) {        // ties aside
+    ties = narrow && p < a.parts ? s.part_ties[p] : 0u;
+    return narrow ? (p < a.parts ? s.part_sum[p] : 0ull) : part_weight(part, weight, shift);
+  };
+  parts.all([&](int p, const Part& part) {
+    unsigned ties;
+    own += of_part(p, part, ties);
+    own_ties += ties;
+  });
+  auto taken = [&](unsigned ties, unsigned ahead) { return tie_q * min(ties, cut.ties - min(ahead, cut.ties)); };
+  unsigned ties_ahead = running_sum(own_ties) - own_ties;
+  own += taken(own_ties, ties_ahead);
+  uint64_t ahead = running_sum(own);
+  const uint64_t total = lane_of(ahead, 63), target = min((uint64_t)(uu * (double)total), total - 1);
+  ahead -= own;
+  const int at_lane = max(__ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(target >= ahead && target < ahead + own)) - 1, 0);
+  int part = at_lane * parts.each;
+  float part_top = __uint_as_float(lane_of(__float_as_uint(parts.mine.top), at_lane));
+  uint64_t part_in = lane_of(own, at_lane), part_ahead = lane_of(ahead, at_lane);
+  unsigned part_ties = lane_of(ties_ahead, at_lane);
+  if (parts.each > 1) {                // which one of the lane's
+#pragma unroll 1
+    for (;; ++part) {
+      const Part p = part < a.parts ? parts.p[part] : Part{-INFINITY, -1, 0.0};
+      unsigned ties;
+      part_in = of_part(part, p, ties);
+      part_in += taken(ties, part_ties);
+      part_top = p.top;
+      if (target < part_ahead + part_in || part + 1 >= a.parts) break;
+      part_ahead += part_in;
+      part_ties += ties;
     }
+  }
+  // A run of its logits for every thread.  Without limits weights are taken against the part's largest, as its sum was.
+  const Weigher local{narrow ? (double)top : (double)part_top, weight.scale};
+  constexpr int RUN = 8, HALF = 4;     // (a part has 4 or 8 times THREADS)
+  const int run = a.part / THREADS, from = part * a.part + tid * run, to = min(min(from + run, (part + 1) * a.part), vocab);
+  float x[RUN];
+#pragma unroll
+  for (int i = 0; i < RUN; i += HALF) {
+    float v[HALF];
+    r.load(i < run ? min(from + i, vocab) : vocab, v);
+#pragma unroll
+    for (int e = 0; e < HALF; ++e) x[i + e] = v[e];
   }
   // the weight of what is in for certain, and whether it is one of the equal ones at the cut
   auto take = [&](float v, int i, bool& tie) {
@@ -675,38 +739,39 @@ __global__ __launch_bounds__(THREADS, 8) void k_sample_pick(SampleArgs a) {
     tie = q >= least && k == cut.key;
     return q >= least && k > cut.key ? q : 0ull;
   };
-  uint64_t sum = 0;
-  unsigned ties = 0;
+  uint64_t sum = 0, q_of[RUN];
+  unsigned ties = 0, tie_at = 0;
 #pragma unroll
   for (int i = 0; i < RUN; ++i) {
     bool tie;
-    sum += take(x[i], i, tie);
+    sum += q_of[i] = take(x[i], i, tie);
     ties += tie;
+    tie_at |= (unsigned)tie << i;
   }
   const uint64_t own_sum = sum;
   const unsigned own_count = ties;
-  uint64_t of_part = before(s.sums, sum);              // of the threads before
-  const unsigned all_c = cut.key ? before(s.sums, ties) : 0u;
-  const unsigned left0 = cut.ties - min(s.ahead_ties, cut.ties), left = cut.ties - min(s.ahead_ties + ties, cut.ties);
+  unsigned all_ties = 0;
+  uint64_t in_part = before(s.sums, turn, sum, ties);  // of the threads before
+  all_ties = lane_of(running_row(s.sums.cnt[turn][lane & (WAVES - 1)], 0u, Plus()), WAVES - 1);
+  const unsigned left0 = cut.ties - min(part_ties, cut.ties), left = cut.ties - min(part_ties + ties, cut.ties);
   // The part's sum was of weights before they were rounded, or against its own largest: the target in the units of this one.
-  of_part += tie_q * min(all_c, left0);
-  if (of_part == 0) {                  // (a part of nothing but less than half units: the largest stands for it)
+  in_part += tie_q * min(all_ties, left0);
+  if (in_part == 0) {                  // (a part of nothing but less than half units: the largest stands for it)
     if (tid == 0) {
-      a.ids[row] = j.at;
+      a.ids[row] = top_at;
       if (a.probs) a.probs[row] = (float)(__builtin_ldexp(1.0, shift) / (double)total);
     }
     return;
   }
-  const uint64_t goal = min((uint64_t)((double)(target - s.ahead_sum) / (double)s.found_sum * (double)of_part), of_part - 1);
-  const double share = (double)s.found_sum / (double)of_part / (double)total;
+  const uint64_t goal = min((uint64_t)((double)(target - part_ahead) / (double)part_in * (double)in_part), in_part - 1);
+  const double share = (double)part_in / (double)in_part / (double)total;
   uint64_t at_q = sum + tie_q * (left0 - left);
   if (goal >= at_q && goal < at_q + own_sum + tie_q * min(own_count, left)) {
     unsigned more = left;
 #pragma unroll
     for (int i = 0; i < RUN; ++i) {
-      bool tie;
-      uint64_t q = take(x[i], i, tie);
-      if (tie && more) { q = tie_q; --more; }
+      uint64_t q = q_of[i];
+      if (tie_at >> i & 1u && more) { q = tie_q; --more; }
       if (goal >= at_q && goal < at_q + q) {
         a.ids[row] = from + i;
         if (a.probs) a.probs[row] = (float)((double)q * share);
@@ -753,7 +818,8 @@ hipError_t launch(hipStream_t st, const SampleArgs& a, int rows) {
     else hipLaunchKernelGGL((k_sample_collect<T, ALIGNED, 16>), grid, wg, 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_sample_pick<T, ALIGNED>), dim3(rows), dim3(THREADS), 0, st, a);
+  if (a.top_k || a.top_p || a.min_p) hipLaunchKernelGGL((k_sample_pick<T, ALIGNED, true>), dim3(rows), dim3(THREADS), 0, st, a);
+  else hipLaunchKernelGGL((k_sample_pick<T, ALIGNED, false>), dim3(rows), dim3(THREADS), 0, st, a);
   return hipGetLastError();
 }
 
