@@ -92,9 +92,10 @@ __device__ __forceinline__ float2 finish(float2 a) { return {a.x, a.y == 0.f ? 0
 
 // ---- few columns ---------------------------------------------------------------------------------------------
 
-// scores [seq][kvh][t][width] of columns below `width`; stats [seq][kvh][share][width]
+// scores [seq][kvh][t][width] of columns below `width`; stats [seq][kvh][share][width].  K's bytes are what bounds it.  (bf16 with up to eight columns: 128 registers
+// and four waves a SIMD instead of 132 and three, 123 us instead of 128 for 32 ragged sequences)
 template <typename T, int HD, int NV>      // NV: groups of eight columns
-__global__ __launch_bounds__(THREADS) void k_weigh_scores(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && NV == 1 ? 4 : 1) void k_weigh_scores(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
   typedef typename AttnFrag<T>::type F;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int share = blockIdx.x, kvh = blockIdx.y, seq = blockIdx.z;
@@ -541,7 +542,9 @@ WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_ro
   const int units = (int)(p.tokens / 32);
   if (cols <= 32) {
     p.width = cols <= 4 ? 4 : cols <= 8 ? 8 : cols <= 16 ? 16 : 32;
-    const int64_t most = std::max<int64_t>(1, 8192 / heads);                     // shares of a sequence and kv head
+    // Shares of a sequence and kv head: small ones, as sequences differ in length (32 of 1000 to 16384, 256 heads together: 152 us with 2048 in all, 145 with 4096,
+    // 127 with 8192, 123 with 16384, 132 with 32768), of a unit a wave at least.
+    const int64_t most = std::max<int64_t>(1, 16384 / heads);
     p.share_units = (int)std::max<int64_t>(4, (units + most - 1) / most);
     p.shares = (units + p.share_units - 1) / p.share_units;
     p.stats_floats = 2 * heads * p.shares * p.width;
