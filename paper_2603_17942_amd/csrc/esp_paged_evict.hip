@@ -6,6 +6,10 @@
 // ones go and how many of those at the cut are in.  Integers alone: the same list every time.
 // k_evict_move: the list's tokens go to slots 0, 1, ...; a token never moves back, so a plane's blocks of 32 new slots are filled one after the other and what
 // is still to be read lies behind what is written, also where old and new pages are the same.
+//
+// The move is bound by memory: a token's K lies in 16-byte pieces (32 tokens of eight features side by side) and its V in single elements, so where half of
+// a block stays all of its lines are read.  4096 to 2048 tokens of 32 layers and 8 kv heads, bf16, 128: 540 MB read and 268 written in 172 us, 4.7 TB/s (a copy:
+// 5.1); 16 ragged sequences 1094 and 534 in 336.  Choosing is a chain of some 20 barriers, 20 to 26 us.
 #include "esp_paged.h"
 #include "esp_scan.h"
 

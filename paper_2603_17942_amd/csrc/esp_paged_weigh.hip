@@ -4,8 +4,13 @@
 // A token's sum needs every row's largest score and sum of exponentials first, so there are two looks at the scores.  Few columns (row, query
 // head of the kv head: up to 32, a decode step's): K is what has to be read, once; the scores, 4 bytes each, go to scratch with the share's
 // statistics, and a second kernel adds up their exponentials, a thread a token.  Many columns (a prompt's): the products are what costs, and are
-// taken twice.  First a wave has 32 columns and goes over the keys, for the statistics; then a wave has 32 or 64 keys and goes over the columns,
-// whose tiles four waves share through LDS, so that a token's sum stays in a lane and nothing is added by atomics: the same bits every time.
+// taken twice.  First a wave has 32 columns (bf16: 64) and goes over the keys, for the statistics; then a wave has 32 keys (bf16: 64) and goes over the
+// columns, whose tiles four waves share through LDS, so that a token's sum stays in a lane and nothing is added by atomics: the same bits every time.
+//
+// What bounds them, at 32 query and 8 kv heads of 128 in bf16: 32 ragged sequences' single rows read 522 MB of K, 101 us at the rate of a copy, and take
+// 123 (scores 109, sums 14).  A prompt of 4096 takes its 137 GF of products in twice 120 to 130 us, 55% of the rate of a large product: matrix
+// instructions for 25% of the time, the exponentials' vector instructions for 40%, and with 217 and 164 registers too few waves (1.1 and 1.7 a SIMD) for one
+// to hide behind the other.
 //
 // Scores are S = Q K^T on 32 x 32 matrix instructions.  With keys as the second operand a lane has one key and the columns
 // 8 (v / 4) + 4 half + v % 4 in its 16 registers; with keys first (the statistics of many columns) one column and those keys.
@@ -218,7 +223,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_weigh_stats(PagedDev kv, ChunkDe
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   // Late columns have the most to do and come first.  Workgroups go to the XCDs in turn, and early columns have no last shares: column groups lie next to
   // each other, shares far apart (eight shares next to each other: 204 us for a prompt of 4096, half of the XCDs idle most of the time; so 158), and
-  // groups are turned by one from head to head.
+  // groups are turned by one from head to head.  (With units' scores among exponentials, below: 120.)
   const int block = gridDim.x - 1 - blockIdx.x, groups = gridDim.x / p.shares, kvh = blockIdx.y, seq = blockIdx.z;
   const int share = block / groups, tile = ((block + kvh) % groups * WAVES + wave) * CT;
   const WeighSeq c = weigh_seq(kv, ch, seq, a.last, a.slots);
@@ -351,7 +356,8 @@ __global__ __launch_bounds__(THREADS) void k_weigh_join(PagedDev kv, ChunkDev ch
   *s = finish(r);
 }
 
-// KU units of 32 keys a wave.  Column tiles go through two places in LDS: the next one is on its way while this one is used.
+// KU units of 32 keys a wave.  Column tiles go through two places in LDS: the next one is on its way while this one is used.  (Three places, and the next tile's
+// scores among this one's exponentials as in the statistics: 236 registers and a wave a SIMD less, 268 us for a prompt of 4096 instead of 240.)
 template <typename T, int HD, int KU>
 __global__ __launch_bounds__(THREADS, 2) void k_weigh_add(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
   typedef typename AttnFrag<T>::type F;
@@ -556,7 +562,7 @@ WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_ro
   const int of_group = WAVES * stat_tiles(dtype == ESP_BF16);
   const int64_t groups = ((cols + 31) / 32 + of_group - 1) / of_group * heads;
   // About 2048 workgroups for the statistics, of 16 units at least where there are many; four shares at most where there are few, which the sums then
-  // join themselves.
+  // join themselves.  The sums: up to 2048 also.  (A prompt of 4096: 250 us, with 4096 of the first 260, with 1024 or 4096 of the second 252.)
   const int64_t most = std::max<int64_t>(1, 2048 / groups);
   if (most <= 4 || units <= 64) p.share_units = (int)std::max<int64_t>(2, (units + std::min<int64_t>(4, most) - 1) / std::min<int64_t>(4, most));
   else p.share_units = (int)std::max<int64_t>(16, (units + most - 1) / most);
