@@ -8,7 +8,7 @@
 // columns, whose tiles four waves share through LDS, so that a token's sum stays in a lane and nothing is added by atomics: the same bits every time.
 //
 // What bounds them, at 32 query and 8 kv heads of 128 in bf16: 32 ragged sequences' single rows read 522 MB of K, 101 us at the rate of a copy, and take
-// 123 (scores 109, sums 14).  A prompt of 4096 takes its 137 GF of products in twice 120 to 130 us, 55% of the rate of a large product: matrix
+// 123 (scores 109, sums 14).  A prompt of 4096 takes its 137 GF of products in twice 120 to 130 us, 45% of the rate of a large product: matrix
 // instructions for 25% of the time, the exponentials' vector instructions for 40%, and with 217 and 164 registers too few waves (1.1 and 1.7 a SIMD) for one
 // to hide behind the other.
 //

@@ -440,10 +440,10 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
     }
 }
 
-struct Survey { uint64_t sum; unsigned cnt, lo, hi; };          // of tokens: what they weigh, how many, least and largest key
+struct Tally { uint64_t sum; unsigned cnt, lo, hi; };          // of tokens: what they weigh, how many, least and largest key
 struct Shared {
   Sums sums;
-  Survey surveys[2][WAVES];
+  Tally tallies[2][WAVES];
   uint64_t sub_sum[THREADS];           // a division: a thread a bin
   unsigned sub_cnt[THREADS];
   uint64_t part_sum[MOST_PARTS];       // what is in
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
   __shared__ Shared s;
   constexpr int N = Row<T, ALIGNED>::N, EACH = LIST / THREADS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, vocab = a.vocab, shift = a.shift;
-  int turn = 0, survey_turn = 0;
+  int turn = 0, tally_turn = 0;
   // all that may be wanted is asked for at once
   const Limits lim = limits(a, row);
   const Row<T, ALIGNED> r(a, row);
@@ -540,16 +540,16 @@ __global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
         }
       }
     };
-    auto survey = [&](auto pass) {
-      Survey v{0, 0u, ~0u, 0u};
+    auto tally = [&](auto pass) {
+      Tally v{0, 0u, ~0u, 0u};
       tokens(pass, [&](unsigned k, int, uint64_t q) { v.sum += q; ++v.cnt; v.lo = min(v.lo, k); v.hi = max(v.hi, k); });
       v = {wave_total(v.sum), wave_total(v.cnt), lane_of(running(v.lo, ~0u, Least()), 63), lane_of(running(v.hi, 0u, Most()), 63)};
-      survey_turn ^= 1;
-      if (lane == 0) s.surveys[survey_turn][wave] = v;
+      tally_turn ^= 1;
+      if (lane == 0) s.tallies[tally_turn][wave] = v;
       __syncthreads();
-      v = s.surveys[survey_turn][lane & (WAVES - 1)];
+      v = s.tallies[tally_turn][lane & (WAVES - 1)];
       constexpr int LAST = WAVES - 1;
-      return Survey{lane_of(running_row(v.sum, 0u, Plus()), LAST), lane_of(running_row(v.cnt, 0u, Plus()), LAST),
+      return Tally{lane_of(running_row(v.sum, 0u, Plus()), LAST), lane_of(running_row(v.cnt, 0u, Plus()), LAST),
                     lane_of(running_row(v.lo, ~0u, Least()), LAST), lane_of(running_row(v.hi, 0u, Most()), LAST)};
     };
     if (tid == 0) s.few_n = 0;
@@ -557,7 +557,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
     s.part_ties[tid] = 0;
     const uint64_t q0 = from_top || !listed ? 0ull : before(s.sums, turn, mine.all);         // of those before the list
     const unsigned c0 = listed && !from_top ? st.before : 0u;
-    Survey left = survey([](unsigned) { return true; });       // (its barrier: all of the above is there)
+    Tally left = tally([](unsigned) { return true; });       // (its barrier: all of the above is there)
     const uint64_t all_in = q0 + left.sum;
     // Among the tokens of `left`, c0 and q0 before them: the cut after `count` tokens (by_sum: before the first one with `goal` or more before it).
     auto find = [&](const bool by_sum, unsigned count, uint64_t goal) {
@@ -604,7 +604,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
           return;
         }
         if (in_step) {                 // more than a few in one step: their keys
-          left = survey(pass);
+          left = tally(pass);
           k_lo = left.lo; k_hi = left.hi;
           in_step = false;
           continue;
@@ -652,7 +652,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
       find(false, (unsigned)lim.top_k, 0);
       if (lim.by_sum) {                // (all that weighs anything is in the list)
         const unsigned in = cut.key;
-        left = survey([&](unsigned k) { return k >= in; });
+        left = tally([&](unsigned k) { return k >= in; });
         to_cut = left.sum - (left.cnt - (unsigned)lim.top_k) * weight.whole(of_key(in), shift);
       }
     }
