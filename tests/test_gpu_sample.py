@@ -343,3 +343,15 @@ def test_the_largest_top_p_below_one(vocab):
         assert torch.allclose(probs.cpu(), torch.tensor([share, 1 - share]), rtol=0, atol=2e-6 + 2.0 ** -24)
         ids, _ = B.sample(x.cuda(), u.cuda(), top_p=p.cuda(), top_k=torch.full((2,), 4000, dtype=torch.int32).cuda(), min_p=torch.full((2,), 1e-12).cuda())
         assert ids.tolist() == [1234, 4321], octaves
+
+
+@pytest.mark.parametrize("vocab", [262145, 300001, 1000003])
+def test_more_parts_than_a_wave_has_lanes(vocab):
+    x, u = logits(16, vocab, 160), torch.rand(16, generator=gen(161))
+    # (a border may be off by 2 (3e-12 + 1000003 2^-43 / W), 2.3e-7 of a row whose W is 1: one of these rows has its top-p's border that near)
+    check(x, u, *limits(16, 162), silent=int(vocab == 1000003))
+    check(x[:4], u[:4])
+    flat = logits(4, vocab, 163, spread=1e-3)[1::2]    # (all parts alike, and a row that cannot be narrowed down)
+    for share in (0.0, 0.3, 0.7, 0.999):
+        check(flat, torch.full((2,), share))
+        check(flat, torch.full((2,), share), k=torch.tensor([vocab // 3, 7], dtype=torch.int32))
