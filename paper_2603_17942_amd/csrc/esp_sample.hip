@@ -692,9 +692,12 @@ __global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
 
   // the part in which the target lies; of tokens at the cut's logit the first by id are in
   const uint64_t tie_q = cut.key ? weight.whole(of_key(cut.key), shift) : 0ull;
+  // Of half a unit and more, against the row's largest.  Without limits a part's sum has what is less in it also: a part of nothing else has no weight, and of
+  // another's tokens those of less are not taken, whatever they are against its own largest.
+  auto counts = [&](float l) { return ((double)l - weight.top) * weight.scale > -(double)(shift + 1); };
   auto of_part = [&](int p, const Part& part, unsigned& ties) {        // ties aside
     ties = narrow && p < a.parts ? s.part_ties[p] : 0u;
-    return narrow ? (p < a.parts ? s.part_sum[p] : 0ull) : part_weight(part, weight, shift);
+    return narrow ? (p < a.parts ? s.part_sum[p] : 0ull) : counts(part.top) ? part_weight(part, weight, shift) : 0ull;
   };
   parts.all([&](int p, const Part& part) {
     unsigned ties;
@@ -741,7 +744,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
   auto take = [&](float v, int i, bool& tie) {
     v = tame(v);
     const unsigned k = key_of(v);
-    const uint64_t q = from + i < to && v > -INFINITY && k >= cut.key ? local.whole(v, shift) : 0ull;
+    const uint64_t q = from + i < to && v > -INFINITY && k >= cut.key && (narrow || counts(v)) ? local.whole(v, shift) : 0ull;
     tie = q >= least && k == cut.key;
     return q >= least && k > cut.key ? q : 0ull;
   };

@@ -355,3 +355,27 @@ def test_more_parts_than_a_wave_has_lanes(vocab):
     for share in (0.0, 0.3, 0.7, 0.999):
         check(flat, torch.full((2,), share))
         check(flat, torch.full((2,), share), k=torch.tensor([vocab // 3, 7], dtype=torch.int32))
+
+
+@pytest.mark.parametrize("rows", [1, 600])
+@pytest.mark.parametrize("vocab,also", [(8192, None), (12288, 100)])
+def test_tokens_of_less_than_half_a_unit_are_not_chosen(vocab, also, rows):
+    """4096 tokens of 2^-50 of the largest, in a part without it (one row) and in a part with it (600 rows of 8192); `also`: among them one that counts.
+    Their sum is 128 units, and none of them may be chosen, whatever the parts are."""
+    x = torch.full((rows, vocab), -math.inf)
+    x[:, :4096] = -50 * math.log(2)
+    x[:, 5000] = 0.0
+    if also is not None:
+        x[:, also] = -20 * math.log(2)
+    x = x.cuda()
+    ones, zeros = torch.ones(rows).cuda(), torch.zeros(rows).cuda()
+    want, share = (5000, 1 / (1 + 2.0 ** -20)) if also is None else (also, 2.0 ** -20)
+    if also is None:
+        share = 1.0
+    for lim in ({}, dict(temperature=ones), dict(top_p=ones), dict(top_k=zeros.int()), dict(min_p=zeros), dict(min_p=1e-30 * ones)):
+        ids, probs = B.sample(x, zeros, **lim)
+        assert (ids == want).all(), (lim, ids[:4])
+        # one rounding of the quotient; 128 units of 2^-45 that the part's sum has more of; the logit's rounding, 2^-24 of 13.9
+        assert ((probs.double().cpu() - share).abs() <= share * (2.0 ** -23 + 14 * 2.0 ** -24) + 128 * 2.0 ** -45).all(), lim
+        ids, _ = B.sample(x, torch.full((rows,), 0.5).cuda(), **lim)
+        assert (ids == 5000).all(), lim
