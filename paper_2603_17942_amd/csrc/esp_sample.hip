@@ -46,7 +46,7 @@ struct Part {
   int at;
   double sum;                          // of the weights against it
 };
-struct PartSums { uint64_t all, in; }; // of what is before the list; less what min-p takes
+struct PartSums { uint64_t all, in; }; // of what is before the list; less what min-p takes and what is below half a unit
 enum { AS_IT_IS = 0, COLLECT = 1, DIVIDE = 2 };        // without list; with it; by going over the row
 struct RowState {
   int mode, first, last;               // steps of the list; what is before `first` is added up
@@ -392,7 +392,9 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
   const float own = a.maxima[mine * PART_THREADS + tid];
   const Weigher weight{(double)st.top, octaves(m)};
   __syncthreads();
-  const double least = m.by_part ? __builtin_rint(__builtin_ldexp((double)fminf(m.min_p, 1.f), a.shift)) - 0.5 : 0.0;
+  // In is what weighs min_p and half a unit; without min-p that is all, unless the steps before the list reach so far down.
+  const double least = (m.by_part ? fmax(__builtin_rint(__builtin_ldexp((double)fminf(m.min_p, 1.f), a.shift)), 1.0) : 1.0) - 0.5;
+  const bool some_out = m.by_part || (int64_t)st.first * (a.shift + 2) > (int64_t)(a.shift + 1) * BINS;
   double all = 0.0, in = 0.0;
   if (own * per >= listed) {
     float x[PIECES][N];
@@ -408,7 +410,7 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
         for (int i = 0; i < N; ++i) {  // (the piece's others weigh 2^-900: side by side they take less time than branches do)
           const double w = weight.real(x[j][i] * per >= ahead ? x[j][i] : -INFINITY, a.shift);
           all += w;
-          if (m.by_part) in += w >= least ? w : 0.0;
+          if (some_out) in += w >= least ? w : 0.0;
         }
       }
       if (most * per >= listed && st.first <= st.last) {
@@ -424,8 +426,8 @@ __global__ __launch_bounds__(PART_THREADS) void k_sample_collect(SampleArgs a) {
     }
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) { all += __shfl_xor(all, o); if (m.by_part) in += __shfl_xor(in, o); }
-  if (lane == 0) { wave_sum[wave][0] = all; wave_sum[wave][1] = m.by_part ? in : all; }
+  for (int o = 32; o > 0; o >>= 1) { all += __shfl_xor(all, o); if (some_out) in += __shfl_xor(in, o); }
+  if (lane == 0) { wave_sum[wave][0] = all; wave_sum[wave][1] = some_out ? in : all; }
   __syncthreads();
   if (tid == 0) {
     a.sums[mine] = {(uint64_t)__builtin_rint((wave_sum[0][0] + wave_sum[1][0]) + (wave_sum[2][0] + wave_sum[3][0])),

@@ -379,3 +379,21 @@ def test_tokens_of_less_than_half_a_unit_are_not_chosen(vocab, also, rows):
         assert ((probs.double().cpu() - share).abs() <= share * (2.0 ** -23 + 14 * 2.0 ** -24) + 128 * 2.0 ** -45).all(), lim
         ids, _ = B.sample(x, torch.full((rows,), 0.5).cuda(), **lim)
         assert (ids == 5000).all(), lim
+
+
+@pytest.mark.parametrize("rows", [1, 400])
+def test_limits_do_not_leave_tokens_of_less_than_half_a_unit(rows):
+    """6000 of 2^-46.6 and 2^-46.3 of the largest, where the steps of log w still reach: a min-p below them, a top-k among them."""
+    vocab = 20000
+    x = torch.full((rows, vocab), -math.inf)
+    x[:, :3000] = -46.3 * math.log(2)
+    x[:, 3000:4000] = -46.6 * math.log(2)
+    x[:, 4096:6096] = -46.6 * math.log(2)
+    x[:, 7000] = -20 * math.log(2)
+    x[:, 19000] = 0.0
+    x = x.cuda()
+    for lim in (dict(min_p=torch.full((rows,), 1e-30)), dict(top_k=torch.full((rows,), 5500, dtype=torch.int32)),
+                dict(top_k=torch.full((rows,), 5500, dtype=torch.int32), min_p=torch.full((rows,), 1e-20)), dict(top_p=torch.full((rows,), 1 - 2.0 ** -24))):      # (2^-24 of all is less than 2^-20)
+        lim = {name: t.cuda() for name, t in lim.items()}
+        ids, _ = B.sample(x, torch.zeros(rows).cuda(), **lim)
+        assert (ids == 7000).all(), (lim, ids[:4])
