@@ -376,7 +376,8 @@ esp_status esp_softmax_topk_static(void *stream, const float *logits, int32_t ro
  * Minus infinity and NaN are tokens that cannot be chosen, plus infinity is as the largest finite fp32 value.  A row without any other, and a row
  * whose temperature is negative or not finite or whose top_p or min_p is NaN, gets -1 and 0.
  * Temperatures between 0 and 1e-20 are as 1e-20, above 1e20 as 1e20.  Weights are taken in fp64 (1.1e-12 of themselves) and added up in units of 2^-S of
- * the largest, S = min(45, 62 - ceil log2 vocab); tokens of less than half a unit are not chosen.  The same call chooses the same tokens.
+ * the largest, S = min(45, 62 - ceil log2 vocab); tokens of less than half a unit are not chosen, and count in W unless there is a top_k.  A border among n
+ * tokens that weigh W of the largest may lie 2 (3e-12 + n 2^-(S+1) / W) of all off: 4e-9 at 128256 tokens and W = 1.  The same call chooses the same tokens.
  *   scratch     device, 16-byte aligned, esp_sample_scratch_bytes(): what is enough for so many rows and for fewer (of a row of 128256 up to 329 KB for 32 rows,
  *               181 KB where there are more; of up to 4096 tokens 16 bytes; of up to 1024 rows: more are done in lots).  Calls that overlap in time need one
  *               each.  Results do not depend on what it held

@@ -660,7 +660,7 @@ __global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
     }
     if (lim.by_sum) {
       uint64_t of = to_cut;
-      if (!lim.by_count && listed) {   // of all tokens, by the parts' sums
+      if (!lim.by_count) {             // of all tokens, by the parts' sums, however the cut is found
         of = 0;
         parts.all([&](int, const Part& p) { of += part_weight(p, weight, shift); });
         of = wave_total(of);

@@ -397,3 +397,20 @@ def test_limits_do_not_leave_tokens_of_less_than_half_a_unit(rows):
         lim = {name: t.cuda() for name, t in lim.items()}
         ids, _ = B.sample(x, torch.zeros(rows).cuda(), **lim)
         assert (ids == 7000).all(), (lim, ids[:4])
+
+
+def test_top_p_is_of_all_weights_however_the_cut_is_found():
+    """The first token, the second one of e^-6.5 and 4 million of 0.9 half units, 1.7e-6 together: top_p lies between what the first one is of all and of the two
+    alone, so the second one is in.  At 40000 the same logits, to the bit, are divided by going over the row."""
+    vocab, faint = 2 ** 22, -7302 / 256
+    second, rest = math.exp(-6.5), (vocab - 2) * math.exp(faint)
+    assert math.exp(faint) < 2.0 ** -41 and 1.6e-6 < rest < 1.8e-6
+    p = torch.full((1,), 0.5 / (1 + second) + 0.5 / (1 + second + rest), dtype=torch.float64).float()
+    assert 1 / (1 + second + rest) + 5e-7 < float(p) < 1 / (1 + second) - 5e-7
+    u = torch.full((1,), 0.9995)
+    for shift in (0.0, 40000.0):
+        x = torch.full((1, vocab), faint + shift)
+        x[0, 100], x[0, 4000000] = shift, shift - 6.5
+        assert float(x[0, 0]) == faint + shift
+        ids, _ = B.sample(x.cuda(), u.cuda(), top_p=p.cuda())
+        assert ids.tolist() == [4000000], shift
