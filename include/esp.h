@@ -509,8 +509,8 @@ esp_status esp_paged_commit(void *stream, const esp_paged_kv *kv, const int32_t 
  *   scratch     device, 16-byte aligned, esp_paged_weigh_scratch_bytes(), which depend on the host's values alone; calls that overlap in time need
  *               one each.  Up to 32 counted (row, query head) pairs a kv head it holds their scores, 4 bytes a pair (in fours), kv head and token of
  *               len_bound: a call with more rows can want less
- * Scores, probabilities and sums are fp32, tokens' sums always in the same order.  Scores may be as large as 5e8.  A row with a score of plus infinity or NaN makes
- * the tokens it sees NaN, a score of minus infinity weighs nothing; a token in a page outside the pool is not seen (its mass is `before`).  A sequence
+ * Scores, probabilities and sums are fp32, tokens' sums always in the same order.  Scores may be as large as 5e8.  A row with a score of plus infinity or NaN makes all
+ * tokens it sees NaN, in another row a score of minus infinity weighs nothing; a token in a page outside the pool is not seen (its mass is `before`).  A sequence
  * with len + rows above mass_slots is as one that is over its bound.
  * Errors: as esp_paged_attn; EINVAL also for last_rows < 0 and mass_slots < 1; ECAPACITY also for more than 65535 kv heads. */
 size_t esp_paged_weigh_scratch_bytes(const esp_paged_kv* kv, const esp_chunk* rows, int32_t n_q_heads, int32_t last_rows);

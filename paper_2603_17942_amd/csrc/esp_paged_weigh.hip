@@ -15,6 +15,7 @@
 // Scores are S = Q K^T on 32 x 32 matrix instructions.  With keys as the second operand a lane has one key and the columns
 // 8 (v / 4) + 4 half + v % 4 in its 16 registers; with keys first (the statistics of many columns) one column and those keys.
 #include <algorithm>
+#include <cfloat>
 
 #include "esp_attn_unit.h"
 #include "esp_paged.h"
@@ -97,6 +98,9 @@ __device__ __forceinline__ float2 finish(float2 a) { return {a.x, a.y == 0.f ? 0
 
 // ---- few columns ---------------------------------------------------------------------------------------------
 
+// What a score is where a column does not see the token.  Not minus infinity: a score can be that, which weighs nothing, but is NaN in a row that is.
+constexpr float NOT_SEEN = -FLT_MAX;
+
 // scores [seq][kvh][t][width] of columns below `width`; stats [seq][kvh][share][width].  K's bytes are what bounds it.  (bf16 with up to eight columns: 128 registers
 // and four waves a SIMD instead of 132 and three, 123 us instead of 128 for 32 ragged sequences)
 template <typename T, int HD, int NV>      // NV: groups of eight columns
@@ -149,7 +153,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && NV == 1 ? 4 : 1) void k_
       const float e = seen ? __builtin_amdgcn_exp2f(fmaf(x[v], a.scale, -top)) : 0.f;
       l[v] = l[v] * __builtin_amdgcn_exp2f(m[v] - top) + e;
       m[v] = top;
-      x[v] = seen ? x[v] : -INFINITY;
+      x[v] = seen ? x[v] : NOT_SEEN;
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -202,8 +206,8 @@ __global__ __launch_bounds__(THREADS) void k_weigh_sum(PagedDev kv, ChunkDev ch,
     for (int i = 0; i < p.width; i += 4) {
       const f32x4_t v = *reinterpret_cast<const f32x4_t*>(x + i);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)      // (minus infinity: not seen, also by a row that is NaN)
-        sum = v[e] == -INFINITY ? sum : fmaf(__builtin_amdgcn_exp2f(fmaf(v[e], a.scale, -col[i + e].x)), col[i + e].y, sum);
+      for (int e = 0; e < 4; ++e)
+        sum = v[e] == NOT_SEEN ? sum : fmaf(__builtin_amdgcn_exp2f(fmaf(v[e], a.scale, -col[i + e].x)), col[i + e].y, sum);
     }
     a.mass[at] = old + sum;
   }

@@ -201,6 +201,28 @@ def test_tokens_that_are_not_finite(dtype, n, what):
     assert torch.equal(got[0, 0, :, s + 1:], before[0, 0, :, s + 1:])
 
 
+@pytest.mark.parametrize("n", [1, 30])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_minus_infinity_among_scores_that_are_not_finite(dtype, n):
+    """A row with a score of plus infinity makes NaN of all that it sees, tokens with a score of minus infinity among them; a row whose scores are all minus
+    infinity gives nothing."""
+    c = Plain(DT[dtype], 1, 2, 64, 32, [70, 40], [n, n], 25)
+    d = np.arange(64)
+    for s, what in ((5, math.inf), (9, -math.inf)):
+        c.kv.k[0, int(c.table[0, 0])].view(2, -1)[:, torch.from_numpy(k_place(s, d, 64)).cuda()] = what
+    for page in c.table[1, :(40 + n + 31) // 32].tolist():
+        c.kv.k[0, page] = -math.inf
+    q = queries(2 * n, 8, 64, DT[dtype], 26).abs()     # (a score of one sign)
+    assert (q > 0).all()
+    before = torch.rand((1, 2, 2, 128), generator=gen(27))
+    mass = before.cuda()
+    B.paged_weigh(c.kv, 0, c.chunk, q, mass)
+    got = mass.cpu()
+    assert torch.isnan(got[0, 0, :, :70 + n]).all() and torch.equal(got[0, 0, :, 70 + n:], before[0, 0, :, 70 + n:])
+    assert torch.equal(got[0, 1, :, :40], before[0, 1, :, :40]) and (got[0, 1, :, 40:40 + n] == 0).all()
+    assert torch.equal(got[0, 1, :, 40 + n:], before[0, 1, :, 40 + n:])
+
+
 @pytest.mark.parametrize("hq", [4, 64])
 def test_rows_that_do_not_see_a_bad_token_are_not_touched_by_it(hq):
     """A row whose scores are NaN makes NaN of what it sees, not of tokens behind it."""
