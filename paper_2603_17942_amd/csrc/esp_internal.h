@@ -332,6 +332,11 @@ hipError_t launch_attn(hipStream_t st, int dtype, const BlockDev& b, const KvDev
 hipError_t launch_attn_merge(hipStream_t st, int dtype, const BlockDev& b, const KvDev& kv, int hq, int hkv, int hd,
                              const float* partials, const AttnPlan& p, void* out, const int32_t* cuts);
 
+// ---- sampling (esp_sample.hip) ----------------------------------------------------------------
+// rows that are done in one go, the i-th of their lots (none behind the last row)
+struct SampleLot { int64_t first; int rows; };
+SampleLot sample_lot(int rows, int i);
+
 // ---- softmax + top-k (esp_topk.hip) -----------------------------------------------------------
 size_t softmax_topk_scratch_floats(int rows, int vocab, int kp);
 // row_map (nullable): logits row of output row r is row_map[r] (negative: 0)

@@ -840,25 +840,30 @@ hipError_t launch(hipStream_t st, const SampleArgs& a, int rows) {
 template <typename T>
 hipError_t launch_rows(hipStream_t st, SampleArgs a, int rows) {
   const bool aligned = (uintptr_t)a.logits % 16 == 0 && a.stride * sizeof(T) % 16 == 0;
-  for (int done = 0; done < rows; done += ROWS_AT_ONCE) {
+  for (int i = 0;; ++i) {
+    const auto [done, n] = sample_lot(rows, i);
+    if (n == 0) return hipSuccess;
     SampleArgs b = a;
-    b.logits = (const T*)a.logits + (int64_t)done * a.stride;
+    b.logits = (const T*)a.logits + done * a.stride;
     if (a.temperature) b.temperature += done;
     if (a.top_k) b.top_k += done;
     if (a.top_p) b.top_p += done;
     if (a.min_p) b.min_p += done;
     b.u += done; b.ids += done;
     if (a.probs) b.probs += done;
-    const int n = std::min(rows - done, ROWS_AT_ONCE);
     const hipError_t e = aligned ? launch<T, true>(st, b, n) : launch<T, false>(st, b, n);
     if (e != hipSuccess) return e;
   }
-  return hipSuccess;
 }
 
 bool too_large(int vocab) { return vocab > MOST_PARTS * 4096; }
 
 }  // namespace
+
+SampleLot sample_lot(int rows, int i) {
+  const int64_t first = std::min<int64_t>((int64_t)i * ROWS_AT_ONCE, rows);
+  return {first, (int)std::min<int64_t>(rows - first, ROWS_AT_ONCE)};
+}
 
 extern "C" size_t esp_sample_scratch_bytes(int32_t rows, int32_t vocab) {
   if (rows < 1 || vocab < 1 || too_large(vocab)) return 0;

@@ -8,6 +8,7 @@ import torch
 
 from paper_2603_17942_amd import binding as B
 from test_paged_abi import BAD_CACHE, ECAPACITY, EDTYPE, EINVAL, ESHAPE, P, chunk, paged
+from util import internal
 
 
 @pytest.fixture(scope="module")
@@ -143,3 +144,19 @@ def test_python_numbers_beyond_32_bits():
     for kw in (dict(keep=2 ** 32 + 8), dict(keep=8, first=2 ** 32), dict(keep=8, recent=2 ** 32 + 1), dict(keep=8, first=-2 ** 32), dict(keep=8, first=5, recent=4)):
         with pytest.raises(ValueError, match="keep: 1 or more wanted"):
             B.paged_evict(kv, mass, **kw)
+
+
+class SampleLot(C.Structure):
+    _fields_ = [("first", C.c_int64), ("rows", C.c_int)]
+
+
+@pytest.mark.parametrize("rows", [0, 1, 1023, 1024, 1025, 2048, 2 ** 31 - 1025, 2 ** 31 - 1024, 2 ** 31 - 1023, 2 ** 31 - 2, 2 ** 31 - 1])
+def test_lots_of_rows_end_where_the_rows_do(rows):
+    """Also where the number behind the last lot is none of 32 bits."""
+    lot = internal("sample_lot", C.c_int, C.c_int, restype=SampleLot)
+    lots = (rows + 1023) // 1024
+    for i in {0, 1, lots - 2, lots - 1, lots, lots + 1}:
+        if i >= 0:
+            got = lot(rows, i)
+            assert got.rows == max(0, min(1024, rows - 1024 * i))
+            assert got.first == min(1024 * i, rows)
