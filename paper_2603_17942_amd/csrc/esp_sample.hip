@@ -839,7 +839,7 @@ hipError_t launch(hipStream_t st, const SampleArgs& a, int rows) {
 // A lot of rows at a time; the rows' arrays move along.
 template <typename T>
 hipError_t launch_rows(hipStream_t st, SampleArgs a, int rows) {
-  const bool aligned = (uintptr_t)a.logits % 16 == 0 && a.stride * sizeof(T) % 16 == 0;
+  const bool aligned = (uintptr_t)a.logits % 16 == 0 && (rows == 1 || a.stride * sizeof(T) % 16 == 0);       // (of one row the stride is not used)
   for (int i = 0;; ++i) {
     const auto [done, n] = sample_lot(rows, i);
     if (n == 0) return hipSuccess;

@@ -414,3 +414,20 @@ def test_top_p_is_of_all_weights_however_the_cut_is_found():
         assert float(x[0, 0]) == faint + shift
         ids, _ = B.sample(x.cuda(), u.cuda(), top_p=p.cuda())
         assert ids.tolist() == [4000000], shift
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [4095, 4097, 50257, 151643])
+def test_one_row_of_an_odd_size_is_as_among_others(vocab, dtype):
+    """By itself and at an aligned address it is read 16 bytes at a time, whatever its stride: what lies behind it would be chosen."""
+    n = 8
+    x, u, lim = logits(n, vocab, 170, dtype=dtype), torch.rand(n, generator=gen(171)), limits(n, 172)
+    want = check(x, u, *lim)
+    probs = B.sample(x.cuda(), u.cuda(), *(t.cuda() for t in lim))[1]
+    for off in (0, 1):
+        big = torch.full((vocab + off + 8,), math.inf, dtype=dtype, device="cuda")
+        for r in range(n):
+            big[off:off + vocab] = x[r].cuda()
+            one = [t[r:r + 1].cuda() for t in (u, *lim)]
+            got = B.sample(big[off:off + vocab].unsqueeze(0), one[0], *one[1:])
+            assert int(got[0]) == int(want[r]) and float(got[1]) == float(probs[r]), (r, off)
