@@ -503,7 +503,8 @@ esp_status esp_paged_commit(void *stream, const esp_paged_kv *kv, const int32_t 
 /* How much attention the chunk's rows give to each token of their sequences, for esp_paged_evict: with p the softmax of esp_paged_attn (causal; K of
  * the rows is in its slots already), mass[t] = before[t] + the sum of p_rt over the sequence's counted rows r and the kv head's query heads, for
  * t < len[b]; the chunk's own tokens get the sum alone, whatever was there.  Slots from len[b] + rows on, and sequences without rows, are not touched.
- * After a verified tree: the accepted rows alone, packed, with len as it was before them.
+ * After a verified tree: esp_paged_commit with a len_out of its own, then this with the accepted rows alone, packed, and len as it was before them; then len is
+ * advanced.
  *   last_rows   0: all rows count; otherwise only the last so many of each sequence's
  *   before, mass device fp32 [n_layers][batch][n_kv_heads][mass_slots]; before NULL: zeros; it may be mass itself, and otherwise must not overlap it
  *   scratch     device, 16-byte aligned, esp_paged_weigh_scratch_bytes(), which depend on the host's values alone; calls that overlap in time need

@@ -834,7 +834,8 @@ def paged_weigh(kv: PagedKv, layer: int, rows: ChunkRows, q: torch.Tensor, mass:
                 last_rows: int = 0, scale: Optional[float] = None, scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Adds to mass [layers, batch, kv heads, slots] (float32), in `layer`, the attention that the chunk's rows (their K appended before) give to each
     token, summed over rows and a kv head's queries; the chunk's own tokens get that alone.  before: what it is added to instead of mass.
-    last_rows: only so many of a sequence's rows count, the last ones (0: all).  scratch: uint8, paged_weigh_scratch_bytes."""
+    last_rows: only so many of a sequence's rows count, the last ones (0: all).  After a verified tree: the accepted rows alone, moved by paged_commit with a
+    len_out of its own, before kv.lens advances.  scratch: uint8, paged_weigh_scratch_bytes."""
     lib = load_library()
     _same_batch(kv, rows)
     dev, dt, hd, n = kv.device, kv.dtype, kv.head_dim, rows.total_rows

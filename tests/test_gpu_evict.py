@@ -262,6 +262,66 @@ def test_pages_outside_the_pool_are_not_seen(rows):
         assert ((got[0, 0, h, :200 + rows].double() - p).abs() <= 2e-5 * (1 + p))[~gone].all()
 
 
+@pytest.mark.parametrize("rows", [1, 50])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sequences_that_share_pages(dtype, rows):
+    """Three sequences begin with the same 64 tokens, on the same pages: weighed, then evicted to pages of their own; the shared ones stay as they are."""
+    c = Plain(DT[dtype], 2, 2, 64, 32, [100, 90, 64], [rows] * 3, 45, keep=48)
+    for b in (1, 2):
+        c.table[b, :2] = c.table[0, :2]
+        c.k[b][:, :64], c.v[b][:, :64] = c.k[0][:, :64], c.v[0][:, :64]
+    c.kv.page_table.copy_(c.table)
+    q = queries(3 * rows, 8, 64, DT[dtype], 46)
+    before = torch.rand((2, 3, 2, 200), generator=gen(47))
+    mass = before.cuda()
+    for layer in range(2):
+        B.paged_weigh(c.kv, layer, c.chunk, q, mass)
+        check_mass(c, layer, q, mass.cpu(), before)
+    c.lens = [n + rows for n in c.lens]
+    c.kv.lens.copy_(i32(c.lens))
+    c.kv.len_bound = max(c.lens)
+    check_evict(c, mass.cpu(), 48, 4, 8, in_place=False)        # (all of the pools against what they were, but the new pages)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 7, 50])
+def test_rows_that_see_nothing(dtype, rows):
+    """Pages outside the pool: all of one sequence's, the first two of another's, whose first rows see nothing and whose later ones see what is behind, and none of a
+    third's."""
+    dt = DT[dtype]
+    c = Plain(dt, 1, 2, 64, 32, [70, 20, 40], [rows] * 3, 48)
+    table = c.table.clone()
+    table[0], table[1, :2] = -1, c.pages
+    c.kv.page_table.copy_(table)
+    q = queries(3 * rows, 8, 64, dt, 49)
+    before = torch.rand((1, 3, 2, 130), generator=gen(50))
+    for bound in (70, 40000):                          # (as planned for their lengths and for long ones)
+        c.kv.len_bound = bound
+        mass = before.cuda()
+        B.paged_weigh(c.kv, 0, c.chunk, q, mass)
+        got = mass.cpu()
+        assert c.kv.device_status() == B.DEV_BAD_PAGE
+        assert torch.equal(got[0, 0, :, :70], before[0, 0, :, :70]) and (got[0, 0, :, 70:70 + rows] == 0).all()
+        assert torch.equal(got[0, 1, :, :20], before[0, 1, :, :20]) and (got[0, 1, :, 20:min(64, 20 + rows)] == 0).all()
+        for b, (l, gone) in enumerate(((70, 70 + rows), (20, 64), (40, 0))):
+            assert torch.equal(got[0, b, :, l + rows:], before[0, b, :, l + rows:])
+            if l + rows <= gone:
+                continue
+            # rows that see something, over what there is
+            seen = (torch.arange(gone, l + rows) <= (l + torch.arange(rows))[:, None])
+            some = seen.any(1)
+            for h in range(2):
+                rq = q[b * rows:(b + 1) * rows].cpu().double()[some, 4 * h:4 * h + 4]
+                x = torch.einsum("rgd,td->rgt", rq, c.k[b][0, gone:, h].double()) * 0.125
+                p = torch.softmax(x.masked_fill(~seen[some][:, None], -math.inf), -1).sum((0, 1))
+                old = before[0, b, h, gone:l + rows].double()
+                old[max(l - gone, 0):] = 0
+                # a score: 64 products, below 64 2^-24 64; twice, and 8 roundings of it; the rest of it as above
+                size = (rq.abs() @ c.k[b][0, gone:, h].double().abs().T * 0.125).amax()
+                tol = 2 * U * 72 * float(size) + 2.0 ** -21 + ((l + rows) / 32 + 68) * U + (4 * rows + 8) * U
+                assert ((got[0, b, h, gone:l + rows].double() - p - old).abs() <= tol * p + 10 * U * old + 1e-30).all(), (b, h)
+
+
 def test_malformed_sequences_are_left_out():
     c = Plain(torch.bfloat16, 1, 2, 64, 32, [40, 50, 60, 70], [1, 1, 1, 1], 51)
     c.kv.lens.copy_(i32([-1, 50, 71, 70]))             # the bound is 70
@@ -591,3 +651,80 @@ def test_a_bounded_serving_loop(dtype):
         assert int(ids[1]) == int(logits[1].argmax()) and 0 <= int(ids[0]) < vocab
         tokens = [ids[b:b + 1].cpu().long() for b in range(2)]
     assert evictions > 35
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_verified_tree_is_weighed(dtype):
+    """Two sequences verify a tree each step: its rows appended, attention by ancestors, the accepted rows moved (new lengths to a tensor of their own), and these alone
+    weighed, with the lengths of before; then eviction.  Masses against the accepted rows' softmax in 64 bits over what the cache holds."""
+    dt, hkv, hq, hd, page, keep, first, recent = DT[dtype], 2, 8, 64, 32, 80, 2, 20
+    g = gen(151)
+    kv = B.PagedKv.zeros(1, 12, hkv, page, hd, 2, 6, dtype=dt)
+    kv.page_table.copy_(torch.randperm(12, generator=g).reshape(2, 6).to(torch.int32))
+    rope, lens, seen = B.rope_spec(hd), [0, 0], [0, 0]
+    mass, after = torch.zeros((1, 2, hkv, 192), device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    rows_k = [torch.zeros((0, hkv, hd)), torch.zeros((0, hkv, hd))]
+    # parents of a tree's rows (-1: the root, row 0), and the paths that are accepted, by steps
+    trees = [[-1, 0, 0, 1, 1, 2, 3, 5, 5, 6], [-1, 0, 1, 0, 3, 3, 2, 2, 4, 4, 8, 8, 10]]
+    paths = [([0, 1, 3, 6, 9], [0, 3, 4, 8, 10, 12]), ([0], [0, 3, 5]), ([0, 2, 5, 8], [0]), ([0, 1, 4], [0, 1, 2, 7])]
+    evictions = 0
+    for step in range(9):
+        rows = [60, 75] if step == 0 else [len(t) for t in trees]
+        starts = [0, rows[0], sum(rows)]
+        x = torch.randn((sum(rows), hq + 2 * hkv, hd), generator=g).to(dt).cuda()
+        ch = B.ChunkRows(i32(starts), starts[-1], max(rows))
+        kv.len_bound = max(lens)
+        if step == 0:                                  # prompts
+            depth, accepted, anc = [list(range(r)) for r in rows], [list(range(r)) for r in rows], None
+        else:
+            depth, accepted = [], list(paths[step % 4])
+            anc = torch.zeros((sum(rows), 1), dtype=torch.int64)
+            for b, t in enumerate(trees):
+                depth.append([])
+                for i, parent in enumerate(t):
+                    depth[b].append(0 if parent < 0 else depth[b][parent] + 1)
+                    anc[starts[b] + i, 0] = (0 if parent < 0 else int(anc[starts[b] + parent, 0])) | 1 << i
+            anc = anc.cuda()
+        pos = torch.cat([s + torch.tensor(d) for s, d in zip(seen, depth)]).to(torch.int32).cuda()
+        q = B.paged_append(kv, 0, ch, x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], rope=rope, positions=pos)
+        _, k_rot = B.rope_qk(None, x[:, hq:hq + hkv].contiguous(), pos, rope)
+        B.paged_attn(kv, 0, ch, q, anc=anc)
+        if anc is None:
+            after.copy_(kv.lens + i32(rows))
+        else:
+            B.paged_commit(kv, i32([len(p) for p in accepted]), i32([p + [0] * (B.MAX_MASKS + 1 - len(p)) for p in accepted]), after)
+        assert after.tolist() == [n + len(p) for n, p in zip(lens, accepted)] and kv.lens.tolist() == lens
+        took = [starts[b] + i for b in range(2) for i in accepted[b]]
+        n = [len(p) for p in accepted]
+        old = mass.cpu()
+        B.paged_weigh(kv, 0, B.ChunkRows(i32([0, n[0], sum(n)]), sum(n), max(n)), q[took].contiguous(), mass)
+        got = mass.cpu()
+        for b in range(2):
+            mine = [starts[b] + i for i in accepted[b]]
+            rows_k[b] = torch.cat([rows_k[b], k_rot[mine].cpu().float()])
+            l, r = lens[b], n[b]
+            hidden = torch.arange(l + r) > (l + torch.arange(r))[:, None]
+            rq = q[mine].cpu().double().view(r, hkv, hq // hkv, hd)
+            s = torch.einsum("rhgd,thd->hgrt", rq, rows_k[b].double()) * hd ** -0.5
+            want = torch.softmax(s.masked_fill(hidden, -math.inf), -1).sum((1, 2))
+            was = old[0, b, :, :l + r].double()
+            was[:, l:] = 0
+            size = torch.einsum("rhgd,thd->hgrt", rq.abs(), rows_k[b].double().abs()).amax() * hd ** -0.5
+            tol = 2 * U * (hd + 8) * float(size) + 2.0 ** -21 + ((l + r) / 32 + 68) * U + (4 * r + 8) * U
+            assert ((got[0, b, :, :l + r].double() - want - was).abs() <= tol * want + 10 * U * was + 1e-30).all(), (step, b)
+            assert torch.equal(got[0, b, :, l + r:], old[0, b, :, l + r:])
+            lens[b], seen[b] = l + r, seen[b] + r
+        kv.lens.copy_(after)
+        kv.len_bound = max(lens)
+        kept = B.paged_evict(kv, mass, keep, first, recent).cpu()
+        assert kv.device_status() == 0
+        for b in range(2):
+            evictions += lens[b] > keep
+            m = min(lens[b], keep)
+            for h in range(hkv):
+                assert kept[0, b, h, :m].tolist() == chosen(got[0, b, h].numpy(), lens[b], keep, first, recent).tolist()
+            rows_k[b] = torch.stack([rows_k[b][kept[0, b, h, :m].long(), h] for h in range(hkv)], 1)
+            lens[b] = m
+            assert torch.equal(B.paged_load(kv, 0, b, 0, m)[0].cpu().float(), rows_k[b])
+        assert kv.lens.tolist() == lens
+    assert evictions == 2 + 6                          # lengths 60, 61, 65, 68, 73, 74, 78, 81, 80 + 5 and 75, 78, 79, 83, 80 + 6, + 3, + 1, + 4, + 6
