@@ -872,9 +872,12 @@ def paged_evict(kv: PagedKv, mass: torch.Tensor, keep: int, first: int = 0, rece
     if not (1 <= keep < 2 ** 31 and first >= 0 and recent >= 0 and first + recent <= keep):
         raise ValueError("keep: 1 or more wanted, and room for first and recent")
     shape = (layers, kv.batch, kv.n_kv_heads, keep)
+    mp, op = _mass(mass, "mass", kv), _mass(to, "mass_out", kv)
+    if keep > to.shape[3] or keep > table.shape[1] * kv.k.shape[3]:
+        raise EspError(3, "esp_paged_evict")       # (before a list of that length is allocated)
     if kept is None:
         kept = torch.empty(shape, dtype=torch.int32, device=dev)
-    _on_device(dev, lib.esp_paged_evict, "esp_paged_evict", kv._ref, _mass(mass, "mass", kv), mass.shape[3], keep, first, recent,
-               _ints(table, "table_out", dev, (kv.batch, table.shape[1])), table.shape[1], _mass(to, "mass_out", kv), to.shape[3],
+    _on_device(dev, lib.esp_paged_evict, "esp_paged_evict", kv._ref, mp, mass.shape[3], keep, first, recent,
+               _ints(table, "table_out", dev, (kv.batch, table.shape[1])), table.shape[1], op, to.shape[3],
                _ints(out, "len_out", dev, (kv.batch,)), _ints(kept, "kept", dev, shape))
     return kept

@@ -160,3 +160,13 @@ def test_lots_of_rows_end_where_the_rows_do(rows):
             got = lot(rows, i)
             assert got.rows == max(0, min(1024, rows - 1024 * i))
             assert got.first == min(1024 * i, rows)
+
+
+@pytest.mark.parametrize("keep", [65, 2 ** 31 - 1])
+def test_keeping_more_than_there_is_room_for_is_refused_before_anything_is_allocated(keep, monkeypatch):
+    k = torch.zeros((1, 4, 2, 32, 64))
+    kv = B.PagedKv(k, k.clone(), torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 0)
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: pytest.fail("allocated"))
+    for slots, pages in ((64, 100), (200, 2)):
+        with pytest.raises(B.EspError, match="ESP_ECAPACITY"):
+            B.paged_evict(kv, torch.zeros((1, 1, 2, slots)), keep, table_out=torch.zeros((1, pages), dtype=torch.int32))
