@@ -571,7 +571,10 @@ WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_ro
   if (most <= 4 || units <= 64) p.share_units = (int)std::max<int64_t>(2, (units + std::min<int64_t>(4, most) - 1) / std::min<int64_t>(4, most));
   else p.share_units = (int)std::max<int64_t>(16, (units + most - 1) / most);
   p.shares = (units + p.share_units - 1) / p.share_units;
-  p.join_here = p.shares > 1 && p.shares <= 4 && cols <= 256;
+  // Few columns: the sums join the shares, a tile of columns a time and a share after the other, which costs less than a launch does (448 tokens, bf16 of 128 and four
+  // shares, joined there / in a launch: 36 columns 14.3 / 15.7 us, 96 16.5 / 16.6, 128 18.3 / 17.5, 256 28.0 / 23.5; fp32 of 64 16.4 / 17.7, 20.6 / 20.5, 23.1 / 22.1,
+  // 33.6 / 29.9; at 960 and 1900 tokens and eight sequences the same turn at 96).
+  p.join_here = p.shares > 1 && p.shares <= 4 && cols <= 96;
   p.stats_floats = 2 * p.columns * p.shares;
   const int keys = WAVES * 32 * (dtype == ESP_BF16 ? 2 : 1);
   const int64_t key_groups = (p.tokens + keys - 1) / keys * heads;
