@@ -379,7 +379,7 @@ esp_status esp_softmax_topk_static(void *stream, const float *logits, int32_t ro
  * the largest, S = min(45, 62 - ceil log2 vocab); tokens of less than half a unit are not chosen, and count in W unless there is a top_k.  A border among n
  * tokens that weigh W of the largest may lie 2 (3e-12 + n 2^-(S+1) / W) of all off: 4e-9 at 128256 tokens and W = 1.  The same call chooses the same tokens.
  *   scratch     device, 16-byte aligned, esp_sample_scratch_bytes(): what is enough for so many rows and for fewer (of a row of 128256 up to 329 KB for 32 rows,
- *               181 KB where there are more; of up to 4096 tokens 16 bytes; of up to 1024 rows: more are done in lots).  Calls that overlap in time need one
+ *               181 KB where there are more; of up to 4096 tokens 16 bytes; of up to 1024 rows: more are done in lots; the same with limits and without).  Calls that overlap in time need one
  *               each.  Results do not depend on what it held
  * Errors: EINVAL (null pointers, rows < 0, vocab < 1), ESHAPE (row_stride < vocab), EDTYPE, ECAPACITY (scratch; vocab above 2^22). */
 size_t esp_sample_scratch_bytes(int32_t rows, int32_t vocab);

@@ -101,7 +101,7 @@ struct WeighArgs {
   float scale;                // with log2 e
   bool whole;                 // q can be read 16 bytes at a time
 };
-WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int last, int len_bound);
+WeighPlan weigh_plan(int dtype, int batch, int hq, int hkv, int total_rows, int max_rows, int last, int len_bound);
 int64_t weigh_workgroups(const WeighPlan& p, int batch, int hkv, int G);
 hipError_t launch_paged_weigh(hipStream_t st, int dtype, int hd, const PagedDev& kv, const ChunkDev& ch, const WeighArgs& a, const WeighPlan& p);
 

@@ -185,7 +185,7 @@ esp_status esp_paged_load(void* stream, const esp_paged_kv* kv, int32_t layer, i
 size_t esp_paged_weigh_scratch_bytes(const esp_paged_kv* kv, const esp_chunk* rows, int32_t n_q, int32_t last_rows) {
   if (check_paged(kv) != ESP_OK || check_chunk(kv, rows) != ESP_OK || n_q < 1 || n_q % kv->n_kv_heads || last_rows < 0) return 0;
   if (rows->total_rows == 0 || rows->max_rows == 0 || too_many_columns(kv, rows, n_q)) return 0;
-  const WeighPlan p = weigh_plan(kv->dtype, kv->head_dim, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, last_rows, kv->len_bound);
+  const WeighPlan p = weigh_plan(kv->dtype, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, last_rows, kv->len_bound);
   return (size_t)p.scratch_floats * 4;
 }
 
@@ -202,7 +202,7 @@ esp_status esp_paged_weigh(void* stream, const esp_paged_kv* kv, int32_t layer, 
   if (q_stride < (int64_t)n_q * kv->head_dim) return ESP_ESHAPE;
   if (kv->n_kv_heads > 65535 || too_many_columns(kv, rows, n_q)) return ESP_ECAPACITY;
   if (rows->total_rows == 0 || rows->max_rows == 0) return ESP_OK;
-  const WeighPlan p = weigh_plan(kv->dtype, kv->head_dim, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, last_rows, kv->len_bound);
+  const WeighPlan p = weigh_plan(kv->dtype, kv->batch, n_q, kv->n_kv_heads, rows->total_rows, rows->max_rows, last_rows, kv->len_bound);
   if (weigh_workgroups(p, kv->batch, kv->n_kv_heads, n_q / kv->n_kv_heads) > MOST_WORKGROUPS) return ESP_ECAPACITY;
   const size_t need = (size_t)p.scratch_floats * 4;
   if (!scratch || scratch_bytes < need) return ESP_ECAPACITY;

@@ -8,9 +8,10 @@
 // columns, whose tiles four waves share through LDS, so that a token's sum stays in a lane and nothing is added by atomics: the same bits every time.
 //
 // What bounds them, at 32 query and 8 kv heads of 128 in bf16: 32 ragged sequences' single rows read 522 MB of K, 101 us at the rate of a copy, and take
-// 123 (scores 109, sums 14).  A prompt of 4096 takes its 137 GF of products in twice 120 to 130 us, 45% of the rate of a large product: matrix
-// instructions for 25% of the time, the exponentials' vector instructions for 40%, and with 217 and 164 registers too few waves (1.1 and 1.7 a SIMD) for one
-// to hide behind the other.
+// 121 (scores 108, sums 14).  A prompt of 4096 takes its 137 GF of products in twice 120 to 133 us, 45% of the rate of a large product: matrix
+// instructions for 25% of the time, the exponentials' vector instructions for 40%, and 1.1 and 1.7 waves a SIMD on average, too few for one to hide behind
+// the other.  The registers (217 and 164) leave room for 2 and 3: the workgroups have unequal work, as shares and parts are of equal size and what a row sees is a
+// triangle, so CUs stand idle towards the end (counted in units, with workgroups taken in turn, at most 1.6 and 2.1 waves a SIMD on average; with equal ones 2 and 2.7).
 //
 // Scores are S = Q K^T on 32 x 32 matrix instructions.  With keys as the second operand a lane has one key and the columns
 // 8 (v / 4) + 4 half + v % 4 in its 16 registers; with keys first (the statistics of many columns) one column and those keys.
@@ -102,7 +103,7 @@ __device__ __forceinline__ float2 finish(float2 a) { return {a.x, a.y == 0.f ? 0
 constexpr float NOT_SEEN = -FLT_MAX;
 
 // scores [seq][kvh][t][width] of columns below `width`; stats [seq][kvh][share][width].  K's bytes are what bounds it.  (bf16 with up to eight columns: 128 registers
-// and four waves a SIMD instead of 132 and three, 123 us instead of 128 for 32 ragged sequences)
+// and four waves a SIMD instead of 132 and three, 123 us instead of 128 for 32 ragged sequences, sums included)
 template <typename T, int HD, int NV>      // NV: groups of eight columns
 __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && NV == 1 ? 4 : 1) void k_weigh_scores(PagedDev kv, ChunkDev ch, WeighArgs a, WeighPlan p) {
   typedef typename AttnFrag<T>::type F;
@@ -518,7 +519,8 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
     else hipLaunchKernelGGL((k_weigh_scores<T, HD, 4>), grid, wg, 0, st, kv, ch, a, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // (four tokens a thread where there are many: the shares are joined by every workgroup)
+    // Four tokens a thread where there are many, as the shares are joined by every workgroup.  Whole calls of a row a sequence, one / four a thread: 2^14 tokens of all
+    // heads 8.8 / 10.4 us, 2^18 21.5 / 22.6, 2^19 33.2 / 33.1, 2^20 62.6 / 59.4 (one sequence of 131072: 71.7 / 64.0), 2^22 252 / 239.
     if (p.tokens * kv.hkv * kv.batch >= (1 << 20)) hipLaunchKernelGGL(k_weigh_sum<4>, dim3((tokens.x + 3) / 4, tokens.y, tokens.z), wg, 0, st, kv, ch, a, p);
     else hipLaunchKernelGGL(k_weigh_sum<1>, tokens, wg, 0, st, kv, ch, a, p);
     return hipGetLastError();
@@ -543,7 +545,7 @@ hipError_t launch(hipStream_t st, const PagedDev& kv, const ChunkDev& ch, const 
 
 }  // namespace
 
-WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_rows, int max_rows, int last, int len_bound) {
+WeighPlan weigh_plan(int dtype, int batch, int hq, int hkv, int total_rows, int max_rows, int last, int len_bound) {
   WeighPlan p{};
   const int G = hq / hkv, rows = std::min(std::min(max_rows, total_rows), last > 0 ? last : max_rows);
   const int64_t cols = (int64_t)rows * G, heads = (int64_t)batch * hkv;
@@ -565,8 +567,10 @@ WeighPlan weigh_plan(int dtype, int hd, int batch, int hq, int hkv, int total_ro
   p.columns = (p.packed ? (int64_t)total_rows : (int64_t)batch * rows) * hq;
   const int of_group = WAVES * stat_tiles(dtype == ESP_BF16);
   const int64_t groups = ((cols + 31) / 32 + of_group - 1) / of_group * heads;
-  // About 2048 workgroups for the statistics, of 16 units at least where there are many; four shares at most where there are few, which the sums then
-  // join themselves.  The sums: up to 2048 also.  (A prompt of 4096: 250 us, with 4096 of the first 260, with 1024 or 4096 of the second 252.)
+  // About 2048 workgroups for the statistics, of 16 units at least where there are many units; four shares at most, of two units, where there are few units or
+  // many columns.  Few: 64 rows of 32 heads over 16 to 62 units take the same time either way, 512 rows by themselves (16 units) 28.3 us instead of 33.0; over
+  // 96 and 126 units the 64 rows take 40.9 and 44.8 instead of 32.2 and 32.0.  The sums: up to 2048 also.  (A prompt of 4096: 229 to 231 us; with 1024 or 4096 of the first
+  // 234 and 239, of the second 234 and 228.  Four of 1500 rows: 155; 152 and 168, 154 and 147.)
   const int64_t most = std::max<int64_t>(1, 2048 / groups);
   if (most <= 4 || units <= 64) p.share_units = (int)std::max<int64_t>(2, (units + std::min<int64_t>(4, most) - 1) / std::min<int64_t>(4, most));
   else p.share_units = (int)std::max<int64_t>(16, (units + most - 1) / most);

@@ -7,20 +7,20 @@
 // workgroup a row and looks at what the parts left.
 //   k_sample_parts  a part's largest logit and the first id that has it; where all tokens' weights count (no limit, or top-p without top-k) their sum
 //                   against that largest one; for top-k and top-p a histogram over equal steps of log w: how many tokens, and where in the step they lie
-//   k_sample_edges  the histograms together say in which steps the cut lies, for certain: counts are exact, weights known to 1e-3 from the places
+//   k_sample_edges  the histograms together say in which steps the cut lies, for certain: counts are exact, weights known to 1e-4 from the places
 //   k_sample_collect the tokens of these steps to a list, what lies before them added up by parts (threads whose largest logit is below do not look again)
 //   k_sample_pick   the list is divided, by equal steps and then by the bits of its logits, until a few tokens (ranked by comparing all with all) or equal
 //                   ones (arithmetic) are left: the cut is a logit and how many of those equal to it are in.  Top-k first, as top-p is of what it leaves.
 //                   The part in which the target lies is looked through.
-// The two in the middle are launched where there are limits and more than 4096 tokens: so many are a list by themselves (top-k of one row: 4096 tokens 14.8 us,
-// 4100 with all four kernels 22.4; top-p 19.2 and 30.4).  Rows that they cannot narrow down (more than 4096 tokens in the steps of the cut, or
-// logits above 2^20 steps) are divided in k_sample_pick by going over the row again and again: 230 to 350 us for a row of 128256, 90 to 130 for one of
-// 40000, all rows side by side.
+// The two in the middle are launched where there are limits and more than 4096 tokens: so many are a list by themselves (top-k of one row: 4096 tokens 14.4 us,
+// 4100 with all four kernels 22.5; top-p 17.0 and 27.9).  Rows that they cannot narrow down (more than 4096 tokens in the steps of the cut, or
+// logits above 2^20 steps) are divided in k_sample_pick by going over the row again and again.  Logits of a normal distribution of 1e-3, with top-k 50 / top-p 0.9 /
+// top-k 5000 and top-p 0.9: 154 / 286 / 339 us for a row of 128256, 63 / 109 / 118 for one of 40000, 184 / 324 / 384 and 72 / 117 / 139 for 64 of them side by side.
 //
-// What bounds it: 320 rows of 151936 bf16 without limits are 97 MB, 19 us at the rate of a copy, and take 55, as the sum is some 20 fp64 and other
-// instructions a weight (64% of the issue slots; with 13 instead of 17 in fp64 and as many more in fp32: 57).  256 rows of 128256 with limits are 131 MB, 26 us, and take
+// What bounds it: 320 rows of 151936 bf16 without limits are 97 MB, 19 us at the rate of a copy, and take 51, as the sum is some 20 fp64 and other
+// instructions a weight (64% of the issue slots; with 13 instead of 17 in fp64 and as many more in fp32 2 us more).  256 rows of 128256 with limits are 131 MB, 26 us, and take
 // 84: parts 36, edges 8, collect 22, pick 18.  A single row is a chain of launches (4, of which parts and collect are 5 us each) and of exchanges inside
-// the two that decide: 24 us with top-k, 31 with top-p, 9 without limits.
+// the two that decide: 24 us with top-k, 32 with top-p, 9.5 without limits.
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -793,8 +793,10 @@ __global__ __launch_bounds__(THREADS, 4) void k_sample_pick(SampleArgs a) {
 }
 
 // Logits of a part: as many as a thread's registers hold with ease (32) where there are many; half of them where a short launch is spread over more CUs.  Measured
-// with halves and wholes, no limits / top-k / top-p, us: 1 row of 128256  9.2 / 24.3 / 33.5 and 10.8 / 24.2 / 36.1; 16 rows  10.4 / 27.5 / 38.2 and
-// 11.3 / 26.0 / 37.9; 64 rows  16.7 / 36.3 / 56.7 and 17.8 / 32.9 / 55.1; 256 rows  37.7 / 69.4 / 117 and 36.4 / 59.3 / 109.
+// with halves and wholes, no limits / top-k 50 / top-p 0.9 / both, us: 1 row of 128256  9.5 / 23.9 / 31.8 / 27.4 and 10.8 / 24.2 / 33.6 / 27.7; 8 rows  9.6 / 26.3 / 34.2 /
+// 29.8 and 11.3 / 25.1 / 36.0 / 28.5; 32 rows (1024 parts, the last halves)  12.2 / 31.2 / 42.8 / 34.6 and 13.0 / 27.8 / 40.9 / 31.1; 64 rows  16.6 / 36.4 / 53.4 / 40.0 and
+// 17.8 / 32.7 / 53.4 / 36.0; 128 rows  24.1 / 46.7 / 74.3 / 50.7 and 24.8 / 40.3 / 73.1 / 44.7.  Without limits halves are ahead up to 128 rows, with top-k wholes from 8 on:
+// the rule lies between them.  It looks at no limits, so that a row with limits that leave everything has the parts, and the sums to the bit, of one without.
 constexpr int SMALL_PARTS = 1024;
 void divide(SampleArgs& a, int rows) {
   a.part = (int64_t)rows * ((a.vocab + 4095) / 4096) > SMALL_PARTS ? 8192 : 4096;
